@@ -294,6 +294,24 @@ zoact_status zoact_linear_fwd_pair(const zoact_linear* L, const zoact_arena* A, 
  * slots per compute unit; a smaller one is used as far as it goes). */
 size_t zoact_linear_workspace_bytes(void);
 
+/* ------------------------------------------------------ adapted linear of a few rows
+ * The layer of a model that answers, without perturbation, for the few rows of one decoding
+ * step (no halves):
+ *   y = epilogue(residual + x W^T + b + p bf16(C)^T)
+ * x [rows][d_in] bf16, p [rows][r] bf16 (zoact_project on x; NULL with r == 0), residual NULL
+ * or [rows][d_out] bf16, y [rows][d_out'] in y_dtype (BF16 or F32).  INT4 weights only (for
+ * others zoact_linear_fwd_pair with sign 0 serves).  C is read from the arena at
+ * L->coef_offset; L->ch and L->ut are not read.  Features [plain_begin, plain_end) have no
+ * correction (any bounds here).  Sums are fp32 and a group's scale multiplies the group's
+ * sum: unlike the products of two or more halves, q * s is not rounded to bf16 first.
+ * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0; d_out % 16 == 0 (32 with SWIGLU); flags:
+ * ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, p, y and residual 16-byte aligned.  L->ws
+ * (optional, as above) lets the depth of narrow layers be split over workgroups; the partial
+ * sums are added in a fixed order. */
+enum { ZOACT_ROWS_MAX = 64 };
+zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, const void* x, int64_t rows, const void* p,
+                               const void* residual, uint32_t flags, void* y, int32_t y_dtype, zoact_stream stream);
+
 /* INT4 weights to bf16: out[n][k] = bf16(q[n][k] * s[n][k / 128]), the dequantised weight
  * the INT4 GEMM forms in registers (same packing as zoact_linear.w).  At large token counts
  * a caller dequantises each INT4 layer once per forward into a bf16 buffer of its own and

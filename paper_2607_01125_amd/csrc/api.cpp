@@ -214,6 +214,41 @@ zoact_status zoact_linear_fwd_pair(const zoact_linear* L, const zoact_arena* A, 
                     "linear_fwd_pm");
 }
 
+zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, const void* x, int64_t rows, const void* p,
+                               const void* residual, uint32_t flags, void* y, int32_t y_dtype, zoact_stream stream) {
+  CHECK(L != nullptr && x && y && L->w, "linear_rows: NULL layer, x, y or w");
+  if (L->w_dtype != ZOACT_INT4_G128) return fail(ZOACT_E_UNSUPPORTED, "linear_rows: INT4 weights only");
+  CHECK(L->w_scales != nullptr, "linear_rows: INT4 needs w_scales");
+  CHECK(rows >= 1 && rows <= ZOACT_ROWS_MAX, "linear_rows: rows=%lld outside [1, %d]", (long long)rows, ZOACT_ROWS_MAX);
+  CHECK(L->d_in >= 128 && L->d_in % 128 == 0 && L->d_in < (1 << 30), "linear_rows: d_in=%lld must be a multiple of 128",
+        (long long)L->d_in);
+  CHECK((flags & ~(uint32_t)(ZOACT_EPI_SWIGLU | ZOACT_EPI_RELU)) == 0, "linear_rows: unknown flags 0x%x", flags);
+  CHECK(!((flags & ZOACT_EPI_SWIGLU) && (flags & ZOACT_EPI_RELU)), "linear_rows: SWIGLU and RELU are exclusive");
+  const int64_t unit = (flags & ZOACT_EPI_SWIGLU) ? 32 : 16;
+  CHECK(L->d_out >= unit && L->d_out % unit == 0 && L->d_out <= (int64_t(1) << 32),
+        "linear_rows: d_out=%lld must be a multiple of %d", (long long)L->d_out, (int)unit);
+  CHECK(float_type(y_dtype), "linear_rows: y must be F32 or BF16");
+  CHECK(L->r >= 0 && L->r <= 256, "linear_rows: r=%d outside [0, 256]", L->r);
+  CHECK(aligned16(x) && aligned16(L->w) && aligned16(y) && (!residual || aligned16(residual)) && (!p || aligned16(p)),
+        "linear_rows: x, w, p, y and residual must be 16-byte aligned");
+  CHECK(L->ws == nullptr || aligned16(L->ws), "linear_rows: ws must be 16-byte aligned");
+  CHECK((reinterpret_cast<uintptr_t>(L->w_scales) & 1) == 0 && (reinterpret_cast<uintptr_t>(L->bias) & 1) == 0,
+        "linear_rows: scales and bias must be 2-byte aligned");
+  if (L->r > 0) {
+    CHECK(p != nullptr, "linear_rows: r > 0 needs p");
+    CHECK(A != nullptr && A->c != nullptr, "linear_rows: r > 0 needs an arena");
+    CHECK(float_type(A->c_dtype), "linear_rows: arena dtype must be F32 or BF16");
+    CHECK(L->plain_begin >= 0 && L->plain_begin <= L->plain_end && L->plain_end <= L->d_out,
+          "linear_rows: plain range [%lld, %lld) outside [0, d_out]", (long long)L->plain_begin, (long long)L->plain_end);
+    const int64_t n = (L->d_out - (L->plain_end - L->plain_begin)) * (int64_t)L->r;
+    CHECK(L->coef_offset >= 0 && L->coef_offset <= A->k && n <= A->k - L->coef_offset,
+          "linear_rows: coefficient block [%lld, %lld) outside the arena (k=%lld)", (long long)L->coef_offset,
+          (long long)(L->coef_offset + n), (long long)A->k);
+  }
+  return hip_status(zoact::launch_linear_rows(*L, A, x, rows, p, residual, flags, y, y_dtype, st(stream)),
+                    "linear_rows");
+}
+
 static zoact_pert_pair pm_pair(const zoact_pert& p) {
   zoact_pert_pair pp{};
   pp.seed = p.seed;

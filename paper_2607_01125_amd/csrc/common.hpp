@@ -47,6 +47,9 @@ hipError_t launch_norm_project(bool layernorm, const void* x, const void* w, con
 hipError_t launch_linear_pm(const zoact_linear& L, const zoact_arena* A, const void* x, int32_t x_dtype, int64_t T,
                             const void* p, const void* residual, uint32_t flags, const zoact_pert_pair& pert,
                             void* y, int32_t y_dtype, hipStream_t s);
+// The unperturbed adapted linear of 1 .. ZOACT_ROWS_MAX rows with INT4 weights.
+hipError_t launch_linear_rows(const zoact_linear& L, const zoact_arena* A, const void* x, int64_t rows, const void* p,
+                              const void* residual, uint32_t flags, void* y, int32_t y_dtype, hipStream_t s);
 // Adapted linear of both halves with the regression loss fused into the epilogue (y not
 // stored): per-tile sums into part [2][tiles], then loss_pm[h] = sum / (T * d_out).
 // y [2 T][N] fp32 = x [2 T][K] w^T, bf16 operands with dense rows (plain GEMM, no correction).

@@ -1,0 +1,203 @@
+"""zoact_linear_rows against the plain formula in float64: widths, ranks, epilogues and rows at the ends
+of their ranges."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from paper_2607_01125_amd import zoact as Z
+
+from gpu_helpers import announce, dev, host, t_bf16, t_f32, t_u8
+
+pytestmark = pytest.mark.gpu
+
+
+def _case(rows, K, N, r, *, flags=0, bias=False, res=False, plain=(0, 0), c_f32=False, seed=0, x_mean=0.0):
+    rng = np.random.default_rng([seed, rows, K, N, r])
+    q = rng.integers(-7, 8, (N, K))
+    packed = ((q[:, ::2] & 15) | ((q[:, 1::2] & 15) << 4)).astype(np.uint8)
+    sc = synth.bf16_round((0.007 * np.exp(rng.normal(0, 0.3, (N, K // 128)))).astype(np.float32))
+    x = synth.bf16_round((rng.normal(0, 1, (rows, K)) + x_mean).astype(np.float32))
+    n_c = N - (plain[1] - plain[0])
+    c = rng.normal(0, 0.05, (n_c, r)).astype(np.float32)
+    if not c_f32:
+        c = synth.bf16_round(c)
+    p = synth.bf16_round(rng.normal(0, 1, (rows, r)).astype(np.float32))
+    b = synth.bf16_round(rng.normal(0, 0.1, N).astype(np.float32)) if bias else None
+    rs = synth.bf16_round(rng.normal(0, 1, (rows, N)).astype(np.float32)) if res else None
+    return dict(rows=rows, K=K, N=N, r=r, flags=flags, plain=plain, c_f32=c_f32, q=q, packed=packed, sc=sc, x=x, c=c,
+                p=p, b=b, rs=rs)
+
+
+def _reference(s):
+    """y and its error bound before the last rounding, both float64."""
+    K, N, rows = s["K"], s["N"], s["rows"]
+    w = (s["q"].reshape(N, -1, 128) * s["sc"].astype(np.float64)[:, :, None]).reshape(N, K)
+    x = s["x"].astype(np.float64)
+    y = x @ w.T
+    # magnitudes that enter the fp32 sums: (24 + q) x and the 24 sum x taken out, times the scale
+    mag = np.abs(x) @ (np.repeat(s["sc"].astype(np.float64), 128, 1) * 55).T
+    if s["r"]:
+        cb = synth.bf16_round(s["c"]).astype(np.float64)
+        feat = np.r_[0:s["plain"][0], s["plain"][1]:N]
+        y[:, feat] += s["p"].astype(np.float64) @ cb.T
+        mag[:, feat] += np.abs(s["p"].astype(np.float64)) @ np.abs(cb).T
+    if s["b"] is not None:
+        y += s["b"].astype(np.float64)
+    if s["rs"] is not None:
+        y += s["rs"].astype(np.float64)
+        mag += np.abs(s["rs"])
+    # steps of a sum: 256 products of a group, its scale, the groups of a wave, eight waves, rank, three terms
+    steps = 256 + K // 128 + 8 + s["r"] + 4
+    tol = steps * 2.0 ** -23 * mag
+    if s["flags"] & Z.EPI_RELU:
+        y = np.maximum(y, 0)
+    if s["flags"] & Z.EPI_SWIGLU:
+        f = np.arange(N // 2)
+        at = f // 16 * 32 + f % 16
+        g, u, tg, tu = y[:, at], y[:, at + 16], tol[:, at], tol[:, at + 16]
+        silu = g / (1 + np.exp(-g))
+        y = silu * u
+        # |silu'| <= 1.1; the exponential, sum, quotient and product round to about 2^-20 together
+        tol = 1.1 * tg * (np.abs(u) + tu) + np.abs(silu) * tu + 2.0 ** -20 * np.abs(y)
+    return y, tol
+
+
+def _run(s, f32_out, ws=False):
+    lin = Z.Linear(t_u8(s["packed"]), s["K"], s["N"], s["r"], None, 0, t_bf16(s["b"]) if s["b"] is not None else None,
+                   t_bf16(s["sc"]), plain=s["plain"])
+    if ws:
+        lin.ws = torch.full((Z.linear_workspace_bytes(),), 255, dtype=torch.uint8, device=dev())
+    arena, pad = None, 24
+    if s["r"]:
+        lin.coef_offset = pad
+        c = np.concatenate([np.full(pad, np.nan, np.float32), s["c"].ravel(), np.full(3, np.nan, np.float32)])
+        ct = t_f32(c) if s["c_f32"] else t_bf16(c)
+        arena = Z.Arena(ct, torch.zeros(1, device=dev()), torch.zeros(1, device=dev()))
+    out = s["N"] // 2 if s["flags"] & Z.EPI_SWIGLU else s["N"]
+    y = torch.full((s["rows"], out), float("nan"), device=dev(), dtype=torch.float32 if f32_out else torch.bfloat16)
+    Z.linear_rows(lin, arena, t_bf16(s["x"]), t_bf16(s["p"]) if s["r"] else None, y,
+                  t_bf16(s["rs"]) if s["rs"] is not None else None, s["flags"])
+    return y
+
+
+def _check(s, f32_out, **kw):
+    y, tol = _reference(s)
+    got = host(_run(s, f32_out, **kw))
+    tol = tol + (2.0 ** -24 if f32_out else 2.0 ** -8) * (np.abs(y) + tol)
+    bad = ~(np.abs(got - y) <= tol)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist(), np.abs(got - y)[bad][:3], tol[bad][:3])
+
+
+CASES = [
+    dict(rows=1, K=128, N=16, r=0),
+    dict(rows=1, K=128, N=32, r=1, flags=Z.EPI_SWIGLU),
+    dict(rows=1, K=4096, N=256, r=32, res=True),
+    dict(rows=2, K=384, N=48, r=5, bias=True),
+    dict(rows=5, K=1152, N=80, r=33, flags=Z.EPI_RELU, bias=True, c_f32=True),
+    dict(rows=15, K=256, N=96, r=8, flags=Z.EPI_SWIGLU, c_f32=True),
+    dict(rows=16, K=512, N=112, r=64, res=True, bias=True),
+    dict(rows=17, K=640, N=64, r=256, plain=(16, 40)),
+    dict(rows=31, K=2048, N=272, r=16, plain=(0, 100), bias=True),
+    dict(rows=33, K=896, N=160, r=100, flags=Z.EPI_SWIGLU, bias=True, res=True),
+    dict(rows=48, K=1024, N=1040, r=32, plain=(500, 1040)),
+    dict(rows=64, K=1408, N=144, r=7, res=True),
+    dict(rows=64, K=128, N=16, r=16, plain=(0, 16)),
+    dict(rows=7, K=20480, N=64, r=64, bias=True, res=True),
+    dict(rows=3, K=14336, N=128, r=32, res=True, x_mean=2.0),
+    dict(rows=1, K=512, N=6144, r=32),
+    dict(rows=64, K=256, N=4112, r=32),
+]
+
+
+@pytest.mark.parametrize("f32_out", [False, True])
+@pytest.mark.parametrize("kw", CASES, ids=lambda k: f"{k['rows']}x{k['K']}x{k['N']}r{k['r']}")
+def test_rows_against_the_formula(kw, f32_out):
+    announce("linear_rows", kw, f32_out)
+    s = _case(**kw)
+    _check(s, f32_out)
+    _check(s, f32_out, ws=True)
+
+
+def test_codes_and_scales_one_by_one():
+    """Rows that are unit vectors read single weights: each of the 16 nibbles' values, at every place of
+    a group, comes out as code times scale exactly (fp32 output; the 24 taken out is exact here)."""
+    K, N = 256, 32
+    q = (np.arange(N)[:, None] + np.arange(K)[None, :]) % 15 - 7
+    packed = ((q[:, ::2] & 15) | ((q[:, 1::2] & 15) << 4)).astype(np.uint8)
+    sc = synth.bf16_round(np.linspace(0.001, 3.0, N * 2).reshape(N, 2).astype(np.float32))
+    lin = Z.Linear(t_u8(packed), K, N, w_scales=t_bf16(sc))
+    want = q * np.repeat(sc, 128, 1)
+    for k0 in range(0, K, 64):
+        x = np.zeros((64, K), np.float32)
+        x[np.arange(64), k0 + np.arange(64)] = 1.0
+        y = torch.empty(64, N, device=dev())
+        announce("linear_rows unit", k0)
+        Z.linear_rows(lin, None, t_bf16(x), None, y)
+        assert np.array_equal(host(y), want[:, k0:k0 + 64].T.astype(np.float64))
+
+
+def test_minus_eight_is_read_as_two_complement():
+    lin = Z.Linear(t_u8(np.full((16, 64), 0x88)), 128, 16, w_scales=t_bf16(np.ones((16, 1))))
+    x = np.zeros((1, 128), np.float32)
+    x[0, 77] = 2.0
+    y = torch.empty(1, 16, device=dev())
+    Z.linear_rows(lin, None, t_bf16(x), None, y)
+    assert np.array_equal(host(y), np.full((1, 16), -16.0))
+
+
+def test_rows_do_not_mix_and_nan_stays_in_its_row():
+    s = _case(9, 512, 64, 8, res=True)
+    full = host(_run(s, True))
+    bad = dict(s, x=s["x"].copy())
+    bad["x"][4, 100] = np.nan
+    got = host(_run(bad, True))
+    assert np.isnan(got[4]).all()
+    keep = [i for i in range(9) if i != 4]
+    assert np.array_equal(got[keep], full[keep])
+
+
+def test_same_bits_twice_on_a_side_stream_and_from_a_graph():
+    s = _case(13, 1024, 320, 32, bias=True)
+    a = _run(s, False)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        b = _run(s, False)
+    torch.cuda.current_stream().wait_stream(st)
+    assert torch.equal(a, b)
+    lin = Z.Linear(t_u8(s["packed"]), 1024, 320, 32, None, 0, t_bf16(s["b"]), t_bf16(s["sc"]))
+    lin.ws = torch.empty(Z.linear_workspace_bytes(), dtype=torch.uint8, device=dev())
+    arena = Z.Arena(t_bf16(s["c"].ravel()), torch.zeros(1, device=dev()), torch.zeros(1, device=dev()))
+    x, p = t_bf16(s["x"]), t_bf16(s["p"])
+    y, eager = torch.empty_like(a), torch.empty_like(a)
+    g = torch.cuda.CUDAGraph()
+    Z.linear_rows(lin, arena, x, p, eager)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        Z.linear_rows(lin, arena, x, p, y)
+    for i in range(4):
+        x.mul_(-0.5)
+        Z.linear_rows(lin, arena, x, p, eager)
+        y.fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager), i
+
+
+def test_refusals_on_device_tensors():
+    s = _case(4, 256, 32, 8)
+    lin = Z.Linear(t_u8(s["packed"]), 256, 32, 0, w_scales=t_bf16(s["sc"]))
+    y = torch.empty(4, 32, device=dev(), dtype=torch.bfloat16)
+    x = t_bf16(s["x"])
+    with pytest.raises(ValueError):
+        Z.linear_rows(lin, None, x.t().contiguous().t(), None, y)
+    with pytest.raises(ValueError):
+        Z.linear_rows(lin, None, x, None, y[:, :16])
+    with pytest.raises(ValueError):
+        Z.linear_rows(lin, None, x.float(), None, y)
+    with pytest.raises(Z.ZoactError):
+        Z.linear_rows(Z.Linear(t_bf16(np.zeros((32, 256))), 256, 32), None, x, None, y)
+    big = torch.zeros(65, 256, device=dev(), dtype=torch.bfloat16)
+    with pytest.raises(Z.ZoactError):
+        Z.linear_rows(lin, None, big, None, torch.empty(65, 32, device=dev(), dtype=torch.bfloat16))
