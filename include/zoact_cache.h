@@ -120,8 +120,8 @@ zoact_status zoact_cache_compact(const zoact_cache* c, void* ws, size_t ws_bytes
  *   code = rint(value / s), or 0 where s == 0
  * in fp32, ties to even.  A block that gets a value that is not finite has a NaN scale and
  * new codes 0: whoever attends to it gets NaN.  Codes of tokens that the sequence does not
- * have yet stay as they were.  16-byte aligned rows: ldk, ldv multiples of 8 (BF16) or
- * 4 (F32).  No slot twice in one batch. */
+ * have yet stay as they were.  Rows and tables 16-byte aligned: ldk, ldv multiples of 8
+ * (BF16) or 4 (F32).  No slot twice in one batch. */
 zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, const void* k, int64_t ldk, const void* v,
                                 int64_t ldv, int32_t dtype, const zoact_cache_batch* b, const float* cos_t,
                                 const float* sin_t, int64_t n_pos, zoact_stream stream);
@@ -130,8 +130,8 @@ zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, const void*
  * token index, q [rows][ldq] with n_heads heads (head h reads key/value head h / (n_heads /
  * n_kv_heads)), out [rows][n_heads * head_dim], both in dtype.  With cos_t, sin_t q is
  * rotated first, as append does.  Scores, softmax and sums fp32; in BF16 the rotated q and
- * the probabilities enter the products as two bf16 terms (16 bits), in F32 as three
- * (24 bits); one rounding of out.
+ * the probabilities are rounded to 11 bits as they enter the products (an unrotated bf16 q
+ * is not changed by this), in F32 to 22 bits or more; one rounding of out.
  * max_len (host): a length that no entry's pos + rows is expected to pass; it only shapes
  * the split of the work, longer entries are served too.  ws: at least
  * zoact_attention_cache_workspace_bytes() bytes let long sequences be split over

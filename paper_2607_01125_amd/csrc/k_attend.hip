@@ -7,10 +7,10 @@
 // per page join the four lanes of a column), and those 16 probabilities are, as they stand, the
 // right operand of O^T = V^T P^T -- the page keeps V's tokens in that order, so nothing moves
 // between lanes and K and V go from memory to the matrix unit in whole 16-byte loads.
-// Codes become bf16 without rounding (magnitudes up to 127 need 7 bits); a K scale multiplies its
-// block's scores, a V scale its block's probabilities.  q and the probabilities enter as NT bf16
-// terms: two carry 16 bits (bf16 activations: beside the output's 8 nothing shows), three carry
-// fp32's 24.
+// Codes become f16 without rounding; a K scale multiplies its block's scores, a V scale its block's
+// probabilities.  q (brought to f16's range by a power of two for each column) and the probabilities
+// enter as NT f16 terms: one carries 11 bits (bf16 activations: the output has 8), two carry 22 and
+// more (fp32).  bf16 terms would need two and three for this.
 #include <math.h>
 
 #include <string>
@@ -34,23 +34,26 @@ struct AttendArgs {
   float2* ml;                  // [n * max_new * H][S] maximum (log2 domain) and sum
 };
 
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {   // exact: the lower halves are zero
-  return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Four int8 codes as f16, exactly: with its sign bit turned over a code is u = code + 128, and the bytes
+// (u, 0x64) are the f16 number 1024 + u.
+__device__ __forceinline__ void codes4(uint32_t w, uint32_t (&o)[2]) {
+  w ^= 0x80808080u;
+  const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400)) + off);
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402)) + off);
 }
-// Eight int8 codes as bf16.
-__device__ __forceinline__ bf16x8 codes8(uint32_t a, uint32_t b) {
-  uint32_t o[4];
-  const uint32_t w[2] = {a, b};
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t x = w[e >> 1] >> (16 * (e & 1));
-    o[e] = pack2((float)(int8_t)x, (float)(int8_t)(x >> 8));
-  }
-  return __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(o));
+__device__ __forceinline__ f16x8 codes8(uint32_t a, uint32_t b) {
+  uint32_t x[2], y[2];
+  codes4(a, x);
+  codes4(b, y);
+  return __builtin_bit_cast(f16x8, make_uint4(x[0], x[1], y[0], y[1]));
 }
-// x as NT bf16 terms, each the nearest to what the ones before it leave.
+// x as NT f16 terms, each the nearest to what the ones before it leave.
 template <int NT>
-__device__ __forceinline__ void terms8(const float (&x)[8], bf16x8 (&t)[NT]) {
+__device__ __forceinline__ void terms8(const float (&x)[8], f16x8 (&t)[NT]) {
   float r[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) r[e] = x[e];
@@ -58,8 +61,8 @@ __device__ __forceinline__ void terms8(const float (&x)[8], bf16x8 (&t)[NT]) {
   for (int k = 0; k < NT; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      t[k][e] = (__bf16)r[e];
-      r[e] -= (float)t[k][e];
+      t[k][e] = (_Float16)r[e];
+      if (k + 1 < NT) r[e] -= (float)t[k][e];
     }
 }
 
@@ -77,6 +80,174 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   }
 }
 
+// A page of one head on its way to the wave: 16 bytes a lane and load (HD 32: K's upper half is not used).
+template <int HD>
+struct KeyLoad {
+  static constexpr int N = HD == 32 ? 4 : HD / 16;
+  uint4 u[N];
+  __device__ __forceinline__ void go(const int8_t* kp, int lane) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int8_t* const kr = kp + (n * 16 + (lane & 15)) * HD;
+      if constexpr (HD == 32) {
+        const uint2 t = *reinterpret_cast<const uint2*>(kr + 8 * g);
+        u[n] = make_uint4(t.x, t.y, 0, 0);
+      } else {
+#pragma unroll
+        for (int h = 0; h < HD / 64; ++h) u[n * (HD / 64) + h] = *reinterpret_cast<const uint4*>(kr + 64 * h + 16 * g);
+      }
+    }
+  }
+};
+template <int HD>
+struct ValueLoad {
+  uint4 u[HD / 16];
+  __device__ __forceinline__ void go(const int8_t* vp, int lane) {
+#pragma unroll
+    for (int d = 0; d < HD / 16; ++d)
+      u[d] = *reinterpret_cast<const uint4*>(vp + (d * 16 + (lane & 15)) * kPage + 16 * (lane >> 4));
+  }
+};
+
+constexpr int kPExp = 14;         // probabilities enter their product times 2^14: f16 then keeps 11 bits
+                                  // of them down to 2^-28, and something down to 2^-38
+constexpr int kNoScale = -200;    // below every exponent of an fp32 number
+
+// V scales of a page's blocks that hold a token up to `last`, times a power of two that keeps p vsc below
+// 2^14; vexp follows, and o's unit 2^(vexp - 14) with it.
+__device__ __forceinline__ void value_scales(const float4& vs, int t0, int last, int& vexp, float (&vsc)[4]) {
+  const float v[4] = {vs.x, vs.y, vs.z, vs.w};
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    vsc[n] = t0 + 16 * n > last ? 0.f : v[n];
+    const int ex = vsc[n] > 0.f ? __builtin_amdgcn_frexp_expf(vsc[n]) : kNoScale;   // (NaN stays NaN)
+    vexp = ex > vexp ? ex : vexp;
+  }
+#pragma unroll
+  for (int n = 0; n < 4; ++n) vsc[n] = __builtin_amdgcn_ldexpf(vsc[n], kPExp - vexp);
+}
+
+// One page's scores (log2 domain) of a lane's column: masks tokens past lim (edge: there may be some),
+// updates the running maximum and sum, and gives the factor of what was summed before and the
+// probabilities times V's scales as terms.
+template <int NT>
+__device__ __forceinline__ void soft_page(float (&s)[4][4], int t0, int lim, bool edge, int g, const float (&vsc)[4],
+                                          float& m, float& l, float& alpha, f16x8 (&pf)[2][NT]) {
+  if (edge) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (t0 + 16 * n + 4 * g + i > lim) s[n][i] = -INFINITY;
+  }
+  float mx = m;
+#pragma unroll
+  for (int n = 0; n < 4; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][i]);
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  const float base = mx == -INFINITY ? 0.f : mx;
+  alpha = __builtin_amdgcn_exp2f(m - base);
+  m = mx;
+  l *= alpha;
+  float lsum = 0.f;
+#pragma unroll
+  for (int n2 = 0; n2 < 2; ++n2) {
+    float p8[8];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float p[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(s[2 * n2 + n][i] - base);
+        p8[4 * n + i] = p[i] * vsc[2 * n2 + n];
+      }
+      lsum += (p[0] + p[1]) + (p[2] + p[3]);
+    }
+    // (a block past the column's last token may have a NaN scale, which other columns see)
+    if (edge) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        if (t0 + 16 * (2 * n2 + n) > lim) p8[4 * n] = p8[4 * n + 1] = p8[4 * n + 2] = p8[4 * n + 3] = 0.f;
+    }
+    terms8<NT>(p8, pf[n2]);
+  }
+  l += lsum;
+}
+
+// q of one column as right operands, dims 64 (s / 2) + 16 g + 8 (s % 2) + 0..7 of step s (HD 32:
+// 8 g + 0..7), rotated, times a power of two that brings the column's largest to [2^14, 2^15).
+// Returns the factor of its scores (log2 domain).
+template <typename T, int HD, int NT>
+__device__ __forceinline__ float load_query(const AttendArgs& a, int64_t row, int h, int64_t pos, int g,
+                                            f16x8 (&qf)[HD / 32][NT]) {
+  constexpr int KS = HD / 32, HALF = HD / 2;
+  const T* const qr = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * HD;
+  const int64_t tp = pos < a.n_pos ? pos : a.n_pos - 1;
+  float x[KS][8], top = 0.f;
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int d = HD == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+    load8(qr + d, x[s]);
+    if (a.ct) {
+#pragma clang fp contract(off)
+      const bool up = d >= HALF;
+      float y[8], cs[8], sn[8];
+      load8(qr + (up ? d - HALF : d + HALF), y);
+      const int64_t base = tp * HALF + (up ? d - HALF : d);
+      load8(a.ct + base, cs);
+      load8(a.st + base, sn);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[s][k] = up ? x[s][k] * cs[k] + y[k] * sn[k] : x[s][k] * cs[k] - y[k] * sn[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(x[s][k]));
+  }
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  int sh = 14 - ((int)(__float_as_uint(top) >> 23) - 127);   // (both powers of two stay normal numbers)
+  sh = top == 0.f ? 0 : sh > 120 ? 120 : sh < -113 ? -113 : sh;
+  const float up2 = __uint_as_float((uint32_t)(127 + sh) << 23);
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[s][k] *= up2;
+    terms8<NT>(x[s], qf[s]);
+  }
+  return __uint_as_float((uint32_t)(127 - sh) << 23) * a.scale;
+}
+
+// A workgroup's key/value head, split and column tile.  Workgroups go to the eight XCDs in turn, so heads,
+// which all have the same work, come first in the order, and an entry's splits start at its number:
+// the late ones, which short sequences leave empty, do not meet on one XCD (with splits first the
+// 48-sequence batch took 113 us, with heads first 71).
+struct Place {
+  int hk, split, tile;
+};
+__device__ __forceinline__ Place place_of(const AttendArgs& a) {
+  const unsigned x = blockIdx.x, hkv = (unsigned)a.c.n_kv_heads, q = x / hkv;
+  Place p;
+  p.hk = (int)(x % hkv);
+  p.tile = (int)(q / a.S);
+  p.split = (int)((q % a.S + blockIdx.z) % a.S);
+  return p;
+}
+
+struct Range {
+  int last, pbeg, pend;     // last visible token, pages of the split
+};
+__device__ __forceinline__ Range split_range(const AttendArgs& a, const CacheEntry& e, int jmax, int split) {
+  Range r;
+  r.last = e.ok ? e.pos + jmax : -1;
+  const int pages = (r.last + kPage) / kPage;
+  r.pbeg = split * a.pps;
+  r.pend = split == a.S - 1 ? pages : (r.pbeg + a.pps < pages ? r.pbeg + a.pps : pages);
+  return r;
+}
+
+// Decoding: at most 16 columns, each wave its own pages.
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
   constexpr int KS = HD / 32;           // 32-deep products of a score
@@ -85,161 +256,111 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
   __shared__ float so[4][16][LD];
   __shared__ float sm[4][16], sl[4][16];
   const zoact_cache& c = a.c;
-  const int hk = blockIdx.y, split = blockIdx.x % a.S, tile = blockIdx.x / a.S;
-  const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0 && hk == 0);
-  const int ncol = e.count * a.G, c0 = tile * 16;
+  const Place at = place_of(a);
+  const int hk = at.hk, split = at.split, c0 = at.tile * 16;
+  const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0);
+  const int ncol = e.count * a.G;
   if (c0 >= ncol) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
-  const int col = c0 + (lane & 15);
-  // (columns past the last repeat it; they are not stored)
-  const int cq = col < ncol ? col : ncol - 1;
-  const int j = cq / a.G, h = hk * a.G + cq % a.G;
-  const int tcol = e.pos + j;                                        // the column's last token
-  const int jmax = (c0 + 15 < ncol ? c0 + 15 : ncol - 1) / a.G;
-  const int last = e.ok ? e.pos + jmax : -1;
-  const int pages = (last + kPage) / kPage;
-  const int pbeg = split * a.pps, pend = split == a.S - 1 ? pages : (pbeg + a.pps < pages ? pbeg + a.pps : pages);
+  const Range rg = split_range(a, e, (c0 + 15 < ncol ? c0 + 15 : ncol - 1) / a.G, split);
 
   floatx4 o[DT];
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  int vexp = kNoScale;   // V scales so far are below 2^vexp; o is kept in units of 2^(vexp - 14)
 
-  if (pbeg + wave < pend) {
-    // q of the column, dims 64 (s / 2) + 16 g + 8 (s % 2) + 0..7 of step s (HD 32: 8 g + 0..7)
-    bf16x8 qf[KS][NT];
-    {
-      const T* const row = static_cast<const T*>(a.q) + (int64_t)(e.row0 + j) * a.ldq + (int64_t)h * HD;
-      const int64_t tp = tcol < a.n_pos ? tcol : a.n_pos - 1;
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int d = HD == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-        float x[8];
-        load8(row + d, x);
-        if (a.ct) {
-#pragma clang fp contract(off)
-          constexpr int half = HD / 2;
-          const bool up = d >= half;
-          float y[8], cs[8], sn[8];
-          load8(row + (up ? d - half : d + half), y);
-          const int64_t base = tp * half + (up ? d - half : d);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            cs[k] = a.ct[base + k];
-            sn[k] = a.st[base + k];
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k) x[k] = up ? x[k] * cs[k] + y[k] * sn[k] : x[k] * cs[k] - y[k] * sn[k];
-        }
-        terms8<NT>(x, qf[s]);
-      }
-    }
+  if (rg.pbeg + wave < rg.pend) {
+    // the first page's keys are on their way before q is ready, each next page's before this one's softmax
     const int* const trow = c.table + (int64_t)e.slot * c.max_pages;
     const int64_t lbase = (int64_t)a.layer * c.n_pages;
-    for (int pg = pbeg + wave; pg < pend; pg += 4) {
-      int pid = __builtin_amdgcn_readfirstlane(trow[pg]);
-      const bool bad = pid < 0 || pid >= c.n_pages;
-      if (bad) {
-        if (lane == 0) raise_status(a.b.status, ZOACT_STATUS_BAD_ENTRY);
-        continue;                                 // as if its tokens were masked
-      }
-      const int64_t head = (lbase + pid) * c.n_kv_heads + hk;
-      const int8_t* const kp = c.k + head * (kPage * HD);
-      const int8_t* const vp = c.v + head * (kPage * HD);
-      const float4 ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
+    auto head_of = [&](int pid, bool& bad) {
+      bad = pid < 0 || pid >= c.n_pages;
+      return (lbase + (bad ? 0 : pid)) * c.n_kv_heads + hk;
+    };
+    int pg = rg.pbeg + wave;
+    bool bad;
+    int64_t head = head_of(__builtin_amdgcn_readfirstlane(trow[pg]), bad);
+    KeyLoad<HD> kl;
+    ValueLoad<HD> vl;
+    kl.go(c.k + head * (kPage * HD), lane);
+    float4 ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
+    int pid1 = pg + 4 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[pg + 4]) : 0;
+
+    const int col = c0 + (lane & 15), cq = col < ncol ? col : ncol - 1;   // (columns past the last repeat it)
+    const int tcol = e.pos + cq / a.G;                                    // the column's last token
+    f16x8 qf[KS][NT];
+    const float qs = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol, g, qf);
+
+    while (true) {
+      vl.go(c.v + head * (kPage * HD), lane);
       const float4 vs = *reinterpret_cast<const float4*>(c.v_scale + head * 4);
-      const float ksc[4] = {ks.x * a.scale, ks.y * a.scale, ks.z * a.scale, ks.w * a.scale};
-      const float vsc[4] = {vs.x, vs.y, vs.z, vs.w};
+      const float ksc[4] = {ks.x, ks.y, ks.z, ks.w};
       float s[4][4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         floatx4 acc{0.f, 0.f, 0.f, 0.f};
-        const int8_t* const kr = kp + (n * 16 + (lane & 15)) * HD;
-        if constexpr (HD == 32) {
-          const uint2 u = *reinterpret_cast<const uint2*>(kr + 8 * g);
-          const bf16x8 kf = codes8(u.x, u.y);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[0][t], acc, 0, 0, 0);
-        } else {
+        for (int k = 0; k < KS; ++k) {
+          const uint4 u = kl.u[n * (KeyLoad<HD>::N / 4) + k / 2];
+          const f16x8 kf = k & 1 ? codes8(u.z, u.w) : codes8(u.x, u.y);
 #pragma unroll
-          for (int sl2 = 0; sl2 < KS / 2; ++sl2) {
-            const uint4 u = *reinterpret_cast<const uint4*>(kr + 64 * sl2 + 16 * g);
-            const bf16x8 k0 = codes8(u.x, u.y), k1 = codes8(u.z, u.w);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[2 * sl2][t], acc, 0, 0, 0);
-              acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[2 * sl2 + 1][t], acc, 0, 0, 0);
-            }
-          }
+          for (int q = 0; q < NT; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[k][q], acc, 0, 0, 0);
         }
+        const float f = ksc[n] * qs;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * ksc[n];
+        for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * f;
       }
-      const int t0 = pg * kPage;
-      const bool edge = t0 + kPage > e.pos + c0 / a.G + 1;      // some column ends inside the page
-      if (edge) {
-#pragma unroll
-        for (int n = 0; n < 4; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (t0 + 16 * n + 4 * g + i > tcol) s[n][i] = -INFINITY;
+      const int t0 = pg * kPage, next = pg + 4;
+      const bool now_bad = bad;
+      if (next < rg.pend) {
+        head = head_of(pid1, bad);
+        kl.go(c.k + head * (kPage * HD), lane);
+        ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
+        pid1 = next + 4 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[next + 4]) : 0;
       }
-      float mx = m;
-#pragma unroll
-      for (int n = 0; n < 4; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float base = mx == -INFINITY ? 0.f : mx;
-      const float alpha = __builtin_amdgcn_exp2f(m - base);
-      m = mx;
-      l *= alpha;
-      bf16x8 pf[2][NT];
-#pragma unroll
-      for (int n2 = 0; n2 < 2; ++n2) {
-        float p8[8];
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = s[2 * n2 + n][i];
-            const float p = __builtin_amdgcn_exp2f(x - base);
-            l += p;
-            // (a masked token's block may hold no scale yet)
-            p8[4 * n + i] = edge && t0 + 16 * (2 * n2 + n) + 4 * g + i > tcol ? 0.f : p * vsc[2 * n2 + n];
-          }
-        terms8<NT>(p8, pf[n2]);
-      }
+      // a page number that is none counts as if its tokens were masked
+      if (now_bad && lane == 0) raise_status(a.b.status, ZOACT_STATUS_BAD_ENTRY);
+      const bool edge = now_bad || t0 + kPage > e.pos + c0 / a.G + 1;    // some column ends inside the page
+      float vsc[4], alpha;
+      const int vold = vexp;
+      value_scales(vs, t0, now_bad ? -1 : rg.last, vexp, vsc);
+      f16x8 pf[2][NT];
+      soft_page<NT>(s, t0, now_bad ? -1 : tcol, edge, g, vsc, m, l, alpha, pf);
+      alpha = __builtin_amdgcn_ldexpf(alpha, vold - vexp);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        const uint4 u = *reinterpret_cast<const uint4*>(vp + (d * 16 + (lane & 15)) * kPage + 16 * g);
-        const bf16x8 v0 = codes8(u.x, u.y), v1 = codes8(u.z, u.w);
+        const f16x8 v0 = codes8(vl.u[d].x, vl.u[d].y), v1 = codes8(vl.u[d].z, vl.u[d].w);
         floatx4 acc = o[d] * alpha;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf[0][t], acc, 0, 0, 0);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf[1][t], acc, 0, 0, 0);
+        for (int q = 0; q < NT; ++q) {
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[0][q], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[1][q], acc, 0, 0, 0);
         }
         o[d] = acc;
       }
+      if (next >= rg.pend) break;
+      pg = next;
     }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
   }
   // the four waves' results
+  constexpr int DV = HD / 16;
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+  for (int d = 0; d < DT; ++d) {
+    floatx4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) so[wave][lane & 15][d * 16 + 4 * g + i] = o[d][i];
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i], vexp - kPExp);
+    *reinterpret_cast<floatx4*>(&so[wave][lane & 15][d * 16 + 4 * g]) = r;
+  }
   if (g == 0) {
     sm[wave][lane] = m;
     sl[wave][lane] = l;
   }
   __syncthreads();
-  constexpr int DV = HD / 16;
-  const int oc = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DV;
-  if (c0 + oc >= ncol) return;
+  const int oc = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * DV, col = c0 + oc;
+  if (col >= ncol) return;
   float M = -INFINITY;
 #pragma unroll
   for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][oc]);
@@ -254,7 +375,7 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
 #pragma unroll
     for (int k = 0; k < DV; ++k) r[k] += f * so[w][oc][d0 + k];
   }
-  const int oj = (c0 + oc) / a.G, oh = hk * a.G + (c0 + oc) % a.G;
+  const int oj = col / a.G, oh = hk * a.G + col % a.G;
   if (a.S == 1) {
     const float div = L == 0.f ? 1.f : L;
     T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
@@ -275,64 +396,269 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
   }
 }
 
-// Joins the splits of one row and head: HD lanes along the columns, 256 / HD groups of splits.
+// Chunks of new rows: 64 CT columns a workgroup, 16 CT a wave; the waves walk the pages together.  Each
+// converts a quarter of a page to f16 in LDS, as operands in the order they are read (1 KB apart and
+// contiguous, so neither side has bank conflicts); two buffers, one barrier a page, the next page's
+// codes on their way meanwhile.
+template <typename T, int HD, int NT, int CT>
+__global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
+  constexpr int KS = HD / 32, DT = HD / 16;
+  constexpr int KL = HD == 32 ? 1 : HD / 64;          // K loads of a wave (its 16 tokens)
+  constexpr int VL = (DT + 3) / 4;                    // V tiles of a wave
+  __shared__ f16x8 kb[2][4][KS][64];
+  __shared__ f16x8 vb[2][DT][2][64];
+  const zoact_cache& c = a.c;
+  const Place at = place_of(a);
+  const int hk = at.hk, split = at.split, c0 = at.tile * (64 * CT);
+  const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0);
+  const int ncol = e.count * a.G;
+  if (c0 >= ncol) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  const Range rg = split_range(a, e, (c0 + 64 * CT - 1 < ncol ? c0 + 64 * CT - 1 : ncol - 1) / a.G, split);
+  const int w0 = c0 + 16 * CT * wave;                 // the wave's first column
+  // (a wave past the last column repeats it, so that every wave reaches every barrier)
+  const int wfirst = e.pos + (w0 < ncol ? w0 : ncol - 1) / a.G;
+  const int wlast = e.pos + (w0 + 16 * CT - 1 < ncol ? w0 + 16 * CT - 1 : ncol - 1) / a.G;
+
+  floatx4 o[CT][DT];
+  float m[CT], l[CT], qs[CT];
+  f16x8 qf[CT][KS][NT];
+  int tcol[CT], vexp = kNoScale;
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[t][d] = floatx4{0.f, 0.f, 0.f, 0.f};
+    m[t] = -INFINITY;
+    l[t] = 0.f;
+  }
+  if (rg.pbeg < rg.pend) {
+    const int* const trow = c.table + (int64_t)e.slot * c.max_pages;
+    const int64_t lbase = (int64_t)a.layer * c.n_pages;
+    uint4 kr[KL], vr[VL];
+    float4 ks, vs;
+    bool bad;
+    auto load = [&](int pid) {
+      bad = pid < 0 || pid >= c.n_pages;
+      const int64_t head = (lbase + (bad ? 0 : pid)) * c.n_kv_heads + hk;
+      const int8_t* const kp = c.k + head * (kPage * HD) + (wave * 16 + (lane & 15)) * HD;
+      if constexpr (HD == 32) {
+        const uint2 u = *reinterpret_cast<const uint2*>(kp + 8 * g);
+        kr[0] = make_uint4(u.x, u.y, 0, 0);
+      } else {
+#pragma unroll
+        for (int h = 0; h < KL; ++h) kr[h] = *reinterpret_cast<const uint4*>(kp + 64 * h + 16 * g);
+      }
+#pragma unroll
+      for (int d = 0; d < VL; ++d) {
+        const int dt = wave * VL + d;
+        if (DT % 4 == 0 || dt < DT)
+          vr[d] = *reinterpret_cast<const uint4*>(c.v + head * (kPage * HD) + (dt * 16 + (lane & 15)) * kPage + 16 * g);
+      }
+      ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
+      vs = *reinterpret_cast<const float4*>(c.v_scale + head * 4);
+    };
+    load(__builtin_amdgcn_readfirstlane(trow[rg.pbeg]));
+    int pid1 = rg.pbeg + 1 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[rg.pbeg + 1]) : 0;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+      const int col = w0 + 16 * t + (lane & 15), cq = col < ncol ? col : ncol - 1;
+      tcol[t] = e.pos + cq / a.G;
+      qs[t] = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol[t], g, qf[t]);
+    }
+    for (int pg = rg.pbeg, buf = 0; pg < rg.pend; ++pg, buf ^= 1) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+        kb[buf][wave][k][lane] = k & 1 ? codes8(kr[k / 2].z, kr[k / 2].w) : codes8(kr[k / 2].x, kr[k / 2].y);
+#pragma unroll
+      for (int d = 0; d < VL; ++d) {
+        const int dt = wave * VL + d;
+        if (DT % 4 == 0 || dt < DT) {
+          vb[buf][dt][0][lane] = codes8(vr[d].x, vr[d].y);
+          vb[buf][dt][1][lane] = codes8(vr[d].z, vr[d].w);
+        }
+      }
+      const float ksc[4] = {ks.x, ks.y, ks.z, ks.w};
+      const float4 vsn = vs;
+      const bool now_bad = bad;
+      if (pg + 1 < rg.pend) {
+        load(pid1);
+        pid1 = pg + 2 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[pg + 2]) : 0;
+      }
+      __syncthreads();
+      const int t0 = pg * kPage;
+      if (now_bad && threadIdx.x == 0) raise_status(a.b.status, ZOACT_STATUS_BAD_ENTRY);
+      if (now_bad || t0 > wlast) continue;            // nothing here that the wave's columns see
+      const bool edge = t0 + kPage > wfirst + 1;
+      float vsc[4];
+      const int vold = vexp;
+      value_scales(vsn, t0, wlast, vexp, vsc);
+      float s[CT][4][4];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        floatx4 acc[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const f16x8 kf = kb[buf][n][k][lane];
+#pragma unroll
+          for (int q = 0; q < NT; ++q)
+#pragma unroll
+            for (int t = 0; t < CT; ++t)
+              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][k][q], acc[t], 0, 0, 0);
+        }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const float f = ksc[n] * qs[t];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[t][n][i] = acc[t][i] * f;
+        }
+      }
+      f16x8 pf[CT][2][NT];
+      float alpha[CT];
+#pragma unroll
+      for (int t = 0; t < CT; ++t) {
+        soft_page<NT>(s[t], t0, tcol[t], edge, g, vsc, m[t], l[t], alpha[t], pf[t]);
+        alpha[t] = __builtin_amdgcn_ldexpf(alpha[t], vold - vexp);
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const f16x8 v0 = vb[buf][d][0][lane], v1 = vb[buf][d][1][lane];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          floatx4 acc = o[t][d] * alpha[t];
+#pragma unroll
+          for (int q = 0; q < NT; ++q) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0][q], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1][q], acc, 0, 0, 0);
+          }
+          o[t][d] = acc;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < CT; ++t) {
+    const int col = w0 + 16 * t + (lane & 15);
+    l[t] += __shfl_xor(l[t], 16, 64);
+    l[t] += __shfl_xor(l[t], 32, 64);
+    if (col >= ncol) continue;
+    const int oj = col / a.G, oh = hk * a.G + col % a.G;
+    const float div = l[t] == 0.f ? 1.f : l[t];
+    const int64_t R = (((int64_t)blockIdx.z * a.b.max_new + oj) * a.H + oh) * a.S + split;
+    if (a.S > 1 && g == 0) a.ml[R] = make_float2(m[t], l[t]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      float r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[t][d][i], vexp - kPExp);
+      const int d0 = d * 16 + 4 * g;
+      if (a.S > 1) {
+        if (l[t] != 0.f) *reinterpret_cast<float4*>(a.part + R * HD + d0) = make_float4(r[0], r[1], r[2], r[3]);
+      } else {
+        T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<uint2*>(op) =
+              make_uint2((uint32_t)f2bf(r[0] / div) | (uint32_t)f2bf(r[1] / div) << 16,
+                         (uint32_t)f2bf(r[2] / div) | (uint32_t)f2bf(r[3] / div) << 16);
+        } else {
+          *reinterpret_cast<float4*>(op) = make_float4(r[0] / div, r[1] / div, r[2] / div, r[3] / div);
+        }
+      }
+    }
+  }
+}
+
+// Joins the splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits.  The
+// statistics come first, a thread each: their maximum and the weights are ready in LDS before the sums
+// are read.
+constexpr int kMaxSplits = 128;
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
-  constexpr int NG = 256 / HD;
-  __shared__ float sr[NG][HD], sw[NG];
+  constexpr int DV = HD / 32;
+  __shared__ float wt[kMaxSplits], sr[8][HD], red[4], redl[2];
   const int i = blockIdx.z, j = blockIdx.y, h = blockIdx.x;
   const CacheEntry e = read_entry(a.c, a.b, i, false);
   if (j >= e.count) return;
-  const int d = threadIdx.x % HD, grp = threadIdx.x / HD;
   const int64_t R = (((int64_t)i * a.b.max_new + j) * a.H + h) * a.S;
-  float M = -INFINITY;
-  for (int s = 0; s < a.S; ++s) M = fmaxf(M, a.ml[R + s].x);
-  const float base = M == -INFINITY ? 0.f : M;
-  float L = 0.f, r = 0.f;
-  for (int s = grp; s < a.S; s += NG) {
-    const float2 ml = a.ml[R + s];
-    if (ml.y == 0.f) continue;
-    const float f = __builtin_amdgcn_exp2f(ml.x - base);
-    L += f * ml.y;
-    r += f * a.part[(R + s) * HD + d];
-  }
-  sr[grp][d] = r;
-  if (d == 0) sw[grp] = L;
-  __syncthreads();
-  if (grp) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  float2 ml = make_float2(-INFINITY, 0.f);
+  if (tid < a.S) ml = a.ml[R + tid];
+  float M = ml.x;
 #pragma unroll
-  for (int k = 1; k < NG; ++k) {
-    r += sr[k][d];
-    L += sw[k];
+  for (int k = 1; k < 64; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
+  if (lane == 0) red[wave] = M;
+  __syncthreads();
+  M = fmaxf(red[0], red[1]);
+  const float base = M == -INFINITY ? 0.f : M;
+  float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - base);
+  if (tid < kMaxSplits) wt[tid] = f;
+  float L = f * ml.y;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) L += __shfl_xor(L, k, 64);
+  if (lane == 0 && wave < 2) redl[wave] = L;
+  __syncthreads();
+  L = redl[0] + redl[1];
+  const int grp = tid >> 5, d0 = (tid & 31) * DV;
+  float r[DV];
+#pragma unroll
+  for (int k = 0; k < DV; ++k) r[k] = 0.f;
+#pragma unroll 4
+  for (int s = grp; s < a.S; s += 8) {
+    const float w = wt[s];
+    if (w == 0.f) continue;      // (an empty split has written no sums)
+#pragma unroll
+    for (int k = 0; k < DV; ++k) r[k] += w * a.part[(R + s) * HD + d0 + k];
   }
-  const float y = L == 0.f ? 0.f : r / L;
-  T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + j) * a.H + h) * HD + d;
+#pragma unroll
+  for (int k = 0; k < DV; ++k) sr[grp][d0 + k] = r[k];
+  __syncthreads();
+  if (tid >= HD) return;
+  float y = sr[0][tid];
+#pragma unroll
+  for (int k = 1; k < 8; ++k) y += sr[k][tid];
+  y = L == 0.f ? 0.f : y / L;
+  T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + j) * a.H + h) * HD + tid;
   if constexpr (sizeof(T) == 2)
     *op = f2bf(y);
   else
     *op = y;
 }
 
+// Query columns of a workgroup: 16 while that holds an entry's (decoding), 64 or 128 for chunks of rows.
+int attend_cols(int32_t dtype, const zoact_cache_batch& b, int G) {
+  const int64_t cols = (int64_t)b.max_new * G;
+  return cols <= 16 ? 16 : cols <= 64 || dtype == ZOACT_F32 ? 64 : 128;
+}
+
 template <typename T, int HD, int NT>
-void run_attend(const AttendArgs& a, hipStream_t s) {
-  const int tiles = (int)(((int64_t)a.b.max_new * a.G + 15) / 16);
-  const dim3 grid((unsigned)(tiles * a.S), (unsigned)a.c.n_kv_heads, (unsigned)a.b.n);
-  attend_kernel<T, HD, NT><<<grid, 256, 0, s>>>(a);
+void run_attend(const AttendArgs& a, int w, hipStream_t s) {
+  const int tiles = (int)(((int64_t)a.b.max_new * a.G + w - 1) / w);
+  const dim3 grid((unsigned)(tiles * a.S * a.c.n_kv_heads), 1, (unsigned)a.b.n);
+  if (w == 16)
+    attend_kernel<T, HD, NT><<<grid, 256, 0, s>>>(a);
+  else if (w == 64)
+    attend_chunk_kernel<T, HD, NT, 1><<<grid, 256, 0, s>>>(a);
+  else if constexpr (NT == 1)
+    attend_chunk_kernel<T, HD, NT, 2><<<grid, 256, 0, s>>>(a);
   if (a.S > 1) {
     const dim3 join((unsigned)a.H, (unsigned)a.b.max_new, (unsigned)a.b.n);
     attend_join_kernel<T, HD><<<join, 256, 0, s>>>(a);
   }
 }
 
-constexpr int kMaxSplits = 128;
-
-// Splits of the length: about four workgroups a compute unit, at least four pages each.
-int attend_splits(const zoact_cache& c, const zoact_cache_batch& b, int n_heads, int64_t max_len) {
-  const int ncu = cu_count();
-  const int64_t tiles = ((int64_t)b.max_new * (n_heads / c.n_kv_heads) + 15) / 16;
+// Splits of the length.  Sixteen pages each (four a wave) where that gives two workgroups a compute unit,
+// else as few as four pages, so that sequences of unequal length end together and a single one fills the
+// chip; the join reads 2 KB for 256 KB of such a split.
+int attend_splits(const zoact_cache& c, const zoact_cache_batch& b, int n_heads, int w, int64_t max_len) {
+  const int G = n_heads / c.n_kv_heads;
+  const int64_t tiles = ((int64_t)b.max_new * G + w - 1) / w;
   const int64_t groups = tiles * c.n_kv_heads * b.n;
   const int64_t pages = (max_len + kPage - 1) / kPage;
-  int64_t s = (4 * (ncu > 0 ? ncu : 256) + groups - 1) / groups;
+  const int64_t want = 2 * (cu_count() > 0 ? cu_count() : 256);
+  int64_t s = (pages + 15) / 16;
+  if (groups * s < want) s = (want + groups - 1) / groups;
+  if (w > 16 && 2 * groups >= want) s = 1;                              // (a chunk's own tiles are many)
   if (s > (pages + 3) / 4) s = (pages + 3) / 4;
   if (s > kMaxSplits) s = kMaxSplits;
   // (the second pass has a grid row per new row)
@@ -359,7 +685,11 @@ extern "C" size_t zoact_attention_cache_workspace_bytes(const zoact_cache* c, co
   if (check_cache(c) != ZOACT_OK || check_batch(b, c) != ZOACT_OK || n_heads < 1 || n_heads % c->n_kv_heads != 0 ||
       max_len < 1)
     return 0;
-  return attend_ws(*c, *b, n_heads, attend_splits(*c, *b, n_heads, max_len));
+  // (of the types' widths the one with more splits)
+  const int G = n_heads / c->n_kv_heads;
+  const int s0 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_BF16, *b, G), max_len);
+  const int s1 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_F32, *b, G), max_len);
+  return attend_ws(*c, *b, n_heads, s0 > s1 ? s0 : s1);
 }
 
 extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t layer, const void* q, int64_t ldq,
@@ -379,14 +709,16 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   ZA(max_len >= 1, "attention_cache: max_len must be at least 1");
   ZA((cos_t == nullptr) == (sin_t == nullptr), "attention_cache: both rotary tables or neither");
   ZA(cos_t == nullptr || n_pos >= 1, "attention_cache: empty rotary table");
+  ZA(al16(cos_t) && al16(sin_t), "attention_cache: rotary tables must be 16-byte aligned");
   AttendArgs a{};
   a.c = *c;
   a.b = *b;
   a.layer = layer;
   a.H = n_heads;
   a.G = n_heads / c->n_kv_heads;
-  ZA((int64_t)b->max_new * a.G < INT32_MAX / kMaxSplits, "attention_cache: too many new rows");
-  a.S = attend_splits(*c, *b, n_heads, max_len);
+  ZA((int64_t)b->max_new * n_heads < INT32_MAX / kMaxSplits, "attention_cache: too many new rows");
+  const int w = attend_cols(dtype, *b, a.G);
+  a.S = attend_splits(*c, *b, n_heads, w, max_len);
   const size_t need = attend_ws(*c, *b, n_heads, a.S);
   if (ws == nullptr || ws_bytes < need) a.S = 1;
   if (a.S > 1) ZA(al16(ws), "attention_cache: ws must be 16-byte aligned");
@@ -404,13 +736,13 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   }
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
 #define ZO_ATTEND(T, NT)                                       \
-  if (c->head_dim == 128) run_attend<T, 128, NT>(a, s);        \
-  else if (c->head_dim == 64) run_attend<T, 64, NT>(a, s);     \
-  else run_attend<T, 32, NT>(a, s);
+  if (c->head_dim == 128) run_attend<T, 128, NT>(a, w, s);        \
+  else if (c->head_dim == 64) run_attend<T, 64, NT>(a, w, s);     \
+  else run_attend<T, 32, NT>(a, w, s);
   if (dtype == ZOACT_BF16) {
-    ZO_ATTEND(uint16_t, 2)
+    ZO_ATTEND(uint16_t, 1)
   } else {
-    ZO_ATTEND(float, 3)
+    ZO_ATTEND(float, 2)
   }
 #undef ZO_ATTEND
   const hipError_t err = hipGetLastError();

@@ -605,6 +605,7 @@ extern "C" zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, 
      "cache_append: rows must hold the heads and be 16-byte aligned");
   ZC((cos_t == nullptr) == (sin_t == nullptr), "cache_append: both rotary tables or neither");
   ZC(cos_t == nullptr || n_pos >= 1, "cache_append: empty rotary table");
+  ZC(al16(cos_t) && al16(sin_t), "cache_append: rotary tables must be 16-byte aligned");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
 #define ZO_APPEND(T, HD) run_append<T, HD>(*c, layer, k, ldk, v, ldv, *b, cos_t, sin_t, n_pos, s)
   if (dtype == ZOACT_BF16) {

@@ -193,14 +193,16 @@ def attend(q, k, v, pos, scale, rope=None):
 def attend_bound(out, mean, mag, n, hd, fp32):
     """Largest error of the kernel's result by its own roundings.
 
-    A score's error is that of q's terms (2^-17 relative in two bf16 terms, 2^-25 in three), of the rotation
-    (two roundings, 2^-23), of the fp32 sum of hd products and of two scale products (hd + 4 steps of at
-    most 2^-23), all relative to sum |q k| scale = mag; the exponential adds 2^-21 and, for its argument's
-    rounding in the log2 domain, 2^-23 times the score again.  A relative error e of the weights moves the
-    result by at most 2 e times the weighted mean of |v|.  Weights enter the second product in the same
-    number of terms; its sum and the normaliser's have n + 8 steps and the joins of waves and splits 140.
+    A score's error is that of q's f16 terms (half a step: 2^-12 relative in one term, 2^-23 in two, as the
+    second rounds what is left, at most 2^-12 of q, to 2^-12 again or -- far below the column's largest --
+    to a fixed 2^-39 of that), of the rotation (two roundings, 2^-23), of the fp32 sum of hd products and of
+    two scale products (hd + 4 steps of at most 2^-23), all relative to sum |q k| scale = mag; the
+    exponential adds 2^-21 and, for its argument's rounding in the log2 domain, 2^-23 times the score again.
+    A relative error e of the weights moves the result by at most 2 e times the weighted mean of |v|.
+    Weights enter the second product in the same number of terms; its sum and the normaliser's have n + 8
+    steps and the joins of waves and splits 140.
     """
-    term = 2.0 ** -25 if fp32 else 2.0 ** -17
+    term = 2.0 ** -23 if fp32 else 2.0 ** -12
     e = mag * (term + (hd + 8) * 2.0 ** -23) + 2.0 ** -21
     t = 2 * e * mean + mean * (2 * term + 2 * (n + 150) * 2.0 ** -23)
     return t + np.abs(out) * (2.0 ** -24 if fp32 else 2.0 ** -8) + 1e-30
