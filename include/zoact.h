@@ -304,10 +304,10 @@ size_t zoact_linear_workspace_bytes(void);
  * L->coef_offset; L->ch and L->ut are not read.  Features [plain_begin, plain_end) have no
  * correction (any bounds here).  Sums are fp32 and a group's scale multiplies the group's
  * sum: unlike the products of two or more halves, q * s is not rounded to bf16 first.
- * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0; d_out % 16 == 0 (32 with SWIGLU); flags:
- * ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, p, y and residual 16-byte aligned.  L->ws
- * (optional, as above) lets the depth of narrow layers be split over workgroups; the partial
- * sums are added in a fixed order. */
+ * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU); flags:
+ * ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, w_scales, p, y and residual 16-byte aligned.
+ * L->ws (optional, as above) lets the depth of narrow layers be split over workgroups; the
+ * partial sums are added in a fixed order.  Calls that overlap on one workspace race. */
 enum { ZOACT_ROWS_MAX = 64 };
 zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, const void* x, int64_t rows, const void* p,
                                const void* residual, uint32_t flags, void* y, int32_t y_dtype, zoact_stream stream);

@@ -220,8 +220,8 @@ zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, cons
   if (L->w_dtype != ZOACT_INT4_G128) return fail(ZOACT_E_UNSUPPORTED, "linear_rows: INT4 weights only");
   CHECK(L->w_scales != nullptr, "linear_rows: INT4 needs w_scales");
   CHECK(rows >= 1 && rows <= ZOACT_ROWS_MAX, "linear_rows: rows=%lld outside [1, %d]", (long long)rows, ZOACT_ROWS_MAX);
-  CHECK(L->d_in >= 128 && L->d_in % 128 == 0 && L->d_in < (1 << 30), "linear_rows: d_in=%lld must be a multiple of 128",
-        (long long)L->d_in);
+  CHECK(L->d_in >= 128 && L->d_in % 128 == 0 && L->d_in <= (1 << 23),
+        "linear_rows: d_in=%lld must be a multiple of 128 up to 2^23", (long long)L->d_in);
   CHECK((flags & ~(uint32_t)(ZOACT_EPI_SWIGLU | ZOACT_EPI_RELU)) == 0, "linear_rows: unknown flags 0x%x", flags);
   CHECK(!((flags & ZOACT_EPI_SWIGLU) && (flags & ZOACT_EPI_RELU)), "linear_rows: SWIGLU and RELU are exclusive");
   const int64_t unit = (flags & ZOACT_EPI_SWIGLU) ? 32 : 16;
@@ -232,8 +232,8 @@ zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, cons
   CHECK(aligned16(x) && aligned16(L->w) && aligned16(y) && (!residual || aligned16(residual)) && (!p || aligned16(p)),
         "linear_rows: x, w, p, y and residual must be 16-byte aligned");
   CHECK(L->ws == nullptr || aligned16(L->ws), "linear_rows: ws must be 16-byte aligned");
-  CHECK((reinterpret_cast<uintptr_t>(L->w_scales) & 1) == 0 && (reinterpret_cast<uintptr_t>(L->bias) & 1) == 0,
-        "linear_rows: scales and bias must be 2-byte aligned");
+  CHECK(aligned16(L->w_scales) && (reinterpret_cast<uintptr_t>(L->bias) & 1) == 0,
+        "linear_rows: w_scales must be 16-byte aligned, bias 2-byte");
   if (L->r > 0) {
     CHECK(p != nullptr, "linear_rows: r > 0 needs p");
     CHECK(A != nullptr && A->c != nullptr, "linear_rows: r > 0 needs an arena");

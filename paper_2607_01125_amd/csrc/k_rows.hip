@@ -10,7 +10,6 @@
 // group's sum from a product of x with a constant -24, which costs one product for all weight rows
 // of the wave.  The group's sum is then scaled: one multiply-add a lane and group, no rounding of
 // q s.  The columns of a word come as pairs (i, i + 4), so x is put in that order instead.
-// The waves of a workgroup share out the groups; their sums meet in LDS in a fixed order.
 #include <string>
 
 #include "common.hpp"
@@ -31,6 +30,8 @@ struct RowsArgs {
   int rows;
   int64_t N;
   int K, groups;       // groups = K / 128
+  int per_split;       // groups of one part of the depth
+  float* part;         // partial sums, or NULL for one part
   void* y;
   int y_f32;
   uint32_t flags;
@@ -57,6 +58,8 @@ __device__ __forceinline__ bf16x8 pair_order(uint4 u) {
 
 // Eight coefficients (or values of p) from column i0 on, zeros past r.
 __device__ __forceinline__ bf16x8 tail8(const uint16_t* row, int i0, int r, bool in) {
+  if ((r & 7) == 0 && ((uintptr_t)row & 15) == 0)      // (whole pieces, all lanes alike: r and the base are scalar)
+    return in && i0 < r ? *reinterpret_cast<const bf16x8*>(row + i0) : bf16x8{};
   uint16_t v[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = in && i0 + e < r ? row[i0 + e] : (uint16_t)0;
@@ -69,78 +72,177 @@ __device__ __forceinline__ bf16x8 tail8(const float* row, int i0, int r, bool in
   return v;
 }
 
-// RT: tiles of 16 weight rows of a workgroup (2 with SwiGLU: a gate and its up tile); NB: blocks
-// of 16 rows of x; NW: waves.
-template <int RT, int NB, int NW>
+// y of one row of x and one feature from its sum (SwiGLU: the gate's; `up` the up feature's, 16 further).
+__device__ __forceinline__ void finish(const RowsArgs& a, int row, int64_t n, float y, float up) {
+  if (a.bias) y += bf2f(a.bias[n]);
+  if (a.res) y += bf2f(a.res[(int64_t)row * a.N + n]);
+  int64_t at = (int64_t)row * a.N + n;
+  if (a.flags & ZOACT_EPI_SWIGLU) {
+    if (a.bias) up += bf2f(a.bias[n + 16]);
+    if (a.res) up += bf2f(a.res[(int64_t)row * a.N + n + 16]);
+    y = y / (1.f + __expf(-y)) * up;
+    at = (int64_t)row * (a.N / 2) + n / 32 * 16 + (n & 15);
+  } else if (a.flags & ZOACT_EPI_RELU) {
+    y = y > 0.f ? y : y != y ? y : 0.f;
+  }
+  if (a.y_f32)
+    static_cast<float*>(a.y)[at] = y;
+  else
+    static_cast<uint16_t*>(a.y)[at] = f2bf(y);
+}
+
+// Coefficient row of feature n, or -1 where it has none.
+__device__ __forceinline__ int64_t coef_row(const RowsArgs& a, int64_t n) {
+  return n >= a.N || (n >= a.plain0 && n < a.plain1) ? -1 : n >= a.plain1 ? n - (a.plain1 - a.plain0) : n;
+}
+
+// RT tiles of 16 weight rows and NB blocks of 16 rows of x a workgroup (XR rows of x in LDS: 4, or 16 NB),
+// depth in stages of WK groups.  Weights and x come in whole rows' pieces (a quad of lanes reads 64
+// contiguous bytes), P stages ahead in registers, and go through LDS to the operands' order: read straight
+// from memory, an operand's load touches 16 rows, four in every quad, and the address unit bounds the
+// kernel (20480 x 5120, 13 rows: 39 us, against 22).  16-byte pieces are swapped by the row's number, so
+// that neither side of LDS has bank conflicts.  Scales come 32 groups at a time for the same reason.
+// Wave w takes group w % WK of a stage and the tiles from w / WK on; the waves' sums meet in LDS in a
+// fixed order.  blockIdx.y: the part of the depth (partial sums go to part, rows_join_kernel adds them).
+// (Tried and left: one workgroup of 16 waves a compute unit with all of x in LDS and weights streamed
+// past it, 7.0 us for 4096 x 4096 at one row, 11.4 at 16; dot products on the vector units for one row,
+// 23 us for 4096 x 28672.)
+constexpr int kWindow = 32;
+template <int RT, int NB, int XR, int NW, int WK, int P>
 __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
-  __shared__ floatx4 sum[NW][RT][NB][64];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int64_t n0 = (int64_t)blockIdx.x * RT * 16;
-  floatx4 tot[RT][NB];
+  constexpr int WR = NW / WK, TW = RT / WR;              // waves along the tiles, tiles of a wave
+  constexpr int WP = 4 * WK, XP = 16 * WK;               // 16-byte pieces of a stage's weight row and x row
+  constexpr int WN = RT * 16 * WP, XN = XR * XP;         // pieces of a stage
+  constexpr int TH = 64 * NW, WL = (WN + TH - 1) / TH, XL = (XN + TH - 1) / TH;
+  constexpr int STAGE = WN + XN;
+  constexpr int SUMS = WK * RT * NB * 64;                // floatx4 of the waves' sums
+  constexpr int LDS = 2 * STAGE > SUMS ? 2 * STAGE : SUMS;
+  constexpr int BN = RT * 16, SL = BN * kWindow / TH;
+  __shared__ uint4 lds[LDS];
+  __shared__ uint16_t scl[2][BN][kWindow + 2];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15,
+            g = lane >> 4;
+  const int wk = wave % WK, wr = wave / WK;
+  const int64_t n0 = (int64_t)blockIdx.x * BN;
+  const int gbeg = blockIdx.y * a.per_split, gend = gbeg + a.per_split < a.groups ? gbeg + a.per_split : a.groups;
+  const int stages = (gend - gbeg + WK - 1) / WK;
+  const int64_t rows_here = a.N - n0 < BN ? a.N - n0 : BN;
+  const __amdgpu_buffer_rsrc_t wrs = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(a.w) + n0 * (a.K / 2), 0, (int)(rows_here * (a.K / 2)), 0x00020000);
+  const __amdgpu_buffer_rsrc_t xrs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x), 0, a.rows * a.K * 2, 0x00020000);
+  const uint16_t* const srow = a.sc + n0 * a.groups;
+  // pieces swapped within 16 (8) by the row's number
+  auto swap = [](int row, int piece) { return WK >= 4 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7); };
+
+  uint4 wv[P][WL], xv[P][XL];
+  uint16_t sv[SL];
+  // (past the part's last group there is nothing: such pieces are asked for outside the descriptor)
+  auto load = [&](int i, int st) {
+    const int gr = gbeg + st * WK;
 #pragma unroll
-  for (int t = 0; t < RT; ++t)
+    for (int j = 0; j < WL; ++j) {
+      const int u = tid + j * TH, row = u / WP, piece = u % WP;
+      if (WN % TH == 0 || u < WN)
+        wv[i][j] = __builtin_bit_cast(
+            uint4, __builtin_amdgcn_raw_buffer_load_b128(
+                       wrs, gr + piece / 4 < gend ? row * (a.K / 2) + gr * 64 + piece * 16 : 0x7FFF0000, 0, 0));
+    }
+#pragma unroll
+    for (int j = 0; j < XL; ++j) {
+      const int u = tid + j * TH, row = u / XP, piece = u % XP;
+      if ((XN % TH == 0 || u < XN) && row < a.rows)
+        xv[i][j] = __builtin_bit_cast(
+            uint4, __builtin_amdgcn_raw_buffer_load_b128(
+                       xrs, gr + piece / 16 < gend ? row * a.K * 2 + gr * 256 + piece * 16 : 0x7FFF0000, 0, 0));
+    }
+  };
+  auto load_scales = [&](int g0) {
+#pragma unroll
+    for (int j = 0; j < SL; ++j) {
+      const int u = tid + j * TH, row = u / kWindow, gr = g0 + u % kWindow;
+      sv[j] = row < rows_here && gr < gend ? srow[(int64_t)row * a.groups + gr] : (uint16_t)0;
+    }
+  };
+  floatx4 tot[TW][NB];
+#pragma unroll
+  for (int t = 0; t < TW; ++t)
 #pragma unroll
     for (int b = 0; b < NB; ++b) tot[t][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-  // weight rows of the lane (rows past the last repeat it; they are not stored)
-  const uint8_t* wrow[RT];
-  const uint16_t* srow[RT];
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    int64_t n = n0 + t * 16 + l16;
-    if (n >= a.N) n = a.N - 1;
-    wrow[t] = a.w + n * (a.K / 2) + 16 * g;
-    srow[t] = a.sc + n * a.groups;
-  }
-  const uint16_t* xrow[NB];
-#pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int t = b * 16 + l16;
-    xrow[b] = a.x + (int64_t)(t < a.rows ? t : a.rows - 1) * a.K + 32 * g;
-  }
   const uint32_t m24 = 0xC1C0C1C0u;                  // (-24, -24)
   const bf16x8 minus24 = __builtin_bit_cast(bf16x8, make_uint4(m24, m24, m24, m24));
-
-#pragma unroll 2
-  for (int gr = wave; gr < a.groups; gr += NW) {
-    uint4 wv[RT];
-    float s[RT];
+  load_scales(gbeg);
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      wv[t] = *reinterpret_cast<const uint4*>(wrow[t] + (int64_t)gr * 64);
-      s[t] = bf2f(srow[t][gr]);
-    }
-    bf16x8 xf[NB][4];
-    floatx4 off[NB];
+  for (int i = 0; i < P; ++i)
+    if (i < stages) load(i, i);
+  // rows of x past the last are never loaded: both buffers start with zeros there
+  for (int u = tid; u < XN; u += TH)
+    if (u / XP >= a.rows) lds[WN + u] = lds[STAGE + WN + u] = make_uint4(0, 0, 0, 0);
+  for (int s0 = 0; s0 < stages; s0 += P) {
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
+    for (int i = 0; i < P; ++i) {
+      const int st = s0 + i;
+      if (st >= stages) break;
+      uint4* const wb = lds + (st & 1) * STAGE;
+      uint4* const xb = wb + WN;
+      const int win = st / (kWindow / WK), in_win = st % (kWindow / WK);
+      if (in_win == 0) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        xf[b][j] = pair_order(*reinterpret_cast<const uint4*>(xrow[b] + (int64_t)gr * 128 + 8 * j));
-      off[b] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) off[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], minus24, off[b], 0, 0, 0);
-    }
-#pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const uint32_t wd[4] = {wv[t].x, wv[t].y, wv[t].z, wv[t].w};
-      floatx4 acc[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b] = off[b];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const bf16x8 wf = nibbles(wd[j]);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], wf, acc[b], 0, 0, 0);
+        for (int j = 0; j < SL; ++j) {
+          const int u = tid + j * TH;
+          scl[win & 1][u / kWindow][u % kWindow] = sv[j];
+        }
+        if (st + kWindow / WK < stages) load_scales(gbeg + (win + 1) * kWindow);
       }
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int j = 0; j < WL; ++j) {
+        const int u = tid + j * TH, row = u / WP, piece = u % WP;
+        if (WN % TH == 0 || u < WN) wb[row * WP + swap(row, piece)] = wv[i][j];
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tot[t][b][i] = fmaf(s[t], acc[b][i], tot[t][b][i]);
+      for (int j = 0; j < XL; ++j) {
+        const int u = tid + j * TH, row = u / XP, piece = u % XP;
+        if ((XN % TH == 0 || u < XN) && row < a.rows) xb[row * XP + (piece ^ (row & 15))] = xv[i][j];
+      }
+      if (st + P < stages) load(i, st + P);
+      __syncthreads();
+      if (gbeg + st * WK + wk >= gend) continue;
+      bf16x8 xf[NB][4];
+      floatx4 off[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int xrow = XR < 16 ? l16 & (XR - 1) : b * 16 + l16;
+        off[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          xf[b][j] = pair_order(xb[xrow * XP + ((wk * 16 + g * 4 + j) ^ (xrow & 15))]);
+          off[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], minus24, off[b], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < TW; ++t) {
+        const int row = (wr * TW + t) * 16 + l16;
+        const uint4 v = wb[row * WP + swap(row, wk * 4 + g)];
+        const uint32_t wd[4] = {v.x, v.y, v.z, v.w};
+        const float sc = bf2f(scl[win & 1][row][in_win * WK + wk]);
+        floatx4 acc[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = off[b];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x8 wf = nibbles(wd[j]);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], wf, acc[b], 0, 0, 0);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) tot[t][b][k] = fmaf(sc, acc[b][k], tot[t][b][k]);
+      }
     }
   }
-  // the correction, 32 ranks a step, the steps shared out over the waves
-  for (int i0 = 32 * wave; i0 < a.r; i0 += 32 * NW) {
+  // the correction, 32 ranks a step, the steps shared out over the waves of a tile
+  for (int i0 = 32 * wk; i0 < a.r && blockIdx.y == 0; i0 += 32 * WK) {
     bf16x8 pf[NB];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -148,69 +250,132 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
       pf[b] = tail8(a.p + (int64_t)(t < a.rows ? t : a.rows - 1) * a.r, i0 + 8 * g, a.r, true);
     }
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int64_t n = n0 + t * 16 + l16;
-      const bool in = n < a.N && !(n >= a.plain0 && n < a.plain1);
-      const int64_t row = !in ? 0 : n >= a.plain1 ? n - (a.plain1 - a.plain0) : n;
-      const bf16x8 cf = a.c_f32 ? tail8(static_cast<const float*>(a.c) + row * a.r, i0 + 8 * g, a.r, in)
-                                : tail8(static_cast<const uint16_t*>(a.c) + row * a.r, i0 + 8 * g, a.r, in);
+    for (int t = 0; t < TW; ++t) {
+      const int64_t c = coef_row(a, n0 + (wr * TW + t) * 16 + l16), row = c < 0 ? 0 : c;
+      const bf16x8 cf = a.c_f32 ? tail8(static_cast<const float*>(a.c) + row * a.r, i0 + 8 * g, a.r, c >= 0)
+                                : tail8(static_cast<const uint16_t*>(a.c) + row * a.r, i0 + 8 * g, a.r, c >= 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b) tot[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[b], cf, tot[t][b], 0, 0, 0);
     }
   }
-#pragma unroll
-  for (int t = 0; t < RT; ++t)
-#pragma unroll
-    for (int b = 0; b < NB; ++b) sum[wave][t][b][lane] = tot[t][b];
   __syncthreads();
-  // lane (g, l16) of a tile: rows 4 g + i of x, feature l16
+  floatx4* const sum = reinterpret_cast<floatx4*>(lds);      // [WK][RT][NB][64]
+#pragma unroll
+  for (int t = 0; t < TW; ++t)
+#pragma unroll
+    for (int b = 0; b < NB; ++b) sum[((wk * RT + wr * TW + t) * NB + b) * 64 + lane] = tot[t][b];
+  __syncthreads();
+  // lane (g, l16) of a tile: rows 4 g + k of x, feature l16
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
-  constexpr int UNITS = RT * NB * 64;
-  for (int u = threadIdx.x; u < UNITS; u += 64 * NW) {
+  for (int u = tid; u < RT * NB * 64; u += TH) {
     const int ul = u & 63, b = (u >> 6) % NB, t = (u >> 6) / NB;
-    if (swiglu && (t & 1)) continue;
+    floatx4 z{0.f, 0.f, 0.f, 0.f}, up{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < WK; ++w) z += sum[((w * RT + t) * NB + b) * 64 + ul];
+    if (a.part) {
+      if (n0 + t * 16 < a.N)
+        reinterpret_cast<floatx4*>(a.part)[(blockIdx.y * (a.N / 16) + blockIdx.x * (int64_t)RT + t) * (NB * 64) + b * 64 + ul] = z;
+      continue;
+    }
     const int64_t n = n0 + t * 16 + (ul & 15);
-    if (n >= a.N) continue;
-    floatx4 z[2];
+    if (n >= a.N || (swiglu && (t & 1))) continue;
+    if (swiglu) {
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (k && !swiglu) break;
-      const int tt = RT > 1 ? t + k : t;
-      floatx4 v = sum[0][tt][b][ul];
-#pragma unroll
-      for (int w = 1; w < NW; ++w) v += sum[w][tt][b][ul];
-      z[k] = v;
+      for (int w = 0; w < WK; ++w) up += sum[((w * RT + t + (RT > 1 ? 1 : 0)) * NB + b) * 64 + ul];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = b * 16 + 4 * (ul >> 4) + i;
-      if (row >= a.rows) continue;
-      float y = z[0][i];
-      if (a.bias) y += bf2f(a.bias[n]);
-      if (a.res) y += bf2f(a.res[(int64_t)row * a.N + n]);
-      int64_t at = (int64_t)row * a.N + n;
-      if (swiglu) {
-        float up = z[1][i];
-        if (a.bias) up += bf2f(a.bias[n + 16]);
-        if (a.res) up += bf2f(a.res[(int64_t)row * a.N + n + 16]);
-        y = y / (1.f + __expf(-y)) * up;
-        at = (int64_t)row * (a.N / 2) + n / 32 * 16 + (n & 15);
-      } else if (a.flags & ZOACT_EPI_RELU) {
-        y = y > 0.f ? y : y != y ? y : 0.f;
-      }
-      if (a.y_f32)
-        static_cast<float*>(a.y)[at] = y;
-      else
-        static_cast<uint16_t*>(a.y)[at] = f2bf(y);
+    for (int k = 0; k < 4; ++k) {
+      const int row = b * 16 + 4 * (ul >> 4) + k;
+      if (row < a.rows) finish(a, row, n, z[k], up[k]);
     }
   }
 }
 
-template <int RT, int NB, int NW>
-hipError_t go(const RowsArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)((a.N + 16 * RT - 1) / (16 * RT));
-  rows_kernel<RT, NB, NW><<<grid, 64 * NW, 0, s>>>(a);
+// Adds the parts of the depth in order and finishes: a thread per four rows of x and feature.  tiles: of
+// 16 features.
+template <int NB>
+__global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a, int splits, int64_t tiles) {
+  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, tile = u / (NB * 64);
+  const int ul = (int)(u & 63), b = (int)(u / 64 % NB);
+  const int64_t n = tile * 16 + (ul & 15);
+  const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
+  if (tile >= tiles || (swiglu && (tile & 1)) || b * 16 + 4 * (ul >> 4) >= a.rows) return;
+  const floatx4* const part = reinterpret_cast<const floatx4*>(a.part);
+  floatx4 z{0.f, 0.f, 0.f, 0.f}, up{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int s = 0; s < splits; ++s) {
+    const floatx4* const p = part + s * tiles * (NB * 64) + u;
+    z += p[0];
+    if (swiglu) up += p[NB * 64];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int row = b * 16 + 4 * (ul >> 4) + k;
+    if (row < a.rows) finish(a, row, n, z[k], up[k]);
+  }
+}
+
+
+// Parts of the depth: as many as wanted, of at least two stages of wk groups, and as the workspace holds.
+int splits_of(const RowsArgs& a, int64_t want, int wk, int NB, size_t ws_bytes) {
+  const int64_t deep = a.groups / wk / 2, room = (int64_t)(ws_bytes / ((size_t)(a.N / 16) * NB * 1024));
+  int64_t n = want < deep ? want : deep;
+  n = n < room ? n : room;
+  return n < 1 ? 1 : n > 64 ? 64 : (int)n;
+}
+
+template <int RT, int NB, int XR, int NW, int WK, int P>
+hipError_t go(RowsArgs a, int splits, void* ws, hipStream_t s) {
+  const unsigned tiles = (unsigned)((a.N + 16 * RT - 1) / (16 * RT));
+  const int stages = (a.groups + WK - 1) / WK, per = (stages + splits - 1) / splits;
+  a.per_split = per * WK;
+  splits = (stages + per - 1) / per;
+  a.part = splits > 1 ? static_cast<float*>(ws) : nullptr;
+  rows_kernel<RT, NB, XR, NW, WK, P><<<dim3(tiles, (unsigned)splits), 64 * NW, 0, s>>>(a);
+  if (splits > 1) rows_join_kernel<NB><<<(unsigned)((a.N / 16 * NB + 3) / 4), 256, 0, s>>>(a, splits, a.N / 16);
   return hipGetLastError();
+}
+
+// One block of 16 rows.  A workgroup's weights in flight and the workgroups of a compute unit (LDS: five of
+// 32 weight rows and four rows of x, three with sixteen) bound the time, so layers of few tiles get eight
+// waves on a tile, deep ones parts of the depth, wide ones larger tiles.  us on cold weights (columns x
+// features, 1 / 13 rows; the bytes alone, read in one piece, take the first figure):
+//   4096 x 4096   3.0: 16 weight rows, 8 waves  5.9 /  7.3;  32, 8 waves  6.8 /  8.5;  32, 4 waves  8.2 /  9.4
+//   4096 x 6144   3.7:                          7.1 / 10.0;               7.1 /  8.8;               8.8 / 11.4
+//   4096 x 28672 10.2: 32 weight rows, 4 waves 16.9 / 24.7;  64, 4 waves 17.7 / 20.8
+//   5120 x 20480  9.6:                         16.5 / 20.9;              20.9 / 24.5
+//   14336 x 4096  6.0: 32, 4 waves, 1 part     23.0 / 27.7;  4 parts     12.6 / 14.7;  8 parts     13.6 / 18.1
+//   20480 x 5120  9.6:                         32.1 / 38.9;              18.8 / 22.4;              18.7 / 22.5
+template <int XR>
+hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
+  const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
+  const int64_t t16 = a.N / 16;
+  if (a.K <= 8192 && t16 <= 2 * cus) {
+    if (t16 <= cus && !swiglu) return go<1, 1, XR, 8, 8, 1>(a, 1, nullptr, s);
+    return go<2, 1, XR, 8, 8, 1>(a, 1, nullptr, s);
+  }
+  const int64_t t32 = (t16 + 1) / 2;
+  if (t32 > (XR == 4 ? 4 : 3) * cus) return go<4, 1, XR, 4, 4, 1>(a, 1, nullptr, s);
+  const int64_t want = t32 < 2 * cus ? (2 * cus + t32 - 1) / t32 : 1;
+  return go<2, 1, XR, 4, 4, 1>(a, splits_of(a, want, 4, 1, ws_bytes), ws, s);
+}
+
+// 17 rows and more: 128 weight rows a workgroup, so that x, which every workgroup reads whole, is read
+// rarely; one workgroup a compute unit (4096 x 28672 at 64 rows 38 us, with 64 weight rows 55; 20480 x 5120
+// 38 us in 6 parts, 63 in 2).
+template <int NB>
+hipError_t pick_more(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
+  const int64_t t128 = (a.N / 16 + 7) / 8;
+  return go<8, NB, 16 * NB, 8, 2, 1>(a, splits_of(a, cus / t128, 2, NB, ws_bytes), ws, s);
+}
+
+hipError_t pick(const RowsArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {
+  const int cus = cu_count() > 0 ? cu_count() : 256;
+  if (a.rows <= 4) return pick16<4>(a, cus, ws, ws_bytes, s);
+  if (a.rows <= 16) return pick16<16>(a, cus, ws, ws_bytes, s);
+  if (a.rows <= 32) return pick_more<2>(a, cus, ws, ws_bytes, s);
+  if (a.rows <= 48) return pick_more<3>(a, cus, ws, ws_bytes, s);
+  return pick_more<4>(a, cus, ws, ws_bytes, s);
 }
 
 }  // namespace
@@ -238,9 +403,7 @@ hipError_t launch_linear_rows(const zoact_linear& L, const zoact_arena* A, const
   a.y = y;
   a.y_f32 = y_dtype == ZOACT_F32;
   a.flags = flags;
-  if (rows <= 16) return go<2, 1, 8>(a, s);
-  if (rows <= 32) return go<2, 2, 8>(a, s);
-  return go<2, 4, 8>(a, s);
+  return pick(a, L.ws, L.ws ? L.ws_bytes : 0, s);
 }
 
 }  // namespace zoact

@@ -542,67 +542,84 @@ STATUS_BAD_ENTRY, STATUS_NO_PAGES = 2, 4
 CACHE_PAGE, CACHE_BLOCK, CACHE_MAX_BATCH, ROWS_MAX = 64, 16, 1024, 64
 
 
-def _on_device(fn, dev: torch.device, stream, *args):
-    """Call `fn` with the stream (the current one of `dev` by default) as its last argument and `dev` as
+def _on_device(fn, dev: int, stream, *args):
+    """Call `fn` with a stream (the current one of device `dev` by default) as its last argument and `dev` as
     the current device: the tensors' device, whichever the caller's current one is."""
-    if stream is not None and stream.device != dev:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {dev}")
-    with torch.cuda.device(dev):
-        _check(fn(*args, _stream(stream)))
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(dev)
+    elif stream.device.index != dev:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{dev}")
+    else:
+        raw = stream.cuda_stream
+    if dev == torch.cuda.current_device():
+        st = fn(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, raw)
+    if st != OK:
+        _check(st)
 
 
-def _arg(t, name: str, dtype, dev: torch.device, shape=None):
-    """Pointer of a contiguous tensor argument (None stays None) after checking type, device and shape."""
+def _device(t: torch.Tensor) -> int:
+    if not t.is_cuda:
+        raise ValueError("expected a device tensor")
+    return t.get_device()
+
+
+def _arg(t, name: str, dtype, dev: int, shape=None):
+    """Address of a contiguous tensor argument (None stays None) after checking type, device and shape."""
     if t is None:
         return None
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
-        raise ValueError(f"{name}: dtype {t.dtype}")
-    if t.device != dev:
-        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return _ptr(t)
+    return t.data_ptr()
 
 
-def _heads_arg(t: torch.Tensor, name: str, dtype, dev: torch.device, rows: int, width: int):
-    """A [rows][width] argument that may be a column slice of a wider row-major buffer."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != width:
+def _heads_arg(t: torch.Tensor, name: str, dtype, dev: int, rows: int, width: int):
+    """Address and row stride of a [rows][width] argument that may be a column slice of a wider
+    row-major buffer."""
+    if t.shape != (rows, width):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, width)}")
-    if t.dtype != dtype or t.device != dev:
-        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {dtype} on {dev}")
-    if t.stride(1) != 1 or (rows > 1 and t.stride(0) < width):
+    if t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name}: {t.dtype} on {t.device}, expected {dtype} on cuda:{dev}")
+    ld, unit = t.stride()
+    if (unit != 1 and width > 1) or (rows > 1 and ld < width):
         raise ValueError(f"{name}: rows must be contiguous and apart")
-    # (the stride of a single row means nothing)
-    return _ptr(t), t.stride(0) if rows > 1 else (t.stride(0) if t.stride(0) >= width else width)
+    return t.data_ptr(), ld if rows > 1 else max(ld, width)     # (the stride of a single row means nothing)
 
 
 def linear_rows(layer: Linear, arena: Arena | None, x: torch.Tensor, p: torch.Tensor | None, y: torch.Tensor,
                 residual: torch.Tensor | None = None, flags: int = 0, stream=None):
     """y = epilogue(residual + x W^T + b + p bf16(C)^T) of 1 .. ROWS_MAX rows, INT4 weights, unperturbed."""
-    dev, bf = x.device, torch.bfloat16
+    dev, bf = _device(x), torch.bfloat16
     rows = x.shape[0] if x.dim() == 2 else -1
     xp = _arg(x, "x", bf, dev, (rows, layer.d_in))
     out = layer.d_out // 2 if flags & EPI_SWIGLU else layer.d_out
-    yp = _arg(y, "y", (bf, torch.float32), dev, (rows, out))
+    yd = dtype_code(y)
+    yp = _arg(y, "y", y.dtype, dev, (rows, out))
     rp = _arg(residual, "residual", bf, dev, (rows, layer.d_out))
     pp = _arg(p, "p", bf, dev, (rows, layer.r)) if layer.r else None
-    if layer.w.dtype == torch.uint8:
+    if layer.w.dtype is torch.uint8:
         _arg(layer.w, "w", torch.uint8, dev, (layer.d_out, layer.d_in // 2))
         _arg(layer.w_scales, "w_scales", bf, dev, (layer.d_out, layer.d_in // 128))
     _arg(layer.bias, "bias", bf, dev, (layer.d_out,))
-    if arena is not None and arena.c.device != dev:
-        raise ValueError(f"the arena is on {arena.c.device}, expected {dev}")
-    d = layer.desc()
-    a = arena.desc() if arena is not None else None
-    _on_device(lib().zoact_linear_rows, dev, stream, ctypes.byref(d), ctypes.byref(a) if a is not None else None, xp,
-               rows, pp, rp, flags, yp, dtype_code(y))
+    a = None
+    if layer.r and arena is not None:
+        _arg(arena.c, "arena.c", arena.c.dtype, dev)
+        a = ctypes.byref(arena.desc())
+    _on_device(lib().zoact_linear_rows, dev, stream, ctypes.byref(layer.desc()), a, xp, rows, pp, rp, flags, yp, yd)
 
 
-@dataclass
+@dataclass(frozen=True)
 class Cache:
-    """Device tensors of a paged 8-bit key/value cache (layouts: zoact_cache.h)."""
+    """Device tensors of a paged 8-bit key/value cache (layouts: zoact_cache.h).  They are checked once,
+    here; their contents change, the tensors do not."""
     k: torch.Tensor         # int8 [n_layers][n_pages][n_kv_heads][64][head_dim]
     v: torch.Tensor         # int8 [n_layers][n_pages][n_kv_heads][head_dim][64]
     k_scale: torch.Tensor   # fp32 [n_layers][n_pages][n_kv_heads][4]
@@ -610,6 +627,23 @@ class Cache:
     table: torch.Tensor     # int32 [n_slots][max_pages]
     len: torch.Tensor       # int32 [n_slots]
     refs: torch.Tensor      # int32 [n_pages]
+
+    def __post_init__(self):
+        if self.k.dim() != 5 or self.table.dim() != 2:
+            raise ValueError("cache: k must have 5 dimensions and table 2")
+        nl, npg, nh, page, hd = self.k.shape
+        if page != CACHE_PAGE:
+            raise ValueError(f"cache: pages of {page} tokens, expected {CACHE_PAGE}")
+        ns, mp = self.table.shape
+        dev, i32 = _device(self.k), torch.int32
+        d = CacheDesc(_arg(self.k, "k", torch.int8, dev), _arg(self.v, "v", torch.int8, dev, (nl, npg, nh, hd, page)),
+                      _arg(self.k_scale, "k_scale", torch.float32, dev, (nl, npg, nh, 4)),
+                      _arg(self.v_scale, "v_scale", torch.float32, dev, (nl, npg, nh, 4)),
+                      _arg(self.table, "table", i32, dev), _arg(self.len, "len", i32, dev, (ns,)),
+                      _arg(self.refs, "refs", i32, dev, (npg,)), npg, nl, nh, hd, ns, mp)
+        object.__setattr__(self, "_desc", d)
+        object.__setattr__(self, "_ref", ctypes.byref(d))
+        object.__setattr__(self, "index", dev)
 
     @classmethod
     def alloc(cls, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
@@ -624,28 +658,21 @@ class Cache:
                    z(n_slots, max_pages), z(n_slots), z(n_pages))
 
     @property
-    def device(self) -> torch.device:
-        return self.k.device
+    def n_kv_heads(self) -> int:
+        return self._desc.n_kv_heads
+
+    @property
+    def head_dim(self) -> int:
+        return self._desc.head_dim
 
     def desc(self) -> CacheDesc:
-        if self.k.dim() != 5 or self.table.dim() != 2:
-            raise ValueError("cache: k must have 5 dimensions and table 2")
-        nl, npg, nh, page, hd = self.k.shape
-        if page != CACHE_PAGE:
-            raise ValueError(f"cache: pages of {page} tokens, expected {CACHE_PAGE}")
-        ns, mp = self.table.shape
-        dev, i32 = self.device, torch.int32
-        return CacheDesc(_arg(self.k, "k", torch.int8, dev), _arg(self.v, "v", torch.int8, dev, (nl, npg, nh, hd, page)),
-                         _arg(self.k_scale, "k_scale", torch.float32, dev, (nl, npg, nh, 4)),
-                         _arg(self.v_scale, "v_scale", torch.float32, dev, (nl, npg, nh, 4)),
-                         _arg(self.table, "table", i32, dev), _arg(self.len, "len", i32, dev, (ns,)),
-                         _arg(self.refs, "refs", i32, dev, (npg,)), npg, nl, nh, hd, ns, mp)
+        return self._desc
 
 
 @dataclass
 class CacheBatch:
     """New rows of one step: entry i is rows row_begin[i] .. row_begin[i + 1] - 1 (or max_new rows each)
-    of slot slots[i] (or slot i); pos [n] int32 is written by cache_extend."""
+    of slot slots[i] (or slot i); pos [n] int32 is written by cache_extend; status [1] int32."""
     pos: torch.Tensor
     max_new: int
     rows: int
@@ -653,83 +680,82 @@ class CacheBatch:
     row_begin: torch.Tensor | None = None
     status: torch.Tensor | None = None
 
-    def desc(self, dev: torch.device) -> CacheBatchDesc:
+    def desc(self, dev: int) -> CacheBatchDesc:
         n, i32 = self.pos.numel(), torch.int32
         return CacheBatchDesc(n, self.max_new, self.rows, _arg(self.slots, "slots", i32, dev, (n,)),
                               _arg(self.row_begin, "row_begin", i32, dev, (n + 1,)), _arg(self.pos, "pos", i32, dev, (n,)),
-                              _arg(self.status, "status", (i32, torch.uint32), dev, (1,)))
+                              _arg(self.status, "status", i32, dev, (1,)))
 
 
-def _ws(ws, dev: torch.device):
+def _ws(ws, dev: int):
     if ws is None:
         return None, 0
-    return _arg(ws, "ws", ws.dtype, dev), ws.numel() * ws.element_size()
+    return _arg(ws, "ws", ws.dtype, dev), ws.nbytes
 
 
-def _rope_args(rope, dev: torch.device, hd: int):
+def _rope_args(rope, dev: int, hd: int):
     if rope is None:
         return None, None, 0
     c, s = rope
-    n = c.shape[0]
-    return _arg(c, "cos", torch.float32, dev, (n, hd // 2)), _arg(s, "sin", torch.float32, dev, (n, hd // 2)), n
+    shape = (c.shape[0], hd // 2)
+    return _arg(c, "cos", torch.float32, dev, shape), _arg(s, "sin", torch.float32, dev, shape), shape[0]
 
 
 def cache_workspace_bytes(cache: Cache) -> int:
     """Workspace of cache_extend, cache_fork and cache_compact."""
-    return int(lib().zoact_cache_workspace_bytes(ctypes.byref(cache.desc())))
+    return int(lib().zoact_cache_workspace_bytes(cache._ref))
 
 
 def cache_extend(cache: Cache, batch: CacheBatch, ws: torch.Tensor, stream=None):
     """Reserve places for the batch's rows; writes batch.pos and the cache's len, table and refs."""
-    dev = cache.device
-    _on_device(lib().zoact_cache_extend, dev, stream, ctypes.byref(cache.desc()), ctypes.byref(batch.desc(dev)),
-               *_ws(ws, dev))
+    dev = cache.index
+    _on_device(lib().zoact_cache_extend, dev, stream, cache._ref, ctypes.byref(batch.desc(dev)), *_ws(ws, dev))
 
 
 def cache_fork(cache: Cache, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, status=None, stream=None):
     """Slots dst[i] become second holders of what slots src[i] hold."""
-    dev, i32 = cache.device, torch.int32
+    dev, i32 = cache.index, torch.int32
     n = src.numel()
-    _on_device(lib().zoact_cache_fork, dev, stream, ctypes.byref(cache.desc()), _arg(src, "src", i32, dev, (n,)),
-               _arg(dst, "dst", i32, dev, (n,)), n, *_ws(ws, dev), _arg(status, "status", (i32, torch.uint32), dev, (1,)))
+    _on_device(lib().zoact_cache_fork, dev, stream, cache._ref, _arg(src, "src", i32, dev, (n,)),
+               _arg(dst, "dst", i32, dev, (n,)), n, *_ws(ws, dev), _arg(status, "status", i32, dev, (1,)))
 
 
 def cache_free(cache: Cache, slots: torch.Tensor, status=None, stream=None):
     """Give the slots' pages back and empty them."""
-    dev, i32 = cache.device, torch.int32
-    _on_device(lib().zoact_cache_free, dev, stream, ctypes.byref(cache.desc()),
-               _arg(slots, "slots", i32, dev, (slots.numel(),)), slots.numel(),
-               _arg(status, "status", (i32, torch.uint32), dev, (1,)))
+    dev, i32, n = cache.index, torch.int32, slots.numel()
+    _on_device(lib().zoact_cache_free, dev, stream, cache._ref, _arg(slots, "slots", i32, dev, (n,)), n,
+               _arg(status, "status", i32, dev, (1,)))
 
 
 def cache_compact(cache: Cache, ws: torch.Tensor, n_used: torch.Tensor | None = None, stream=None):
     """Move the used pages to the front of the pool; n_used [1] int32 gets their number."""
-    dev = cache.device
-    _on_device(lib().zoact_cache_compact, dev, stream, ctypes.byref(cache.desc()), *_ws(ws, dev),
+    dev = cache.index
+    _on_device(lib().zoact_cache_compact, dev, stream, cache._ref, *_ws(ws, dev),
                _arg(n_used, "n_used", torch.int32, dev, (1,)))
 
 
 def cache_append(cache: Cache, layer: int, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, rope=None, stream=None):
     """Quantise the batch's keys (rotated with rope = (cos, sin)) and values into `layer`; k and v may
     be column slices of a wider buffer."""
-    dev, (nh, hd) = cache.device, (cache.k.shape[2], cache.k.shape[4])
-    kp, ldk = _heads_arg(k, "k", k.dtype, dev, batch.rows, nh * hd)
-    vp, ldv = _heads_arg(v, "v", k.dtype, dev, batch.rows, nh * hd)
-    _on_device(lib().zoact_cache_append, dev, stream, ctypes.byref(cache.desc()), layer, kp, ldk, vp, ldv,
-               dtype_code(k), ctypes.byref(batch.desc(dev)), *_rope_args(rope, dev, hd))
+    dev, hd = cache.index, cache.head_dim
+    kp, ldk = _heads_arg(k, "k", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
+    vp, ldv = _heads_arg(v, "v", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
+    _on_device(lib().zoact_cache_append, dev, stream, cache._ref, layer, kp, ldk, vp, ldv, dtype_code(k),
+               ctypes.byref(batch.desc(dev)), *_rope_args(rope, dev, hd))
 
 
 def attention_cache_workspace_bytes(cache: Cache, batch: CacheBatch, n_heads: int, max_len: int) -> int:
-    return int(lib().zoact_attention_cache_workspace_bytes(ctypes.byref(cache.desc()),
-                                                           ctypes.byref(batch.desc(cache.device)), n_heads, max_len))
+    with torch.cuda.device(cache.index):
+        return int(lib().zoact_attention_cache_workspace_bytes(cache._ref, ctypes.byref(batch.desc(cache.index)),
+                                                               n_heads, max_len))
 
 
 def attention_cache(cache: Cache, layer: int, q: torch.Tensor, out: torch.Tensor, batch: CacheBatch, n_heads: int,
                     scale: float, max_len: int, rope=None, ws: torch.Tensor | None = None, stream=None):
     """Causal attention of the batch's rows over their slots' tokens in `layer` (q may be a column slice
     of a wider buffer; rope = (cos, sin) rotates it first)."""
-    dev, hd = cache.device, cache.k.shape[4]
+    dev, hd = cache.index, cache.head_dim
     qp, ldq = _heads_arg(q, "q", out.dtype, dev, batch.rows, n_heads * hd)
-    op = _arg(out, "out", (torch.bfloat16, torch.float32), dev, (batch.rows, n_heads * hd))
-    _on_device(lib().zoact_attention_cache, dev, stream, ctypes.byref(cache.desc()), layer, qp, ldq, dtype_code(out),
-               n_heads, ctypes.byref(batch.desc(dev)), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))
+    op = _arg(out, "out", out.dtype, dev, (batch.rows, n_heads * hd))
+    _on_device(lib().zoact_attention_cache, dev, stream, cache._ref, layer, qp, ldq, dtype_code(out), n_heads,
+               ctypes.byref(batch.desc(dev)), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))

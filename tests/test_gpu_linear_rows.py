@@ -63,11 +63,11 @@ def _reference(s):
     return y, tol
 
 
-def _run(s, f32_out, ws=False):
+def _run(s, f32_out, ws=0):
     lin = Z.Linear(t_u8(s["packed"]), s["K"], s["N"], s["r"], None, 0, t_bf16(s["b"]) if s["b"] is not None else None,
                    t_bf16(s["sc"]), plain=s["plain"])
-    if ws:
-        lin.ws = torch.full((Z.linear_workspace_bytes(),), 255, dtype=torch.uint8, device=dev())
+    if ws:      # (NaN everywhere)
+        lin.ws = torch.full((ws,), 255, dtype=torch.uint8, device=dev())
     arena, pad = None, 24
     if s["r"]:
         lin.coef_offset = pad
@@ -107,6 +107,15 @@ CASES = [
     dict(rows=3, K=14336, N=128, r=32, res=True, x_mean=2.0),
     dict(rows=1, K=512, N=6144, r=32),
     dict(rows=64, K=256, N=4112, r=32),
+    dict(rows=1, K=57472, N=48, r=0),
+    dict(rows=16, K=8832, N=32, r=3, flags=Z.EPI_SWIGLU, bias=True),
+    dict(rows=4, K=4352, N=8224, r=16, bias=True, res=True),
+    dict(rows=12, K=640, N=13344, r=24, flags=Z.EPI_SWIGLU, res=True),
+    dict(rows=2, K=8832, N=48, r=40, bias=True),
+    dict(rows=10, K=12928, N=160, r=32, flags=Z.EPI_SWIGLU),
+    dict(rows=6, K=1024, N=27680, r=8, flags=Z.EPI_SWIGLU),
+    dict(rows=3, K=384, N=33040, r=0, res=True),
+    dict(rows=20, K=4736, N=352, r=32, flags=Z.EPI_SWIGLU, bias=True),
 ]
 
 
@@ -116,7 +125,8 @@ def test_rows_against_the_formula(kw, f32_out):
     announce("linear_rows", kw, f32_out)
     s = _case(**kw)
     _check(s, f32_out)
-    _check(s, f32_out, ws=True)
+    _check(s, f32_out, ws=Z.linear_workspace_bytes())
+    _check(s, f32_out, ws=3 * (s["N"] // 16) * 1024)       # room for fewer parts than wanted, or none
 
 
 def test_codes_and_scales_one_by_one():
@@ -127,6 +137,7 @@ def test_codes_and_scales_one_by_one():
     packed = ((q[:, ::2] & 15) | ((q[:, 1::2] & 15) << 4)).astype(np.uint8)
     sc = synth.bf16_round(np.linspace(0.001, 3.0, N * 2).reshape(N, 2).astype(np.float32))
     lin = Z.Linear(t_u8(packed), K, N, w_scales=t_bf16(sc))
+    lin.ws = torch.empty(Z.linear_workspace_bytes(), dtype=torch.uint8, device=dev())
     want = q * np.repeat(sc, 128, 1)
     for k0 in range(0, K, 64):
         x = np.zeros((64, K), np.float32)
