@@ -80,33 +80,52 @@ __device__ __forceinline__ void load8(const T* p, float (&x)[8]) {
   }
 }
 
-// A page of one head on its way to the wave: 16 bytes a lane and load (HD 32: K's upper half is not used).
+// Loads of what all lanes share and no one writes meanwhile (scales, page numbers): through the scalar
+// cache, into scalar registers.
+__device__ __forceinline__ floatx4 scalar4(const float* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) floatx4*>(reinterpret_cast<uintptr_t>(p));
+}
+__device__ __forceinline__ int scalar1(const int* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int*>(reinterpret_cast<uintptr_t>(p));
+}
+
+// A page of one head on its way to the wave, 16 bytes a lane and load (HD 32: K's upper half is not used).
+// Through a descriptor of the page: the lane's part of the address stays, the rest is scalar.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t page_rsrc(const int8_t* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p), 0, bytes, 0x00020000);
+}
+template <int HD>
+__device__ __forceinline__ uint4 load_keys(__amdgpu_buffer_rsrc_t rs, int lane, int n, int h) {
+  const int vo = (lane & 15) * HD + (HD == 32 ? 8 : 16) * (lane >> 4), so = n * 16 * HD + 64 * h;
+  if constexpr (HD == 32) {
+    const uint2 t = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, vo, so, 0));
+    return make_uint4(t.x, t.y, 0, 0);
+  } else {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, vo, so, 0));
+  }
+}
+template <int HD>
+__device__ __forceinline__ uint4 load_values(__amdgpu_buffer_rsrc_t rs, int lane, int d) {
+  return __builtin_bit_cast(
+      uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, (lane & 15) * kPage + 16 * (lane >> 4), d * 16 * kPage, 0));
+}
 template <int HD>
 struct KeyLoad {
-  static constexpr int N = HD == 32 ? 4 : HD / 16;
+  static constexpr int H = HD == 32 ? 1 : HD / 64, N = 4 * H;
   uint4 u[N];
   __device__ __forceinline__ void go(const int8_t* kp, int lane) {
-    const int g = lane >> 4;
+    const __amdgpu_buffer_rsrc_t rs = page_rsrc(kp, kPage * HD);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int8_t* const kr = kp + (n * 16 + (lane & 15)) * HD;
-      if constexpr (HD == 32) {
-        const uint2 t = *reinterpret_cast<const uint2*>(kr + 8 * g);
-        u[n] = make_uint4(t.x, t.y, 0, 0);
-      } else {
-#pragma unroll
-        for (int h = 0; h < HD / 64; ++h) u[n * (HD / 64) + h] = *reinterpret_cast<const uint4*>(kr + 64 * h + 16 * g);
-      }
-    }
+    for (int i = 0; i < N; ++i) u[i] = load_keys<HD>(rs, lane, i / H, i % H);
   }
 };
 template <int HD>
 struct ValueLoad {
   uint4 u[HD / 16];
   __device__ __forceinline__ void go(const int8_t* vp, int lane) {
+    const __amdgpu_buffer_rsrc_t rs = page_rsrc(vp, kPage * HD);
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d)
-      u[d] = *reinterpret_cast<const uint4*>(vp + (d * 16 + (lane & 15)) * kPage + 16 * (lane >> 4));
+    for (int d = 0; d < HD / 16; ++d) u[d] = load_values<HD>(rs, lane, d);
   }
 };
 
@@ -116,8 +135,8 @@ constexpr int kNoScale = -200;    // below every exponent of an fp32 number
 
 // V scales of a page's blocks that hold a token up to `last`, times a power of two that keeps p vsc below
 // 2^14; vexp follows, and o's unit 2^(vexp - 14) with it.
-__device__ __forceinline__ void value_scales(const float4& vs, int t0, int last, int& vexp, float (&vsc)[4]) {
-  const float v[4] = {vs.x, vs.y, vs.z, vs.w};
+__device__ __forceinline__ void value_scales(const floatx4& vs, int t0, int last, int& vexp, float (&vsc)[4]) {
+  const float v[4] = {vs[0], vs[1], vs[2], vs[3]};
 #pragma unroll
   for (int n = 0; n < 4; ++n) {
     vsc[n] = t0 + 16 * n > last ? 0.f : v[n];
@@ -177,46 +196,60 @@ __device__ __forceinline__ void soft_page(float (&s)[4][4], int t0, int lim, boo
   l += lsum;
 }
 
-// q of one column as right operands, dims 64 (s / 2) + 16 g + 8 (s % 2) + 0..7 of step s (HD 32:
+// q of one column as right operands: step s of a lane holds dims 64 (s / 2) + 16 g + 8 (s % 2) + 0..7 (HD 32:
 // 8 g + 0..7), rotated, times a power of two that brings the column's largest to [2^14, 2^15).
-// Returns the factor of its scores (log2 domain).
+template <typename T, int HD>
+__device__ __forceinline__ void query_step(const AttendArgs& a, int64_t row, int h, int64_t pos, int g, int s,
+                                           float (&x)[8]) {
+  constexpr int HALF = HD / 2;
+  const T* const qr = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * HD;
+  const int d = HD == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
+  load8(qr + d, x);
+  if (a.ct) {
+#pragma clang fp contract(off)
+    const bool up = d >= HALF;
+    const int64_t base = (pos < a.n_pos ? pos : a.n_pos - 1) * HALF + (up ? d - HALF : d);
+    float y[8], cs[8], sn[8];
+    load8(qr + (up ? d - HALF : d + HALF), y);
+    load8(a.ct + base, cs);
+    load8(a.st + base, sn);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = up ? x[k] * cs[k] + y[k] * sn[k] : x[k] * cs[k] - y[k] * sn[k];
+  }
+}
+// Largest magnitude of a column in a lane's values and its three partners'.
+__device__ __forceinline__ float column_top(const float (&x)[8], float top) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(x[k]));
+  return top;
+}
+// Factor of the values, and of the scores (log2 domain) in return; both powers of two stay normal numbers.
+__device__ __forceinline__ float column_shift(const AttendArgs& a, float top, float& factor) {
+  int sh = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
+  sh = top == 0.f ? 0 : sh > 120 ? 120 : sh < -113 ? -113 : sh;
+  factor = __uint_as_float((uint32_t)(127 + sh) << 23);
+  return __uint_as_float((uint32_t)(127 - sh) << 23) * a.scale;
+}
 template <typename T, int HD, int NT>
 __device__ __forceinline__ float load_query(const AttendArgs& a, int64_t row, int h, int64_t pos, int g,
                                             f16x8 (&qf)[HD / 32][NT]) {
-  constexpr int KS = HD / 32, HALF = HD / 2;
-  const T* const qr = static_cast<const T*>(a.q) + row * a.ldq + (int64_t)h * HD;
-  const int64_t tp = pos < a.n_pos ? pos : a.n_pos - 1;
-  float x[KS][8], top = 0.f;
+  constexpr int KS = HD / 32;
+  float x[KS][8], top = 0.f, factor;
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    const int d = HD == 32 ? 8 * g : 64 * (s >> 1) + 16 * g + 8 * (s & 1);
-    load8(qr + d, x[s]);
-    if (a.ct) {
-#pragma clang fp contract(off)
-      const bool up = d >= HALF;
-      float y[8], cs[8], sn[8];
-      load8(qr + (up ? d - HALF : d + HALF), y);
-      const int64_t base = tp * HALF + (up ? d - HALF : d);
-      load8(a.ct + base, cs);
-      load8(a.st + base, sn);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[s][k] = up ? x[s][k] * cs[k] + y[k] * sn[k] : x[s][k] * cs[k] - y[k] * sn[k];
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(x[s][k]));
+    query_step<T, HD>(a, row, h, pos, g, s, x[s]);
+    top = column_top(x[s], top);
   }
   top = fmaxf(top, __shfl_xor(top, 16, 64));
   top = fmaxf(top, __shfl_xor(top, 32, 64));
-  int sh = 14 - ((int)(__float_as_uint(top) >> 23) - 127);   // (both powers of two stay normal numbers)
-  sh = top == 0.f ? 0 : sh > 120 ? 120 : sh < -113 ? -113 : sh;
-  const float up2 = __uint_as_float((uint32_t)(127 + sh) << 23);
+  const float qs = column_shift(a, top, factor);
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[s][k] *= up2;
+    for (int k = 0; k < 8; ++k) x[s][k] *= factor;
     terms8<NT>(x[s], qf[s]);
   }
-  return __uint_as_float((uint32_t)(127 - sh) << 23) * a.scale;
+  return qs;
 }
 
 // A workgroup's key/value head, split and column tile.  Workgroups go to the eight XCDs in turn, so heads,
@@ -249,11 +282,14 @@ __device__ __forceinline__ Range split_range(const AttendArgs& a, const CacheEnt
 
 // Decoding: at most 16 columns, each wave its own pages.
 template <typename T, int HD, int NT>
-__global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs a) {
   constexpr int KS = HD / 32;           // 32-deep products of a score
   constexpr int DT = HD / 16;           // 16-wide tiles of the output
   constexpr int LD = HD + 4;
-  __shared__ float so[4][16][LD];
+  __shared__ __align__(16) char lds[4 * 16 * LD * 4];
+  float(*const so)[16][LD] = reinterpret_cast<float(*)[16][LD]>(lds);      // at the end
+  f16x8(*const sq)[NT][64] = reinterpret_cast<f16x8(*)[NT][64]>(lds);      // q, until the waves have read it
+  static_assert(KS * NT * 1024 <= 4 * 16 * LD * 4, "q fits");
   __shared__ float sm[4][16], sl[4][16];
   const zoact_cache& c = a.c;
   const Place at = place_of(a);
@@ -261,7 +297,7 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
   const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0);
   const int ncol = e.count * a.G;
   if (c0 >= ncol) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const Range rg = split_range(a, e, (c0 + 15 < ncol ? c0 + 15 : ncol - 1) / a.G, split);
 
   floatx4 o[DT];
@@ -270,7 +306,7 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
   float m = -INFINITY, l = 0.f;
   int vexp = kNoScale;   // V scales so far are below 2^vexp; o is kept in units of 2^(vexp - 14)
 
-  if (rg.pbeg + wave < rg.pend) {
+  if (rg.pbeg < rg.pend) {
     // the first page's keys are on their way before q is ready, each next page's before this one's softmax
     const int* const trow = c.table + (int64_t)e.slot * c.max_pages;
     const int64_t lbase = (int64_t)a.layer * c.n_pages;
@@ -279,23 +315,52 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
       return (lbase + (bad ? 0 : pid)) * c.n_kv_heads + hk;
     };
     int pg = rg.pbeg + wave;
-    bool bad;
-    int64_t head = head_of(__builtin_amdgcn_readfirstlane(trow[pg]), bad);
+    const bool any = pg < rg.pend;
+    bool bad = false;
+    int64_t head = 0;
     KeyLoad<HD> kl;
     ValueLoad<HD> vl;
-    kl.go(c.k + head * (kPage * HD), lane);
-    float4 ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
-    int pid1 = pg + 4 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[pg + 4]) : 0;
-
+    floatx4 ks;
+    int pid1 = 0;
+    if (any) {
+      head = head_of(scalar1(trow + pg), bad);
+      kl.go(c.k + head * (kPage * HD), lane);
+      ks = scalar4(c.k_scale + head * 4);
+      if (pg + 4 < rg.pend) pid1 = scalar1(trow + pg + 4);
+    }
+    // the columns are the same in all waves: each prepares one step of q for all
     const int col = c0 + (lane & 15), cq = col < ncol ? col : ncol - 1;   // (columns past the last repeat it)
     const int tcol = e.pos + cq / a.G;                                    // the column's last token
+    float x[8], top = 0.f, factor;
+    if (wave < KS) {
+      query_step<T, HD>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol, g, wave, x);
+      top = column_top(x, 0.f);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+    }
+    if (g == 0) sm[wave][lane] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(sm[0][lane & 15], sm[1][lane & 15]), fmaxf(sm[2][lane & 15], sm[3][lane & 15]));
+    const float qs = column_shift(a, top, factor);
+    if (wave < KS) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] *= factor;
+      f16x8 t[NT];
+      terms8<NT>(x, t);
+#pragma unroll
+      for (int q = 0; q < NT; ++q) sq[wave][q][lane] = t[q];
+    }
+    __syncthreads();
     f16x8 qf[KS][NT];
-    const float qs = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol, g, qf);
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int q = 0; q < NT; ++q) qf[s][q] = sq[s][q][lane];
 
-    while (true) {
+    while (any) {
       vl.go(c.v + head * (kPage * HD), lane);
-      const float4 vs = *reinterpret_cast<const float4*>(c.v_scale + head * 4);
-      const float ksc[4] = {ks.x, ks.y, ks.z, ks.w};
+      const floatx4 vs = scalar4(c.v_scale + head * 4);
+      const float ksc[4] = {ks[0], ks[1], ks[2], ks[3]};
       float s[4][4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
@@ -310,14 +375,15 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
         const float f = ksc[n] * qs;
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * f;
+        __builtin_amdgcn_sched_barrier(0);      // (codes converted early would not fit three waves' registers)
       }
       const int t0 = pg * kPage, next = pg + 4;
       const bool now_bad = bad;
       if (next < rg.pend) {
         head = head_of(pid1, bad);
         kl.go(c.k + head * (kPage * HD), lane);
-        ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
-        pid1 = next + 4 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[next + 4]) : 0;
+        ks = scalar4(c.k_scale + head * 4);
+        pid1 = next + 4 < rg.pend ? scalar1(trow + next + 4) : 0;
       }
       // a page number that is none counts as if its tokens were masked
       if (now_bad && lane == 0) raise_status(a.b.status, ZOACT_STATUS_BAD_ENTRY);
@@ -338,12 +404,14 @@ __global__ void __launch_bounds__(256, 2) attend_kernel(AttendArgs a) {
           acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[1][q], acc, 0, 0, 0);
         }
         o[d] = acc;
+        if (d & 1) __builtin_amdgcn_sched_barrier(0);
       }
       if (next >= rg.pend) break;
       pg = next;
     }
   }
-  // the four waves' results
+  // the four waves' results (q and its maxima have been read by all)
+  __syncthreads();
   constexpr int DV = HD / 16;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -413,7 +481,7 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
   const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0);
   const int ncol = e.count * a.G;
   if (c0 >= ncol) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
   const Range rg = split_range(a, e, (c0 + 64 * CT - 1 < ncol ? c0 + 64 * CT - 1 : ncol - 1) / a.G, split);
   const int w0 = c0 + 16 * CT * wave;                 // the wave's first column
   // (a wave past the last column repeats it, so that every wave reaches every barrier)
@@ -435,30 +503,25 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
     const int* const trow = c.table + (int64_t)e.slot * c.max_pages;
     const int64_t lbase = (int64_t)a.layer * c.n_pages;
     uint4 kr[KL], vr[VL];
-    float4 ks, vs;
+    floatx4 ks, vs;
     bool bad;
     auto load = [&](int pid) {
       bad = pid < 0 || pid >= c.n_pages;
       const int64_t head = (lbase + (bad ? 0 : pid)) * c.n_kv_heads + hk;
-      const int8_t* const kp = c.k + head * (kPage * HD) + (wave * 16 + (lane & 15)) * HD;
-      if constexpr (HD == 32) {
-        const uint2 u = *reinterpret_cast<const uint2*>(kp + 8 * g);
-        kr[0] = make_uint4(u.x, u.y, 0, 0);
-      } else {
+      const __amdgpu_buffer_rsrc_t krs = page_rsrc(c.k + head * (kPage * HD), kPage * HD);
+      const __amdgpu_buffer_rsrc_t vrs = page_rsrc(c.v + head * (kPage * HD), kPage * HD);
 #pragma unroll
-        for (int h = 0; h < KL; ++h) kr[h] = *reinterpret_cast<const uint4*>(kp + 64 * h + 16 * g);
-      }
+      for (int h = 0; h < KL; ++h) kr[h] = load_keys<HD>(krs, lane, wave, h);
 #pragma unroll
       for (int d = 0; d < VL; ++d) {
         const int dt = wave * VL + d;
-        if (DT % 4 == 0 || dt < DT)
-          vr[d] = *reinterpret_cast<const uint4*>(c.v + head * (kPage * HD) + (dt * 16 + (lane & 15)) * kPage + 16 * g);
+        if (DT % 4 == 0 || dt < DT) vr[d] = load_values<HD>(vrs, lane, dt);
       }
-      ks = *reinterpret_cast<const float4*>(c.k_scale + head * 4);
-      vs = *reinterpret_cast<const float4*>(c.v_scale + head * 4);
+      ks = scalar4(c.k_scale + head * 4);
+      vs = scalar4(c.v_scale + head * 4);
     };
-    load(__builtin_amdgcn_readfirstlane(trow[rg.pbeg]));
-    int pid1 = rg.pbeg + 1 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[rg.pbeg + 1]) : 0;
+    load(scalar1(trow + rg.pbeg));
+    int pid1 = rg.pbeg + 1 < rg.pend ? scalar1(trow + rg.pbeg + 1) : 0;
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
       const int col = w0 + 16 * t + (lane & 15), cq = col < ncol ? col : ncol - 1;
@@ -477,12 +540,12 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
           vb[buf][dt][1][lane] = codes8(vr[d].z, vr[d].w);
         }
       }
-      const float ksc[4] = {ks.x, ks.y, ks.z, ks.w};
-      const float4 vsn = vs;
+      const float ksc[4] = {ks[0], ks[1], ks[2], ks[3]};
+      const floatx4 vsn = vs;
       const bool now_bad = bad;
       if (pg + 1 < rg.pend) {
         load(pid1);
-        pid1 = pg + 2 < rg.pend ? __builtin_amdgcn_readfirstlane(trow[pg + 2]) : 0;
+        pid1 = pg + 2 < rg.pend ? scalar1(trow + pg + 2) : 0;
       }
       __syncthreads();
       const int t0 = pg * kPage;
