@@ -632,54 +632,57 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
   }
 }
 
-// Joins the splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits.  The
-// statistics come first, a thread each: their maximum and the weights are ready in LDS before the sums
-// are read.
+// Joins the splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits, up to NI each.
+// A thread's sums are on their way while the statistics, a thread a split, give the weights.
 constexpr int kMaxSplits = 128;
-template <typename T, int HD>
+template <typename T, int HD, int NI>
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
-  constexpr int DV = HD / 32;
-  __shared__ float wt[kMaxSplits], sr[8][HD], red[4], redl[2];
+  constexpr int DV = HD / 32, NG = 8;
+  typedef float vec __attribute__((ext_vector_type(DV)));
+  __shared__ float wt[kMaxSplits], red[2], redl[2];
+  __shared__ vec sr[NG][32];
   const int i = blockIdx.z, j = blockIdx.y, h = blockIdx.x;
   const CacheEntry e = read_entry(a.c, a.b, i, false);
   if (j >= e.count) return;
   const int64_t R = (((int64_t)i * a.b.max_new + j) * a.H + h) * a.S;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, grp = tid >> 5;
   float2 ml = make_float2(-INFINITY, 0.f);
   if (tid < a.S) ml = a.ml[R + tid];
-  float M = ml.x;
+  vec v[NI];
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
-  if (lane == 0) red[wave] = M;
-  __syncthreads();
-  M = fmaxf(red[0], red[1]);
-  const float base = M == -INFINITY ? 0.f : M;
-  float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - base);
-  if (tid < kMaxSplits) wt[tid] = f;
-  float L = f * ml.y;
+  for (int k = 0; k < NI; ++k)
+    if (grp + k * NG < a.S) v[k] = *reinterpret_cast<const vec*>(a.part + (R + grp + k * NG) * HD + (tid & 31) * DV);
+  if (wave < kMaxSplits / 64) {
+    float M = ml.x;
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) L += __shfl_xor(L, k, 64);
-  if (lane == 0 && wave < 2) redl[wave] = L;
-  __syncthreads();
-  L = redl[0] + redl[1];
-  const int grp = tid >> 5, d0 = (tid & 31) * DV;
-  float r[DV];
-#pragma unroll
-  for (int k = 0; k < DV; ++k) r[k] = 0.f;
-#pragma unroll 4
-  for (int s = grp; s < a.S; s += 8) {
-    const float w = wt[s];
-    if (w == 0.f) continue;      // (an empty split has written no sums)
-#pragma unroll
-    for (int k = 0; k < DV; ++k) r[k] += w * a.part[(R + s) * HD + d0 + k];
+    for (int k = 1; k < 64; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
+    if (lane == 0) red[wave] = M;
   }
+  __syncthreads();
+  if (wave < kMaxSplits / 64) {
+    const float M = fmaxf(red[0], red[1]), base = M == -INFINITY ? 0.f : M;
+    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - base);
+    wt[tid] = f;
+    float L = f * ml.y;
 #pragma unroll
-  for (int k = 0; k < DV; ++k) sr[grp][d0 + k] = r[k];
+    for (int k = 1; k < 64; k <<= 1) L += __shfl_xor(L, k, 64);
+    if (lane == 0) redl[wave] = L;
+  }
+  __syncthreads();
+  vec r = 0.f;
+#pragma unroll
+  for (int k = 0; k < NI; ++k)
+    if (grp + k * NG < a.S) {
+      const float w = wt[grp + k * NG];
+      if (w != 0.f) r += w * v[k];      // (an empty split has written no sums; a NaN weight counts)
+    }
+  sr[grp][tid & 31] = r;
   __syncthreads();
   if (tid >= HD) return;
-  float y = sr[0][tid];
+  float y = 0.f;
 #pragma unroll
-  for (int k = 1; k < 8; ++k) y += sr[k][tid];
+  for (int k = 0; k < NG; ++k) y += reinterpret_cast<const float*>(sr[k])[tid];
+  const float L = redl[0] + redl[1];
   y = L == 0.f ? 0.f : y / L;
   T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + j) * a.H + h) * HD + tid;
   if constexpr (sizeof(T) == 2)
@@ -691,7 +694,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
 // Query columns of a workgroup: 16 while that holds an entry's (decoding), 64 or 128 for chunks of rows.
 int attend_cols(int32_t dtype, const zoact_cache_batch& b, int G) {
   const int64_t cols = (int64_t)b.max_new * G;
-  return cols <= 16 ? 16 : cols <= 64 || dtype == ZOACT_F32 ? 64 : 128;
+  return cols <= 16 ? 16 : 64;
 }
 
 template <typename T, int HD, int NT>
@@ -706,7 +709,10 @@ void run_attend(const AttendArgs& a, int w, hipStream_t s) {
     attend_chunk_kernel<T, HD, NT, 2><<<grid, 256, 0, s>>>(a);
   if (a.S > 1) {
     const dim3 join((unsigned)a.H, (unsigned)a.b.max_new, (unsigned)a.b.n);
-    attend_join_kernel<T, HD><<<join, 256, 0, s>>>(a);
+    if (a.S <= 8)
+      attend_join_kernel<T, HD, 1><<<join, 256, 0, s>>>(a);
+    else
+      attend_join_kernel<T, HD, kMaxSplits / 8><<<join, 256, 0, s>>>(a);
   }
 }
 
@@ -721,6 +727,8 @@ int attend_splits(const zoact_cache& c, const zoact_cache_batch& b, int n_heads,
   const int64_t want = 2 * (cu_count() > 0 ? cu_count() : 256);
   int64_t s = (pages + 15) / 16;
   if (groups * s < want) s = (want + groups - 1) / groups;
+  // (between one and two rounds of three workgroups a compute unit: one)
+  if (groups * s > want + want / 2 && groups * s < 3 * want && groups <= want) s = (want + want / 2) / groups;
   if (w > 16 && 2 * groups >= want) s = 1;                              // (a chunk's own tiles are many)
   if (s > (pages + 3) / 4) s = (pages + 3) / 4;
   if (s > kMaxSplits) s = kMaxSplits;
