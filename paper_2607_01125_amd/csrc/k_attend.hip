@@ -691,10 +691,12 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
     *op = y;
 }
 
-// Query columns of a workgroup: 16 while that holds an entry's (decoding), 64 or 128 for chunks of rows.
-int attend_cols(int32_t dtype, const zoact_cache_batch& b, int G) {
-  const int64_t cols = (int64_t)b.max_new * G;
-  return cols <= 16 ? 16 : 64;
+// Query columns of a workgroup: 16 while that holds an entry's (decoding); for chunks of rows 64, or 128
+// (bf16) where that still makes four workgroups a compute unit: 16 chunks of 256 rows behind 500 tokens,
+// 32/8 heads of 128, 101 us with 64 and 87 with 128, but one of 512 rows 19 and 39.
+int attend_cols(int32_t dtype, const zoact_cache& c, const zoact_cache_batch& b, int G) {
+  const int64_t cols = (int64_t)b.max_new * G, wide = (cols + 127) / 128 * c.n_kv_heads * b.n;
+  return cols <= 16 ? 16 : dtype == ZOACT_BF16 && wide >= 4 * (cu_count() > 0 ? cu_count() : 256) ? 128 : 64;
 }
 
 template <typename T, int HD, int NT>
@@ -758,8 +760,8 @@ extern "C" size_t zoact_attention_cache_workspace_bytes(const zoact_cache* c, co
     return 0;
   // (of the types' widths the one with more splits)
   const int G = n_heads / c->n_kv_heads;
-  const int s0 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_BF16, *b, G), max_len);
-  const int s1 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_F32, *b, G), max_len);
+  const int s0 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_BF16, *c, *b, G), max_len);
+  const int s1 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_F32, *c, *b, G), max_len);
   return attend_ws(*c, *b, n_heads, s0 > s1 ? s0 : s1);
 }
 
@@ -788,7 +790,7 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   a.H = n_heads;
   a.G = n_heads / c->n_kv_heads;
   ZA((int64_t)b->max_new * n_heads < INT32_MAX / kMaxSplits, "attention_cache: too many new rows");
-  const int w = attend_cols(dtype, *b, a.G);
+  const int w = attend_cols(dtype, *c, *b, a.G);
   a.S = attend_splits(*c, *b, n_heads, w, max_len);
   const size_t need = attend_ws(*c, *b, n_heads, a.S);
   if (ws == nullptr || ws_bytes < need) a.S = 1;

@@ -10,18 +10,18 @@ namespace zoact {
 namespace {
 
 // ---------------------------------------------------------------- append
-// One workgroup per (page of an entry's new tokens, key/value head, entry); wave w holds the
-// page's block w, lane l a quarter (l & 3) of token l >> 2's values, so the block's maximum is
-// a reduction over the wave and a token's row leaves as whole 16-byte stores.  V goes through
-// LDS to its transposed place.
-template <typename T, int HD, bool ROPE>
-__device__ __forceinline__ void load_quarter(const T* row, int d0, const float* ct, const float* st, int64_t ti,
-                                             float (&x)[HD / 4]) {
-#pragma clang fp contract(off)
-  constexpr int Q = HD / 4, V = 16 / sizeof(T);
-  constexpr int half = HD / 2;
-  auto ld = [&](int d, float* o) {
-    const uint4 u = *reinterpret_cast<const uint4*>(row + d);
+// One workgroup per (page of an entry's new tokens, keys or values of a head, entry); wave w holds the
+// page's block w.  The four lanes of a token take its 16-byte pieces in turn (a quad reads 64 contiguous
+// bytes), so the partner of a rotated value lies in the same lane, and the block's maximum is a reduction
+// over the wave.  V goes through LDS to its transposed place.
+// Value i of a lane is dim ((i / V) * 4 + quarter) * V + i % V, V values a piece.
+template <typename T, int HD>
+struct Quarter {
+  static constexpr int Q = HD / 4, V = 16 / (int)sizeof(T), HALF = HD / 2;
+  static constexpr bool kInLane = Q / V >= 2;      // (bf16, HD 32: one piece a lane, the partner two lanes on)
+  __device__ static int dim(int i, int q) { return ((i / V) * 4 + q) * V + i % V; }
+  __device__ static void load_piece(const T* p, float* o) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -30,24 +30,37 @@ __device__ __forceinline__ void load_quarter(const T* row, int d0, const float* 
       else
         o[e] = __uint_as_float(w[e]);
     }
-  };
+  }
+  __device__ static void load(const T* row, int q, float (&x)[Q]) {
 #pragma unroll
-  for (int j = 0; j < Q; j += V) {
-    ld(d0 + j, &x[j]);
-    if constexpr (ROPE) {
-      const bool up = d0 >= half;       // (a quarter lies in one half)
-      float y[V];
-      ld(up ? d0 + j - half : d0 + j + half, y);
-      const int64_t base = ti * half + (up ? d0 - half : d0) + j;
+    for (int i = 0; i < Q; i += V) load_piece(row + dim(i, q), &x[i]);
+  }
+  // (lo, hi) -> (lo c - hi s, hi c + lo s), one rounding per operation
+  __device__ static void rotate(float (&x)[Q], int q, const float* ct, const float* st) {
+#pragma clang fp contract(off)
+    if constexpr (kInLane) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float c = ct[base + e], s = st[base + e];
-        // (lo, hi) -> (lo c - hi s, hi c + lo s), one rounding per operation
-        x[j + e] = up ? x[j + e] * c + y[e] * s : x[j + e] * c - y[e] * s;
+      for (int i = 0; i < Q / 2; i += 4) {
+        const float4 c4 = *reinterpret_cast<const float4*>(ct + dim(i, q));
+        const float4 s4 = *reinterpret_cast<const float4*>(st + dim(i, q));
+        const float c[4] = {c4.x, c4.y, c4.z, c4.w}, s[4] = {s4.x, s4.y, s4.z, s4.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float lo = x[i + e], hi = x[Q / 2 + i + e];
+          x[i + e] = lo * c[e] - hi * s[e];
+          x[Q / 2 + i + e] = hi * c[e] + lo * s[e];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        const float y = __shfl_xor(x[i], 2, 64);
+        const int d = dim(i, q) % HALF;
+        x[i] = q >= 2 ? x[i] * ct[d] + y * st[d] : x[i] * ct[d] - y * st[d];
       }
     }
   }
-}
+};
 
 // Code of a value under the block's scale (a NaN scale: 0; s == 0: every value is 0).
 __device__ __forceinline__ int quantise(float x, float s) {
@@ -93,86 +106,97 @@ __device__ __forceinline__ float block_scale(float amax, bool held, float old, f
   return s;
 }
 
-template <typename T, int HD, bool ROPE>
+template <typename T, int HD>
 __global__ void __launch_bounds__(256) append_kernel(zoact_cache c, int layer, const T* __restrict__ k, int64_t ldk,
                                                      const T* __restrict__ v, int64_t ldv, zoact_cache_batch b,
                                                      const float* __restrict__ ct, const float* __restrict__ st,
                                                      int64_t n_pos) {
-  constexpr int Q = HD / 4;
+  typedef Quarter<T, HD> Qt;
+  constexpr int Q = Qt::Q;
   __shared__ uint32_t tile[HD * kPage / 4];      // V's page as stored: [HD][64]
-  const int hk = blockIdx.y;
-  const CacheEntry e = read_entry(c, b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0 && hk == 0);
+  const bool is_v = blockIdx.y >= (unsigned)c.n_kv_heads;
+  const int hk = is_v ? blockIdx.y - c.n_kv_heads : blockIdx.y;
+  const CacheEntry e = read_entry(c, b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
   if (!e.ok || e.count == 0) return;
   const int pg = e.pos / kPage + blockIdx.x, end = e.pos + e.count;
   if (pg * kPage >= end) return;
   const int pid = c.table[(int64_t)e.slot * c.max_pages + pg];
-  if (pid < 0 || pid >= c.n_pages) {
-    if (threadIdx.x == 0 && hk == 0) raise_status(b.status, ZOACT_STATUS_BAD_ENTRY);
-    return;
-  }
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane & 3;
   const int t0 = pg * kPage + wave * kBlock;     // the block's first token
   const bool live = t0 + kBlock > e.pos && t0 < end;
-  const int64_t head = ((int64_t)layer * c.n_pages + pid) * c.n_kv_heads + hk;
+  const int tok = t0 + (lane >> 2);
+  const bool in = tok >= e.pos && tok < end, held = t0 < e.pos;
+  float x[Q];
   if (live) {
-    const int tok = t0 + (lane >> 2), d0 = (lane & 3) * Q;
-    const bool in = tok >= e.pos && tok < end, held = t0 < e.pos, old = tok < e.pos;
+    // (lanes without a new token take one that there is)
     const int64_t row = e.row0 + (tok < e.pos ? 0 : tok >= end ? e.count - 1 : tok - e.pos);
-    const int64_t ti = tok < n_pos ? tok : n_pos - 1;
-    // keys
-    {
-      float x[Q], ratio;
-      load_quarter<T, HD, ROPE>(k + row * ldk + (int64_t)hk * HD, d0, ct, st, ti, x);
-      float* const sp = c.k_scale + head * kPageBlocks + wave;
-      const float before = held ? *sp : 0.f;
-      const float s = block_scale(wave_absmax<Q>(x, in), held, before, ratio);
-      uint32_t* const kp = reinterpret_cast<uint32_t*>(c.k + (head * kPage + wave * kBlock + (lane >> 2)) * HD + d0);
-      if (in) {
-#pragma unroll
-        for (int j = 0; j < Q; j += 4) {
-          uint32_t o = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o |= (uint32_t)(quantise(x[j + i], s) & 255) << (8 * i);
-          kp[j / 4] = o;
-        }
-      } else if (old && ratio != 1.f) {
-#pragma unroll
-        for (int j = 0; j < Q / 4; ++j) kp[j] = requantise4(kp[j], ratio);
-      }
-      if (lane == 0 && !(s == before && held)) *sp = s;
+    Qt::load((is_v ? v + row * ldv : k + row * ldk) + (int64_t)hk * HD, q, x);
+  }
+  if (pid < 0 || pid >= c.n_pages) {
+    if (threadIdx.x == 0 && blockIdx.y == 0) raise_status(b.status, ZOACT_STATUS_BAD_ENTRY);
+    return;
+  }
+  const int64_t head = ((int64_t)layer * c.n_pages + pid) * c.n_kv_heads + hk;
+  float* const sp = (is_v ? c.v_scale : c.k_scale) + head * kPageBlocks + wave;
+  if (!is_v) {
+    if (!live) return;
+    const float before = held ? *sp : 0.f;
+    if (ct) {
+      const int64_t ti = tok < n_pos ? tok : n_pos - 1;
+      Qt::rotate(x, q, ct + ti * (HD / 2), st + ti * (HD / 2));
     }
-    // values: the block's words of old codes, then the new ones over them
-    {
-      float x[Q], ratio;
-      load_quarter<T, HD, false>(v + row * ldv + (int64_t)hk * HD, d0, nullptr, nullptr, 0, x);
-      float* const sp = c.v_scale + head * kPageBlocks + wave;
-      const float before = held ? *sp : 0.f;
-      const float s = block_scale(wave_absmax<Q>(x, in), held, before, ratio);
-      uint32_t* const vp = reinterpret_cast<uint32_t*>(c.v + head * kPage * HD);
-      const bool whole = t0 >= e.pos && t0 + kBlock <= end;
-      if (!whole) {
-        // word (d, g) holds tokens 4 g .. 4 g + 3 of the block; only those before pos are the sequence's
-        for (int i = lane; i < HD * 4; i += 64) {
-          const int d = i >> 2, g = i & 3, at = d * 16 + g * 4 + wave;
-          const uint32_t w = vp[at];
-          const int n = e.pos - (t0 + 4 * g);      // earlier tokens of this word
-          const uint32_t keep = n <= 0 ? 0u : n >= 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
-          tile[at] = ratio != 1.f && keep ? (requantise4(w, ratio) & keep) | (w & ~keep) : w;
-        }
-        __builtin_amdgcn_wave_barrier();
-        __threadfence_block();
-      }
-      if (in) {
-        const int i = lane >> 2;                   // token of the block: group i >> 2, byte i & 3
-        uint8_t* const tb = reinterpret_cast<uint8_t*>(tile) + (i >> 2) * 16 + wave * 4 + (i & 3);
+    float ratio;
+    const float s = block_scale(wave_absmax<Q>(x, in), held, before, ratio);
+    int8_t* const kp = c.k + (head * kPage + wave * kBlock + (lane >> 2)) * HD;
 #pragma unroll
-        for (int j = 0; j < Q; ++j) tb[(d0 + j) * kPage] = (uint8_t)quantise(x[j], s);
+    for (int i = 0; i < Q; i += 4) {
+      uint32_t* const at = reinterpret_cast<uint32_t*>(kp + Qt::dim(i, q));
+      if (in) {
+        uint32_t o = 0;
+#pragma unroll
+        for (int e2 = 0; e2 < 4; ++e2) o |= (uint32_t)(quantise(x[i + e2], s) & 255) << (8 * e2);
+        *at = o;
+      } else if (tok < e.pos && ratio != 1.f) {
+        *at = requantise4(*at, ratio);
       }
-      if (lane == 0 && !(s == before && held)) *sp = s;
     }
+    if (lane == 0 && !(held && s == before)) *sp = s;
+    return;
+  }
+  uint32_t* const vp = reinterpret_cast<uint32_t*>(c.v + head * kPage * HD);
+  if (live) {
+    const float before = held ? *sp : 0.f;
+    // the block's words of old codes, unless all are new
+    constexpr int W = HD / 16;
+    const bool whole = t0 >= e.pos && t0 + kBlock <= end;
+    uint32_t w[W];
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = vp[((lane >> 2) + i * 16) * 16 + q * 4 + wave];
+    }
+    float ratio;
+    const float s = block_scale(wave_absmax<Q>(x, in), held, before, ratio);
+    if (!whole) {
+      // word (d, g) holds tokens 4 g .. 4 g + 3 of the block; only those before pos are the sequence's
+      const int n = e.pos - (t0 + 4 * q);
+      const uint32_t keep = n <= 0 ? 0u : n >= 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1u;
+#pragma unroll
+      for (int i = 0; i < W; ++i)
+        tile[((lane >> 2) + i * 16) * 16 + q * 4 + wave] =
+            ratio != 1.f && keep ? (requantise4(w[i], ratio) & keep) | (w[i] & ~keep) : w[i];
+      __builtin_amdgcn_wave_barrier();
+      __threadfence_block();
+    }
+    // the new codes over them
+    if (in) {
+      const int i = lane >> 2;                     // token of the block: group i >> 2, byte i & 3
+      uint8_t* const tb = reinterpret_cast<uint8_t*>(tile) + (i >> 2) * 16 + wave * 4 + (i & 3);
+#pragma unroll
+      for (int j = 0; j < Q; ++j) tb[Qt::dim(j, q) * kPage] = (uint8_t)quantise(x[j], s);
+    }
+    if (lane == 0 && !(held && s == before)) *sp = s;
   }
   __syncthreads();
-  uint32_t* const vp = reinterpret_cast<uint32_t*>(c.v + head * kPage * HD);
   if (pg * kPage + kPage <= end && e.pos < pg * kPage + kBlock) {   // all four blocks
     for (int i = threadIdx.x; i < HD * kPage / 16; i += 256)
       reinterpret_cast<uint4*>(vp)[i] = reinterpret_cast<const uint4*>(tile)[i];
@@ -486,7 +510,7 @@ zoact_status check_cache(const zoact_cache* c) {
      "cache: table, len and refs must be 4-byte aligned");
   ZC(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128, "cache: head_dim must be 32, 64 or 128");
   ZC(c->n_layers >= 1 && c->n_layers <= 32767, "cache: n_layers outside [1, 32767]");
-  ZC(c->n_kv_heads >= 1 && c->n_kv_heads <= 65535, "cache: n_kv_heads outside [1, 65535]");
+  ZC(c->n_kv_heads >= 1 && c->n_kv_heads <= 32767, "cache: n_kv_heads outside [1, 32767]");
   ZC(c->n_slots >= 1 && c->max_pages >= 1 && c->n_pages >= 1, "cache: empty table or pool");
   ZC(c->n_pages < INT32_MAX - 4096, "cache: too many pages");
   ZC((int64_t)c->max_pages * kPage < INT32_MAX, "cache: max_pages * 64 must be below 2^31");
@@ -513,11 +537,8 @@ zoact_status done(const char* who) {
 template <typename T, int HD>
 void run_append(const zoact_cache& c, int layer, const void* k, int64_t ldk, const void* v, int64_t ldv,
                 const zoact_cache_batch& b, const float* ct, const float* st, int64_t n_pos, hipStream_t s) {
-  const dim3 grid((unsigned)((b.max_new + kPage - 2) / kPage + 1), (unsigned)c.n_kv_heads, (unsigned)b.n);
-  if (ct)
-    append_kernel<T, HD, true><<<grid, 256, 0, s>>>(c, layer, (const T*)k, ldk, (const T*)v, ldv, b, ct, st, n_pos);
-  else
-    append_kernel<T, HD, false><<<grid, 256, 0, s>>>(c, layer, (const T*)k, ldk, (const T*)v, ldv, b, ct, st, n_pos);
+  const dim3 grid((unsigned)((b.max_new + kPage - 2) / kPage + 1), (unsigned)(2 * c.n_kv_heads), (unsigned)b.n);
+  append_kernel<T, HD><<<grid, 256, 0, s>>>(c, layer, (const T*)k, ldk, (const T*)v, ldv, b, ct, st, n_pos);
 }
 }  // namespace
 
