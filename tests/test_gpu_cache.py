@@ -454,3 +454,80 @@ def test_refusals_on_device_tensors():
         Z.cache_extend(pr.c, b, pr.ws[:64])
     with pytest.raises(ValueError):
         Z.cache_extend(pr.c, b, pr.ws.cpu())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_many_chunks_at_once(hd, dtype):
+    """Enough chunks of rows that workgroups take 128 columns each (bf16), ragged, behind lengths that end
+    anywhere in a page; three of the entries against float64, one of no rows."""
+    rng = np.random.default_rng(hd)
+    n, H, hkv = 40, 32, 8
+    lens = [int(x) for x in rng.integers(0, 100, n)]
+    counts = [int(x) for x in rng.integers(60, 131, n)]
+    counts[3], counts[7], lens[9] = 130, 0, 64
+    c = Z.Cache.alloc(1, sum(-(-(a + b) // 64) for a, b in zip(lens, counts)), hkv, hd, n, 4, dev())
+    ws = torch.empty(Z.cache_workspace_bytes(c), dtype=torch.uint8, device=dev())
+    rp = _rope(240, hd)
+    for part in (lens, counts):
+        begin = np.concatenate([[0], np.cumsum(part)])
+        b = Z.CacheBatch(torch.empty(n, dtype=torch.int32, device=dev()), max(part), int(begin[-1]),
+                         row_begin=t_i32(begin), status=torch.zeros(1, dtype=torch.int32, device=dev()))
+        Z.cache_extend(c, b, ws)
+        x = _rows(int(begin[-1]), (H + 2 * hkv) * hd, dtype, sum(part))
+        Z.cache_append(c, 0, x[:, H * hd:(H + hkv) * hd], x[:, (H + hkv) * hd:], b, rope=rp)
+    out = torch.full((b.rows, H * hd), float("nan"), dtype=dtype, device=dev())
+    announce("many chunks", hd, dtype)
+    Z.attention_cache(c, 0, x[:, :H * hd], out, b, H, hd ** -0.5, 240, rope=rp)
+    assert torch.isfinite(out).all() and int(b.status) == 0 and b.pos.tolist() == lens
+    m = cm.Model(1, c.refs.numel(), hkv, hd, n, 4)
+    for a, t in ((m.k, c.k), (m.v, c.v), (m.ks, c.k_scale), (m.vs, c.v_scale), (m.table, c.table)):
+        a[...] = t.cpu().numpy()
+    rh = tuple(t.cpu().numpy() for t in rp)
+    for i in (3, 9, n - 1):
+        r0, r1, L = int(begin[i]), int(begin[i + 1]), lens[i]
+        k, v = m.values(0, i, L + counts[i])
+        want, mean, mag = cm.attend(host(x[r0:r1, :H * hd]).reshape(-1, H, hd), k, v, L, float(np.float32(hd ** -0.5)), rh)
+        tol = cm.attend_bound(want, mean, mag, L + counts[i], hd, dtype == torch.float32)
+        bad = ~(np.abs(host(out[r0:r1]).reshape(-1, H, hd) - want) <= tol)
+        assert not bad.any(), (i, int(bad.sum()), np.argwhere(bad)[:3].tolist())
+
+
+def test_pools_past_two_gigabytes():
+    """Pages and layers whose bytes lie past 2^31: the same values as in a small pool."""
+    hkv, hd, H, big_pages = 1, 128, 4, 150_000
+    small = Z.Cache.alloc(1, 12, hkv, hd, 2, 8, dev())
+    big = Z.Cache.alloc(3, big_pages, hkv, hd, 2, 8, dev())
+    big.refs[:big_pages - 9] = 1                    # the free ones are the last
+    outs = []
+    x = _rows(300 + 131, (H + 2 * hkv) * hd, torch.bfloat16, 3)
+    for c, layer in ((small, 0), (big, 2)):
+        ws = torch.empty(Z.cache_workspace_bytes(c), dtype=torch.uint8, device=dev())
+        st = torch.zeros(1, dtype=torch.int32, device=dev())
+        b = Z.CacheBatch(torch.empty(2, dtype=torch.int32, device=dev()), 300, 431, row_begin=t_i32([0, 300, 431]),
+                         status=st)
+        announce("large pool", c.refs.numel(), layer)
+        Z.cache_extend(c, b, ws)
+        Z.cache_append(c, layer, x[:, H * hd:(H + hkv) * hd], x[:, (H + hkv) * hd:], b)
+        out = torch.empty(431, H * hd, dtype=torch.bfloat16, device=dev())
+        Z.attention_cache(c, layer, x[:, :H * hd], out, b, H, 0.1, 300)
+        assert int(st) == 0
+        # one token more of a forked sequence: the copy of its last page lies far out too
+        Z.cache_free(c, t_i32([1]), st)
+        Z.cache_fork(c, t_i32([0]), t_i32([1]), ws, st)
+        one = Z.CacheBatch(torch.empty(2, dtype=torch.int32, device=dev()), 1, 2, status=st)
+        Z.cache_extend(c, one, ws)
+        Z.cache_append(c, layer, x[:2, H * hd:(H + hkv) * hd], x[:2, (H + hkv) * hd:], one)
+        last = torch.empty(2, H * hd, dtype=torch.bfloat16, device=dev())
+        Z.attention_cache(c, layer, x[:2, :H * hd], last, one, H, 0.1, 301)
+        assert int(st) == 0
+        outs.append((out, last, c.table.cpu() - (big_pages - 9 if c is big else 0)))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    assert int(outs[1][2][0, :5].min()) >= 0
+    big.refs[:big_pages - 9] = 0
+    used = torch.empty(1, dtype=torch.int32, device=dev())
+    Z.cache_compact(big, torch.empty(Z.cache_workspace_bytes(big), dtype=torch.uint8, device=dev()), used)
+    assert int(used) == int((big.refs > 0).sum()) and int(big.table[:, :5].max()) < int(used)
+    again = torch.empty(2, H * hd, dtype=torch.bfloat16, device=dev())
+    Z.attention_cache(big, 2, x[:2, :H * hd], again, one, H, 0.1, 301)
+    assert torch.equal(again, outs[1][1])
