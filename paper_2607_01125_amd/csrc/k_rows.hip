@@ -37,23 +37,27 @@ struct RowsArgs {
   uint32_t flags;
 };
 
-__device__ __forceinline__ bf16x8 nibbles(uint32_t v) {
-  v ^= 0x88888888u;
+// Eight codes of a word as 16 + u: each pair is shifted to the mantissas' top and, in one operation, masked
+// and combined with 16 and the turned sign bit.  `base` is kBase held in a vector register: an instruction
+// reads one constant, the mask, from the scalar ones.
+constexpr uint32_t kBase = 0x41C041C0u;
+__device__ __forceinline__ bf16x8 nibbles(uint32_t v, uint32_t base) {
+  constexpr uint32_t mask = 0x00780078u, and_xor = 0x6A;
   uint4 o;
-  o.x = ((v << 3) & 0x00780078u) | 0x41804180u;
-  o.y = ((v >> 1) & 0x00780078u) | 0x41804180u;
-  o.z = ((v >> 5) & 0x00780078u) | 0x41804180u;
-  o.w = ((v >> 9) & 0x00780078u) | 0x41804180u;
+  o.x = __builtin_amdgcn_bitop3_b32(v << 3, mask, base, and_xor);
+  o.y = __builtin_amdgcn_bitop3_b32(v >> 1, mask, base, and_xor);
+  o.z = __builtin_amdgcn_bitop3_b32(v >> 5, mask, base, and_xor);
+  o.w = __builtin_amdgcn_bitop3_b32(v >> 9, mask, base, and_xor);
   return __builtin_bit_cast(bf16x8, o);
 }
 // Eight consecutive values in the order of a word's nibble pairs: (0, 4), (1, 5), (2, 6), (3, 7).
-__device__ __forceinline__ bf16x8 pair_order(uint4 u) {
+__device__ __forceinline__ uint4 pair_order(uint4 u) {
   uint4 o;
   o.x = __builtin_amdgcn_perm(u.z, u.x, 0x05040100);
   o.y = __builtin_amdgcn_perm(u.z, u.x, 0x07060302);
   o.z = __builtin_amdgcn_perm(u.w, u.y, 0x05040100);
   o.w = __builtin_amdgcn_perm(u.w, u.y, 0x07060302);
-  return __builtin_bit_cast(bf16x8, o);
+  return o;
 }
 
 // Eight coefficients (or values of p) from column i0 on, zeros past r.
@@ -72,23 +76,46 @@ __device__ __forceinline__ bf16x8 tail8(const float* row, int i0, int r, bool in
   return v;
 }
 
-// y of one row of x and one feature from its sum (SwiGLU: the gate's; `up` the up feature's, 16 further).
-__device__ __forceinline__ void finish(const RowsArgs& a, int row, int64_t n, float y, float up) {
-  if (a.bias) y += bf2f(a.bias[n]);
-  if (a.res) y += bf2f(a.res[(int64_t)row * a.N + n]);
-  int64_t at = (int64_t)row * a.N + n;
-  if (a.flags & ZOACT_EPI_SWIGLU) {
-    if (a.bias) up += bf2f(a.bias[n + 16]);
-    if (a.res) up += bf2f(a.res[(int64_t)row * a.N + n + 16]);
-    y = y / (1.f + __expf(-y)) * up;
-    at = (int64_t)row * (a.N / 2) + n / 32 * 16 + (n & 15);
-  } else if (a.flags & ZOACT_EPI_RELU) {
-    y = y > 0.f ? y : y != y ? y : 0.f;
+// What is added to the sums of four rows of x, from `row` on, and one feature (SwiGLU: and the up feature,
+// 16 further), as loaded.
+struct Extras {
+  uint16_t b[2], res[2][4];
+};
+__device__ __forceinline__ Extras load_extras(const RowsArgs& a, int row, int64_t n) {
+  Extras e{};
+  const int halves = a.flags & ZOACT_EPI_SWIGLU ? 2 : 1;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (h < halves && n + 16 * h < a.N) {
+      if (a.bias) e.b[h] = a.bias[n + 16 * h];
+      if (a.res) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (row + k < a.rows) e.res[h][k] = a.res[(int64_t)(row + k) * a.N + n + 16 * h];
+      }
+    }
+  return e;
+}
+
+// y of those rows and the feature from the sums (SwiGLU: z the gate's, up the up feature's).
+__device__ __forceinline__ void finish(const RowsArgs& a, int row, int64_t n, const floatx4& z, const floatx4& up,
+                                       const Extras& e) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (row + k >= a.rows) return;
+    float y = z[k] + bf2f(e.b[0]) + bf2f(e.res[0][k]);
+    int64_t at = (int64_t)(row + k) * a.N + n;
+    if (a.flags & ZOACT_EPI_SWIGLU) {
+      y = y / (1.f + __expf(-y)) * (up[k] + bf2f(e.b[1]) + bf2f(e.res[1][k]));
+      at = (int64_t)(row + k) * (a.N / 2) + n / 32 * 16 + (n & 15);
+    } else if (a.flags & ZOACT_EPI_RELU) {
+      y = y > 0.f ? y : y != y ? y : 0.f;
+    }
+    if (a.y_f32)
+      static_cast<float*>(a.y)[at] = y;
+    else
+      static_cast<uint16_t*>(a.y)[at] = f2bf(y);
   }
-  if (a.y_f32)
-    static_cast<float*>(a.y)[at] = y;
-  else
-    static_cast<uint16_t*>(a.y)[at] = f2bf(y);
 }
 
 // Coefficient row of feature n, or -1 where it has none.
@@ -108,7 +135,7 @@ __device__ __forceinline__ int64_t coef_row(const RowsArgs& a, int64_t n) {
 // past it, 7.0 us for 4096 x 4096 at one row, 11.4 at 16; dot products on the vector units for one row,
 // 23 us for 4096 x 28672.)
 constexpr int kWindow = 32;
-template <int RT, int NB, int XR, int NW, int WK, int P>
+template <int RT, int NB, int XR, int NW, int WK>
 __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
   constexpr int WR = NW / WK, TW = RT / WR;              // waves along the tiles, tiles of a wave
   constexpr int WP = 4 * WK, XP = 16 * WK;               // 16-byte pieces of a stage's weight row and x row
@@ -135,16 +162,16 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
   // pieces swapped within 16 (8) by the row's number
   auto swap = [](int row, int piece) { return WK >= 4 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7); };
 
-  uint4 wv[P][WL], xv[P][XL];
+  uint4 wv[WL], xv[XL];
   uint16_t sv[SL];
   // (past the part's last group there is nothing: such pieces are asked for outside the descriptor)
-  auto load = [&](int i, int st) {
+  auto load = [&](int st) {
     const int gr = gbeg + st * WK;
 #pragma unroll
     for (int j = 0; j < WL; ++j) {
       const int u = tid + j * TH, row = u / WP, piece = u % WP;
       if (WN % TH == 0 || u < WN)
-        wv[i][j] = __builtin_bit_cast(
+        wv[j] = __builtin_bit_cast(
             uint4, __builtin_amdgcn_raw_buffer_load_b128(
                        wrs, gr + piece / 4 < gend ? row * (a.K / 2) + gr * 64 + piece * 16 : 0x7FFF0000, 0, 0));
     }
@@ -152,7 +179,7 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
     for (int j = 0; j < XL; ++j) {
       const int u = tid + j * TH, row = u / XP, piece = u % XP;
       if ((XN % TH == 0 || u < XN) && row < a.rows)
-        xv[i][j] = __builtin_bit_cast(
+        xv[j] = __builtin_bit_cast(
             uint4, __builtin_amdgcn_raw_buffer_load_b128(
                        xrs, gr + piece / 16 < gend ? row * a.K * 2 + gr * 256 + piece * 16 : 0x7FFF0000, 0, 0));
     }
@@ -170,78 +197,18 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) tot[t][b] = floatx4{0.f, 0.f, 0.f, 0.f};
   const uint32_t m24 = 0xC1C0C1C0u;                  // (-24, -24)
+  uint32_t base = kBase;
+  asm("" : "+v"(base));
   const bf16x8 minus24 = __builtin_bit_cast(bf16x8, make_uint4(m24, m24, m24, m24));
   load_scales(gbeg);
-#pragma unroll
-  for (int i = 0; i < P; ++i)
-    if (i < stages) load(i, i);
-  // rows of x past the last are never loaded: both buffers start with zeros there
-  for (int u = tid; u < XN; u += TH)
-    if (u / XP >= a.rows) lds[WN + u] = lds[STAGE + WN + u] = make_uint4(0, 0, 0, 0);
-  for (int s0 = 0; s0 < stages; s0 += P) {
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const int st = s0 + i;
-      if (st >= stages) break;
-      uint4* const wb = lds + (st & 1) * STAGE;
-      uint4* const xb = wb + WN;
-      const int win = st / (kWindow / WK), in_win = st % (kWindow / WK);
-      if (in_win == 0) {
-#pragma unroll
-        for (int j = 0; j < SL; ++j) {
-          const int u = tid + j * TH;
-          scl[win & 1][u / kWindow][u % kWindow] = sv[j];
-        }
-        if (st + kWindow / WK < stages) load_scales(gbeg + (win + 1) * kWindow);
-      }
-#pragma unroll
-      for (int j = 0; j < WL; ++j) {
-        const int u = tid + j * TH, row = u / WP, piece = u % WP;
-        if (WN % TH == 0 || u < WN) wb[row * WP + swap(row, piece)] = wv[i][j];
-      }
-#pragma unroll
-      for (int j = 0; j < XL; ++j) {
-        const int u = tid + j * TH, row = u / XP, piece = u % XP;
-        if ((XN % TH == 0 || u < XN) && row < a.rows) xb[row * XP + (piece ^ (row & 15))] = xv[i][j];
-      }
-      if (st + P < stages) load(i, st + P);
-      __syncthreads();
-      if (gbeg + st * WK + wk >= gend) continue;
-      bf16x8 xf[NB][4];
-      floatx4 off[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int xrow = XR < 16 ? l16 & (XR - 1) : b * 16 + l16;
-        off[b] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          xf[b][j] = pair_order(xb[xrow * XP + ((wk * 16 + g * 4 + j) ^ (xrow & 15))]);
-          off[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], minus24, off[b], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int t = 0; t < TW; ++t) {
-        const int row = (wr * TW + t) * 16 + l16;
-        const uint4 v = wb[row * WP + swap(row, wk * 4 + g)];
-        const uint32_t wd[4] = {v.x, v.y, v.z, v.w};
-        const float sc = bf2f(scl[win & 1][row][in_win * WK + wk]);
-        floatx4 acc[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) acc[b] = off[b];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x8 wf = nibbles(wd[j]);
-#pragma unroll
-          for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], wf, acc[b], 0, 0, 0);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) tot[t][b][k] = fmaf(sc, acc[b][k], tot[t][b][k]);
-      }
-    }
-  }
-  // the correction, 32 ranks a step, the steps shared out over the waves of a tile
+  load(0);
+  // (a thread's share of the outputs, where it is one: what is added to them is on its way from here on)
+  constexpr bool kEarly = RT * NB * 64 <= TH;
+  Extras ex{};
+  if (kEarly && tid < RT * NB * 64 && !a.part)
+    ex = load_extras(a, (tid >> 6) % NB * 16 + 4 * (lane >> 4), n0 + (tid >> 6) / NB * 16 + l16);
+  // the correction, 32 ranks a step, the steps shared out over the waves of a tile; here its loads come with
+  // the first stage's
   for (int i0 = 32 * wk; i0 < a.r && blockIdx.y == 0; i0 += 32 * WK) {
     bf16x8 pf[NB];
 #pragma unroll
@@ -256,6 +223,67 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
                                 : tail8(static_cast<const uint16_t*>(a.c) + row * a.r, i0 + 8 * g, a.r, c >= 0);
 #pragma unroll
       for (int b = 0; b < NB; ++b) tot[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[b], cf, tot[t][b], 0, 0, 0);
+    }
+  }
+  // rows of x past the last are never loaded: both buffers start with zeros there
+  for (int u = tid; u < XN; u += TH)
+    if (u / XP >= a.rows) lds[WN + u] = lds[STAGE + WN + u] = make_uint4(0, 0, 0, 0);
+  for (int st = 0; st < stages; ++st) {
+    uint4* const wb = lds + (st & 1) * STAGE;
+    uint4* const xb = wb + WN;
+    const int win = st / (kWindow / WK), in_win = st % (kWindow / WK);
+    if (in_win == 0) {
+#pragma unroll
+      for (int j = 0; j < SL; ++j) {
+        const int u = tid + j * TH;
+        scl[win & 1][u / kWindow][u % kWindow] = sv[j];
+      }
+      if (st + kWindow / WK < stages) load_scales(gbeg + (win + 1) * kWindow);
+    }
+#pragma unroll
+    for (int j = 0; j < WL; ++j) {
+      const int u = tid + j * TH, row = u / WP, piece = u % WP;
+      if (WN % TH == 0 || u < WN) wb[row * WP + swap(row, piece)] = wv[j];
+    }
+#pragma unroll
+    for (int j = 0; j < XL; ++j) {
+      const int u = tid + j * TH, row = u / XP, piece = u % XP;
+      if ((XN % TH == 0 || u < XN) && row < a.rows) xb[row * XP + (piece ^ (row & 15))] = pair_order(xv[j]);
+    }
+    if (st + 1 < stages) load(st + 1);
+    __syncthreads();
+    if (gbeg + st * WK + wk >= gend) continue;
+    bf16x8 xf[NB][4];
+    floatx4 off[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int xrow = XR < 16 ? l16 & (XR - 1) : b * 16 + l16;
+      off[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        xf[b][j] = __builtin_bit_cast(bf16x8, xb[xrow * XP + ((wk * 16 + g * 4 + j) ^ (xrow & 15))]);
+        off[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], minus24, off[b], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+      const int row = (wr * TW + t) * 16 + l16;
+      const uint4 v = wb[row * WP + swap(row, wk * 4 + g)];
+      const uint32_t wd[4] = {v.x, v.y, v.z, v.w};
+      const float sc = bf2f(scl[win & 1][row][in_win * WK + wk]);
+      floatx4 acc[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = off[b];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8 wf = nibbles(wd[j], base);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], wf, acc[b], 0, 0, 0);
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) tot[t][b][k] = fmaf(sc, acc[b][k], tot[t][b][k]);
     }
   }
   __syncthreads();
@@ -283,11 +311,8 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int w = 0; w < WK; ++w) up += sum[((w * RT + t + (RT > 1 ? 1 : 0)) * NB + b) * 64 + ul];
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int row = b * 16 + 4 * (ul >> 4) + k;
-      if (row < a.rows) finish(a, row, n, z[k], up[k]);
-    }
+    const int row = b * 16 + 4 * (ul >> 4);
+    finish(a, row, n, z, up, kEarly ? ex : load_extras(a, row, n));
   }
 }
 
@@ -299,7 +324,9 @@ __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a, int splits, 
   const int ul = (int)(u & 63), b = (int)(u / 64 % NB);
   const int64_t n = tile * 16 + (ul & 15);
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
-  if (tile >= tiles || (swiglu && (tile & 1)) || b * 16 + 4 * (ul >> 4) >= a.rows) return;
+  const int row = b * 16 + 4 * (ul >> 4);
+  if (tile >= tiles || (swiglu && (tile & 1)) || row >= a.rows) return;
+  const Extras ex = load_extras(a, row, n);
   const floatx4* const part = reinterpret_cast<const floatx4*>(a.part);
   floatx4 z{0.f, 0.f, 0.f, 0.f}, up{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -308,11 +335,7 @@ __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a, int splits, 
     z += p[0];
     if (swiglu) up += p[NB * 64];
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int row = b * 16 + 4 * (ul >> 4) + k;
-    if (row < a.rows) finish(a, row, n, z[k], up[k]);
-  }
+  finish(a, row, n, z, up, ex);
 }
 
 
@@ -324,14 +347,14 @@ int splits_of(const RowsArgs& a, int64_t want, int wk, int NB, size_t ws_bytes) 
   return n < 1 ? 1 : n > 64 ? 64 : (int)n;
 }
 
-template <int RT, int NB, int XR, int NW, int WK, int P>
+template <int RT, int NB, int XR, int NW, int WK>
 hipError_t go(RowsArgs a, int splits, void* ws, hipStream_t s) {
   const unsigned tiles = (unsigned)((a.N + 16 * RT - 1) / (16 * RT));
   const int stages = (a.groups + WK - 1) / WK, per = (stages + splits - 1) / splits;
   a.per_split = per * WK;
   splits = (stages + per - 1) / per;
   a.part = splits > 1 ? static_cast<float*>(ws) : nullptr;
-  rows_kernel<RT, NB, XR, NW, WK, P><<<dim3(tiles, (unsigned)splits), 64 * NW, 0, s>>>(a);
+  rows_kernel<RT, NB, XR, NW, WK><<<dim3(tiles, (unsigned)splits), 64 * NW, 0, s>>>(a);
   if (splits > 1) rows_join_kernel<NB><<<(unsigned)((a.N / 16 * NB + 3) / 4), 256, 0, s>>>(a, splits, a.N / 16);
   return hipGetLastError();
 }
@@ -351,13 +374,13 @@ hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStre
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
   const int64_t t16 = a.N / 16;
   if (a.K <= 8192 && t16 <= 2 * cus) {
-    if (t16 <= cus && !swiglu) return go<1, 1, XR, 8, 8, 1>(a, 1, nullptr, s);
-    return go<2, 1, XR, 8, 8, 1>(a, 1, nullptr, s);
+    if (t16 <= cus && !swiglu) return go<1, 1, XR, 8, 8>(a, 1, nullptr, s);
+    return go<2, 1, XR, 8, 8>(a, 1, nullptr, s);
   }
   const int64_t t32 = (t16 + 1) / 2;
-  if (t32 > (XR == 4 ? 4 : 3) * cus) return go<4, 1, XR, 4, 4, 1>(a, 1, nullptr, s);
+  if (t32 > (XR == 4 ? 4 : 3) * cus) return go<4, 1, XR, 4, 4>(a, 1, nullptr, s);
   const int64_t want = t32 < 2 * cus ? (2 * cus + t32 - 1) / t32 : 1;
-  return go<2, 1, XR, 4, 4, 1>(a, splits_of(a, want, 4, 1, ws_bytes), ws, s);
+  return go<2, 1, XR, 4, 4>(a, splits_of(a, want, 4, 1, ws_bytes), ws, s);
 }
 
 // 17 rows and more: 128 weight rows a workgroup, so that x, which every workgroup reads whole, is read
@@ -366,7 +389,7 @@ hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStre
 template <int NB>
 hipError_t pick_more(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
   const int64_t t128 = (a.N / 16 + 7) / 8;
-  return go<8, NB, 16 * NB, 8, 2, 1>(a, splits_of(a, cus / t128, 2, NB, ws_bytes), ws, s);
+  return go<8, NB, 16 * NB, 8, 2>(a, splits_of(a, cus / t128, 2, NB, ws_bytes), ws, s);
 }
 
 hipError_t pick(const RowsArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {
