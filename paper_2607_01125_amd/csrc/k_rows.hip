@@ -2,14 +2,13 @@
 //
 //   y[t][n] = epi(res + b + sum_g s[n][g] sum_{k in g} q[n][k] x[t][k] + sum_i p[t][i] bf16(C[n][i]))
 //
-// Bound by the weights' bytes: each is read once, 16 bytes a lane, straight into the registers that
-// feed the matrix unit.  A lane's 16 bytes are 32 of the 128 columns of one scale group of one weight
-// row, so one load instruction covers 16 rows and one group.  A nibble becomes a bf16 number without
+// Bound by the weights' bytes, each read once.  A lane's 16 bytes of an operand are 32 of the 128 columns
+// of one scale group of one weight row.  A nibble becomes a bf16 number without
 // arithmetic: its bits (with the sign bit turned over, u = q + 8) are put at the top of the mantissa
 // of 16, which gives 16 + u = q + 24 exactly; the surplus 24 sum x is taken out by starting the
 // group's sum from a product of x with a constant -24, which costs one product for all weight rows
 // of the wave.  The group's sum is then scaled: one multiply-add a lane and group, no rounding of
-// q s.  The columns of a word come as pairs (i, i + 4), so x is put in that order instead.
+// q s.  The columns of a word come as pairs (i, i + 4), so x is put in that order as it is staged.
 #include <string>
 
 #include "common.hpp"
@@ -60,53 +59,59 @@ __device__ __forceinline__ uint4 pair_order(uint4 u) {
   return o;
 }
 
-// Eight coefficients (or values of p) from column i0 on, zeros past r.
-__device__ __forceinline__ bf16x8 tail8(const uint16_t* row, int i0, int r, bool in) {
-  if ((r & 7) == 0 && ((uintptr_t)row & 15) == 0)      // (whole pieces, all lanes alike: r and the base are scalar)
-    return in && i0 < r ? *reinterpret_cast<const bf16x8*>(row + i0) : bf16x8{};
-  uint16_t v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = in && i0 + e < r ? row[i0 + e] : (uint16_t)0;
-  return __builtin_bit_cast(bf16x8, *reinterpret_cast<uint4*>(v));
-}
-__device__ __forceinline__ bf16x8 tail8(const float* row, int i0, int r, bool in) {
+// Eight coefficients (or values of p) as bf16 from column i0 on, zeros past r.
+template <typename T>
+__device__ __forceinline__ bf16x8 tail8(const T* row, int i0, int r, bool in) {
   bf16x8 v;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = (__bf16)(in && i0 + e < r ? row[i0 + e] : 0.f);
+  for (int e = 0; e < 8; ++e) {
+    const T x = in && i0 + e < r ? row[i0 + e] : (T)0;
+    if constexpr (sizeof(T) == 2)
+      v[e] = __builtin_bit_cast(__bf16, x);
+    else
+      v[e] = (__bf16)x;
+  }
   return v;
+}
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ bf16x8 keep_if(const u32x4& u, bool c) {
+  return __builtin_bit_cast(bf16x8, u & (c ? 0xFFFFFFFFu : 0u));
 }
 
 // What is added to the sums of four rows of x, from `row` on, and one feature (SwiGLU: and the up feature,
-// 16 further), as loaded.
+// 16 further).  What there is none of is loaded from x instead and dropped at the end: a branch around a load
+// would wait for it where the branches meet.
 struct Extras {
   uint16_t b[2], res[2][4];
+  bool has_b[2], has_res[2];
 };
 __device__ __forceinline__ Extras load_extras(const RowsArgs& a, int row, int64_t n) {
-  Extras e{};
-  const int halves = a.flags & ZOACT_EPI_SWIGLU ? 2 : 1;
+  Extras e;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-    if (h < halves && n + 16 * h < a.N) {
-      if (a.bias) e.b[h] = a.bias[n + 16 * h];
-      if (a.res) {
+  for (int h = 0; h < 2; ++h) {
+    const int64_t f = n + 16 * h;
+    const bool in = f < a.N && (h == 0 || a.flags & ZOACT_EPI_SWIGLU);
+    e.has_b[h] = in && a.bias;
+    e.has_res[h] = in && a.res;
+    e.b[h] = *(e.has_b[h] ? a.bias + f : a.x);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (row + k < a.rows) e.res[h][k] = a.res[(int64_t)(row + k) * a.N + n + 16 * h];
-      }
-    }
+    for (int k = 0; k < 4; ++k)
+      e.res[h][k] = *(e.has_res[h] && row + k < a.rows ? a.res + (int64_t)(row + k) * a.N + f : a.x);
+  }
   return e;
 }
 
+__device__ __forceinline__ float plus(float y, bool has, uint16_t v) { return has ? y + bf2f(v) : y; }
 // y of those rows and the feature from the sums (SwiGLU: z the gate's, up the up feature's).
 __device__ __forceinline__ void finish(const RowsArgs& a, int row, int64_t n, const floatx4& z, const floatx4& up,
                                        const Extras& e) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     if (row + k >= a.rows) return;
-    float y = z[k] + bf2f(e.b[0]) + bf2f(e.res[0][k]);
+    float y = plus(plus(z[k], e.has_b[0], e.b[0]), e.has_res[0], e.res[0][k]);
     int64_t at = (int64_t)(row + k) * a.N + n;
     if (a.flags & ZOACT_EPI_SWIGLU) {
-      y = y / (1.f + __expf(-y)) * (up[k] + bf2f(e.b[1]) + bf2f(e.res[1][k]));
+      y = y / (1.f + __expf(-y)) * plus(plus(up[k], e.has_b[1], e.b[1]), e.has_res[1], e.res[1][k]);
       at = (int64_t)(row + k) * (a.N / 2) + n / 32 * 16 + (n & 15);
     } else if (a.flags & ZOACT_EPI_RELU) {
       y = y > 0.f ? y : y != y ? y : 0.f;
@@ -123,12 +128,84 @@ __device__ __forceinline__ int64_t coef_row(const RowsArgs& a, int64_t n) {
   return n >= a.N || (n >= a.plain0 && n < a.plain1) ? -1 : n >= a.plain1 ? n - (a.plain1 - a.plain0) : n;
 }
 
+// 32 ranks of the correction, from i0 on, for the first `tiles` of TW tiles of features from n0 on and NB blocks
+// of 16 rows of x.  All operands are asked for before one is used, and without branches, as above (one after
+// another they cost 4096 x 6144, 48 rows, 3 us).  Only where rows of p and C are whole 16-byte pieces
+// (elsewhere it adds nothing, see add_odd_ranks).
+__device__ __forceinline__ bool whole_ranks(const RowsArgs& a) {
+  return (a.r & 7) == 0 && ((uintptr_t)a.c & 15) == 0;
+}
+template <int TW, int NB>
+struct Correction {
+  u32x4 p[NB], c[TW], c_hi[TW];        // as loaded (c_hi: the second half of F32 coefficients)
+  bool in, has[TW];
+  __device__ __forceinline__ void load(const RowsArgs& a, int64_t n0, int b0, int i0, int tiles) {
+    const int l16 = threadIdx.x & 15, i = i0 + 8 * ((threadIdx.x & 63) >> 4);
+    in = i < a.r && whole_ranks(a);
+    const u32x4* const other = reinterpret_cast<const u32x4*>(a.x);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int t = (b0 + b) * 16 + l16;               // (rows past the last take row 0)
+      p[b] = *(in ? reinterpret_cast<const u32x4*>(a.p + (int64_t)(t < a.rows ? t : 0) * a.r + i) : other);
+    }
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+      const int64_t row = coef_row(a, n0 + t * 16 + l16);
+      has[t] = in && row >= 0 && t < tiles;
+      const char* const at = static_cast<const char*>(a.c) + ((row * a.r + i) << (a.c_f32 ? 2 : 1));
+      const u32x4* const cr = has[t] ? reinterpret_cast<const u32x4*>(at) : other;
+      c[t] = cr[0];
+      c_hi[t] = cr[a.c_f32];
+    }
+  }
+  __device__ __forceinline__ void apply(const RowsArgs& a, floatx4 (&tot)[TW][NB]) const {
+    bf16x8 cf[TW];
+#pragma unroll
+    for (int t = 0; t < TW; ++t) {
+      if (a.c_f32) {
+        #pragma unroll
+        for (int e = 0; e < 8; ++e)
+          cf[t][e] = (__bf16)(has[t] ? __uint_as_float(e < 4 ? c[t][e & 3] : c_hi[t][e & 3]) : 0.f);
+      } else {
+        cf[t] = keep_if(c[t], has[t]);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const bf16x8 pf = keep_if(p[b], in);
+#pragma unroll
+      for (int t = 0; t < TW; ++t) tot[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf, cf[t], tot[t][b], 0, 0, 0);
+    }
+  }
+};
+
+// The correction where r is not a multiple of 8 or C not aligned: `step` is the waves' share, as above.
+template <int TW, int NB>
+__device__ __forceinline__ void add_odd_ranks(const RowsArgs& a, int64_t n0, int b0, int i0, int step,
+                                              floatx4 (&tot)[TW][NB]) {
+  const int l16 = threadIdx.x & 15;
+  for (i0 += 8 * ((threadIdx.x & 63) >> 4); __any(i0 < a.r); i0 += step) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int row = (b0 + b) * 16 + l16;
+      const bf16x8 pf = tail8(a.p + (int64_t)(row < a.rows ? row : 0) * a.r, i0, a.r, true);
+#pragma unroll
+      for (int t = 0; t < TW; ++t) {
+        const int64_t c = coef_row(a, n0 + t * 16 + l16), at = (c < 0 ? 0 : c) * a.r;
+        const bf16x8 cf = a.c_f32 ? tail8(static_cast<const float*>(a.c) + at, i0, a.r, c >= 0)
+                                  : tail8(static_cast<const uint16_t*>(a.c) + at, i0, a.r, c >= 0);
+        tot[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf, cf, tot[t][b], 0, 0, 0);
+      }
+    }
+  }
+}
+
 // RT tiles of 16 weight rows and NB blocks of 16 rows of x a workgroup (XR rows of x in LDS: 4, or 16 NB),
 // depth in stages of WK groups.  Weights and x come in whole rows' pieces (a quad of lanes reads 64
-// contiguous bytes), P stages ahead in registers, and go through LDS to the operands' order: read straight
-// from memory, an operand's load touches 16 rows, four in every quad, and the address unit bounds the
-// kernel (20480 x 5120, 13 rows: 39 us, against 22).  16-byte pieces are swapped by the row's number, so
-// that neither side of LDS has bank conflicts.  Scales come 32 groups at a time for the same reason.
+// contiguous bytes), a stage ahead in registers (two stages ahead: the same times), and go through LDS to the
+// operands' order; read from memory in that order, where a quad touches four rows, 4096 x 28672 took 23 us at
+// one row and 27 at 13.  16-byte pieces are swapped by the row's number, so that neither side of LDS has bank
+// conflicts.  Scales come 32 groups at a time for the same reason.
 // Wave w takes group w % WK of a stage and the tiles from w / WK on; the waves' sums meet in LDS in a
 // fixed order.  blockIdx.y: the part of the depth (partial sums go to part, rows_join_kernel adds them).
 // (Tried and left: one workgroup of 16 waves a compute unit with all of x in LDS and weights streamed
@@ -207,22 +284,17 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
   Extras ex{};
   if (kEarly && tid < RT * NB * 64 && !a.part)
     ex = load_extras(a, (tid >> 6) % NB * 16 + 4 * (lane >> 4), n0 + (tid >> 6) / NB * 16 + l16);
-  // the correction, 32 ranks a step, the steps shared out over the waves of a tile; here its loads come with
-  // the first stage's
-  for (int i0 = 32 * wk; i0 < a.r && blockIdx.y == 0; i0 += 32 * WK) {
-    bf16x8 pf[NB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int t = b * 16 + l16;
-      pf[b] = tail8(a.p + (int64_t)(t < a.rows ? t : a.rows - 1) * a.r, i0 + 8 * g, a.r, true);
-    }
-#pragma unroll
-    for (int t = 0; t < TW; ++t) {
-      const int64_t c = coef_row(a, n0 + (wr * TW + t) * 16 + l16), row = c < 0 ? 0 : c;
-      const bf16x8 cf = a.c_f32 ? tail8(static_cast<const float*>(a.c) + row * a.r, i0 + 8 * g, a.r, c >= 0)
-                                : tail8(static_cast<const uint16_t*>(a.c) + row * a.r, i0 + 8 * g, a.r, c >= 0);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) tot[t][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pf[b], cf, tot[t][b], 0, 0, 0);
+  // the correction (of one part; else rows_join_kernel's), 32 ranks a step, the steps shared out over the
+  // waves of a tile; here its loads come with the first stage's
+  if (!a.part) {
+    if (whole_ranks(a)) {
+      for (int i0 = 32 * wk; i0 < a.r; i0 += 32 * WK) {
+        Correction<TW, NB> corr;
+        corr.load(a, n0 + wr * TW * 16, 0, i0, TW);
+        corr.apply(a, tot);
+      }
+    } else {
+      add_odd_ranks<TW, NB>(a, n0 + wr * TW * 16, 0, 32 * wk, 32 * WK, tot);
     }
   }
   // rows of x past the last are never loaded: both buffers start with zeros there
@@ -302,7 +374,7 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
     for (int w = 0; w < WK; ++w) z += sum[((w * RT + t) * NB + b) * 64 + ul];
     if (a.part) {
       if (n0 + t * 16 < a.N)
-        reinterpret_cast<floatx4*>(a.part)[(blockIdx.y * (a.N / 16) + blockIdx.x * (int64_t)RT + t) * (NB * 64) + b * 64 + ul] = z;
+        reinterpret_cast<floatx4*>(a.part)[(blockIdx.y * (a.N / 16) + n0 / 16 + t) * (NB * 64) + b * 64 + ul] = z;
       continue;
     }
     const int64_t n = n0 + t * 16 + (ul & 15);
@@ -316,32 +388,43 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
   }
 }
 
-// Adds the parts of the depth in order and finishes: a thread per four rows of x and feature.  tiles: of
-// 16 features.
+// Adds the parts of the depth in order and the correction, and finishes: a wave per tile of 16 features and
+// block of 16 rows of x, whose sums lie as a product's do.  4 us after a product that took 8 to 15, most of
+// it the launch and one trip to memory: bias, residual, correction and sums are all asked for at once.
 template <int NB>
 __global__ void __launch_bounds__(256) rows_join_kernel(RowsArgs a, int splits, int64_t tiles) {
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, tile = u / (NB * 64);
-  const int ul = (int)(u & 63), b = (int)(u / 64 % NB);
-  const int64_t n = tile * 16 + (ul & 15);
+  const int lane = threadIdx.x & 63, b = (int)(u / 64 % NB), row = b * 16 + 4 * (lane >> 4);
+  const int64_t n = tile * 16 + (lane & 15);
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
-  const int row = b * 16 + 4 * (ul >> 4);
-  if (tile >= tiles || (swiglu && (tile & 1)) || row >= a.rows) return;
+  if (tile >= tiles || (swiglu && (tile & 1))) return;
   const Extras ex = load_extras(a, row, n);
+  Correction<2, 1> corr;
+  corr.load(a, tile * 16, b, 0, swiglu ? 2 : 1);
   const floatx4* const part = reinterpret_cast<const floatx4*>(a.part);
-  floatx4 z{0.f, 0.f, 0.f, 0.f}, up{0.f, 0.f, 0.f, 0.f};
+  floatx4 z[2][1] = {{floatx4{0.f, 0.f, 0.f, 0.f}}, {floatx4{0.f, 0.f, 0.f, 0.f}}};
+  const int up = swiglu ? NB * 64 : 0;     // (without SwiGLU the second sum repeats the first and is not used)
 #pragma unroll 4
   for (int s = 0; s < splits; ++s) {
     const floatx4* const p = part + s * tiles * (NB * 64) + u;
-    z += p[0];
-    if (swiglu) up += p[NB * 64];
+    z[0][0] += p[0];
+    z[1][0] += p[up];
   }
-  finish(a, row, n, z, up, ex);
+  corr.apply(a, z);
+  if (whole_ranks(a)) {
+    for (int i0 = 32; i0 < a.r; i0 += 32) {
+      corr.load(a, tile * 16, b, i0, swiglu ? 2 : 1);
+      corr.apply(a, z);
+    }
+  } else {
+    add_odd_ranks<2, 1>(a, tile * 16, b, 0, 32, z);
+  }
+  finish(a, row, n, z[0][0], z[1][0], ex);
 }
 
-
-// Parts of the depth: as many as wanted, of at least two stages of wk groups, and as the workspace holds.
-int splits_of(const RowsArgs& a, int64_t want, int wk, int NB, size_t ws_bytes) {
-  const int64_t deep = a.groups / wk / 2, room = (int64_t)(ws_bytes / ((size_t)(a.N / 16) * NB * 1024));
+// Parts of the depth: as many as wanted, of at least `least` groups, and as the workspace holds.
+int splits_of(const RowsArgs& a, int64_t want, int least, int NB, size_t ws_bytes) {
+  const int64_t deep = a.groups / least, room = (int64_t)(ws_bytes / ((size_t)(a.N / 16) * NB * 1024));
   int64_t n = want < deep ? want : deep;
   n = n < room ? n : room;
   return n < 1 ? 1 : n > 64 ? 64 : (int)n;
@@ -359,28 +442,31 @@ hipError_t go(RowsArgs a, int splits, void* ws, hipStream_t s) {
   return hipGetLastError();
 }
 
-// One block of 16 rows.  A workgroup's weights in flight and the workgroups of a compute unit (LDS: five of
-// 32 weight rows and four rows of x, three with sixteen) bound the time, so layers of few tiles get eight
-// waves on a tile, deep ones parts of the depth, wide ones larger tiles.  us on cold weights (columns x
-// features, 1 / 13 rows; the bytes alone, read in one piece, take the first figure):
-//   4096 x 4096   3.0: 16 weight rows, 8 waves  5.9 /  7.3;  32, 8 waves  6.8 /  8.5;  32, 4 waves  8.2 /  9.4
-//   4096 x 6144   3.7:                          7.1 / 10.0;               7.1 /  8.8;               8.8 / 11.4
-//   4096 x 28672 10.2: 32 weight rows, 4 waves 16.9 / 24.7;  64, 4 waves 17.7 / 20.8
-//   5120 x 20480  9.6:                         16.5 / 20.9;              20.9 / 24.5
-//   14336 x 4096  6.0: 32, 4 waves, 1 part     23.0 / 27.7;  4 parts     12.6 / 14.7;  8 parts     13.6 / 18.1
-//   20480 x 5120  9.6:                         32.1 / 38.9;              18.8 / 22.4;              18.7 / 22.5
+// One block of 16 rows.  What counts is the weights in flight on a compute unit and how few workgroups read x
+// again, so layers of few tiles get eight waves on a tile, deep ones parts of the depth (of six stages at
+// least), wide ones larger tiles, and with more than four rows, whose x weighs more than the tile, those
+// also where parts fill the chip.  us on cold weights (columns x features, 1 / 13 rows; the bytes alone,
+// read in one piece, take the first figure):
+//   4096 x 4096   3.0: 16 weight rows, 8 waves  6.0 /  8.1;  32, 8 waves  7.2 /  8.9;  64, 4 parts  8.3 /  8.6
+//   4096 x 6144   3.7:                          6.8 / 14.2;               7.5 /  9.3;               9.3 /  9.9
+//   4096 x 28672 10.2: 32 weight rows, 4 waves 14.9 / 23.9;  64, 8 waves 14.6 / 17.8
+//   5120 x 20480  9.6:                         14.8 / 19.2;              16.4 / 19.4
+//   14336 x 4096  6.0: 1 part                  22.6 / 27.7;              25.0 / 27.7
+//                      4 parts                 12.5 / 14.4;              12.7 / 13.6;  8 parts     12.6 / 14.0
+//   20480 x 5120  9.6: 1 part                  31.0 / 38.7;              33.4 / 38.7
+//                      4 parts                 16.7 / 21.1;              18.3 / 21.6
+//                      6 parts                 16.3 / 22.9;              16.6 / 18.3;  8 parts     18.4 / 19.7
 template <int XR>
 hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
-  const int64_t t16 = a.N / 16;
+  const int64_t t16 = a.N / 16, t32 = (t16 + 1) / 2, t64 = (t16 + 3) / 4;
   if (a.K <= 8192 && t16 <= 2 * cus) {
-    if (t16 <= cus && !swiglu) return go<1, 1, XR, 8, 8>(a, 1, nullptr, s);
+    if (t16 <= (XR == 4 ? 2 : 1) * cus && !swiglu) return go<1, 1, XR, 8, 8>(a, 1, nullptr, s);
     return go<2, 1, XR, 8, 8>(a, 1, nullptr, s);
   }
-  const int64_t t32 = (t16 + 1) / 2;
-  if (t32 > (XR == 4 ? 4 : 3) * cus) return go<4, 1, XR, 4, 4>(a, 1, nullptr, s);
-  const int64_t want = t32 < 2 * cus ? (2 * cus + t32 - 1) / t32 : 1;
-  return go<2, 1, XR, 4, 4>(a, splits_of(a, want, 4, 1, ws_bytes), ws, s);
+  if constexpr (XR == 4)
+    if (t32 <= 3 * cus) return go<2, 1, XR, 4, 4>(a, splits_of(a, 4 * cus / t32, 24, 1, ws_bytes), ws, s);
+  return go<4, 1, XR, 8, 4>(a, splits_of(a, 2 * cus / t64, 24, 1, ws_bytes), ws, s);
 }
 
 // 17 rows and more: 128 weight rows a workgroup, so that x, which every workgroup reads whole, is read
@@ -389,7 +475,7 @@ hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStre
 template <int NB>
 hipError_t pick_more(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
   const int64_t t128 = (a.N / 16 + 7) / 8;
-  return go<8, NB, 16 * NB, 8, 2>(a, splits_of(a, cus / t128, 2, NB, ws_bytes), ws, s);
+  return go<8, NB, 16 * NB, 8, 2>(a, splits_of(a, cus / t128, 4, NB, ws_bytes), ws, s);
 }
 
 hipError_t pick(const RowsArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {

@@ -116,6 +116,11 @@ CASES = [
     dict(rows=6, K=1024, N=27680, r=8, flags=Z.EPI_SWIGLU),
     dict(rows=3, K=384, N=33040, r=0, res=True),
     dict(rows=20, K=4736, N=352, r=32, flags=Z.EPI_SWIGLU, bias=True),
+    dict(rows=13, K=20480, N=320, r=72, bias=True, c_f32=True),
+    dict(rows=40, K=4096, N=512, r=32, plain=(100, 300), res=True, c_f32=True),
+    dict(rows=9, K=14336, N=96, r=37, flags=Z.EPI_SWIGLU, c_f32=True),
+    dict(rows=1, K=14336, N=1040, r=24, plain=(0, 1040), c_f32=True),
+    dict(rows=2, K=4096, N=6160, r=16, res=True, c_f32=True),
 ]
 
 
