@@ -215,37 +215,72 @@ __device__ __forceinline__ bool good_len(const zoact_cache& c, int L) {
 }
 __device__ __forceinline__ int page_count(int L) { return (int)(((int64_t)L + kPage - 1) / kPage); }
 
-// Inclusive scan over a workgroup of 1024 threads (sh: 16 ints); `total` is the last value.
-__device__ __forceinline__ int scan1024(int v, int* sh, int& total) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int t = __shfl_up(v, o, 64);
-    if (lane >= o) v += t;
-  }
-  __syncthreads();
-  if (lane == 63) sh[w] = v;
+// Inclusive scan over a workgroup of TH threads: within the rows of 16 lanes, over a wave's four rows, then over
+// the waves through sh (TH / 64 ints); `total` is the last value.  One barrier: a scan that follows takes other
+// words of LDS, the one after it may take these again.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_lane(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+template <int TH>
+__device__ __forceinline__ int scan(int v, int* sh, int& total) {
+  constexpr int NW = TH / 64;
+  const int w = threadIdx.x >> 6;
+  v = add_lane<0x111, 0xF>(v);     // from one, two, four, eight lanes before
+  v = add_lane<0x112, 0xF>(v);
+  v = add_lane<0x114, 0xF>(v);
+  v = add_lane<0x118, 0xF>(v);
+  v = add_lane<0x142, 0xA>(v);     // the first row's last to the second, the third's to the fourth
+  v = add_lane<0x143, 0xC>(v);     // the second's last to the third and fourth
+  if ((threadIdx.x & 63) == 63) sh[w] = v;
   __syncthreads();
   int base = 0;
   total = 0;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int t = sh[i];
-    base += i < w ? t : 0;
-    total += t;
+  for (int i = 0; i < NW; i += 4) {
+    const int4 q = *reinterpret_cast<const int4*>(sh + i);
+    const int t[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      base += i + k < w ? t[k] : 0;
+      total += t[k];
+    }
   }
   return base + v;
 }
 
+// How many of v[0 .. i - 1] (LDS, n of them set) are x: four a load and no branches, as a thread's loop of
+// tests one by one took most of extend's time.
+__device__ __forceinline__ int count_before(const int* v, int i, int x, int n) {
+  const int end = n < (int)(threadIdx.x | 63) ? n : (int)(threadIdx.x | 63);      // (the wave's last)
+  int k = 0;
+#pragma unroll 4
+  for (int j = 0; j < end; j += 4) {
+    const int4 q = *reinterpret_cast<const int4*>(v + j);
+    k += (q.x == x && j < i) + (q.y == x && j + 1 < i) + (q.z == x && j + 2 < i) + (q.w == x && j + 3 < i);
+  }
+  return k;
+}
+
 // Bookkeeping of extend: one workgroup, a thread per entry.  ws: pairs[n] (source and target of a
-// page to copy, source -1 for none), then the free pages handed out.
-__global__ void __launch_bounds__(1024) extend_kernel(zoact_cache c, zoact_cache_batch b, int2* __restrict__ pairs,
-                                                      int* __restrict__ fresh) {
-  __shared__ int slot_of[1024], last_of[1024], upto[1024], sh[16];
+// page to copy, source -1 for none), then the free pages handed out past the first kFresh, which stay in LDS.
+// Bound by the trips to memory that wait for each other (slot, length, page, its holders), @@ us;
+// the first free pages are looked for meanwhile.
+constexpr int kFresh = 2048;
+template <int TH>
+__global__ void __launch_bounds__(TH) extend_kernel(zoact_cache c, zoact_cache_batch b, int2* __restrict__ pairs,
+                                                      int* __restrict__ more) {
+  __shared__ __align__(16) int slot_of[TH], last_of[TH], sh[3][TH / 64];
+  __shared__ int upto[TH], first[kFresh];
   const int i = threadIdx.x;
+  const int64_t n_pages = c.n_pages;
+  auto holders = [&](int64_t p) { return c.refs[p < n_pages ? p : n_pages - 1]; };
+  int held[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) held[q] = holders(4 * i + q);
   CacheEntry e{};
   e.slot = -1;
-  int L = 0, last = -1;
+  int L = 0, last = -1, holding = 0;
   bool ok = false;
   if (i < b.n) {
     entry_rows(b, i, e);
@@ -257,41 +292,45 @@ __global__ void __launch_bounds__(1024) extend_kernel(zoact_cache c, zoact_cache
     if (ok && e.count > 0 && L % kPage) {
       last = c.table[(int64_t)e.slot * c.max_pages + L / kPage];
       ok = good_page(c, last);
+      if (ok) holding = c.refs[last];
     }
   }
   slot_of[i] = i < b.n ? e.slot : -1;
   __syncthreads();
-  for (int j = 0; j < i && i < b.n; ++j) ok = ok && slot_of[j] != e.slot;   // named before in the batch
+  if (count_before(slot_of, i, e.slot, b.n) > 0) ok = false;               // named before in the batch
   if (!ok) last = -1;
   last_of[i] = last;
   __syncthreads();
   // a shared last page is copied by every entry that writes to it but its last holder
+  const int before = count_before(last_of, i, last, b.n);
   bool cow = false;
   if (last >= 0) {
-    int before = 0;
-    for (int j = 0; j < i; ++j) before += last_of[j] == last;
-    cow = before < c.refs[last] - 1;
+    cow = before < holding - 1;
   }
   const int grow = ok ? page_count(L + e.count) - page_count(L) : 0;
   const int need = grow + (cow ? 1 : 0);
   int total;
-  const int incl = scan1024(need, sh, total);
+  const int incl = scan<TH>(need, sh[2], total);
   upto[i] = incl;
   // free pages, lowest number first
   int found = 0;
-  const int64_t n_pages = c.n_pages;
-  for (int64_t p0 = 0; p0 < n_pages && found < total; p0 += 4096) {
+  auto fresh = [&](int at) { return at < kFresh ? first[at] : more[at]; };
+  for (int64_t p0 = 0, round = 0; p0 < n_pages && found < total; p0 += 4 * TH, ++round) {
     const int64_t p = p0 + 4 * i;
     int f[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) f[q] = p + q < n_pages && c.refs[p + q] == 0;
+    for (int q = 0; q < 4; ++q) {
+      f[q] = p + q < n_pages && held[q] == 0;
+      held[q] = holders(p + 4 * TH + q);       // (of the next round, if there is one)
+    }
     const int mine = f[0] + f[1] + f[2] + f[3];
     int n;
-    int at = found + scan1024(mine, sh, n) - mine;
+    int at = found + scan<TH>(mine, sh[round & 1], n) - mine;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       if (f[q]) {
-        if (at < total) fresh[at] = (int)(p + q);
+        if (at < total && at < kFresh) first[at] = (int)(p + q);
+        if (at < total && at >= kFresh) more[at] = (int)(p + q);
         ++at;
       }
     found += n;
@@ -308,7 +347,7 @@ __global__ void __launch_bounds__(1024) extend_kernel(zoact_cache c, zoact_cache
     if (served) {
       c.len[e.slot] = L + e.count;
       if (cow) {
-        const int p = fresh[incl - need];
+        const int p = fresh(incl - need);
         pair = make_int2(last, p);
         atomicSub(&c.refs[last], 1);
         c.table[(int64_t)e.slot * c.max_pages + L / kPage] = p;
@@ -320,13 +359,13 @@ __global__ void __launch_bounds__(1024) extend_kernel(zoact_cache c, zoact_cache
   __syncthreads();
   if (!enough) return;
   // tables and counts, a thread per page handed out
-  for (int t = i; t < total; t += 1024) {
+  for (int t = i; t < total; t += TH) {
     int lo = 0, hi = b.n - 1;              // the entry whose pages hold t
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (upto[mid] > t) hi = mid; else lo = mid + 1;
     }
-    const int p = fresh[t], j = t - (lo ? upto[lo - 1] : 0);
+    const int p = fresh(t), j = t - (lo ? upto[lo - 1] : 0);
     c.refs[p] = 1;
     // (a copied page is j = 0: the same entry of the table as written above)
     c.table[(int64_t)slot_of[lo] * c.max_pages + last_of[lo] + j] = p;
@@ -356,25 +395,35 @@ __global__ void __launch_bounds__(256) copy_pairs_kernel(zoact_cache c, const in
   copy_page(c, p.x, p.y, blockIdx.y >> 1, blockIdx.y & 1, blockIdx.z, kCopyParts);
 }
 
-// Fork, first half: a block per entry stages its source's length and pages in ws and adds the
-// destination as a holder (integer sums: any order gives the same counts).
-__global__ void __launch_bounds__(256) fork_read_kernel(zoact_cache c, const int* __restrict__ src,
-                                                        const int* __restrict__ dst, int n, int* __restrict__ ws,
-                                                        uint32_t* status) {
-  const int i = blockIdx.x, s = src[i], d = dst[i];
-  bool ok = s >= 0 && s < c.n_slots && d >= 0 && d < c.n_slots;
+// Whether v[i] is among the values before it: by the W threads of an entry (a workgroup of 256, or half a wave).
+template <int W>
+__device__ __forceinline__ bool named_before(const int* v, int i, int lane) {
+  const int x = v[i];
   bool again = false;
-  for (int j = threadIdx.x; j < i; j += 256) again |= dst[j] == d;
-  ok = !__syncthreads_or(again) && ok;
+  for (int j = lane; j < i; j += W) again |= v[j] == x;
+  if constexpr (W == 32)
+    return (__ballot(again) >> (threadIdx.x & 32)) & 0xFFFFFFFFull;
+  else
+    return __syncthreads_or(again);
+}
+
+// Fork, first half, by an entry's W threads: stages its source's length and pages in ws and adds the
+// destination as a holder (integer sums: any order gives the same counts).
+template <int W>
+__device__ __forceinline__ void fork_read(const zoact_cache& c, const int* src, const int* dst, int n, int i, int lane,
+                                          int* ws, uint32_t* status) {
+  const int s = src[i], d = dst[i];
+  bool ok = s >= 0 && s < c.n_slots && d >= 0 && d < c.n_slots;
+  ok = !named_before<W>(dst, i, lane) && ok;
   const int L = ok ? c.len[s] : 0;
   ok = ok && good_len(c, L) && good_len(c, c.len[d]);
-  if (threadIdx.x == 0) {
+  if (lane == 0) {
     ws[i] = ok ? L : -1;
     if (!ok) raise_status(status, ZOACT_STATUS_BAD_ENTRY);
   }
   if (!ok) return;
   int* const row = ws + n + (int64_t)i * c.max_pages;
-  for (int j = threadIdx.x; j < page_count(L); j += 256) {
+  for (int j = lane; j < page_count(L); j += W) {
     const int p = c.table[(int64_t)s * c.max_pages + j];
     row[j] = p;
     if (good_page(c, p))
@@ -384,40 +433,62 @@ __global__ void __launch_bounds__(256) fork_read_kernel(zoact_cache c, const int
   }
 }
 
-__device__ __forceinline__ void release_slot(const zoact_cache& c, int slot, uint32_t* status) {
+template <int W>
+__device__ __forceinline__ void release_slot(const zoact_cache& c, int slot, int lane, uint32_t* status) {
   const int n = page_count(c.len[slot]);
-  for (int j = threadIdx.x; j < n; j += 256) {
+  for (int j = lane; j < n; j += W) {
     const int p = c.table[(int64_t)slot * c.max_pages + j];
     if (good_page(c, p))
       atomicSub(&c.refs[p], 1);
     else
       raise_status(status, ZOACT_STATUS_BAD_ENTRY);
   }
-  __syncthreads();
 }
 
-// Fork, second half: each destination gives back what it held and takes the staged row.
-__global__ void __launch_bounds__(256) fork_write_kernel(zoact_cache c, const int* __restrict__ dst, int n,
-                                                         const int* __restrict__ ws, uint32_t* status) {
-  const int i = blockIdx.x, L = ws[i];
+// Second half: the destination gives back what it held and takes the staged row.  (A thread gives back and
+// writes the same places of the row; the length is written when all have read it.)
+template <int W>
+__device__ __forceinline__ void fork_write(const zoact_cache& c, const int* dst, int n, int i, int lane, const int* ws,
+                                           uint32_t* status) {
+  const int L = ws[i];
   if (L < 0) return;
   const int d = dst[i];
-  release_slot(c, d, status);
+  release_slot<W>(c, d, lane, status);
   const int* const row = ws + n + (int64_t)i * c.max_pages;
-  for (int j = threadIdx.x; j < page_count(L); j += 256) c.table[(int64_t)d * c.max_pages + j] = row[j];
-  if (threadIdx.x == 0) c.len[d] = L;
+  for (int j = lane; j < page_count(L); j += W) c.table[(int64_t)d * c.max_pages + j] = row[j];
+  if constexpr (W > 64) __syncthreads();
+  if (lane == 0) c.len[d] = L;
+}
+
+__global__ void __launch_bounds__(256) fork_read_kernel(zoact_cache c, const int* __restrict__ src,
+                                                        const int* __restrict__ dst, int n, int* __restrict__ ws,
+                                                        uint32_t* status) {
+  fork_read<256>(c, src, dst, n, blockIdx.x, threadIdx.x, ws, status);
+}
+__global__ void __launch_bounds__(256) fork_write_kernel(zoact_cache c, const int* __restrict__ dst, int n,
+                                                         const int* __restrict__ ws, uint32_t* status) {
+  fork_write<256>(c, dst, n, blockIdx.x, threadIdx.x, ws, status);
+}
+// Both halves in one workgroup, half a wave per entry.
+constexpr int kForkSmall = 4096;
+__global__ void __launch_bounds__(1024) fork_kernel(zoact_cache c, const int* __restrict__ src,
+                                                    const int* __restrict__ dst, int n, int* ws, uint32_t* status) {
+  const int lane = threadIdx.x & 31, first = threadIdx.x >> 5;
+  for (int i = first; i < n; i += 32) fork_read<32>(c, src, dst, n, i, lane, ws, status);
+  __threadfence_block();
+  __syncthreads();
+  for (int i = first; i < n; i += 32) fork_write<32>(c, dst, n, i, lane, ws, status);
 }
 
 __global__ void __launch_bounds__(256) free_kernel(zoact_cache c, const int* __restrict__ slots, uint32_t* status) {
   const int i = blockIdx.x, s = slots[i];
-  bool again = false;
-  for (int j = threadIdx.x; j < i; j += 256) again |= slots[j] == s;
-  if (__syncthreads_or(again)) return;
+  if (named_before<256>(slots, i, threadIdx.x)) return;
   if (s < 0 || s >= c.n_slots || !good_len(c, c.len[s])) {
     if (threadIdx.x == 0) raise_status(status, ZOACT_STATUS_BAD_ENTRY);
     return;
   }
-  release_slot(c, s, status);
+  release_slot<256>(c, s, threadIdx.x, status);
+  __syncthreads();
   if (threadIdx.x == 0) c.len[s] = 0;
 }
 
@@ -427,20 +498,20 @@ __global__ void __launch_bounds__(256) free_kernel(zoact_cache c, const int* __r
 __global__ void __launch_bounds__(1024) compact_plan_kernel(zoact_cache c, int* __restrict__ head,
                                                             int* __restrict__ map, int* __restrict__ src,
                                                             int* __restrict__ dst, int* __restrict__ n_used) {
-  __shared__ int sh[16];
+  __shared__ __align__(16) int sh[3][16];
   const int i = threadIdx.x;
   const int64_t N = c.n_pages;
   int mine = 0, used;
   for (int64_t p = i; p < N; p += 1024) mine += c.refs[p] > 0;
-  scan1024(mine, sh, used);
+  scan<1024>(mine, sh[2], used);
   int ns = 0, nd = 0;
-  for (int64_t p0 = 0; p0 < N; p0 += 1024) {
+  for (int64_t p0 = 0, round = 0; p0 < N; p0 += 1024, ++round) {
     const int64_t p = p0 + i;
     const bool in = p < N, u = in && c.refs[p] > 0;
     const int move = u && p >= used, hole = in && !u && p < used;
     int tot;
     // (both ranks in one scan: at most 1024 of each)
-    const int r = scan1024(move | hole << 16, sh, tot);
+    const int r = scan<1024>(move | hole << 16, sh[round & 1], tot);
     if (move) src[ns + (r & 0xFFFF) - 1] = (int)p;
     if (hole) dst[nd + (r >> 16) - 1] = (int)p;
     ns += tot & 0xFFFF;
@@ -566,7 +637,11 @@ extern "C" zoact_status zoact_cache_extend(const zoact_cache* c, const zoact_cac
   ZC((int64_t)b->n * (b->max_new / kPage + 2) < INT32_MAX, "cache_extend: n * max_new too large");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   int2* const pairs = static_cast<int2*>(ws);
-  extend_kernel<<<1, 1024, 0, s>>>(*c, *b, pairs, reinterpret_cast<int*>(pairs + ZOACT_CACHE_MAX_BATCH));
+  int* const more = reinterpret_cast<int*>(pairs + ZOACT_CACHE_MAX_BATCH);
+  if (b->n <= 256)
+    extend_kernel<256><<<1, 256, 0, s>>>(*c, *b, pairs, more);
+  else
+    extend_kernel<1024><<<1, 1024, 0, s>>>(*c, *b, pairs, more);
   const dim3 grid((unsigned)b->n, (unsigned)(2 * c->n_layers), kCopyParts);
   copy_pairs_kernel<<<grid, 256, 0, s>>>(*c, pairs);
   return done("cache_extend");
@@ -581,8 +656,12 @@ extern "C" zoact_status zoact_cache_fork(const zoact_cache* c, const int32_t* sr
   st = check_ws(*c, ws, ws_bytes, "cache_fork");
   if (st != ZOACT_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  fork_read_kernel<<<(unsigned)n, 256, 0, s>>>(*c, src, dst, n, static_cast<int*>(ws), status);
-  fork_write_kernel<<<(unsigned)n, 256, 0, s>>>(*c, dst, n, static_cast<const int*>(ws), status);
+  if ((int64_t)n * c->max_pages <= kForkSmall) {
+    fork_kernel<<<1, 1024, 0, s>>>(*c, src, dst, n, static_cast<int*>(ws), status);
+  } else {
+    fork_read_kernel<<<(unsigned)n, 256, 0, s>>>(*c, src, dst, n, static_cast<int*>(ws), status);
+    fork_write_kernel<<<(unsigned)n, 256, 0, s>>>(*c, dst, n, static_cast<const int*>(ws), status);
+  }
   return done("cache_fork");
 }
 

@@ -551,7 +551,7 @@ def _on_device(fn, dev: int, stream, *args):
         raise ValueError(f"the stream belongs to {stream.device}, the tensors to cuda:{dev}")
     else:
         raw = stream.cuda_stream
-    if dev == torch.cuda.current_device():
+    if dev == torch._C._cuda_getDevice():
         st = fn(*args, raw)
     else:
         with torch.cuda.device(dev):
@@ -605,15 +605,17 @@ def linear_rows(layer: Linear, arena: Arena | None, x: torch.Tensor, p: torch.Te
     yp = _arg(y, "y", y.dtype, dev, (rows, out))
     rp = _arg(residual, "residual", bf, dev, (rows, layer.d_out))
     pp = _arg(p, "p", bf, dev, (rows, layer.r)) if layer.r else None
-    if layer.w.dtype is torch.uint8:
-        _arg(layer.w, "w", torch.uint8, dev, (layer.d_out, layer.d_in // 2))
-        _arg(layer.w_scales, "w_scales", bf, dev, (layer.d_out, layer.d_in // 128))
-    _arg(layer.bias, "bias", bf, dev, (layer.d_out,))
+    int4, w, sc, ws = layer.w.dtype is torch.uint8, layer.w, layer.w_scales, layer.ws
+    d = LinearDesc(INT4_G128 if int4 else dtype_code(w),
+                   _arg(w, "w", w.dtype, dev, (layer.d_out, layer.d_in // 2) if int4 else None),
+                   _arg(sc, "w_scales", bf, dev, (layer.d_out, layer.d_in // 128)) if int4 else None,
+                   _arg(layer.bias, "bias", bf, dev, (layer.d_out,)), None, layer.d_in, layer.d_out, layer.r,
+                   layer.coef_offset, None, 0, *layer.plain, *_ws(ws, dev))
     a = None
     if layer.r and arena is not None:
-        _arg(arena.c, "arena.c", arena.c.dtype, dev)
-        a = ctypes.byref(arena.desc())
-    _on_device(lib().zoact_linear_rows, dev, stream, ctypes.byref(layer.desc()), a, xp, rows, pp, rp, flags, yp, yd)
+        c = arena.c
+        a = ctypes.byref(ArenaDesc(dtype_code(c), _arg(c, "arena.c", c.dtype, dev), None, None, c.numel()))
+    _on_device(lib().zoact_linear_rows, dev, stream, ctypes.byref(d), a, xp, rows, pp, rp, flags, yp, yd)
 
 
 @dataclass(frozen=True)
@@ -672,7 +674,8 @@ class Cache:
 @dataclass
 class CacheBatch:
     """New rows of one step: entry i is rows row_begin[i] .. row_begin[i + 1] - 1 (or max_new rows each)
-    of slot slots[i] (or slot i); pos [n] int32 is written by cache_extend; status [1] int32."""
+    of slot slots[i] (or slot i); pos [n] int32 is written by cache_extend; status [1] int32.  Checked when
+    first used, and again after a field is set; the tensors' contents may change, the tensors do not."""
     pos: torch.Tensor
     max_new: int
     rows: int
@@ -680,11 +683,20 @@ class CacheBatch:
     row_begin: torch.Tensor | None = None
     status: torch.Tensor | None = None
 
-    def desc(self, dev: int) -> CacheBatchDesc:
-        n, i32 = self.pos.numel(), torch.int32
-        return CacheBatchDesc(n, self.max_new, self.rows, _arg(self.slots, "slots", i32, dev, (n,)),
-                              _arg(self.row_begin, "row_begin", i32, dev, (n + 1,)), _arg(self.pos, "pos", i32, dev, (n,)),
-                              _arg(self.status, "status", i32, dev, (1,)))
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_ref", None)
+
+    def ref(self, dev: int):
+        """The batch's descriptor, by reference, for a cache on device `dev`."""
+        r = self.__dict__.get("_ref")
+        if r is None or r[0] != dev:
+            n, i32 = self.pos.numel(), torch.int32
+            d = CacheBatchDesc(n, self.max_new, self.rows, _arg(self.slots, "slots", i32, dev, (n,)),
+                               _arg(self.row_begin, "row_begin", i32, dev, (n + 1,)),
+                               _arg(self.pos, "pos", i32, dev, (n,)), _arg(self.status, "status", i32, dev, (1,)))
+            r = self.__dict__["_ref"] = (dev, ctypes.byref(d))
+        return r[1]
 
 
 def _ws(ws, dev: int):
@@ -709,7 +721,7 @@ def cache_workspace_bytes(cache: Cache) -> int:
 def cache_extend(cache: Cache, batch: CacheBatch, ws: torch.Tensor, stream=None):
     """Reserve places for the batch's rows; writes batch.pos and the cache's len, table and refs."""
     dev = cache.index
-    _on_device(lib().zoact_cache_extend, dev, stream, cache._ref, ctypes.byref(batch.desc(dev)), *_ws(ws, dev))
+    _on_device(lib().zoact_cache_extend, dev, stream, cache._ref, batch.ref(dev), *_ws(ws, dev))
 
 
 def cache_fork(cache: Cache, src: torch.Tensor, dst: torch.Tensor, ws: torch.Tensor, status=None, stream=None):
@@ -741,12 +753,12 @@ def cache_append(cache: Cache, layer: int, k: torch.Tensor, v: torch.Tensor, bat
     kp, ldk = _heads_arg(k, "k", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
     vp, ldv = _heads_arg(v, "v", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
     _on_device(lib().zoact_cache_append, dev, stream, cache._ref, layer, kp, ldk, vp, ldv, dtype_code(k),
-               ctypes.byref(batch.desc(dev)), *_rope_args(rope, dev, hd))
+               batch.ref(dev), *_rope_args(rope, dev, hd))
 
 
 def attention_cache_workspace_bytes(cache: Cache, batch: CacheBatch, n_heads: int, max_len: int) -> int:
     with torch.cuda.device(cache.index):
-        return int(lib().zoact_attention_cache_workspace_bytes(cache._ref, ctypes.byref(batch.desc(cache.index)),
+        return int(lib().zoact_attention_cache_workspace_bytes(cache._ref, batch.ref(cache.index),
                                                                n_heads, max_len))
 
 
@@ -758,4 +770,4 @@ def attention_cache(cache: Cache, layer: int, q: torch.Tensor, out: torch.Tensor
     qp, ldq = _heads_arg(q, "q", out.dtype, dev, batch.rows, n_heads * hd)
     op = _arg(out, "out", out.dtype, dev, (batch.rows, n_heads * hd))
     _on_device(lib().zoact_attention_cache, dev, stream, cache._ref, layer, qp, ldq, dtype_code(out), n_heads,
-               ctypes.byref(batch.desc(dev)), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))
+               batch.ref(dev), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))

@@ -199,6 +199,23 @@ def test_fork_permutes_and_copies_on_write():
     assert len({int(pr.m.table[s, 1]) for s in (1, 2, 4)}) == 3
 
 
+@pytest.mark.parametrize("n_slots,max_pages", [(40, 2000), (40, 90), (300, 14)])
+def test_forks_of_wide_tables_and_many_slots(n_slots, max_pages):
+    """Forks that go to one workgroup and to one a slot, of sequences of no page to more than 64."""
+    rng = np.random.default_rng(n_slots)
+    pr = Pair(n_pages=2500, hkv=1, hd=32, n_slots=n_slots, max_pages=max_pages, garbage=False)
+    top = min(max_pages * 64, 5000)
+    pr.extend([int(x) for x in rng.integers(0, top + 1, n_slots) * (rng.random(n_slots) < 0.5)])
+    for n in (1, 2, 33, n_slots):
+        announce("fork", n, n_slots, max_pages)
+        pr.fork([int(x) for x in rng.integers(0, n_slots, n)], [int(x) for x in rng.permutation(n_slots)[:n]])
+        pr.check_pages()
+        pr.fork([int(x) for x in rng.integers(-1, n_slots + 1, n)], [int(x) for x in rng.integers(-1, n_slots + 1, n)])
+        pr.check_pages()
+        pr.free([int(x) for x in rng.integers(0, n_slots, max(1, n // 8))])
+        pr.check_pages()
+
+
 def test_extend_serves_all_or_nobody():
     pr = Pair(n_pages=4, n_slots=3, max_pages=8)
     pr.extend([64, 65, 0])
