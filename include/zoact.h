@@ -307,7 +307,8 @@ size_t zoact_linear_workspace_bytes(void);
  * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU); flags:
  * ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, w_scales, p, y and residual 16-byte aligned.
  * L->ws (optional, as above) lets the depth of narrow layers be split over workgroups; the
- * partial sums are added in a fixed order.  Calls that overlap on one workspace race. */
+ * partial sums are added in a fixed order.  Calls that overlap on one workspace race.  y must
+ * not overlap x, p or the layer; it may be the residual itself (BF16, without SWIGLU). */
 enum { ZOACT_ROWS_MAX = 64 };
 zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, const void* x, int64_t rows, const void* p,
                                const void* residual, uint32_t flags, void* y, int32_t y_dtype, zoact_stream stream);

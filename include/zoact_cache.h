@@ -34,7 +34,8 @@
  * more than max_new, places past the table, a page number outside the cache -- is left out
  * and ORs a bit into *status (nullable): extend gives it pos -1, append writes nothing for
  * it, attention writes zeros to its rows where their range is one.  pos[i] < 0 is left
- * out without a bit.  Rows that belong to no entry stay as they were.
+ * out without a bit.  Rows that belong to no entry stay as they were; a batch of no rows at
+ * all is served (its q, k, v and out may be NULL).  Outputs must not overlap inputs.
  */
 #ifndef ZOACT_CACHE_H
 #define ZOACT_CACHE_H

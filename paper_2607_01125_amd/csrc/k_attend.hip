@@ -104,7 +104,6 @@ __device__ __forceinline__ uint4 load_keys(__amdgpu_buffer_rsrc_t rs, int lane, 
     return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, vo, so, 0));
   }
 }
-template <int HD>
 __device__ __forceinline__ uint4 load_values(__amdgpu_buffer_rsrc_t rs, int lane, int d) {
   return __builtin_bit_cast(
       uint4, __builtin_amdgcn_raw_buffer_load_b128(rs, (lane & 15) * kPage + 16 * (lane >> 4), d * 16 * kPage, 0));
@@ -125,7 +124,7 @@ struct ValueLoad {
   __device__ __forceinline__ void go(const int8_t* vp, int lane) {
     const __amdgpu_buffer_rsrc_t rs = page_rsrc(vp, kPage * HD);
 #pragma unroll
-    for (int d = 0; d < HD / 16; ++d) u[d] = load_values<HD>(rs, lane, d);
+    for (int d = 0; d < HD / 16; ++d) u[d] = load_values(rs, lane, d);
   }
 };
 
@@ -515,7 +514,7 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
 #pragma unroll
       for (int d = 0; d < VL; ++d) {
         const int dt = wave * VL + d;
-        if (DT % 4 == 0 || dt < DT) vr[d] = load_values<HD>(vrs, lane, dt);
+        if (DT % 4 == 0 || dt < DT) vr[d] = load_values(vrs, lane, dt);
       }
       ks = scalar4(c.k_scale + head * 4);
       vs = scalar4(c.v_scale + head * 4);
@@ -743,6 +742,11 @@ size_t attend_ws(const zoact_cache& c, const zoact_cache_batch& b, int n_heads, 
   return S > 1 ? (size_t)b.n * b.max_new * n_heads * S * (c.head_dim + 2) * sizeof(float) : 0;
 }
 
+int64_t within(const zoact_cache& c, int64_t max_len) {
+  const int64_t most = (int64_t)c.max_pages * kPage;
+  return max_len < most ? max_len : most;
+}
+
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
@@ -758,6 +762,7 @@ extern "C" size_t zoact_attention_cache_workspace_bytes(const zoact_cache* c, co
   if (check_cache(c) != ZOACT_OK || check_batch(b, c) != ZOACT_OK || n_heads < 1 || n_heads % c->n_kv_heads != 0 ||
       max_len < 1)
     return 0;
+  max_len = within(*c, max_len);
   // (of the types' widths the one with more splits)
   const int G = n_heads / c->n_kv_heads;
   const int s0 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_BF16, *c, *b, G), max_len);
@@ -774,7 +779,7 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   if (st != ZOACT_OK) return st;
   ZA(layer >= 0 && layer < c->n_layers, "attention_cache: layer outside the cache");
   ZA(dtype == ZOACT_F32 || dtype == ZOACT_BF16, "attention_cache: dtype must be F32 or BF16");
-  ZA(q && out, "attention_cache: NULL pointer");
+  ZA((q && out) || b->rows == 0, "attention_cache: NULL pointer");
   ZA(n_heads >= 1 && n_heads % c->n_kv_heads == 0, "attention_cache: n_heads must be a multiple of n_kv_heads");
   const int vec = dtype == ZOACT_BF16 ? 8 : 4;
   ZA(ldq >= (int64_t)n_heads * c->head_dim && ldq % vec == 0 && al16(q) && al16(out),
@@ -783,6 +788,8 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   ZA((cos_t == nullptr) == (sin_t == nullptr), "attention_cache: both rotary tables or neither");
   ZA(cos_t == nullptr || n_pos >= 1, "attention_cache: empty rotary table");
   ZA(al16(cos_t) && al16(sin_t), "attention_cache: rotary tables must be 16-byte aligned");
+  if (b->rows == 0) return ZOACT_OK;
+  max_len = within(*c, max_len);
   AttendArgs a{};
   a.c = *c;
   a.b = *b;

@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) append_kernel(zoact_cache c, int layer, c
   const CacheEntry e = read_entry(c, b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0 && blockIdx.y == 0);
   if (!e.ok || e.count == 0) return;
   const int pg = e.pos / kPage + blockIdx.x, end = e.pos + e.count;
-  if (pg * kPage >= end) return;
+  if ((int64_t)pg * kPage >= end) return;
   const int pid = c.table[(int64_t)e.slot * c.max_pages + pg];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, q = lane & 3;
   const int t0 = pg * kPage + wave * kBlock;     // the block's first token
@@ -250,7 +250,7 @@ __device__ __forceinline__ int scan(int v, int* sh, int& total) {
 }
 
 // How many of v[0 .. i - 1] (LDS, n of them set) are x: four a load and no branches, as a thread's loop of
-// tests one by one took most of extend's time.
+// tests one by one is a branch and a wait each.
 __device__ __forceinline__ int count_before(const int* v, int i, int x, int n) {
   const int end = n < (int)(threadIdx.x | 63) ? n : (int)(threadIdx.x | 63);      // (the wave's last)
   int k = 0;
@@ -264,8 +264,8 @@ __device__ __forceinline__ int count_before(const int* v, int i, int x, int n) {
 
 // Bookkeeping of extend: one workgroup, a thread per entry.  ws: pairs[n] (source and target of a
 // page to copy, source -1 for none), then the free pages handed out past the first kFresh, which stay in LDS.
-// Bound by the trips to memory that wait for each other (slot, length, page, its holders), @@ us;
-// the first free pages are looked for meanwhile.
+// Bound by the trips to memory that wait for each other (slot, length, page, its holders)
+// and the scans: 5.8 us for 32 entries (on 1024 threads 8.1); the first free pages are asked for meanwhile.
 constexpr int kFresh = 2048;
 template <int TH>
 __global__ void __launch_bounds__(TH) extend_kernel(zoact_cache c, zoact_cache_batch b, int2* __restrict__ pairs,
@@ -469,15 +469,16 @@ __global__ void __launch_bounds__(256) fork_write_kernel(zoact_cache c, const in
                                                          const int* __restrict__ ws, uint32_t* status) {
   fork_write<256>(c, dst, n, blockIdx.x, threadIdx.x, ws, status);
 }
-// Both halves in one workgroup, half a wave per entry.
-constexpr int kForkSmall = 4096;
+// Both halves in one workgroup, half a wave per entry, up to 32 entries of 64 pages: 8 full slots of 16 pages 3.3
+// us and 5.4 in two launches, 32 of 16 pages 4.2 and 5.7, 32 of 60 5.4 and 5.5, 32 of 120 7.4 and 5.5, 64 of 60
+// 8.8 and 5.6.
 __global__ void __launch_bounds__(1024) fork_kernel(zoact_cache c, const int* __restrict__ src,
                                                     const int* __restrict__ dst, int n, int* ws, uint32_t* status) {
-  const int lane = threadIdx.x & 31, first = threadIdx.x >> 5;
-  for (int i = first; i < n; i += 32) fork_read<32>(c, src, dst, n, i, lane, ws, status);
+  const int lane = threadIdx.x & 31, i = threadIdx.x >> 5;
+  if (i < n) fork_read<32>(c, src, dst, n, i, lane, ws, status);
   __threadfence_block();
   __syncthreads();
-  for (int i = first; i < n; i += 32) fork_write<32>(c, dst, n, i, lane, ws, status);
+  if (i < n) fork_write<32>(c, dst, n, i, lane, ws, status);
 }
 
 __global__ void __launch_bounds__(256) free_kernel(zoact_cache c, const int* __restrict__ slots, uint32_t* status) {
@@ -593,6 +594,8 @@ zoact_status check_batch(const zoact_cache_batch* b, const zoact_cache* c) {
   ZC(b->n >= 1 && b->n <= ZOACT_CACHE_MAX_BATCH, "cache batch: n outside [1, 1024]");
   ZC(b->max_new >= 1 && b->rows >= 0 && b->rows < INT32_MAX, "cache batch: bad max_new or rows");
   ZC(b->pos != nullptr, "cache batch: NULL pos");
+  ZC((((uintptr_t)b->pos | (uintptr_t)b->slots | (uintptr_t)b->row_begin | (uintptr_t)b->status) & 3) == 0,
+     "cache batch: slots, row_begin, pos and status must be 4-byte aligned");
   ZC(b->slots != nullptr || b->n <= c->n_slots, "cache batch: more entries than slots");
   ZC(b->row_begin != nullptr || (int64_t)b->n * b->max_new <= b->rows, "cache batch: n * max_new exceeds rows");
   return ZOACT_OK;
@@ -608,7 +611,9 @@ zoact_status done(const char* who) {
 template <typename T, int HD>
 void run_append(const zoact_cache& c, int layer, const void* k, int64_t ldk, const void* v, int64_t ldv,
                 const zoact_cache_batch& b, const float* ct, const float* st, int64_t n_pos, hipStream_t s) {
-  const dim3 grid((unsigned)((b.max_new + kPage - 2) / kPage + 1), (unsigned)(2 * c.n_kv_heads), (unsigned)b.n);
+  // (an entry that touches more pages than a slot has does not fit, and is left out)
+  const int64_t pages = ((int64_t)b.max_new + kPage - 2) / kPage + 1;
+  const dim3 grid((unsigned)(pages < c.max_pages ? pages : c.max_pages), (unsigned)(2 * c.n_kv_heads), (unsigned)b.n);
   append_kernel<T, HD><<<grid, 256, 0, s>>>(c, layer, (const T*)k, ldk, (const T*)v, ldv, b, ct, st, n_pos);
 }
 }  // namespace
@@ -656,7 +661,7 @@ extern "C" zoact_status zoact_cache_fork(const zoact_cache* c, const int32_t* sr
   st = check_ws(*c, ws, ws_bytes, "cache_fork");
   if (st != ZOACT_OK) return st;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  if ((int64_t)n * c->max_pages <= kForkSmall) {
+  if (n <= 32 && c->max_pages <= 64) {
     fork_kernel<<<1, 1024, 0, s>>>(*c, src, dst, n, static_cast<int*>(ws), status);
   } else {
     fork_read_kernel<<<(unsigned)n, 256, 0, s>>>(*c, src, dst, n, static_cast<int*>(ws), status);
@@ -698,7 +703,7 @@ extern "C" zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, 
   if (st != ZOACT_OK) return st;
   ZC(layer >= 0 && layer < c->n_layers, "cache_append: layer outside the cache");
   ZC(dtype == ZOACT_F32 || dtype == ZOACT_BF16, "cache_append: dtype must be F32 or BF16");
-  ZC(k && v, "cache_append: NULL pointer");
+  ZC((k && v) || b->rows == 0, "cache_append: NULL pointer");
   const int64_t width = (int64_t)c->n_kv_heads * c->head_dim;
   const int vec = dtype == ZOACT_BF16 ? 8 : 4;
   ZC(ldk >= width && ldv >= width && ldk % vec == 0 && ldv % vec == 0 && al16(k) && al16(v),
@@ -706,6 +711,7 @@ extern "C" zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, 
   ZC((cos_t == nullptr) == (sin_t == nullptr), "cache_append: both rotary tables or neither");
   ZC(cos_t == nullptr || n_pos >= 1, "cache_append: empty rotary table");
   ZC(al16(cos_t) && al16(sin_t), "cache_append: rotary tables must be 16-byte aligned");
+  if (b->rows == 0) return ZOACT_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
 #define ZO_APPEND(T, HD) run_append<T, HD>(*c, layer, k, ldk, v, ldv, *b, cos_t, sin_t, n_pos, s)
   if (dtype == ZOACT_BF16) {

@@ -22,7 +22,8 @@ from . import zoact as Z
 class Session:
     """Sequences in slots 0 .. max_seqs - 1 of up to max_tokens tokens each, over n_pages pages of 64 tokens
     (default: enough for all at full length).  max_rows: most new rows of one call; longer prompts are
-    taken in chunks.  Calls on one Session follow each other on one stream."""
+    taken in chunks.  Calls on one Session, and on all Sessions of one decoder, whose workspaces they share,
+    follow each other on one stream of its device, the current one."""
 
     def __init__(self, decoder, max_seqs: int, max_tokens: int, *, n_pages: int | None = None, max_rows: int = 2048):
         d = self.dec = decoder
@@ -115,6 +116,9 @@ class Session:
         ids = self._slots(slots)
         if tokens.dtype != torch.int32 or tokens.shape != (rows,) or not tokens.is_contiguous():
             raise ValueError(f"tokens must be a contiguous int32 [{rows}]")
+        if tokens.get_device() != self.cache.index or torch.cuda.current_device() != self.cache.index:
+            raise ValueError(f"tokens on {tokens.device}, cuda:{torch.cuda.current_device()} is the current device, "
+                             f"the cache is on cuda:{self.cache.index}")
         for sl, c in zip(slots, counts):
             if self.lens[sl] + c > self.max_pages * Z.CACHE_PAGE:
                 raise ValueError(f"slot {sl} would pass {self.max_pages * Z.CACHE_PAGE} tokens")

@@ -114,6 +114,26 @@ def test_every_call_refuses_a_batch_that_is_none(i):
         assert b"batch" in Z.lib().zoact_last_error()
 
 
+@pytest.mark.parametrize("field", ["pos", "slots", "row_begin", "status"])
+def test_every_call_refuses_misaligned_batches(field):
+    for f in (_extend, _append, _attend):
+        assert f(b=_batch(**{field: 258})) == Z.E_INVALID
+        assert b"aligned" in Z.lib().zoact_last_error()
+
+
+def test_a_batch_of_no_rows_is_served_without_buffers():
+    b = _batch(rows=0, row_begin=256)
+    assert _append(b=b, k=None, v=None) == Z.OK and _attend(b=b, q=None, out=None) == Z.OK
+    assert _append(b=b, k=None, v=None, layer=2) == Z.E_INVALID and _attend(b=b, q=None, out=None, H=3) == Z.E_INVALID
+    assert _append(k=None) == Z.E_INVALID and _attend(out=None) == Z.E_INVALID
+
+
+def test_lengths_past_the_table_do_not_enlarge_the_workspace():
+    f = lambda n: Z.lib().zoact_attention_cache_workspace_bytes(ctypes.byref(_cache(max_pages=4096)),
+                                                                ctypes.byref(_batch()), 4, n)
+    assert f(4096 * 64) == f(2 ** 63 - 1) > 0
+
+
 def test_workspaces():
     need = Z.lib().zoact_cache_workspace_bytes(ctypes.byref(_cache()))
     assert need > 0

@@ -434,6 +434,49 @@ def test_a_step_captured_and_replayed():
     assert int(a.c.len[0]) == 120 + 10 and int(a.status) == 0
 
 
+def test_bounds_far_past_the_table():
+    """max_new and max_len are bounds only: large ones give what the exact ones give."""
+    outs = []
+    for far in (False, True):
+        pr = Pair(n_pages=12, n_slots=2, hkv=2, hd=64, max_pages=6, garbage=False)
+        x = _rows(230, 3 * 128, torch.bfloat16, 4)
+        for lens in ([100, 130], [1, 60]):
+            rows = sum(lens)
+            b = pr.batch(lens, max_new=2 ** 31 - 1 if far else None)
+            announce("bounds", far, lens)
+            Z.cache_extend(pr.c, b, pr.ws)
+            Z.cache_append(pr.c, 0, x[:rows, 128:256], x[:rows, 256:], b)
+        b.max_new = 2 ** 17 if far else 60
+        out = torch.empty(61, 128, dtype=torch.bfloat16, device=dev())
+        Z.attention_cache(pr.c, 0, x[:61, :128], out, b, 2, 0.1, 2 ** 63 - 1 if far else 190)
+        outs.append((out.float(), pr.c.table, pr.c.len, b.pos))
+    for a, b in zip(outs[0][1:], outs[1][1:]):
+        assert torch.equal(a, b)
+    # both within a rounding of the probabilities (2^-12) and of bf16 (2^-8) of means of values
+    assert float((outs[0][0] - outs[1][0]).abs().max()) <= 2 * (2.0 ** -12 + 2.0 ** -8) * float(x.float().abs().max())
+
+
+def test_a_batch_of_no_rows():
+    pr = Pair(n_pages=4, n_slots=3)
+    b = pr.batch([0, 0])
+    none = torch.empty(0, 128, dtype=torch.bfloat16, device=dev())
+    Z.cache_extend(pr.c, b, pr.ws)
+    Z.cache_append(pr.c, 0, none, none, b)
+    Z.attention_cache(pr.c, 0, none, torch.empty_like(none), b, 2, 1.0, 1)
+    assert b.pos.tolist() == [0, 0] and pr.c.len.tolist() == [0, 0, 0]
+
+
+def test_a_batch_is_checked_again_after_a_change():
+    pr = Pair()
+    b, _ = pr.extend([1, 1])
+    b.slots = torch.zeros(2, dtype=torch.int64, device=dev())
+    with pytest.raises(ValueError):
+        Z.cache_extend(pr.c, b, pr.ws)
+    b.slots = t_i32([1, 0])
+    Z.cache_extend(pr.c, b, pr.ws)
+    assert pr.c.len.tolist()[:2] == [2, 2]
+
+
 def test_two_streams_with_their_own_caches():
     """The same work on two streams at once, each with its cache and workspaces, gives the same bits."""
     res = []

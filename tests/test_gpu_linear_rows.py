@@ -134,6 +134,19 @@ def test_rows_against_the_formula(kw, f32_out):
     _check(s, f32_out, ws=3 * (s["N"] // 16) * 1024)       # room for fewer parts than wanted, or none
 
 
+@pytest.mark.parametrize("rows,K,N", [(1, 512, 64), (13, 20480, 320), (40, 4096, 512)])
+def test_the_residual_may_be_y(rows, K, N):
+    announce("in place", rows, K, N)
+    s = _case(rows, K, N, 32, res=True)
+    want = _run(s, False, ws=Z.linear_workspace_bytes())
+    lin = Z.Linear(t_u8(s["packed"]), K, N, 32, w_scales=t_bf16(s["sc"]),
+                   ws=torch.empty(Z.linear_workspace_bytes(), dtype=torch.uint8, device=dev()))
+    z = torch.zeros(1, device=dev())
+    y = t_bf16(s["rs"])
+    Z.linear_rows(lin, Z.Arena(t_bf16(s["c"].ravel()), z, z), t_bf16(s["x"]), t_bf16(s["p"]), y, y)
+    assert torch.equal(y, want)
+
+
 def test_codes_and_scales_one_by_one():
     """Rows that are unit vectors read single weights: each of the 16 nibbles' values, at every place of
     a group, comes out as code times scale exactly (fp32 output; the 24 taken out is exact here)."""
