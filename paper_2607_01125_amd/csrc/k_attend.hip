@@ -467,13 +467,15 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
 // converts a quarter of a page to f16 in LDS, as operands in the order they are read (1 KB apart and
 // contiguous, so neither side has bank conflicts); two buffers, one barrier a page, the next page's
 // codes on their way meanwhile.
+constexpr int chunk_buffers(int HD, int NT, int CT) { return HD == 128 && NT == 1 && CT == 1 ? 1 : 2; }
 template <typename T, int HD, int NT, int CT>
-__global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(256, chunk_buffers(HD, NT, CT) == 1 ? 3 : 2) attend_chunk_kernel(AttendArgs a) {
   constexpr int KS = HD / 32, DT = HD / 16;
   constexpr int KL = HD == 32 ? 1 : HD / 64;          // K loads of a wave (its 16 tokens)
   constexpr int VL = (DT + 3) / 4;                    // V tiles of a wave
-  __shared__ f16x8 kb[2][4][KS][64];
-  __shared__ f16x8 vb[2][DT][2][64];
+  constexpr int NBUF = chunk_buffers(HD, NT, CT);
+  __shared__ f16x8 kb[NBUF][4][KS][64];
+  __shared__ f16x8 vb[NBUF][DT][2][64];
   const zoact_cache& c = a.c;
   const Place at = place_of(a);
   const int hk = at.hk, split = at.split, c0 = at.tile * (64 * CT);
@@ -527,7 +529,8 @@ __global__ void __launch_bounds__(256, 2) attend_chunk_kernel(AttendArgs a) {
       tcol[t] = e.pos + cq / a.G;
       qs[t] = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol[t], g, qf[t]);
     }
-    for (int pg = rg.pbeg, buf = 0; pg < rg.pend; ++pg, buf ^= 1) {
+    for (int pg = rg.pbeg, buf = 0; pg < rg.pend; ++pg, buf ^= NBUF - 1) {
+      if (NBUF == 1 && pg > rg.pbeg) __syncthreads();
 #pragma unroll
       for (int k = 0; k < KS; ++k)
         kb[buf][wave][k][lane] = k & 1 ? codes8(kr[k / 2].z, kr[k / 2].w) : codes8(kr[k / 2].x, kr[k / 2].y);
