@@ -463,43 +463,42 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
   }
 }
 
-// Chunks of new rows: 64 CT columns a workgroup, 16 CT a wave; the waves walk the pages together.  Each
-// converts a quarter of a page to f16 in LDS, as operands in the order they are read (1 KB apart and
-// contiguous, so neither side has bank conflicts); two buffers, one barrier a page, the next page's
-// codes on their way meanwhile.
-constexpr int chunk_buffers(int HD, int NT, int CT) { return HD == 128 && NT == 1 && CT == 1 ? 1 : 2; }
-template <typename T, int HD, int NT, int CT>
-__global__ void __launch_bounds__(256, chunk_buffers(HD, NT, CT) == 1 ? 3 : 2) attend_chunk_kernel(AttendArgs a) {
+// Chunks of new rows: 64 columns a workgroup, 16 a wave; the waves walk the pages together.  Each converts a
+// quarter of a page to f16 in LDS, as operands in the order they are read (1 KB apart and contiguous, so
+// neither side has bank conflicts), the next page's codes on their way meanwhile.  Two buffers and one barrier
+// a page, or one buffer and two where that lets a compute unit hold a third workgroup.
+// Bound by the vector units' share (16 scores a lane and page: scale, maximum, exponential, rounding), the LDS
+// reads and the products in turn: 333 rows of three sequences behind 500 to 1500, 40 heads of 128, 55 us, 366
+// TFLOP/s (with two buffers 63); 4 times 2048 rows, 32/8 heads, 212 us.  128 columns a workgroup, which halve the
+// LDS reads but take 248 registers, are no faster: 71 us and 213.
+constexpr int chunk_buffers(int HD, int NT) { return HD == 128 && NT == 1 ? 1 : 2; }
+template <typename T, int HD, int NT>
+__global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) attend_chunk_kernel(AttendArgs a) {
   constexpr int KS = HD / 32, DT = HD / 16;
   constexpr int KL = HD == 32 ? 1 : HD / 64;          // K loads of a wave (its 16 tokens)
   constexpr int VL = (DT + 3) / 4;                    // V tiles of a wave
-  constexpr int NBUF = chunk_buffers(HD, NT, CT);
+  constexpr int NBUF = chunk_buffers(HD, NT);
   __shared__ f16x8 kb[NBUF][4][KS][64];
   __shared__ f16x8 vb[NBUF][DT][2][64];
   const zoact_cache& c = a.c;
   const Place at = place_of(a);
-  const int hk = at.hk, split = at.split, c0 = at.tile * (64 * CT);
+  const int hk = at.hk, split = at.split, c0 = at.tile * 64;
   const CacheEntry e = read_entry(c, a.b, blockIdx.z, threadIdx.x == 0 && blockIdx.x == 0);
   const int ncol = e.count * a.G;
   if (c0 >= ncol) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, g = lane >> 4;
-  const Range rg = split_range(a, e, (c0 + 64 * CT - 1 < ncol ? c0 + 64 * CT - 1 : ncol - 1) / a.G, split);
-  const int w0 = c0 + 16 * CT * wave;                 // the wave's first column
+  const Range rg = split_range(a, e, (c0 + 63 < ncol ? c0 + 63 : ncol - 1) / a.G, split);
+  const int w0 = c0 + 16 * wave;                 // the wave's first column
   // (a wave past the last column repeats it, so that every wave reaches every barrier)
   const int wfirst = e.pos + (w0 < ncol ? w0 : ncol - 1) / a.G;
-  const int wlast = e.pos + (w0 + 16 * CT - 1 < ncol ? w0 + 16 * CT - 1 : ncol - 1) / a.G;
+  const int wlast = e.pos + (w0 + 15 < ncol ? w0 + 15 : ncol - 1) / a.G;
 
-  floatx4 o[CT][DT];
-  float m[CT], l[CT], qs[CT];
-  f16x8 qf[CT][KS][NT];
-  int tcol[CT], vexp = kNoScale;
+  const int col = w0 + (lane & 15), cq = col < ncol ? col : ncol - 1;
+  floatx4 o[DT];
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[t][d] = floatx4{0.f, 0.f, 0.f, 0.f};
-    m[t] = -INFINITY;
-    l[t] = 0.f;
-  }
+  for (int d = 0; d < DT; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;
+  int vexp = kNoScale;
   if (rg.pbeg < rg.pend) {
     const int* const trow = c.table + (int64_t)e.slot * c.max_pages;
     const int64_t lbase = (int64_t)a.layer * c.n_pages;
@@ -523,12 +522,9 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT, CT) == 1 ? 3 : 2) a
     };
     load(scalar1(trow + rg.pbeg));
     int pid1 = rg.pbeg + 1 < rg.pend ? scalar1(trow + rg.pbeg + 1) : 0;
-#pragma unroll
-    for (int t = 0; t < CT; ++t) {
-      const int col = w0 + 16 * t + (lane & 15), cq = col < ncol ? col : ncol - 1;
-      tcol[t] = e.pos + cq / a.G;
-      qs[t] = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol[t], g, qf[t]);
-    }
+    const int tcol = e.pos + cq / a.G;
+    f16x8 qf[KS][NT];
+    const float qs = load_query<T, HD, NT>(a, e.row0 + cq / a.G, hk * a.G + cq % a.G, tcol, g, qf);
     for (int pg = rg.pbeg, buf = 0; pg < rg.pend; ++pg, buf ^= NBUF - 1) {
       if (NBUF == 1 && pg > rg.pbeg) __syncthreads();
 #pragma unroll
@@ -557,89 +553,115 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT, CT) == 1 ? 3 : 2) a
       float vsc[4];
       const int vold = vexp;
       value_scales(vsn, t0, wlast, vexp, vsc);
-      float s[CT][4][4];
+      float s[4][4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        floatx4 acc[CT];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) acc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+        floatx4 acc{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           const f16x8 kf = kb[buf][n][k][lane];
 #pragma unroll
-          for (int q = 0; q < NT; ++q)
-#pragma unroll
-            for (int t = 0; t < CT; ++t)
-              acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][k][q], acc[t], 0, 0, 0);
+          for (int q = 0; q < NT; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[k][q], acc, 0, 0, 0);
         }
+        const float f = ksc[n] * qs;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          const float f = ksc[n] * qs[t];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][n][i] = acc[t][i] * f;
-        }
+        for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * f;
       }
-      f16x8 pf[CT][2][NT];
-      float alpha[CT];
-#pragma unroll
-      for (int t = 0; t < CT; ++t) {
-        soft_page<NT>(s[t], t0, tcol[t], edge, g, vsc, m[t], l[t], alpha[t], pf[t]);
-        alpha[t] = __builtin_amdgcn_ldexpf(alpha[t], vold - vexp);
-      }
+      f16x8 pf[2][NT];
+      float alpha;
+      soft_page<NT>(s, t0, tcol, edge, g, vsc, m, l, alpha, pf);
+      alpha = __builtin_amdgcn_ldexpf(alpha, vold - vexp);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const f16x8 v0 = vb[buf][d][0][lane], v1 = vb[buf][d][1][lane];
+        floatx4 acc = o[d] * alpha;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          floatx4 acc = o[t][d] * alpha[t];
-#pragma unroll
-          for (int q = 0; q < NT; ++q) {
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[t][0][q], acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[t][1][q], acc, 0, 0, 0);
-          }
-          o[t][d] = acc;
+        for (int q = 0; q < NT; ++q) {
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, pf[0][q], acc, 0, 0, 0);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, pf[1][q], acc, 0, 0, 0);
         }
+        o[d] = acc;
       }
     }
   }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (col >= ncol) return;
+  const int oj = col / a.G, oh = hk * a.G + col % a.G;
+  const float div = l == 0.f ? 1.f : l;
+  const int64_t R = (((int64_t)blockIdx.z * a.b.max_new + oj) * a.H + oh) * a.S + split;
+  if (a.S > 1 && g == 0) a.ml[R] = make_float2(m, l);
 #pragma unroll
-  for (int t = 0; t < CT; ++t) {
-    const int col = w0 + 16 * t + (lane & 15);
-    l[t] += __shfl_xor(l[t], 16, 64);
-    l[t] += __shfl_xor(l[t], 32, 64);
-    if (col >= ncol) continue;
-    const int oj = col / a.G, oh = hk * a.G + col % a.G;
-    const float div = l[t] == 0.f ? 1.f : l[t];
-    const int64_t R = (((int64_t)blockIdx.z * a.b.max_new + oj) * a.H + oh) * a.S + split;
-    if (a.S > 1 && g == 0) a.ml[R] = make_float2(m[t], l[t]);
+  for (int d = 0; d < DT; ++d) {
+    float r[4];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      float r[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[t][d][i], vexp - kPExp);
-      const int d0 = d * 16 + 4 * g;
-      if (a.S > 1) {
-        if (l[t] != 0.f) *reinterpret_cast<float4*>(a.part + R * HD + d0) = make_float4(r[0], r[1], r[2], r[3]);
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i], vexp - kPExp);
+    const int d0 = d * 16 + 4 * g;
+    if (a.S > 1) {
+      if (l != 0.f) *reinterpret_cast<float4*>(a.part + R * HD + d0) = make_float4(r[0], r[1], r[2], r[3]);
+    } else {
+      T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint2*>(op) = make_uint2((uint32_t)f2bf(r[0] / div) | (uint32_t)f2bf(r[1] / div) << 16,
+                                                   (uint32_t)f2bf(r[2] / div) | (uint32_t)f2bf(r[3] / div) << 16);
       } else {
-        T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<uint2*>(op) =
-              make_uint2((uint32_t)f2bf(r[0] / div) | (uint32_t)f2bf(r[1] / div) << 16,
-                         (uint32_t)f2bf(r[2] / div) | (uint32_t)f2bf(r[3] / div) << 16);
-        } else {
-          *reinterpret_cast<float4*>(op) = make_float4(r[0] / div, r[1] / div, r[2] / div, r[3] / div);
-        }
+        *reinterpret_cast<float4*>(op) = make_float4(r[0] / div, r[1] / div, r[2] / div, r[3] / div);
       }
     }
   }
 }
 
-// Joins the splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits, up to NI each.
-// A thread's sums are on their way while the statistics, a thread a split, give the weights.
 constexpr int kMaxSplits = 128;
-template <typename T, int HD, int NI>
+// Joins up to eight splits of a row and head in half a wave, HD / 32 columns a lane; sums and statistics (a lane
+// holds those of split lane % 8) are asked for at once.
+constexpr int kFewSplits = 8;
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
+  constexpr int DV = HD / 32;
+  typedef float vec __attribute__((ext_vector_type(DV)));
+  const CacheEntry e = read_entry(a.c, a.b, blockIdx.z, false);
+  const int lane = threadIdx.x & 63, d0 = (lane & 31) * DV;
+  const int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int64_t R = ((int64_t)blockIdx.z * a.b.max_new * a.H + row) * a.S;
+  if (row >= (int64_t)e.count * a.H) return;
+  const int k0 = lane & 7;
+  const float2 got = a.ml[R + (k0 < a.S ? k0 : 0)];
+  vec v[kFewSplits];
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k)
+    v[k] = *reinterpret_cast<const vec*>(a.part + (R + (k < a.S ? k : 0)) * HD + d0);
+  const float m = k0 < a.S ? got.x : -INFINITY, l = k0 < a.S ? got.y : 0.f;
+  float M = m;
+#pragma unroll
+  for (int k = 1; k < 8; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
+  const float base = M == -INFINITY ? 0.f : M;
+  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - base);
+  float L = f * l;
+#pragma unroll
+  for (int k = 1; k < 8; k <<= 1) L += __shfl_xor(L, k, 64);
+  vec r = 0.f;
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {
+    const float w = __shfl(f, (lane & ~7) | k, 64);
+    if (w != 0.f) r += w * v[k];        // (an empty split has written no sums; a NaN weight counts)
+  }
+  const float div = L == 0.f ? 1.f : L;
+  T* const op = static_cast<T*>(a.out) + ((int64_t)e.row0 * a.H + row) * HD + d0;
+#pragma unroll
+  for (int d = 0; d < DV; ++d) {
+    const float y = L == 0.f ? 0.f : r[d] / div;
+    if constexpr (sizeof(T) == 2)
+      op[d] = f2bf(y);
+    else
+      op[d] = y;
+  }
+}
+
+// Joins more splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits, up to NI each.
+// A thread's sums are on their way while the statistics, a thread a split, give the weights.
+template <typename T, int HD>
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
-  constexpr int DV = HD / 32, NG = 8;
+  constexpr int DV = HD / 32, NG = 8, NI = kMaxSplits / NG;
   typedef float vec __attribute__((ext_vector_type(DV)));
   __shared__ float wt[kMaxSplits], red[2], redl[2];
   __shared__ vec sr[NG][32];
@@ -652,8 +674,10 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   if (tid < a.S) ml = a.ml[R + tid];
   vec v[NI];
 #pragma unroll
-  for (int k = 0; k < NI; ++k)
-    if (grp + k * NG < a.S) v[k] = *reinterpret_cast<const vec*>(a.part + (R + grp + k * NG) * HD + (tid & 31) * DV);
+  for (int k = 0; k < NI; ++k) {
+    const int at = grp + k * NG < a.S ? grp + k * NG : 0;
+    v[k] = *reinterpret_cast<const vec*>(a.part + (R + at) * HD + (tid & 31) * DV);
+  }
   if (wave < kMaxSplits / 64) {
     float M = ml.x;
 #pragma unroll
@@ -693,13 +717,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
     *op = y;
 }
 
-// Query columns of a workgroup: 16 while that holds an entry's (decoding); for chunks of rows 64, or 128
-// (bf16) where that still makes four workgroups a compute unit: 16 chunks of 256 rows behind 500 tokens,
-// 32/8 heads of 128, 101 us with 64 and 87 with 128, but one of 512 rows 19 and 39.
-int attend_cols(int32_t dtype, const zoact_cache& c, const zoact_cache_batch& b, int G) {
-  const int64_t cols = (int64_t)b.max_new * G, wide = (cols + 127) / 128 * c.n_kv_heads * b.n;
-  return cols <= 16 ? 16 : dtype == ZOACT_BF16 && wide >= 4 * (cu_count() > 0 ? cu_count() : 256) ? 128 : 64;
-}
+// Query columns of a workgroup: 16 while that holds an entry's (decoding), 64 for chunks of rows.
+int attend_cols(const zoact_cache_batch& b, int G) { return (int64_t)b.max_new * G <= 16 ? 16 : 64; }
 
 template <typename T, int HD, int NT>
 void run_attend(const AttendArgs& a, int w, hipStream_t s) {
@@ -707,34 +726,42 @@ void run_attend(const AttendArgs& a, int w, hipStream_t s) {
   const dim3 grid((unsigned)(tiles * a.S * a.c.n_kv_heads), 1, (unsigned)a.b.n);
   if (w == 16)
     attend_kernel<T, HD, NT><<<grid, 256, 0, s>>>(a);
-  else if (w == 64)
-    attend_chunk_kernel<T, HD, NT, 1><<<grid, 256, 0, s>>>(a);
-  else if constexpr (NT == 1)
-    attend_chunk_kernel<T, HD, NT, 2><<<grid, 256, 0, s>>>(a);
-  if (a.S > 1) {
+  else
+    attend_chunk_kernel<T, HD, NT><<<grid, 256, 0, s>>>(a);
+  if (a.S > kFewSplits) {
     const dim3 join((unsigned)a.H, (unsigned)a.b.max_new, (unsigned)a.b.n);
-    if (a.S <= 8)
-      attend_join_kernel<T, HD, 1><<<join, 256, 0, s>>>(a);
-    else
-      attend_join_kernel<T, HD, kMaxSplits / 8><<<join, 256, 0, s>>>(a);
+    attend_join_kernel<T, HD><<<join, 256, 0, s>>>(a);
+  } else if (a.S > 1) {
+    const dim3 join((unsigned)(((int64_t)a.b.max_new * a.H + 7) / 8), 1, (unsigned)a.b.n);
+    attend_join_few_kernel<T, HD><<<join, 256, 0, s>>>(a);
   }
 }
 
-// Splits of the length.  Sixteen pages each (four a wave) where that gives two workgroups a compute unit,
-// else as few as four pages, so that sequences of unequal length end together and a single one fills the
-// chip; the join reads 2 KB for 256 KB of such a split.
-int attend_splits(const zoact_cache& c, const zoact_cache_batch& b, int n_heads, int w, int64_t max_len) {
+// Splits of the length.  Decoding: sixteen pages each (four a wave) where that gives two workgroups a compute
+// unit, else as few as four pages, so that sequences of unequal length end together and a single one fills the
+// chip; the join reads 2 KB for 256 KB of such a split.  Chunks: one round of the workgroups that compute
+// units hold (three in bf16, two in fp32), of eight pages at least, as their partial results weigh more: 512
+// rows, 32/8 heads of 128, behind 4000 tokens 115 us unsplit, 88 in two, 79 in three, 83 in six; behind none
+// 19, 26, 25 and 30.  Chunks of up to 16 rows may go down to four pages too: 16 rows behind 9000 tokens 25 us
+// in 16 splits, 20 in 32.
+int attend_splits(const zoact_cache& c, const zoact_cache_batch& b, int n_heads, int w, int32_t dtype,
+                  int64_t max_len) {
   const int G = n_heads / c.n_kv_heads;
   const int64_t tiles = ((int64_t)b.max_new * G + w - 1) / w;
   const int64_t groups = tiles * c.n_kv_heads * b.n;
-  const int64_t pages = (max_len + kPage - 1) / kPage;
-  const int64_t want = 2 * (cu_count() > 0 ? cu_count() : 256);
-  int64_t s = (pages + 15) / 16;
-  if (groups * s < want) s = (want + groups - 1) / groups;
-  // (between one and two rounds of three workgroups a compute unit: one)
-  if (groups * s > want + want / 2 && groups * s < 3 * want && groups <= want) s = (want + want / 2) / groups;
-  if (w > 16 && 2 * groups >= want) s = 1;                              // (a chunk's own tiles are many)
-  if (s > (pages + 3) / 4) s = (pages + 3) / 4;
+  const int64_t pages = (max_len + kPage - 1) / kPage, cus = cu_count() > 0 ? cu_count() : 256;
+  int64_t s, most = (pages + 3) / 4;
+  if (w > 16) {
+    s = (dtype == ZOACT_BF16 ? 3 : 2) * cus / groups;
+    if (b.max_new > 16) most = pages / 8;
+  } else {
+    const int64_t want = 2 * cus;
+    s = (pages + 15) / 16;
+    if (groups * s < want) s = (want + groups - 1) / groups;
+    // (between one and two rounds of three workgroups a compute unit: one)
+    if (groups * s > want + want / 2 && groups * s < 3 * want && groups <= want) s = (want + want / 2) / groups;
+  }
+  if (s > most) s = most;
   if (s > kMaxSplits) s = kMaxSplits;
   // (the second pass has a grid row per new row)
   if (b.max_new > 65535) s = 1;
@@ -766,11 +793,9 @@ extern "C" size_t zoact_attention_cache_workspace_bytes(const zoact_cache* c, co
       max_len < 1)
     return 0;
   max_len = within(*c, max_len);
-  // (of the types' widths the one with more splits)
-  const int G = n_heads / c->n_kv_heads;
-  const int s0 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_BF16, *c, *b, G), max_len);
-  const int s1 = attend_splits(*c, *b, n_heads, attend_cols(ZOACT_F32, *c, *b, G), max_len);
-  return attend_ws(*c, *b, n_heads, s0 > s1 ? s0 : s1);
+  // (of the types the one with more splits: bf16, see attend_splits)
+  const int w = attend_cols(*b, n_heads / c->n_kv_heads);
+  return attend_ws(*c, *b, n_heads, attend_splits(*c, *b, n_heads, w, ZOACT_BF16, max_len));
 }
 
 extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t layer, const void* q, int64_t ldq,
@@ -800,8 +825,8 @@ extern "C" zoact_status zoact_attention_cache(const zoact_cache* c, int32_t laye
   a.H = n_heads;
   a.G = n_heads / c->n_kv_heads;
   ZA((int64_t)b->max_new * n_heads < INT32_MAX / kMaxSplits, "attention_cache: too many new rows");
-  const int w = attend_cols(dtype, *c, *b, a.G);
-  a.S = attend_splits(*c, *b, n_heads, w, max_len);
+  const int w = attend_cols(*b, a.G);
+  a.S = attend_splits(*c, *b, n_heads, w, dtype, max_len);
   const size_t need = attend_ws(*c, *b, n_heads, a.S);
   if (ws == nullptr || ws_bytes < need) a.S = 1;
   if (a.S > 1) ZA(al16(ws), "attention_cache: ws must be 16-byte aligned");
