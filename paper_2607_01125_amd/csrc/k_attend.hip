@@ -146,24 +146,28 @@ __device__ __forceinline__ void value_scales(const floatx4& vs, int t0, int last
   for (int n = 0; n < 4; ++n) vsc[n] = __builtin_amdgcn_ldexpf(vsc[n], kPExp - vexp);
 }
 
-// One page's scores (log2 domain) of a lane's column: masks tokens past lim (edge: there may be some),
-// updates the running maximum and sum, and gives the factor of what was summed before and the
-// probabilities times V's scales as terms.
+// One page's scores of a lane's column, s times its block's f >= 0 (log2 domain): masks tokens past lim (edge:
+// there may be some), updates the running maximum and sum, and gives the factor of what was summed before and
+// the probabilities times V's scales as terms.  The maximum is taken before the factor, a product a block, and
+// the factor and the maximum's subtraction are one multiply-add a score.
 template <int NT>
-__device__ __forceinline__ void soft_page(float (&s)[4][4], int t0, int lim, bool edge, int g, const float (&vsc)[4],
-                                          float& m, float& l, float& alpha, f16x8 (&pf)[2][NT]) {
+__device__ __forceinline__ void soft_page(float (&s)[4][4], float (&f)[4], int t0, int lim, bool edge, int g,
+                                          const float (&vsc)[4], float& m, float& l, float& alpha,
+                                          f16x8 (&pf)[2][NT]) {
   if (edge) {
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
+    for (int n = 0; n < 4; ++n) {
+      // (no factor 0 or NaN meets an infinity that stands for a masked token)
+      const int first = t0 + 16 * n + 4 * g;
+      const bool none = first > lim, zero = f[n] == 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (t0 + 16 * n + 4 * g + i > lim) s[n][i] = -INFINITY;
+      for (int i = 0; i < 4; ++i) s[n][i] = first + i > lim ? -INFINITY : zero ? s[n][i] * 0.f : s[n][i];
+      if (none || zero) f[n] = 1.f;
+    }
   }
   float mx = m;
 #pragma unroll
-  for (int n = 0; n < 4; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[n][i]);
+  for (int n = 0; n < 4; ++n) mx = fmaxf(mx, fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])) * f[n]);
   mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
   mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
   const float base = mx == -INFINITY ? 0.f : mx;
@@ -179,7 +183,7 @@ __device__ __forceinline__ void soft_page(float (&s)[4][4], int t0, int lim, boo
       float p[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(s[2 * n2 + n][i] - base);
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s[2 * n2 + n][i], f[2 * n2 + n], -base));
         p8[4 * n + i] = p[i] * vsc[2 * n2 + n];
       }
       lsum += (p[0] + p[1]) + (p[2] + p[3]);
@@ -222,12 +226,13 @@ __device__ __forceinline__ float column_top(const float (&x)[8], float top) {
   for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(x[k]));
   return top;
 }
-// Factor of the values, and of the scores (log2 domain) in return; both powers of two stay normal numbers.
+// Factor of the values, and of the scores (log2 domain) in return, that one not negative; both powers of two
+// stay normal numbers.
 __device__ __forceinline__ float column_shift(const AttendArgs& a, float top, float& factor) {
   int sh = 14 - ((int)(__float_as_uint(top) >> 23) - 127);
   sh = top == 0.f ? 0 : sh > 120 ? 120 : sh < -113 ? -113 : sh;
-  factor = __uint_as_float((uint32_t)(127 + sh) << 23);
-  return __uint_as_float((uint32_t)(127 - sh) << 23) * a.scale;
+  factor = copysignf(__uint_as_float((uint32_t)(127 + sh) << 23), a.scale);
+  return __uint_as_float((uint32_t)(127 - sh) << 23) * fabsf(a.scale);
 }
 template <typename T, int HD, int NT>
 __device__ __forceinline__ float load_query(const AttendArgs& a, int64_t row, int h, int64_t pos, int g,
@@ -360,7 +365,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
       vl.go(c.v + head * (kPage * HD), lane);
       const floatx4 vs = scalar4(c.v_scale + head * 4);
       const float ksc[4] = {ks[0], ks[1], ks[2], ks[3]};
-      float s[4][4];
+      float s[4][4], f[4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         floatx4 acc{0.f, 0.f, 0.f, 0.f};
@@ -371,9 +376,9 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
 #pragma unroll
           for (int q = 0; q < NT; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[k][q], acc, 0, 0, 0);
         }
-        const float f = ksc[n] * qs;
+        f[n] = ksc[n] * qs;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * f;
+        for (int i = 0; i < 4; ++i) s[n][i] = acc[i];
         __builtin_amdgcn_sched_barrier(0);      // (codes converted early would not fit three waves' registers)
       }
       const int t0 = pg * kPage, next = pg + 4;
@@ -391,7 +396,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
       const int vold = vexp;
       value_scales(vs, t0, now_bad ? -1 : rg.last, vexp, vsc);
       f16x8 pf[2][NT];
-      soft_page<NT>(s, t0, now_bad ? -1 : tcol, edge, g, vsc, m, l, alpha, pf);
+      soft_page<NT>(s, f, t0, now_bad ? -1 : tcol, edge, g, vsc, m, l, alpha, pf);
       alpha = __builtin_amdgcn_ldexpf(alpha, vold - vexp);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
@@ -553,7 +558,7 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
       float vsc[4];
       const int vold = vexp;
       value_scales(vsn, t0, wlast, vexp, vsc);
-      float s[4][4];
+      float s[4][4], f[4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         floatx4 acc{0.f, 0.f, 0.f, 0.f};
@@ -563,13 +568,13 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
 #pragma unroll
           for (int q = 0; q < NT; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[k][q], acc, 0, 0, 0);
         }
-        const float f = ksc[n] * qs;
+        f[n] = ksc[n] * qs;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[n][i] = acc[i] * f;
+        for (int i = 0; i < 4; ++i) s[n][i] = acc[i];
       }
       f16x8 pf[2][NT];
       float alpha;
-      soft_page<NT>(s, t0, tcol, edge, g, vsc, m, l, alpha, pf);
+      soft_page<NT>(s, f, t0, tcol, edge, g, vsc, m, l, alpha, pf);
       alpha = __builtin_amdgcn_ldexpf(alpha, vold - vexp);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {

@@ -137,6 +137,24 @@ def test_append_zero_tiny_and_non_finite_values():
     pr.check_codes()
 
 
+@pytest.mark.parametrize("hd", [32, 128])
+def test_append_values_next_to_the_middle_between_codes(hd):
+    """Quotients k + 1/2, and the numbers beside them, under scales that are powers of two and others."""
+    pr = Pair(hd=hd, hkv=1, n_pages=8, n_slots=1, max_pages=8)
+    mids = np.arange(-127, 127, dtype=np.float32) + np.float32(0.5)
+    up, down = np.nextafter(mids, np.float32(np.inf)), np.nextafter(mids, np.float32(-np.inf))
+    for unit in (1.0, 2.0 ** -40, 0.7, 1e-3, 3e30, 2.0 ** -99, 2.0 ** -101, 2.0 ** -126, 2.0 ** -140):
+        s = np.float32(127 * unit) * np.float32(1 / 127)
+        vals = np.concatenate([mids, up, down]) * s
+        vals = np.resize(vals, (-(-vals.size // (hd - 1)), hd - 1))
+        rows = np.concatenate([np.full((len(vals), 1), 127 * unit), vals], 1).astype(np.float32)
+        rows = np.clip(rows, -np.float32(127 * unit), np.float32(127 * unit))[:48]
+        b, pos = pr.extend([len(rows)])
+        t = torch.from_numpy(np.ascontiguousarray(rows)).to(dev())
+        pr.append(0, t, t, b, pos, [len(rows)])
+        pr.check_codes()
+
+
 def test_append_leaves_out_what_it_cannot_place():
     """pos below 0, a slot or place outside the cache, rows outside the buffers, a page number outside the
     pool: nothing is written for these entries, the others are served."""
@@ -317,6 +335,26 @@ def test_attention_of_a_long_sequence_in_many_splits(dtype):
     again = torch.empty_like(out)
     Z.attention_cache(pr.c, 1, q, again, b, 8, float(np.float32(64 ** -0.5)), 5000, rope=rp, ws=ws)
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [-0.4, 0.4])
+@pytest.mark.parametrize("lens,counts", [([40, 130, 16], [1, 1, 2]), ([40, 0, 150], [40, 70, 20])])
+def test_attention_blocks_of_zero_keys_and_a_negative_scale(lens, counts, scale, dtype):
+    """Blocks whose keys are all zero have scale 0: their scores are 0, neither masked nor NaN, also where the
+    row's own end lies in one."""
+    H, hkv, hd = 4, 2, 64
+    pr = Pair(n_pages=16, hkv=hkv, hd=hd, n_slots=3, max_pages=4)
+    for part in (lens, counts):
+        b, pos = pr.extend(part)
+        x = _rows(sum(part), (H + 2 * hkv) * hd, dtype, 7 + sum(part))
+        keys = x[:, H * hd:(H + hkv) * hd]
+        at = torch.cat([torch.arange(p, p + c) for p, c in zip(pos, part)]).to(dev())
+        keys[(at < 16) | ((at >= 32) & (at < 48)) | (at >= 112)] = 0
+        pr.append(0, keys, x[:, (H + hkv) * hd:], b, pos, part)
+    pr.check_codes()
+    for split in (False, True):
+        _check_attention(pr, b, pos, x[:, :H * hd], counts, H, dtype, None, 220, split=split, scale=scale)
 
 
 def test_attention_sharp_and_flat_scores():
