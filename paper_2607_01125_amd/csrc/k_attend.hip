@@ -284,7 +284,11 @@ __device__ __forceinline__ Range split_range(const AttendArgs& a, const CacheEnt
   return r;
 }
 
-// Decoding: at most 16 columns, each wave its own pages.
+// Decoding: at most 16 columns, each wave its own pages.  Bound by the pages' bytes: one row behind 131071 tokens,
+// 8 key/value heads of 128 (268 MB), 51 us and 5 for the join, 5.3 TB/s; the same pages read in the same way
+// and nothing done with them, 45 us.  48 rows behind 70 to 8000 tokens (271 MB): 60 and 5.  Half of a wave's
+// cycles wait for memory, a third issue vector instructions.  (Pages through LDS in whole rows' order: 67 us
+// where this order took 61.)
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs a) {
   constexpr int KS = HD / 32;           // 32-deep products of a score
@@ -618,7 +622,8 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
 
 constexpr int kMaxSplits = 128;
 // Joins up to eight splits of a row and head in half a wave, HD / 32 columns a lane; sums and statistics (a lane
-// holds those of split lane % 8) are asked for at once.
+// holds those of split lane % 8) are asked for at once.  Bound by the launch and one trip to memory: 48 rows of 32
+// heads in eight splits 5 us; for 512 rows in three, a workgroup a row and head took 13 us more.
 constexpr int kFewSplits = 8;
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
@@ -663,7 +668,8 @@ __global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
 }
 
 // Joins more splits of one row and head: 32 lanes of HD / 32 columns, eight groups of splits, up to NI each.
-// A thread's sums are on their way while the statistics, a thread a split, give the weights.
+// A thread's sums are on their way while the statistics, a thread a split, give the weights.  32 heads of one row
+// in 96 splits: 5 us.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   constexpr int DV = HD / 32, NG = 8, NI = kMaxSplits / NG;
