@@ -158,7 +158,9 @@ class Session:
             if not few:
                 return d._apply(lb, x, T, y, pert, ut, residual=residual, flags=flags, adapt=ut is not None)
             adapted = blk is not None and ut is not None
-            lin.r = d.r if adapted else 0
+            r = d.r if adapted else 0
+            if lin.r != r:
+                lin.r = r
             Z.linear_rows(lin, d.arena if adapted else None, x[:rows], B["p"][:rows] if adapted else None, y[:rows],
                           residual[:rows] if residual is not None else None, flags)
 

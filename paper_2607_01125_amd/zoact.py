@@ -223,6 +223,24 @@ class Linear:
     plain: tuple = (0, 0)               # output features [begin, end) not adapted (no coefficient rows)
     ws: torch.Tensor | None = None      # optional workspace (linear_workspace_bytes)
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_rows", None)
+
+    def rows_ref(self, dev: int):
+        """What linear_rows reads of the layer, by reference: checked when first used on device `dev`, and again
+        after a field is set (the tensors' contents may change, the tensors do not)."""
+        r = self.__dict__.get("_rows")
+        if r is None or r[0] != dev:
+            int4, bf = self.w.dtype is torch.uint8, torch.bfloat16
+            d = LinearDesc(INT4_G128 if int4 else dtype_code(self.w),
+                           _arg(self.w, "w", self.w.dtype, dev, (self.d_out, self.d_in // 2) if int4 else None),
+                           _arg(self.w_scales, "w_scales", bf, dev, (self.d_out, self.d_in // 128)) if int4 else None,
+                           _arg(self.bias, "bias", bf, dev, (self.d_out,)), None, self.d_in, self.d_out, self.r,
+                           self.coef_offset, None, 0, *self.plain, *_ws(self.ws, dev))
+            r = self.__dict__["_rows"] = (dev, ctypes.byref(d))
+        return r[1]
+
     def desc(self) -> LinearDesc:
         wd = INT4_G128 if self.w.dtype == torch.uint8 else dtype_code(self.w)
         return LinearDesc(wd, self.w.data_ptr(), self.w_scales.data_ptr() if self.w_scales is not None else None,
@@ -243,6 +261,19 @@ class Arena:
     @property
     def k(self) -> int:
         return self.c.numel()
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_coef", None)
+
+    def coef_ref(self, dev: int):
+        """The coefficients alone, by reference, checked as Linear.rows_ref says."""
+        r = self.__dict__.get("_coef")
+        if r is None or r[0] != dev:
+            c = self.c
+            d = ArenaDesc(dtype_code(c), _arg(c, "arena.c", c.dtype, dev), None, None, c.numel())
+            r = self.__dict__["_coef"] = (dev, ctypes.byref(d))
+        return r[1]
 
     def desc(self) -> ArenaDesc:
         return ArenaDesc(dtype_code(self.c), self.c.data_ptr(), self.m.data_ptr(), self.v.data_ptr(), self.k)
@@ -570,15 +601,15 @@ def _arg(t, name: str, dtype, dev: int, shape=None):
     """Address of a contiguous tensor argument (None stays None) after checking type, device and shape."""
     if t is None:
         return None
+    if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (shape is None or t.shape == shape):
+        return t.data_ptr()
     if t.dtype is not dtype:
         raise ValueError(f"{name}: dtype {t.dtype}, expected {dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return t.data_ptr()
+    raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _heads_arg(t: torch.Tensor, name: str, dtype, dev: int, rows: int, width: int):
@@ -597,25 +628,14 @@ def _heads_arg(t: torch.Tensor, name: str, dtype, dev: int, rows: int, width: in
 def linear_rows(layer: Linear, arena: Arena | None, x: torch.Tensor, p: torch.Tensor | None, y: torch.Tensor,
                 residual: torch.Tensor | None = None, flags: int = 0, stream=None):
     """y = epilogue(residual + x W^T + b + p bf16(C)^T) of 1 .. ROWS_MAX rows, INT4 weights, unperturbed."""
-    dev, bf = _device(x), torch.bfloat16
+    dev, bf, r = _device(x), torch.bfloat16, layer.r
     rows = x.shape[0] if x.dim() == 2 else -1
     xp = _arg(x, "x", bf, dev, (rows, layer.d_in))
-    out = layer.d_out // 2 if flags & EPI_SWIGLU else layer.d_out
-    yd = dtype_code(y)
-    yp = _arg(y, "y", y.dtype, dev, (rows, out))
+    yp = _arg(y, "y", y.dtype, dev, (rows, layer.d_out // 2 if flags & EPI_SWIGLU else layer.d_out))
     rp = _arg(residual, "residual", bf, dev, (rows, layer.d_out))
-    pp = _arg(p, "p", bf, dev, (rows, layer.r)) if layer.r else None
-    int4, w, sc, ws = layer.w.dtype is torch.uint8, layer.w, layer.w_scales, layer.ws
-    d = LinearDesc(INT4_G128 if int4 else dtype_code(w),
-                   _arg(w, "w", w.dtype, dev, (layer.d_out, layer.d_in // 2) if int4 else None),
-                   _arg(sc, "w_scales", bf, dev, (layer.d_out, layer.d_in // 128)) if int4 else None,
-                   _arg(layer.bias, "bias", bf, dev, (layer.d_out,)), None, layer.d_in, layer.d_out, layer.r,
-                   layer.coef_offset, None, 0, *layer.plain, *_ws(ws, dev))
-    a = None
-    if layer.r and arena is not None:
-        c = arena.c
-        a = ctypes.byref(ArenaDesc(dtype_code(c), _arg(c, "arena.c", c.dtype, dev), None, None, c.numel()))
-    _on_device(lib().zoact_linear_rows, dev, stream, ctypes.byref(d), a, xp, rows, pp, rp, flags, yp, yd)
+    pp = _arg(p, "p", bf, dev, (rows, r)) if r else None
+    _on_device(lib().zoact_linear_rows, dev, stream, layer.rows_ref(dev), arena.coef_ref(dev) if r and arena else None,
+               xp, rows, pp, rp, flags, yp, dtype_code(y))
 
 
 @dataclass(frozen=True)
@@ -645,7 +665,8 @@ class Cache:
                       _arg(self.refs, "refs", i32, dev, (npg,)), npg, nl, nh, hd, ns, mp)
         object.__setattr__(self, "_desc", d)
         object.__setattr__(self, "_ref", ctypes.byref(d))
-        object.__setattr__(self, "index", dev)
+        for name, value in (("index", dev), ("n_kv_heads", nh), ("head_dim", hd)):
+            object.__setattr__(self, name, value)
 
     @classmethod
     def alloc(cls, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
@@ -658,14 +679,6 @@ class Cache:
                    e(n_layers, n_pages, n_kv_heads, 4, dt=torch.float32),
                    e(n_layers, n_pages, n_kv_heads, 4, dt=torch.float32),
                    z(n_slots, max_pages), z(n_slots), z(n_pages))
-
-    @property
-    def n_kv_heads(self) -> int:
-        return self._desc.n_kv_heads
-
-    @property
-    def head_dim(self) -> int:
-        return self._desc.head_dim
 
     def desc(self) -> CacheDesc:
         return self._desc

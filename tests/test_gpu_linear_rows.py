@@ -230,3 +230,26 @@ def test_refusals_on_device_tensors():
     big = torch.zeros(65, 256, device=dev(), dtype=torch.bfloat16)
     with pytest.raises(Z.ZoactError):
         Z.linear_rows(lin, None, big, None, torch.empty(65, 32, device=dev(), dtype=torch.bfloat16))
+
+
+def test_a_layer_is_checked_again_after_a_change():
+    s, t = _case(2, 256, 32, 8), _case(2, 256, 32, 8, seed=1)
+    z = torch.zeros(1, device=dev())
+    lin = Z.Linear(t_u8(s["packed"]), 256, 32, 8, w_scales=t_bf16(s["sc"]))
+    arena = Z.Arena(t_bf16(s["c"].ravel()), z, z)
+    x, p, y = t_bf16(s["x"]), t_bf16(s["p"]), torch.empty(2, 32, dtype=torch.bfloat16, device=dev())
+    Z.linear_rows(lin, arena, x, p, y)
+    assert torch.equal(y, _run(s, False))
+    lin.w, lin.w_scales, arena.c = t_u8(t["packed"]), t_bf16(t["sc"]), t_bf16(t["c"].ravel())
+    Z.linear_rows(lin, arena, t_bf16(t["x"]), t_bf16(t["p"]), y)
+    assert torch.equal(y, _run(t, False))
+    lin.r = 0
+    Z.linear_rows(lin, arena, t_bf16(t["x"]), None, y)
+    t["r"] = 0
+    assert torch.equal(y, _run(t, False))
+    lin.w = lin.w.cpu()
+    with pytest.raises(ValueError):
+        Z.linear_rows(lin, arena, x, None, y)
+    lin.w, lin.r, arena.c = t_u8(t["packed"]), 8, arena.c[:200]
+    with pytest.raises(Z.ZoactError):
+        Z.linear_rows(lin, arena, x, p, y)
