@@ -227,6 +227,9 @@ class Linear:
         object.__setattr__(self, name, value)
         self.__dict__.pop("_rows", None)
 
+    def __getstate__(self):             # (a copy is checked anew)
+        return {k: v for k, v in self.__dict__.items() if k != "_rows"}
+
     def rows_ref(self, dev: int):
         """What linear_rows reads of the layer, by reference: checked when first used on device `dev`, and again
         after a field is set (the tensors' contents may change, the tensors do not)."""
@@ -265,6 +268,9 @@ class Arena:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         self.__dict__.pop("_coef", None)
+
+    def __getstate__(self):             # (a copy is checked anew)
+        return {k: v for k, v in self.__dict__.items() if k != "_coef"}
 
     def coef_ref(self, dev: int):
         """The coefficients alone, by reference, checked as Linear.rows_ref says."""
@@ -668,6 +674,9 @@ class Cache:
         for name, value in (("index", dev), ("n_kv_heads", nh), ("head_dim", hd)):
             object.__setattr__(self, name, value)
 
+    def __reduce__(self):               # (a copy is checked anew)
+        return Cache, (self.k, self.v, self.k_scale, self.v_scale, self.table, self.len, self.refs)
+
     @classmethod
     def alloc(cls, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
               device="cuda"):
@@ -699,6 +708,9 @@ class CacheBatch:
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
         self.__dict__.pop("_ref", None)
+
+    def __getstate__(self):             # (a copy is checked anew)
+        return {k: v for k, v in self.__dict__.items() if k != "_ref"}
 
     def ref(self, dev: int):
         """The batch's descriptor, by reference, for a cache on device `dev`."""

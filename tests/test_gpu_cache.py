@@ -1,5 +1,7 @@
 """The paged 8-bit cache on the GPU: codes and scales bit for bit, pages against a model in Python,
 attention against float64 with bounds from its own roundings, and all of them as one step."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -513,6 +515,17 @@ def test_a_batch_is_checked_again_after_a_change():
     b.slots = t_i32([1, 0])
     Z.cache_extend(pr.c, b, pr.ws)
     assert pr.c.len.tolist()[:2] == [2, 2]
+
+
+def test_copies_are_caches_and_batches_of_their_own():
+    pr = Pair()
+    b, _ = pr.extend([3, 70])
+    c2, b2 = copy.deepcopy(pr.c), copy.deepcopy(b)
+    assert (c2.index, c2.n_kv_heads, c2.head_dim) == (pr.c.index, pr.c.n_kv_heads, pr.c.head_dim)
+    Z.cache_extend(c2, b2, pr.ws)
+    assert c2.len.tolist()[:2] == [6, 140] and pr.c.len.tolist()[:2] == [3, 70]
+    assert b2.pos.tolist() == [3, 70] and b.pos.tolist() == [0, 0]
+    pr.check_pages()
 
 
 def test_two_streams_with_their_own_caches():

@@ -1,5 +1,7 @@
 """zoact_linear_rows against the plain formula in float64: widths, ranks, epilogues and rows at the ends
 of their ranges."""
+import copy
+
 import numpy as np
 import pytest
 import torch
@@ -240,6 +242,7 @@ def test_a_layer_is_checked_again_after_a_change():
     x, p, y = t_bf16(s["x"]), t_bf16(s["p"]), torch.empty(2, 32, dtype=torch.bfloat16, device=dev())
     Z.linear_rows(lin, arena, x, p, y)
     assert torch.equal(y, _run(s, False))
+    assert torch.equal(copy.deepcopy(lin).w, lin.w) and torch.equal(copy.deepcopy(arena).c, arena.c)
     lin.w, lin.w_scales, arena.c = t_u8(t["packed"]), t_bf16(t["sc"]), t_bf16(t["c"].ravel())
     Z.linear_rows(lin, arena, t_bf16(t["x"]), t_bf16(t["p"]), y)
     assert torch.equal(y, _run(t, False))
