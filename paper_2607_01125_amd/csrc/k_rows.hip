@@ -3,14 +3,12 @@
 //   y[t][n] = epi(res + b + sum_g s[n][g] sum_{k in g} q[n][k] x[t][k] + sum_i p[t][i] bf16(C[n][i]))
 //
 // Bound by the weights' bytes, each read once.  A lane's 16 bytes of an operand are 32 of the 128 columns
-// of one scale group of one weight row.  A nibble becomes a bf16 number without
-// arithmetic: its bits (with the sign bit turned over, u = q + 8) are put at the top of the mantissa
-// of 16, which gives 16 + u = q + 24 exactly; the surplus 24 sum x is taken out by starting the
-// group's sum from a product of x with a constant -24, which costs one product for all weight rows
-// of the wave.  The group's sum is then scaled: one multiply-add a lane and group, no rounding of
-// q s.  The columns of a word come as pairs (i, i + 4), so x is put in that order as it is staged.
-#include <string>
-
+// of one scale group of one weight row.  A nibble becomes a bf16 number without arithmetic: its bits
+// (with the sign bit turned over, u = q + 8) are put at the top of the mantissa of 16, which gives
+// 16 + u = q + 24 exactly; the surplus 24 sum x is taken out by starting the group's sum from a product
+// of x with a constant -24, which costs one product for all weight rows of the wave.  The group's sum is
+// then scaled: one multiply-add a lane and group, no rounding of q s.  The columns of a word come as
+// pairs (i, i + 4), so x is put in that order as it is staged.
 #include "common.hpp"
 
 namespace zoact {

@@ -689,9 +689,6 @@ class Cache:
                    e(n_layers, n_pages, n_kv_heads, 4, dt=torch.float32),
                    z(n_slots, max_pages), z(n_slots), z(n_pages))
 
-    def desc(self) -> CacheDesc:
-        return self._desc
-
 
 @dataclass
 class CacheBatch:
