@@ -132,7 +132,8 @@ zoact_status zoact_cache_append(const zoact_cache* c, int32_t layer, const void*
  * n_kv_heads)), out [rows][n_heads * head_dim], both in dtype.  With cos_t, sin_t q is
  * rotated first, as append does.  Scores, softmax and sums fp32; in BF16 the rotated q and
  * the probabilities are rounded to 11 bits as they enter the products (an unrotated bf16 q
- * is not changed by this), in F32 to 22 bits or more; one rounding of out.
+ * is not changed by this), in F32 to 22 bits or more, a probability times its value scale to
+ * no finer than 2^-39 of the largest value scale the row attends to; one rounding of out.
  * max_len (host): a length that no entry's pos + rows is expected to pass; it only shapes
  * the split of the work, longer entries are served too.  ws: at least
  * zoact_attention_cache_workspace_bytes() bytes let long sequences be split over

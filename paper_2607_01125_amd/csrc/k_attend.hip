@@ -149,20 +149,19 @@ __device__ __forceinline__ void value_scales(const floatx4& vs, int t0, int last
 // One page's scores of a lane's column, s times its block's f >= 0 (log2 domain): masks tokens past lim (edge:
 // there may be some), updates the running maximum and sum, and gives the factor of what was summed before and
 // the probabilities times V's scales as terms.  The maximum is taken before the factor, a product a block, and
-// the factor and the maximum's subtraction are one multiply-add a score.
+// the factor and the maximum's subtraction are one multiply-add a score.  That one does not round the product
+// as the maximum's was, which scores below 2^20 allow (a probability stays below 2^(1/16)): |s| < 2^29 (128
+// values below 2^15 times 127), so f <= 2^-9 will do, and larger ones are multiplied first, as masked pages are.
 template <int NT>
 __device__ __forceinline__ void soft_page(float (&s)[4][4], float (&f)[4], int t0, int lim, bool edge, int g,
                                           const float (&vsc)[4], float& m, float& l, float& alpha,
                                           f16x8 (&pf)[2][NT]) {
-  if (edge) {
+  if (edge || __any(fmaxf(fmaxf(f[0], f[1]), fmaxf(f[2], f[3])) > 0x1p-9f)) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
-      // (no factor 0 or NaN meets an infinity that stands for a masked token)
-      const int first = t0 + 16 * n + 4 * g;
-      const bool none = first > lim, zero = f[n] == 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[n][i] = first + i > lim ? -INFINITY : zero ? s[n][i] * 0.f : s[n][i];
-      if (none || zero) f[n] = 1.f;
+      for (int i = 0; i < 4; ++i) s[n][i] = t0 + 16 * n + 4 * g + i > lim ? -INFINITY : s[n][i] * f[n];
+      f[n] = 1.f;
     }
   }
   float mx = m;

@@ -359,6 +359,39 @@ def test_attention_blocks_of_zero_keys_and_a_negative_scale(lens, counts, scale,
         _check_attention(pr, b, pos, x[:, :H * hd], counts, H, dtype, None, 220, split=split, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("size", [1e2, 1e4, 1e8])
+@pytest.mark.parametrize("lens,counts", [([300, 64], [1, 1]), ([130, 1], [40, 70])])
+def test_attention_of_very_large_scores_takes_the_largest(lens, counts, size, dtype):
+    """Scores of up to 2^60, whose rounding alone passes the exponential's range: each row is the value of
+    its largest score (rows whose two largest are closer than their rounding left out)."""
+    H, hkv, hd = 4, 2, 64
+    pr, b, pos, q, _ = _filled(lens, counts, H, hkv, hd, dtype, False)
+    pr.c.k_scale.mul_(size)
+    pr.m.ks *= np.float32(size)
+    big = (q.float() * size).to(dtype)
+    qh = host(big).reshape(-1, H, hd)
+    for ws in (None, torch.empty(Z.attention_cache_workspace_bytes(pr.c, b, H, 400), dtype=torch.uint8, device=dev())):
+        out = torch.empty(b.rows, H * hd, dtype=dtype, device=dev())
+        Z.attention_cache(pr.c, 0, big, out, b, H, 0.125, 400, ws=ws)
+        got, r, seen = host(out).reshape(-1, H, hd), 0, 0
+        for i, (p, c) in enumerate(zip(pos, counts)):
+            k, v = pr.m.values(0, i, p + c)
+            for j in range(c):
+                for h in range(H):
+                    kk, vv = (x[:p + j + 1, h // (H // hkv)].astype(np.float64) for x in (k, v))
+                    sc = kk @ qh[r + j, h] * 0.125
+                    top = np.argsort(sc)[::-1][:2]
+                    err = 2.0 ** -10 * 0.125 * float(np.abs(kk).max(0) @ np.abs(qh[r + j, h]))
+                    if len(top) > 1 and sc[top[0]] - sc[top[1]] < err + 60:
+                        continue
+                    seen += 1
+                    want = vv[top[0]]
+                    assert np.all(np.abs(got[r + j, h] - want) <= 2.0 ** -7 * np.abs(want) + 1e-12), (i, j, h)
+            r += c
+        assert seen >= b.rows * H // 3
+
+
 def test_attention_sharp_and_flat_scores():
     """A scale that makes the softmax nearly a choice, and one that makes it nearly a mean."""
     pr, b, pos, q, rp = _filled([400, 90], [1, 3], 4, 2, 64, torch.float32, False)
