@@ -256,3 +256,30 @@ def test_a_layer_is_checked_again_after_a_change():
     lin.w, lin.r, arena.c = t_u8(t["packed"]), 8, arena.c[:200]
     with pytest.raises(Z.ZoactError):
         Z.linear_rows(lin, arena, x, p, y)
+
+
+@pytest.mark.parametrize("rows,K,N,flags", [(2, 14336, 96, 0), (13, 20480, 320, Z.EPI_SWIGLU), (50, 4096, 512, Z.EPI_RELU)])
+def test_parts_of_the_depth_from_a_graph(rows, K, N, flags):
+    """The product and its join, captured once and replayed with eager calls between on a workspace of their own."""
+    announce("graph", rows, K, N, flags)
+    s = _case(rows, K, N, 40, bias=True, c_f32=True, flags=flags)
+    lins = [Z.Linear(t_u8(s["packed"]), K, N, 40, None, 0, t_bf16(s["b"]), t_bf16(s["sc"]),
+                     ws=torch.full((Z.linear_workspace_bytes(),), 255, dtype=torch.uint8, device=dev())) for _ in range(2)]
+    z = torch.zeros(1, device=dev())
+    arena = Z.Arena(t_f32(s["c"].ravel()), z, z)
+    x, p = t_bf16(s["x"]), t_bf16(s["p"])
+    y, eager = (torch.empty(rows, N // 2 if flags & Z.EPI_SWIGLU else N, dtype=torch.bfloat16, device=dev())
+                for _ in range(2))
+    Z.linear_rows(lins[0], arena, x, p, y, flags=flags)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        Z.linear_rows(lins[0], arena, x, p, y, flags=flags)
+    for i in range(5):
+        x.mul_(-0.5)
+        Z.linear_rows(lins[1], arena, x, p, eager, flags=flags)
+        y.fill_(7.0)
+        lins[0].ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager), i
