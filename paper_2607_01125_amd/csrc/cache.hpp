@@ -18,21 +18,25 @@ __device__ __forceinline__ void raise_status(uint32_t* status, uint32_t bit) {
   if (status) atomicOr(status, bit);
 }
 
+// (Loads do not wait for one another: where there is no list, a word of pos is read and dropped.)
 __device__ __forceinline__ void entry_rows(const zoact_cache_batch& b, int i, CacheEntry& e) {
-  const int64_t r0 = b.row_begin ? b.row_begin[i] : (int64_t)i * b.max_new;
-  const int64_t r1 = b.row_begin ? b.row_begin[i + 1] : r0 + b.max_new;
+  const int32_t* const rows = (b.row_begin ? b.row_begin : b.pos) + i;
+  const int32_t* const slot = (b.slots ? b.slots : b.pos) + i;
+  const int32_t v0 = rows[0], v1 = rows[b.row_begin ? 1 : 0], s = *slot, p = b.pos[i];
+  const int64_t r0 = b.row_begin ? v0 : (int64_t)i * b.max_new;
+  const int64_t r1 = b.row_begin ? v1 : r0 + b.max_new;
+  e.pos = p;
   e.row0 = (int)r0;
   e.count = (int)(r1 - r0);
   e.rows_ok = r0 >= 0 && r1 >= r0 && r1 <= b.rows && r1 - r0 <= b.max_new;
   if (!e.rows_ok) e.count = 0;
-  e.slot = b.slots ? b.slots[i] : i;
+  e.slot = b.slots ? s : i;
 }
 
 // Entry i with the place extend gave it.  A bad one raises the status bit once (by `report`).
 __device__ __forceinline__ CacheEntry read_entry(const zoact_cache& c, const zoact_cache_batch& b, int i, bool report) {
   CacheEntry e;
   entry_rows(b, i, e);
-  e.pos = b.pos[i];
   const bool fits = e.rows_ok && e.slot >= 0 && e.slot < c.n_slots &&
                     (int64_t)e.pos + e.count <= (int64_t)c.max_pages * kPage;
   e.ok = fits && e.pos >= 0;
