@@ -65,7 +65,7 @@ struct Quarter {
 };
 
 // Codes of four values of a lane under their block's scale (the same in all lanes; NaN: 0, s == 0: every value
-// is 0), rint(x / s).  A division is a dozen instructions (32 single tokens 9.5 us with them, 8.4 so); x times
+// is 0), rint(x / s).  A division is a dozen instructions (32 single tokens 9.5 us with them, 8.4 without); x times
 // inverse is off by no more than 3 half steps of 127, 2^-15.4, so the quotients are formed only where it comes
 // within 2^-14 of the middle between two codes.  Scales near the smallest numbers (inverse 0) always take
 // them, and only there a quotient passes 127.
