@@ -469,11 +469,16 @@ hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStre
 
 // 17 rows and more: 128 weight rows a workgroup, so that x, which every workgroup reads whole, is read
 // rarely; one workgroup a compute unit (4096 x 28672 at 64 rows 38 us, with 64 weight rows 55; 20480 x 5120
-// 38 us in 6 parts, 63 in 2).
+// 38 us in 6 parts, 63 in 2).  Up to 32 rows layers of few tiles take 32, whose stages are shorter: 4096 x 4096
+// 10.4 us in two parts, with 128 in eight 12.1, 4096 x 6144 12.4 and 13.8 (but 4096 x 28672 44 and 24; at 48
+// rows 4096 x 4096 takes 14.1 either way, 4096 x 6144 16.5 and 16.1).
 template <int NB>
 hipError_t pick_more(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
-  const int64_t t128 = (a.N / 16 + 7) / 8;
-  return go<8, NB, 16 * NB, 8, 2>(a, splits_of(a, cus / t128, 4, NB, ws_bytes), ws, s);
+  const int64_t t16 = a.N / 16;
+  if constexpr (NB == 2)
+    if (a.K <= 8192 && t16 <= 2 * cus)
+      return go<2, NB, 16 * NB, 8, 4>(a, splits_of(a, cus / ((t16 + 1) / 2), 8, NB, ws_bytes), ws, s);
+  return go<8, NB, 16 * NB, 8, 2>(a, splits_of(a, cus / ((t16 + 7) / 8), 4, NB, ws_bytes), ws, s);
 }
 
 hipError_t pick(const RowsArgs& a, void* ws, size_t ws_bytes, hipStream_t s) {

@@ -123,6 +123,10 @@ CASES = [
     dict(rows=9, K=14336, N=96, r=37, flags=Z.EPI_SWIGLU, c_f32=True),
     dict(rows=1, K=14336, N=1040, r=24, plain=(0, 1040), c_f32=True),
     dict(rows=2, K=4096, N=6160, r=16, res=True, c_f32=True),
+    dict(rows=24, K=9216, N=160, r=32, bias=True),
+    dict(rows=32, K=384, N=8224, r=16, flags=Z.EPI_SWIGLU, c_f32=True),
+    dict(rows=29, K=4096, N=4096, r=32, res=True),
+    dict(rows=18, K=3200, N=80, r=9, flags=Z.EPI_RELU, bias=True),
 ]
 
 
