@@ -51,7 +51,9 @@ __device__ __forceinline__ f16x8 codes8(uint32_t a, uint32_t b) {
   codes4(b, y);
   return __builtin_bit_cast(f16x8, make_uint4(x[0], x[1], y[0], y[1]));
 }
-// x as NT f16 terms, each the nearest to what the ones before it leave.
+// x as NT f16 terms, each the nearest to what the ones before it leave.  What a term is taken from is held in a
+// register: where the compiler forms one rounding from x's own product and another from its fp32 value, the two
+// differ by a step now and then, and the second term would belong to a first that is not the one used.
 template <int NT>
 __device__ __forceinline__ void terms8(const float (&x)[8], f16x8 (&t)[NT]) {
   float r[8];
@@ -61,6 +63,7 @@ __device__ __forceinline__ void terms8(const float (&x)[8], f16x8 (&t)[NT]) {
   for (int k = 0; k < NT; ++k)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      if constexpr (NT > 1) asm("" : "+v"(r[e]));
       t[k][e] = (_Float16)r[e];
       if (k + 1 < NT) r[e] -= (float)t[k][e];
     }
@@ -132,8 +135,9 @@ constexpr int kPExp = 14;         // probabilities enter their product times 2^1
                                   // of them down to 2^-28, and something down to 2^-38
 constexpr int kNoScale = -200;    // below every exponent of an fp32 number
 
-// V scales of a page's blocks that hold a token up to `last`, times a power of two that keeps p vsc below
-// 2^14; vexp follows, and o's unit 2^(vexp - 14) with it.
+// V scales of a page's blocks that hold a token up to `last`, the column's own, times a power of two that keeps
+// p vsc below 2^14; vexp follows, and o's unit 2^(vexp - 14) with it.  Each column has its own vexp: later tokens'
+// scales, which columns of the same wave may see, take none of its bits.
 __device__ __forceinline__ void value_scales(const floatx4& vs, int t0, int last, int& vexp, float (&vsc)[4]) {
   const float v[4] = {vs[0], vs[1], vs[2], vs[3]};
 #pragma unroll
@@ -186,12 +190,6 @@ __device__ __forceinline__ void soft_page(float (&s)[4][4], float (&f)[4], int t
         p8[4 * n + i] = p[i] * vsc[2 * n2 + n];
       }
       lsum += (p[0] + p[1]) + (p[2] + p[3]);
-    }
-    // (a block past the column's last token may have a NaN scale, which other columns see)
-    if (edge) {
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-        if (t0 + 16 * (2 * n2 + n) > lim) p8[4 * n] = p8[4 * n + 1] = p8[4 * n + 2] = p8[4 * n + 3] = 0.f;
     }
     terms8<NT>(p8, pf[n2]);
   }
@@ -311,7 +309,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = floatx4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
-  int vexp = kNoScale;   // V scales so far are below 2^vexp; o is kept in units of 2^(vexp - 14)
+  int vexp = kNoScale;   // V scales the column has seen are below 2^vexp; o is kept in units of 2^(vexp - 14)
 
   if (rg.pbeg < rg.pend) {
     // the first page's keys are on their way before q is ready, each next page's before this one's softmax
@@ -397,7 +395,7 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
       const bool edge = now_bad || t0 + kPage > e.pos + c0 / a.G + 1;    // some column ends inside the page
       float vsc[4], alpha;
       const int vold = vexp;
-      value_scales(vs, t0, now_bad ? -1 : rg.last, vexp, vsc);
+      value_scales(vs, t0, now_bad ? -1 : tcol, vexp, vsc);
       f16x8 pf[2][NT];
       soft_page<NT>(s, f, t0, now_bad ? -1 : tcol, edge, g, vsc, m, l, alpha, pf);
       alpha = __builtin_amdgcn_ldexpf(alpha, vold - vexp);
@@ -560,7 +558,7 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
       const bool edge = t0 + kPage > wfirst + 1;
       float vsc[4];
       const int vold = vexp;
-      value_scales(vsn, t0, wlast, vexp, vsc);
+      value_scales(vsn, t0, tcol, vexp, vsc);
       float s[4][4], f[4];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {

@@ -675,3 +675,96 @@ def test_pools_past_two_gigabytes():
     again = torch.empty(2, H * hd, dtype=torch.bfloat16, device=dev())
     Z.attention_cache(big, 2, x[:2, :H * hd], again, one, H, 0.1, 301)
     assert torch.equal(again, outs[1][1])
+
+
+# ------------------------------------------------------------------ value scales that differ between blocks
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("larger", [2.0 ** 20, 2.0 ** 45])
+@pytest.mark.parametrize("lens,counts,H,hkv", [([10], [12], 1, 1), ([0, 60], [40, 50], 4, 2), ([14, 47], [4, 4], 8, 2)])
+def test_rows_do_not_see_the_scales_of_later_values(lens, counts, H, hkv, larger, dtype):
+    """New rows of one page, the values of its later blocks 2^20 and 2^45 times larger: a row that sees only the
+    earlier blocks keeps the precision it has alone.  (A probability times its value scale is a number of f16 whose
+    unit puts the row's largest scale below 2^14, so it is off by 2^-25 of that unit at most beside its relative error:
+    2^-38 of the largest scale the row sees, 127 times that in the result for each token.)"""
+    hd = 64
+    pr = Pair(hkv=hkv, hd=hd, n_slots=len(lens), max_pages=3)
+    for part in (lens, counts):
+        b, pos = pr.extend(part)
+        x = _rows(sum(part), (H + 2 * hkv) * hd, dtype, 21 + sum(part))
+        v = x[:, (H + hkv) * hd:]
+        at = torch.cat([torch.arange(p, p + c) for p, c in zip(pos, part)]).to(dev())
+        # (in the second half of the new rows' blocks)
+        from_ = [L + c // 2 if part is counts else 10 ** 6 for L, c in zip(lens, counts)]
+        first = torch.repeat_interleave(torch.tensor(from_), torch.tensor(part)).to(dev())
+        big = at // 16 >= first // 16
+        v[big] *= larger
+        seen = (~big).cpu().numpy()
+        pr.append(0, x[:, H * hd:(H + hkv) * hd], v, b, pos, part)
+    pr.check_codes()
+    assert seen.any() and not seen.all()
+    scale, out = float(np.float32(hd ** -0.5)), torch.empty(sum(counts), H * hd, dtype=dtype, device=dev())
+    announce("later scales", pos, counts, H, hkv, larger, dtype)
+    Z.attention_cache(pr.c, 0, x[:, :H * hd], out, b, H, scale, 128)
+    r = 0
+    for i, (p, c) in enumerate(zip(pos, counts)):
+        k, v = pr.m.values(0, i, p + c)
+        want, mean, mag = cm.attend(host(x[r:r + c, :H * hd]).reshape(c, H, hd), k, v, p, scale)
+        tol = cm.attend_bound(want, mean, mag, p + c, hd, dtype == torch.float32)
+        vs = np.concatenate([pr.m.vs[0, page].T for page in pr.m.held(i)]).max(1)        # [blocks], of all heads
+        top = np.array([vs[:t // 16 + 1].max() for t in range(p, p + c)])
+        tol += (np.arange(p, p + c) + 1)[:, None, None] * 127 * 2.0 ** -38 * top[:, None, None]
+        bad = ~(np.abs(host(out[r:r + c]).reshape(c, H, hd) - want) <= tol)
+        assert not bad.any(), (i, int(bad.sum()), np.argwhere(bad)[:3].tolist())
+        r += c
+    # the small rows against the same rows of a cache that ends before the large ones
+    alone = [int(s.sum()) for s in np.split(seen, np.cumsum(counts)[:-1])]
+    begin = t_i32(np.concatenate([[0], np.cumsum(alone)]))
+    few = Z.CacheBatch(t_i32(pos), max(counts), sum(alone), row_begin=begin)
+    keep = torch.from_numpy(np.flatnonzero(seen)).to(dev())
+    got = torch.empty(sum(alone), H * hd, dtype=dtype, device=dev())
+    Z.attention_cache(pr.c, 0, x[keep][:, :H * hd].contiguous(), got, few, H, scale, 128)
+    assert torch.equal(out[keep], got)
+
+
+def _pages_f64(c, slots, n_pages):
+    """Keys and values [slots][tokens][hkv][hd] of the first pages of a layer's slots, dequantised, float64."""
+    t = c.table[:slots, :n_pages].long()
+    hkv, hd = c.n_kv_heads, c.head_dim
+    k = c.k[0][t].double() * c.k_scale[0][t].double().repeat_interleave(16, -1)[..., None]     # [s][p][h][64][d]
+    place = torch.tensor([cm.v_place(i) for i in range(64)], device=dev())
+    v = c.v[0][t][..., place].double() * c.v_scale[0][t].double().repeat_interleave(16, -1)[..., None, :]
+    return (k.permute(0, 1, 3, 2, 4).reshape(slots, -1, hkv, hd), v.permute(0, 1, 4, 2, 3).reshape(slots, -1, hkv, hd))
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("slots,count", [(512, 1), (64, 8)])
+def test_fp32_rows_of_few_weighty_tokens_keep_their_bits(slots, count, hd):
+    """Rows whose weight lies on six tokens (two blocks of a whole page and of a partial one, the rest e^-80 below),
+    in both tile forms: where a term of p vsc is cut wrongly it shows, for 2^-11 of it is lost.  The bound is the
+    usual one over those six."""
+    H, hkv, L = 32, 8, 96
+    sel = [5, 22, 39, 60, 70, 90]
+    pr = Pair(n_pages=3 * slots, hkv=hkv, hd=hd, n_slots=slots, max_pages=3, garbage=False)
+    rng = torch.Generator(device="cuda").manual_seed(hd + count)
+    for n in (L, count):
+        b = pr.batch([n] * slots)
+        Z.cache_extend(pr.c, b, pr.ws)
+        kv = torch.randn(2, slots * n, hkv, hd, generator=rng, device=dev()) * 0.2
+        kv[0, :, :, 0] = -1.0
+        if n == L:
+            kv[0].view(slots, n, hkv, hd)[:, sel, :, 0] = 0.0
+        Z.cache_append(pr.c, 0, kv[0].view(-1, hkv * hd), kv[1].view(-1, hkv * hd), b)
+    q = torch.randn(slots * count, H, hd, generator=rng, device=dev())
+    q[:, :, 0] = 640.0
+    scale = 0.125
+    out = torch.empty(slots * count, H * hd, device=dev())
+    announce("few tokens", slots, count, hd)
+    Z.attention_cache(pr.c, 0, q.view(-1, H * hd), out, b, H, scale, L + count)
+    k, v = (x[:, sel].repeat_interleave(H // hkv, 2) for x in _pages_f64(pr.c, slots, 2))      # [s][6][H][d]
+    q64 = q.double().view(slots, count, 1, H, hd)
+    w = ((q64 * k[:, None]).sum(-1) * scale).softmax(2)[..., None]                             # [s][c][6][H][1]
+    want, mean = ((w * x[:, None]).sum(2) for x in (v, v.abs()))
+    mag = ((q64.abs() * k[:, None].abs()).sum(-1) * scale).amax(2)[..., None]
+    tol = cm.attend_bound(want.cpu().numpy(), mean.cpu().numpy(), mag.cpu().numpy(), len(sel), hd, True)
+    bad = ~(np.abs(host(out).reshape(want.shape) - want.cpu().numpy()) <= tol)
+    assert not bad.any(), (int(bad.any(-1).sum()), np.argwhere(bad)[:3].tolist())
