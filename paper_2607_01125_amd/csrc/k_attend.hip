@@ -618,6 +618,12 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
 }
 
 constexpr int kMaxSplits = 128;
+// Weight of a split with sum l and maximum m in a row whose maximum is the base: below zero for an empty one, which
+// has written no sums.  Any other counts with its sums, even where the weight is 0, so that a NaN among its values
+// reaches the row as it does unsplit.
+__device__ __forceinline__ float split_weight(float m, float l, float base) {
+  return l == 0.f ? -1.f : __builtin_amdgcn_exp2f(m - base);
+}
 // Joins up to eight splits of a row and head in half a wave, HD / 32 columns a lane; sums and statistics (a lane
 // holds those of split lane % 8) are asked for at once.  Bound by the launch and one trip to memory: 48 rows of 32
 // heads in eight splits 5 us; for 512 rows in three, a workgroup a row and head took 13 us more.
@@ -642,7 +648,7 @@ __global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
 #pragma unroll
   for (int k = 1; k < 8; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
   const float base = M == -INFINITY ? 0.f : M;
-  const float f = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - base);
+  const float f = split_weight(m, l, base);
   float L = f * l;
 #pragma unroll
   for (int k = 1; k < 8; k <<= 1) L += __shfl_xor(L, k, 64);
@@ -650,7 +656,7 @@ __global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
 #pragma unroll
   for (int k = 0; k < kFewSplits; ++k) {
     const float w = __shfl(f, (lane & ~7) | k, 64);
-    if (w != 0.f) r += w * v[k];        // (an empty split has written no sums; a NaN weight counts)
+    if (!(w < 0.f)) r += w * v[k];      // (a NaN weight counts)
   }
   const float div = L == 0.f ? 1.f : L;
   T* const op = static_cast<T*>(a.out) + ((int64_t)e.row0 * a.H + row) * HD + d0;
@@ -695,7 +701,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   __syncthreads();
   if (wave < kMaxSplits / 64) {
     const float M = fmaxf(red[0], red[1]), base = M == -INFINITY ? 0.f : M;
-    const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - base);
+    const float f = split_weight(ml.x, ml.y, base);
     wt[tid] = f;
     float L = f * ml.y;
 #pragma unroll
@@ -708,7 +714,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   for (int k = 0; k < NI; ++k)
     if (grp + k * NG < a.S) {
       const float w = wt[grp + k * NG];
-      if (w != 0.f) r += w * v[k];      // (an empty split has written no sums; a NaN weight counts)
+      if (!(w < 0.f)) r += w * v[k];    // (a NaN weight counts)
     }
   sr[grp][tid & 31] = r;
   __syncthreads();

@@ -768,3 +768,37 @@ def test_fp32_rows_of_few_weighty_tokens_keep_their_bits(slots, count, hd):
     tol = cm.attend_bound(want.cpu().numpy(), mean.cpu().numpy(), mag.cpu().numpy(), len(sel), hd, True)
     bad = ~(np.abs(host(out).reshape(want.shape) - want.cpu().numpy()) <= tol)
     assert not bad.any(), (int(bad.any(-1).sum()), np.argwhere(bad)[:3].tolist())
+
+
+# ------------------------------------------------------------------ splits
+@pytest.mark.parametrize("lens,count,H", [([2000, 70], 1, 2), ([6000, 9], 1, 1), ([2000, 70], 20, 2), ([9000, 1], 1, 20)])
+def test_a_value_that_is_not_finite_reaches_those_who_see_it_through_splits(lens, count, H):
+    """A NaN value 130 nats below the row's largest score, in another split (few-split and wide joins, both
+    tile forms): the row gives NaN, as without a workspace; a row that does not see it does not."""
+    hd, n = 32, len(lens)
+    pr = Pair(n_pages=sum(-(-(L + count) // 64) for L in lens), hkv=1, hd=hd, n_slots=n, max_pages=-(-max(lens) // 64) + 1,
+              garbage=False)
+    counts = [count] * n
+    for part in (lens, counts):
+        b = pr.batch(part)
+        Z.cache_extend(pr.c, b, pr.ws)
+        rows = sum(part)
+        k, v = torch.zeros(rows, hd, device=dev()), _rows(rows, hd, torch.float32, 8)
+        k[:, 0] = 1.0
+        if part is lens:
+            k[:lens[0] // 2, 0] = -1.0             # entry 0: far below the rest, in its first half
+            v[100, 5] = float("nan")
+        Z.cache_append(pr.c, 0, k, v, b)
+    q = torch.zeros(sum(counts), H * hd, device=dev())
+    q[:, ::hd] = 65.0
+    outs = []
+    nb = Z.attention_cache_workspace_bytes(pr.c, b, H, max(lens) + count)
+    assert nb > 0
+    for ws in (None, torch.full((nb,), 255, dtype=torch.uint8, device=dev())):
+        out = torch.zeros(sum(counts), H * hd, device=dev())
+        announce("nan in a split", lens, count, H, ws is not None)
+        Z.attention_cache(pr.c, 0, q, out, b, H, 1.0, max(lens) + count, ws=ws)
+        o = host(out).reshape(n, count, H, hd)
+        assert np.isnan(o[0]).all() and np.isfinite(o[1]).all()
+        outs.append(np.isnan(o))
+    assert np.array_equal(*outs)
