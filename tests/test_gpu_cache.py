@@ -802,3 +802,29 @@ def test_a_value_that_is_not_finite_reaches_those_who_see_it_through_splits(lens
         assert np.isnan(o[0]).all() and np.isfinite(o[1]).all()
         outs.append(np.isnan(o))
     assert np.array_equal(*outs)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,counts,H,hkv,hd", [
+    ([1500, 30, 700], [70, 40, 65], 4, 2, 64),        # chunks in up to eight splits, some of them empty
+    ([2300, 5], [17, 33], 2, 1, 128),
+    ([9000, 40, 2], [1, 1, 1], 20, 1, 32),            # a tile of more than 16 columns and more than eight splits
+    ([5000, 600], [9, 3], 6, 2, 64),
+])
+def test_chunks_behind_long_prompts_in_splits(lens, counts, H, hkv, hd, dtype):
+    """The 64-column form with partial results: against float64, the same on every run, and with an entry that has no
+    place between the others."""
+    pr, b, pos, q, rp = _filled(lens, counts, H, hkv, hd, dtype, True)
+    n = max(L + c for L, c in zip(lens, counts))
+    out, ws = _check_attention(pr, b, pos, q, counts, H, dtype, rp, n)
+    assert ws is not None and max(counts) * (H // hkv) > 16
+    again = torch.full_like(out, 3.0)
+    scale = float(np.float32(hd ** -0.5))
+    ws.fill_(255)
+    Z.attention_cache(pr.c, 0, q, again, b, H, scale, n, rope=rp, ws=ws)
+    assert torch.equal(out, again)
+    b.pos[1] = -1
+    ws.fill_(255)
+    Z.attention_cache(pr.c, 0, q, again, b, H, scale, n, rope=rp, ws=ws)
+    r0, r1 = counts[0], counts[0] + counts[1]
+    assert torch.equal(again[:r0], out[:r0]) and torch.equal(again[r1:], out[r1:]) and (again[r0:r1] == 0).all()
