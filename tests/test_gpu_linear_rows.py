@@ -287,3 +287,59 @@ def test_parts_of_the_depth_from_a_graph(rows, K, N, flags):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, eager), i
+
+
+INF_CASES = [
+    dict(rows=1, K=512, N=64, r=8), dict(rows=3, K=1024, N=9216, r=0, flags=Z.EPI_RELU),
+    dict(rows=2, K=14336, N=96, r=8, bias=True), dict(rows=13, K=4096, N=64, r=5, res=True),
+    dict(rows=9, K=20480, N=320, r=16), dict(rows=20, K=4736, N=352, r=32, bias=True),
+    dict(rows=29, K=384, N=8224, r=8), dict(rows=40, K=4096, N=512, r=32, res=True), dict(rows=64, K=1408, N=144, r=7),
+]
+
+
+@pytest.mark.parametrize("kw", INF_CASES, ids=lambda k: f"{k['rows']}x{k['K']}x{k['N']}r{k['r']}")
+def test_infinities_are_what_the_formula_says(kw):
+    """One infinite x gives its row's features +-inf by the code's sign, and NaN where the code is 0; other rows
+    keep their bits."""
+    s = _case(**kw)
+    row, at = kw["rows"] // 2, 300
+    bad = dict(s, x=s["x"].copy())
+    bad["x"][row, at] = -np.inf
+    for ws in (0, Z.linear_workspace_bytes()):
+        announce("infinity", kw, ws)
+        full, got = host(_run(s, True, ws=ws)), host(_run(bad, True, ws=ws))
+        keep = [i for i in range(kw["rows"]) if i != row]
+        assert np.array_equal(got[keep], full[keep])
+        with np.errstate(invalid="ignore"):
+            want = s["q"][:, at] * -np.inf
+        if kw.get("flags"):
+            want = np.where(want < 0, 0.0, want)
+        assert np.array_equal(got[row], want, equal_nan=True)
+    # SwiGLU's two factors: whatever torch makes of the same infinities
+    if kw["N"] % 32 == 0 and not kw.get("flags"):
+        g = dict(bad, flags=Z.EPI_SWIGLU)
+        with np.errstate(invalid="ignore"):
+            z = s["q"][:, at] * -np.inf
+        f = np.arange(kw["N"] // 2)
+        gate, up = (torch.from_numpy(z[f // 16 * 32 + f % 16 + o]) for o in (0, 16))
+        got, full = host(_run(g, True)), host(_run(dict(s, flags=Z.EPI_SWIGLU), True))
+        assert np.array_equal(got[keep], full[keep])
+        assert np.array_equal(got[row], (gate / (1 + torch.exp(-gate)) * up).numpy(), equal_nan=True)
+
+
+@pytest.mark.parametrize("kw", INF_CASES, ids=lambda k: f"{k['rows']}x{k['K']}x{k['N']}r{k['r']}")
+@pytest.mark.parametrize("size", [2.0 ** 121, 2.0 ** 126])
+def test_values_near_the_top_overflow_no_earlier_than_the_result(kw, size):
+    """x up to 2^127 with scales of 0.007: results of up to 2^125 are finite and within the bound of the sums
+    (which grows with x), though 24 x and the sums of codes times x pass fp32's range."""
+    s = _case(**dict(kw, flags=0))
+    row = kw["rows"] // 2
+    s["x"][row] = 0
+    s["x"][row, 128:256:9] = size * np.where(np.arange(128, 256, 9) % 2, 1, -1)
+    for ws in (0, Z.linear_workspace_bytes()):
+        announce("near the top", kw, size, ws)
+        y, tol = _reference(s)
+        assert np.abs(y).max() < 3e38 and np.abs(y[row]).max() > size * 0.01
+        got = host(_run(s, True, ws=ws))
+        tol = tol + 2.0 ** -24 * (np.abs(y) + tol)
+        assert np.all(np.abs(got - y) <= tol), np.argwhere(~(np.abs(got - y) <= tol))[:3]
