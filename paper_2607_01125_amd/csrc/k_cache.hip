@@ -587,6 +587,7 @@ size_t cache_ws(const zoact_cache& c) {
 }
 
 bool al16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool al4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 }  // namespace
 
@@ -598,7 +599,7 @@ zoact_status check_cache(const zoact_cache* c) {
   ZC(c->k && c->v && c->k_scale && c->v_scale && c->table && c->len && c->refs, "cache: NULL pointer in the cache");
   ZC(al16(c->k) && al16(c->v) && al16(c->k_scale) && al16(c->v_scale),
      "cache: pools and scales must be 16-byte aligned");
-  ZC(((uintptr_t)c->table & 3) == 0 && ((uintptr_t)c->len & 3) == 0 && ((uintptr_t)c->refs & 3) == 0,
+  ZC(al4(c->table) && al4(c->len) && al4(c->refs),
      "cache: table, len and refs must be 4-byte aligned");
   ZC(c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128, "cache: head_dim must be 32, 64 or 128");
   ZC(c->n_layers >= 1 && c->n_layers <= 32767, "cache: n_layers outside [1, 32767]");
@@ -677,6 +678,7 @@ extern "C" zoact_status zoact_cache_fork(const zoact_cache* c, const int32_t* sr
   zoact_status st = check_cache(c);
   if (st != ZOACT_OK) return st;
   ZC(src && dst, "cache_fork: NULL slots");
+  ZC(al4(src) && al4(dst) && al4(status), "cache_fork: src, dst and status must be 4-byte aligned");
   ZC(n >= 1 && n <= c->n_slots, "cache_fork: n outside [1, n_slots]");
   st = check_ws(*c, ws, ws_bytes, "cache_fork");
   if (st != ZOACT_OK) return st;
@@ -695,6 +697,7 @@ extern "C" zoact_status zoact_cache_free(const zoact_cache* c, const int32_t* sl
   const zoact_status st = check_cache(c);
   if (st != ZOACT_OK) return st;
   ZC(slots, "cache_free: NULL slots");
+  ZC(al4(slots) && al4(status), "cache_free: slots and status must be 4-byte aligned");
   ZC(n >= 1 && n <= c->n_slots, "cache_free: n outside [1, n_slots]");
   free_kernel<<<(unsigned)n, 256, 0, reinterpret_cast<hipStream_t>(stream)>>>(*c, slots, status);
   return done("cache_free");
@@ -705,6 +708,7 @@ extern "C" zoact_status zoact_cache_compact(const zoact_cache* c, void* ws, size
   zoact_status st = check_cache(c);
   if (st == ZOACT_OK) st = check_ws(*c, ws, ws_bytes, "cache_compact");
   if (st != ZOACT_OK) return st;
+  ZC(al4(n_used), "cache_compact: n_used must be 4-byte aligned");
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   int* const head = static_cast<int*>(ws);
   int* const map = head + 4;

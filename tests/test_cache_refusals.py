@@ -167,3 +167,17 @@ def test_slots():
 ])
 def test_rows_and_tables(call):
     assert call() == Z.E_INVALID
+
+
+def test_lists_and_words_that_are_misaligned():
+    """A status word off its four bytes would fault in the atomic that sets a bit."""
+    L, c = Z.lib(), ctypes.byref(_cache())
+    for a in range(3):
+        src, dst, status = (ODD if a == i else P for i in range(3))
+        assert L.zoact_cache_fork(c, src, dst, 1, P, BIG, status, None) == Z.E_INVALID
+        assert b"aligned" in L.zoact_last_error()
+    for slots, status in ((ODD, P), (P, ODD)):
+        assert L.zoact_cache_free(c, slots, 1, status, None) == Z.E_INVALID
+        assert b"aligned" in L.zoact_last_error()
+    assert L.zoact_cache_compact(c, P, BIG, ODD, None) == Z.E_INVALID
+    assert b"aligned" in L.zoact_last_error()
