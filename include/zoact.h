@@ -307,8 +307,8 @@ size_t zoact_linear_workspace_bytes(void);
  * infinite x gives +-inf by the weight's sign, NaN where the weight is 0; finite x overflow
  * only where the result does (outputs that come out infinite or NaN are formed a second time,
  * about 0.1 ms a call).
- * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU); flags:
- * ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, w_scales, p, y and residual 16-byte aligned.
+ * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU), below
+ * 2^29; flags: ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, w_scales, p, y and residual 16-byte aligned.
  * L->ws (optional, as above) lets the depth of narrow layers be split over workgroups; the
  * partial sums are added in a fixed order.  Calls that overlap on one workspace race.  y must
  * not overlap x, p or the layer; it may be the residual itself (BF16, without SWIGLU). */

@@ -225,8 +225,9 @@ zoact_status zoact_linear_rows(const zoact_linear* L, const zoact_arena* A, cons
   CHECK((flags & ~(uint32_t)(ZOACT_EPI_SWIGLU | ZOACT_EPI_RELU)) == 0, "linear_rows: unknown flags 0x%x", flags);
   CHECK(!((flags & ZOACT_EPI_SWIGLU) && (flags & ZOACT_EPI_RELU)), "linear_rows: SWIGLU and RELU are exclusive");
   const int64_t unit = (flags & ZOACT_EPI_SWIGLU) ? 32 : 16;
-  CHECK(L->d_out >= unit && L->d_out % unit == 0 && L->d_out <= (int64_t(1) << 32),
-        "linear_rows: d_out=%lld must be a multiple of %d", (long long)L->d_out, (int)unit);
+  // (a launch holds fewer than 2^32 threads, and wide layers take 512 for 64 features)
+  CHECK(L->d_out >= unit && L->d_out % unit == 0 && L->d_out < (int64_t(1) << 29),
+        "linear_rows: d_out=%lld must be a multiple of %d below 2^29", (long long)L->d_out, (int)unit);
   CHECK(float_type(y_dtype), "linear_rows: y must be F32 or BF16");
   CHECK(L->r >= 0 && L->r <= 256, "linear_rows: r=%d outside [0, 256]", L->r);
   CHECK(aligned16(x) && aligned16(L->w) && aligned16(y) && (!residual || aligned16(residual)) && (!p || aligned16(p)),

@@ -181,3 +181,9 @@ def test_lists_and_words_that_are_misaligned():
         assert b"aligned" in L.zoact_last_error()
     assert L.zoact_cache_compact(c, P, BIG, ODD, None) == Z.E_INVALID
     assert b"aligned" in L.zoact_last_error()
+
+
+def test_more_features_than_a_launch_has_threads_for():
+    for rows in (1, 20, 64):
+        assert _rows(_lin(d_in=128, d_out=1 << 29), rows=rows) == Z.E_INVALID
+        assert b"d_out" in Z.lib().zoact_last_error()
