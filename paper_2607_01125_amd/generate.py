@@ -93,13 +93,16 @@ class Session:
         self.cache_ws = torch.empty(Z.cache_workspace_bytes(new), dtype=torch.uint8, device=self.dec.dev)
 
     def check(self):
-        """Raise if a call since the last check found no place for what it was given (waits for the GPU)."""
+        """Raise if a call since the last check found no place for what it was given (waits for the GPU).
+        From that call on, nothing that was given until this check has been taken (logits of such calls mean
+        nothing): each sequence holds a beginning of what it was given, lens says how long a one."""
         bits = int(self.status)
         if bits:
             self.status.zero_()
             self.lens = self.cache.len.tolist()
         if bits & Z.STATUS_NO_PAGES:
-            raise RuntimeError("the cache has too few free pages: free sequences or resize")
+            raise RuntimeError("the cache has too few free pages: free sequences or resize, and go on from what lens "
+                               "says the sequences hold")
         if bits:
             raise RuntimeError(f"the cache refused an entry (status {bits})")
 
@@ -123,7 +126,8 @@ class Session:
             if self.lens[sl] + c > self.max_pages * Z.CACHE_PAGE:
                 raise ValueError(f"slot {sl} would pass {self.max_pages * Z.CACHE_PAGE} tokens")
         ends = np.cumsum(counts)
-        begin = torch.tensor([0, *ends.tolist()], dtype=torch.int32, device=d.dev)
+        # (no rows for anybody once a call was refused, so that no later one leaves a hole in a sequence)
+        begin = torch.tensor([0, *ends.tolist()], dtype=torch.int32, device=d.dev).mul_(self.status == 0)
         batch = Z.CacheBatch(torch.empty(n, dtype=torch.int32, device=d.dev), max(counts), rows,
                              slots=ids, row_begin=begin, status=self.status)
         Z.cache_extend(self.cache, batch, self.cache_ws)

@@ -201,3 +201,23 @@ def test_too_few_pages_and_bad_calls():
             bad()
     ses.check()
     assert ses.lens == ses.cache.len.tolist() == [100, 3]
+
+
+def test_a_prompt_whose_middle_chunk_finds_no_page_has_no_hole():
+    """Chunks of 100, 100 and 10 tokens where pages for the first alone are free: the last, which would fit behind the
+    first, is not taken either, and the sequence goes on from what it holds."""
+    _, g, _ = _tuned(synth.TINY, "fp32")
+    p = _prompts(synth.TINY, [210], 15)[0]
+    ses = G.Session(g, 2, 256, n_pages=3, max_rows=100)
+    ses.prefill([0], [p])
+    t = torch.zeros(1, dtype=torch.int32, device=dev())
+    ses.decode([0], t)                       # (nor is anything else before the refusal is seen)
+    ses.decode([1], t)
+    with pytest.raises(RuntimeError, match="pages"):
+        ses.check()
+    assert ses.lens == ses.cache.len.tolist() == [100, 0]
+    ses.check()
+    ses.resize(8)
+    got = ses.prefill([0], [p[100:]])
+    ses.check()
+    assert torch.equal(got, G.Session(g, 2, 256, max_rows=100).prefill([0], [p]))
