@@ -165,8 +165,12 @@ class Session:
             r = d.r if adapted else 0
             if lin.r != r:
                 lin.r = r
+            if d.linear_hook:
+                d.linear_hook("pre", lin, rows, flags)
             Z.linear_rows(lin, d.arena if adapted else None, x[:rows], B["p"][:rows] if adapted else None, y[:rows],
                           residual[:rows] if residual is not None else None, flags)
+            if d.linear_hook:
+                d.linear_hook("post", lin, rows, flags)
 
         for l, P in enumerate(d.layers):
             ut = d._norm_site(l, "attn", h, P["n1"], P.get("n1b"), B["a"], True, None, 2 * T)

@@ -197,7 +197,7 @@ class Decoder:
         # version and the forward forms the perturbation again
         self._ch_next = None
         # optional callable(stage, lin, T, flags) around every linear launch ("pre"/"post"),
-        # for per-launch timing
+        # for per-launch timing (T: tokens per half; the rows of an answering INT4 layer's few)
         self.linear_hook = None
         # layer 0 reads the same embedding in both halves: its first projection forms x W^T
         # and x U once (ZOACT_SHARED_X) when the layer qualifies

@@ -221,3 +221,15 @@ def test_a_prompt_whose_middle_chunk_finds_no_page_has_no_hole():
     got = ses.prefill([0], [p[100:]])
     ses.check()
     assert torch.equal(got, G.Session(g, 2, 256, max_rows=100).prefill([0], [p]))
+
+
+def test_the_linear_hook_sees_every_launch_of_a_session():
+    for mode, rows in (("int4", 3), ("int4", 70), ("bf16", 3)):
+        _, g, _ = _tuned(LLAMA_S, mode)
+        calls = []
+        g.linear_hook = lambda stage, lin, T, flags: calls.append((stage, lin.d_in, lin.d_out, flags))
+        G.Session(g, 1, 128).prefill([0], _prompts(LLAMA_S, [rows], 3))
+        g.linear_hook = None
+        per_layer = sum(isinstance(v, tuple) for v in g.layers[0].values())
+        assert [c[0] for c in calls] == ["pre", "post"] * (per_layer * LLAMA_S.n_layers), (mode, rows)
+        assert sum(c[3] == Z.EPI_SWIGLU for c in calls) == 2 * LLAMA_S.n_layers
