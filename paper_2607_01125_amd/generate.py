@@ -21,7 +21,7 @@ from . import zoact as Z
 
 class Session:
     """Sequences in slots 0 .. max_seqs - 1 of up to max_tokens tokens each, over n_pages pages of 64 tokens
-    (default: enough for all at full length).  max_rows: most new rows of one call; longer prompts are
+    (default: enough for all at full length).  Decoders with heads of 32, 64 or 128 values.  max_rows: most new rows of one call; longer prompts are
     taken in chunks.  Calls on one Session, and on all Sessions of one decoder, whose workspaces they share,
     follow each other on one stream of its device, the current one."""
 
@@ -31,6 +31,8 @@ class Session:
             raise ValueError(f"max_seqs must be in [1, {Z.CACHE_MAX_BATCH}]")
         if max_rows < max_seqs:
             raise ValueError("max_rows must hold one row of every sequence")
+        if d.hd not in (32, 64, 128):
+            raise ValueError(f"the cache holds heads of 32, 64 or 128 values, not {d.hd}")
         self.max_pages = -(-max_tokens // Z.CACHE_PAGE)
         self.cache = Z.Cache.alloc(d.s.n_layers, n_pages or max_seqs * self.max_pages, d.Hkv, d.hd, max_seqs,
                                    self.max_pages, d.dev)
@@ -125,6 +127,8 @@ class Session:
         for sl, c in zip(slots, counts):
             if self.lens[sl] + c > self.max_pages * Z.CACHE_PAGE:
                 raise ValueError(f"slot {sl} would pass {self.max_pages * Z.CACHE_PAGE} tokens")
+        if not d._adapted_sites <= d.ut.keys():      # (before places are reserved that would get no keys)
+            raise RuntimeError("adapted sites without a basis: run basis_init or set_basis first")
         ends = np.cumsum(counts)
         # (no rows for anybody once a call was refused, so that no later one leaves a hole in a sequence)
         begin = torch.tensor([0, *ends.tolist()], dtype=torch.int32, device=d.dev).mul_(self.status == 0)

@@ -233,3 +233,20 @@ def test_the_linear_hook_sees_every_launch_of_a_session():
         per_layer = sum(isinstance(v, tuple) for v in g.layers[0].values())
         assert [c[0] for c in calls] == ["pre", "post"] * (per_layer * LLAMA_S.n_layers), (mode, rows)
         assert sum(c[3] == Z.EPI_SWIGLU for c in calls) == 2 * LLAMA_S.n_layers
+
+
+def test_a_session_refuses_a_model_it_cannot_serve():
+    """Heads of a width that the cache does not have, and a decoder without bases: before anything is reserved."""
+    shape = synth.shrink(synth.TINY, n_heads=8, n_kv_heads=8)
+    assert shape.head_dim not in (32, 64, 128)
+    _, g, _ = _tuned(shape, "fp32")
+    with pytest.raises(ValueError, match="head"):
+        G.Session(g, 1, 64)
+    _, g, _ = _tuned(synth.TINY, "fp32")
+    ses = G.Session(g, 1, 64)
+    ut, g.ut = g.ut, {}
+    with pytest.raises(RuntimeError, match="basis"):
+        ses.prefill([0], [[1, 2, 3]])
+    g.ut = ut
+    assert ses.lens == ses.cache.len.tolist() == [0]
+    assert torch.equal(ses.prefill([0], [[1, 2, 3]]), G.Session(g, 1, 64).prefill([0], [[1, 2, 3]]))
