@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import weakref
 from dataclasses import dataclass
 
 import torch
@@ -207,6 +208,15 @@ def dtype_code(t: torch.Tensor) -> int:
     raise ValueError(f"unsupported activation dtype {t.dtype}")
 
 
+def _none():
+    return None
+
+
+def _weak(t):
+    """What returns t while it lives (None for None)."""
+    return _none if t is None else weakref.ref(t)
+
+
 @dataclass
 class Linear:
     """Device tensors of one adapted layer (w: [d_out][d_in] or packed int4 [d_out][d_in/2])."""
@@ -223,26 +233,30 @@ class Linear:
     plain: tuple = (0, 0)               # output features [begin, end) not adapted (no coefficient rows)
     ws: torch.Tensor | None = None      # optional workspace (linear_workspace_bytes)
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_rows", None)
-
     def __getstate__(self):             # (a copy is checked anew)
         return {k: v for k, v in self.__dict__.items() if k != "_rows"}
 
     def rows_ref(self, dev: int):
         """What linear_rows reads of the layer, by reference: checked when first used on device `dev`, and again
-        after a field is set (the tensors' contents may change, the tensors do not)."""
-        r = self.__dict__.get("_rows")
-        if r is None or r[0] != dev:
-            int4, bf = self.w.dtype is torch.uint8, torch.bfloat16
-            d = LinearDesc(INT4_G128 if int4 else dtype_code(self.w),
-                           _arg(self.w, "w", self.w.dtype, dev, (self.d_out, self.d_in // 2) if int4 else None),
-                           _arg(self.w_scales, "w_scales", bf, dev, (self.d_out, self.d_in // 128)) if int4 else None,
-                           _arg(self.bias, "bias", bf, dev, (self.d_out,)), None, self.d_in, self.d_out, self.r,
-                           self.coef_offset, None, 0, *self.plain, *_ws(self.ws, dev))
-            r = self.__dict__["_rows"] = (dev, ctypes.byref(d))
-        return r[1]
+        where a field is another one or a tensor has other memory (its `.data` set, `set_`, `resize_`)."""
+        w, sc, bias, ws, k = self.w, self.w_scales, self.bias, self.ws, self.__dict__.get("_rows")
+        # (the tensors are held weakly: a layer whose weights are replaced does not keep the old ones)
+        if (k is not None and k[0]() is w and k[1] == w.data_ptr() and k[2]() is sc and k[3] == sc.data_ptr()
+                and k[4]() is bias and k[5] == (None if bias is None else bias.data_ptr())
+                and k[6]() is ws and k[7] == (None if ws is None else ws.data_ptr())
+                and k[8] == (dev, self.d_in, self.d_out, self.r, self.coef_offset, self.plain)):
+            return k[9]
+        int4, bf, plain = w.dtype is torch.uint8, torch.bfloat16, tuple(self.plain)
+        d = LinearDesc(INT4_G128 if int4 else dtype_code(w),
+                       _arg(w, "w", w.dtype, dev, (self.d_out, self.d_in // 2) if int4 else None),
+                       _arg(sc, "w_scales", bf, dev, (self.d_out, self.d_in // 128)) if int4 else None,
+                       _arg(bias, "bias", bf, dev, (self.d_out,)), None, self.d_in, self.d_out, self.r,
+                       self.coef_offset, None, 0, *plain, *_ws(ws, dev))
+        ref = ctypes.byref(d)
+        if int4:
+            self.__dict__["_rows"] = (_weak(w), d.w, _weak(sc), d.w_scales, _weak(bias), d.bias, _weak(ws), d.ws,
+                                      (dev, self.d_in, self.d_out, self.r, self.coef_offset, plain), ref)
+        return ref
 
     def desc(self) -> LinearDesc:
         wd = INT4_G128 if self.w.dtype == torch.uint8 else dtype_code(self.w)
@@ -265,21 +279,16 @@ class Arena:
     def k(self) -> int:
         return self.c.numel()
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_coef", None)
-
     def __getstate__(self):             # (a copy is checked anew)
         return {k: v for k, v in self.__dict__.items() if k != "_coef"}
 
     def coef_ref(self, dev: int):
         """The coefficients alone, by reference, checked as Linear.rows_ref says."""
-        r = self.__dict__.get("_coef")
-        if r is None or r[0] != dev:
-            c = self.c
+        c, k = self.c, self.__dict__.get("_coef")
+        if k is None or k[0]() is not c or k[1] != c.data_ptr() or k[2] != dev:
             d = ArenaDesc(dtype_code(c), _arg(c, "arena.c", c.dtype, dev), None, None, c.numel())
-            r = self.__dict__["_coef"] = (dev, ctypes.byref(d))
-        return r[1]
+            k = self.__dict__["_coef"] = (_weak(c), d.c, dev, ctypes.byref(d))
+        return k[3]
 
     def desc(self) -> ArenaDesc:
         return ArenaDesc(dtype_code(self.c), self.c.data_ptr(), self.m.data_ptr(), self.v.data_ptr(), self.k)
@@ -646,8 +655,8 @@ def linear_rows(layer: Linear, arena: Arena | None, x: torch.Tensor, p: torch.Te
 
 @dataclass(frozen=True)
 class Cache:
-    """Device tensors of a paged 8-bit key/value cache (layouts: zoact_cache.h).  They are checked once,
-    here; their contents change, the tensors do not."""
+    """Device tensors of a paged 8-bit key/value cache (layouts: zoact_cache.h).  They are checked here, and
+    again where a call finds one with other memory; their contents change."""
     k: torch.Tensor         # int8 [n_layers][n_pages][n_kv_heads][64][head_dim]
     v: torch.Tensor         # int8 [n_layers][n_pages][n_kv_heads][head_dim][64]
     k_scale: torch.Tensor   # fp32 [n_layers][n_pages][n_kv_heads][4]
@@ -669,13 +678,23 @@ class Cache:
                       _arg(self.v_scale, "v_scale", torch.float32, dev, (nl, npg, nh, 4)),
                       _arg(self.table, "table", i32, dev), _arg(self.len, "len", i32, dev, (ns,)),
                       _arg(self.refs, "refs", i32, dev, (npg,)), npg, nl, nh, hd, ns, mp)
-        object.__setattr__(self, "_desc", d)
-        object.__setattr__(self, "_ref", ctypes.byref(d))
+        object.__setattr__(self, "_kept", (self._places(), ctypes.byref(d)))
         for name, value in (("index", dev), ("n_kv_heads", nh), ("head_dim", hd)):
             object.__setattr__(self, name, value)
 
+    def _places(self):
+        return (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                self.table.data_ptr(), self.len.data_ptr(), self.refs.data_ptr())
+
     def __reduce__(self):               # (a copy is checked anew)
         return Cache, (self.k, self.v, self.k_scale, self.v_scale, self.table, self.len, self.refs)
+
+    @property
+    def _ref(self):
+        """The cache's descriptor, by reference."""
+        if self._kept[0] != self._places():
+            self.__post_init__()
+        return self._kept[1]
 
     @classmethod
     def alloc(cls, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
@@ -694,7 +713,7 @@ class Cache:
 class CacheBatch:
     """New rows of one step: entry i is rows row_begin[i] .. row_begin[i + 1] - 1 (or max_new rows each)
     of slot slots[i] (or slot i); pos [n] int32 is written by cache_extend; status [1] int32.  Checked when
-    first used, and again after a field is set; the tensors' contents may change, the tensors do not."""
+    first used, and again where a field is set or a tensor has other memory."""
     pos: torch.Tensor
     max_new: int
     rows: int
@@ -704,21 +723,23 @@ class CacheBatch:
 
     def __setattr__(self, name, value):
         object.__setattr__(self, name, value)
-        self.__dict__.pop("_ref", None)
+        self.__dict__.pop("_kept", None)
 
     def __getstate__(self):             # (a copy is checked anew)
-        return {k: v for k, v in self.__dict__.items() if k != "_ref"}
+        return {k: v for k, v in self.__dict__.items() if k != "_kept"}
 
     def ref(self, dev: int):
         """The batch's descriptor, by reference, for a cache on device `dev`."""
-        r = self.__dict__.get("_ref")
-        if r is None or r[0] != dev:
-            n, i32 = self.pos.numel(), torch.int32
-            d = CacheBatchDesc(n, self.max_new, self.rows, _arg(self.slots, "slots", i32, dev, (n,)),
-                               _arg(self.row_begin, "row_begin", i32, dev, (n + 1,)),
-                               _arg(self.pos, "pos", i32, dev, (n,)), _arg(self.status, "status", i32, dev, (1,)))
-            r = self.__dict__["_ref"] = (dev, ctypes.byref(d))
-        return r[1]
+        k, slots, begin, status = self.__dict__.get("_kept"), self.slots, self.row_begin, self.status
+        if (k is not None and k[0] == dev and k[1] == self.pos.data_ptr() and (slots is None or k[2] == slots.data_ptr())
+                and (begin is None or k[3] == begin.data_ptr()) and (status is None or k[4] == status.data_ptr())):
+            return k[5]
+        n, i32 = self.pos.numel(), torch.int32
+        d = CacheBatchDesc(n, self.max_new, self.rows, _arg(slots, "slots", i32, dev, (n,)),
+                           _arg(begin, "row_begin", i32, dev, (n + 1,)), _arg(self.pos, "pos", i32, dev, (n,)),
+                           _arg(status, "status", i32, dev, (1,)))
+        self.__dict__["_kept"] = (dev, d.pos, d.slots, d.row_begin, d.status, ctypes.byref(d))
+        return self.__dict__["_kept"][5]
 
 
 def _ws(ws, dev: int):
@@ -771,10 +792,10 @@ def cache_compact(cache: Cache, ws: torch.Tensor, n_used: torch.Tensor | None = 
 def cache_append(cache: Cache, layer: int, k: torch.Tensor, v: torch.Tensor, batch: CacheBatch, rope=None, stream=None):
     """Quantise the batch's keys (rotated with rope = (cos, sin)) and values into `layer`; k and v may
     be column slices of a wider buffer."""
-    dev, hd = cache.index, cache.head_dim
+    ref, dev, hd = cache._ref, cache.index, cache.head_dim
     kp, ldk = _heads_arg(k, "k", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
     vp, ldv = _heads_arg(v, "v", k.dtype, dev, batch.rows, cache.n_kv_heads * hd)
-    _on_device(lib().zoact_cache_append, dev, stream, cache._ref, layer, kp, ldk, vp, ldv, dtype_code(k),
+    _on_device(lib().zoact_cache_append, dev, stream, ref, layer, kp, ldk, vp, ldv, dtype_code(k),
                batch.ref(dev), *_rope_args(rope, dev, hd))
 
 
@@ -788,8 +809,8 @@ def attention_cache(cache: Cache, layer: int, q: torch.Tensor, out: torch.Tensor
                     scale: float, max_len: int, rope=None, ws: torch.Tensor | None = None, stream=None):
     """Causal attention of the batch's rows over their slots' tokens in `layer` (q may be a column slice
     of a wider buffer; rope = (cos, sin) rotates it first)."""
-    dev, hd = cache.index, cache.head_dim
+    ref, dev, hd = cache._ref, cache.index, cache.head_dim
     qp, ldq = _heads_arg(q, "q", out.dtype, dev, batch.rows, n_heads * hd)
     op = _arg(out, "out", out.dtype, dev, (batch.rows, n_heads * hd))
-    _on_device(lib().zoact_attention_cache, dev, stream, cache._ref, layer, qp, ldq, dtype_code(out), n_heads,
+    _on_device(lib().zoact_attention_cache, dev, stream, ref, layer, qp, ldq, dtype_code(out), n_heads,
                batch.ref(dev), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))
