@@ -250,3 +250,52 @@ def test_a_session_refuses_a_model_it_cannot_serve():
     g.ut = ut
     assert ses.lens == ses.cache.len.tolist() == [0]
     assert torch.equal(ses.prefill([0], [[1, 2, 3]]), G.Session(g, 1, 64).prefill([0], [[1, 2, 3]]))
+
+
+def _plain_beams(g, prompt, n_new, beams, eos):
+    """Beam search that runs every candidate from its prompt on, one sequence at a time.  Returns the best's tokens,
+    whether a step's survivors were in another order than their parents, whether one had ended, and the smallest
+    difference of scores that decided something."""
+    ses = G.Session(g, 1, len(prompt) + n_new)
+
+    def after(tokens):
+        ses.free([0])
+        logits = ses.prefill([0], [prompt])
+        for t in tokens:
+            logits = ses.decode([0], torch.tensor([t], dtype=torch.int32, device=dev()))
+        ses.check()
+        return torch.log_softmax(logits[0], 0).cpu().numpy().astype(np.float64)
+
+    held, moved, ended, gap = [(0.0, [])], False, False, np.inf
+    for step in range(n_new):
+        if step and all(eos in t for _, t in held):
+            break
+        nxt = []
+        for i, (score, t) in enumerate(held):
+            if eos is not None and eos in t:
+                nxt.append((score, t + [eos], i))
+                ended = True
+            else:
+                nxt += [(score + float(p), t + [k], i) for k, p in enumerate(after(t))]
+        nxt.sort(key=lambda c: -c[0])
+        gap = min([gap] + [a[0] - b[0] for a, b in zip(nxt[:beams], nxt[1:beams + 1])])
+        held = [c[:2] for c in nxt[:beams]]
+        moved = moved or (step > 0 and [c[2] for c in nxt[:beams]] != list(range(beams)))
+    best = held[0][1]
+    return best[:best.index(eos)] if eos is not None and eos in best else best, moved, ended, gap
+
+
+@pytest.mark.parametrize("beams", [2, 4])
+def test_beams_of_several_steps_against_a_plain_search(beams):
+    """Survivors in other orders than their parents, histories and ended candidates over five steps.  (The scores of
+    two runs differ by the sums' order, some 1e-6: all decisions are by more.)"""
+    shape = synth.shrink(synth.TINY, vocab=64)
+    _, g, _ = _tuned(shape, "fp32")
+    prompts = _prompts(shape, [9, 30], 23)
+    plain = [_plain_beams(g, p, 5, beams, None) for p in prompts]
+    assert all(p[1] for p in plain) and min(p[3] for p in plain) > 1e-4, [p[1:] for p in plain]
+    assert g.generate(prompts, 5, beams=beams) == [p[0] for p in plain]
+    eos = plain[0][0][1]
+    cut = [_plain_beams(g, p, 5, beams, eos) for p in prompts]
+    assert cut[0][2] and min(p[3] for p in cut) > 1e-4, [p[1:] for p in cut]
+    assert g.generate(prompts, 5, beams=beams, eos=eos) == [p[0] for p in cut]
