@@ -303,7 +303,7 @@ def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int
     score, tok = torch.log_softmax(logits, dim=1).topk(beams, dim=1)            # [n][beams]
     done = tok == eos if eos is not None else torch.zeros_like(tok, dtype=torch.bool)
     hist = tok[:, :, None]
-    for _ in range(n_new - 1):
+    for step in range(1, n_new):
         if bool(done.all()):
             break
         logits = ses.decode(slots, tok.reshape(-1).to(torch.int32).contiguous())
@@ -320,7 +320,7 @@ def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int
         if eos is not None:
             done = done | (tok == eos)
         src = (parent + torch.arange(n, device=dev)[:, None] * beams).reshape(-1).tolist()
-        if src != slots:
+        if src != slots and step < n_new - 1:
             ses.fork(src, slots)
     best = hist[:, 0].tolist()
     return [row[:row.index(eos)] if eos is not None and eos in row else row for row in best]
