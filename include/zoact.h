@@ -303,8 +303,9 @@ size_t zoact_linear_workspace_bytes(void);
  * others zoact_linear_fwd_pair with sign 0 serves).  C is read from the arena at
  * L->coef_offset; L->ch and L->ut are not read.  Features [plain_begin, plain_end) have no
  * correction (any bounds here).  Sums are fp32 and a group's scale multiplies the group's
- * sum: unlike the products of two or more halves, q * s is not rounded to bf16 first.  An
- * infinite x gives +-inf by the weight's sign, NaN where the weight is 0; finite x overflow
+ * sum: unlike the products of two or more halves, q * s is not rounded to bf16 first (their
+ * weight is up to 2^-9 away; outputs differ by 1.3e-3 of their norm, less than their own
+ * rounding to bf16 takes).  An infinite x gives +-inf by the weight's sign, NaN where the weight is 0; finite x overflow
  * only where the result does (outputs that come out infinite or NaN are formed a second time,
  * about 0.1 ms a call).
  * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU), below

@@ -8,6 +8,13 @@ tokens from the logits.
 Layers with INT4 weights run on zoact_linear_rows up to ROWS_MAX rows; larger chunks, and bf16 and fp32
 models, run the two-halves linears of the training forward with sign 0, the rows shared out over the
 halves.
+
+The two do not have the same INT4 weight: linear_rows multiplies a group's sum by its scale (the weight is
+q s), the training forward's products read bf16(q s), up to 2^-9 away from it.  A layer's outputs differ by
+1.3e-3 of their norm before they are rounded to bf16 (which takes 1.7e-3), the logits of 32 layers of the
+Llama-3-8B shape with random weights by 8.8e-2, where taking the prompt in two chunks instead of one moves them by
+4.9e-2 and a bf16 step of the embeddings by 2.0e-1.  With trained_weights every call has the weights that C was
+tuned on: a token of one sequence takes 6.2 ms instead of 5.1 there, of 48 sequences 6.9 instead of 5.2.
 """
 from __future__ import annotations
 
@@ -22,10 +29,12 @@ from . import zoact as Z
 class Session:
     """Sequences in slots 0 .. max_seqs - 1 of up to max_tokens tokens each, over n_pages pages of 64 tokens
     (default: enough for all at full length).  Decoders with heads of 32, 64 or 128 values.  max_rows: most new rows of one call; longer prompts are
-    taken in chunks.  Calls on one Session, and on all Sessions of one decoder, whose workspaces they share,
+    taken in chunks.  trained_weights: INT4 weights as the training forward rounds them in calls of few rows
+    too (see above).  Calls on one Session, and on all Sessions of one decoder, whose workspaces they share,
     follow each other on one stream of its device, the current one."""
 
-    def __init__(self, decoder, max_seqs: int, max_tokens: int, *, n_pages: int | None = None, max_rows: int = 2048):
+    def __init__(self, decoder, max_seqs: int, max_tokens: int, *, n_pages: int | None = None, max_rows: int = 2048,
+                 trained_weights: bool = False):
         d = self.dec = decoder
         if not 1 <= max_seqs <= Z.CACHE_MAX_BATCH:
             raise ValueError(f"max_seqs must be in [1, {Z.CACHE_MAX_BATCH}]")
@@ -38,6 +47,7 @@ class Session:
                                    self.max_pages, d.dev)
         self.lens = [0] * max_seqs                 # the lengths the cache has, on the host
         self.max_rows = max_rows + max_rows % 2
+        self.few_rows = Z.ROWS_MAX if d.mode == "int4" and not trained_weights else 0
         self.status = torch.zeros(1, dtype=torch.int32, device=d.dev)
         self.cache_ws = torch.empty(Z.cache_workspace_bytes(self.cache), dtype=torch.uint8, device=d.dev)
         self.rope = d._rope_tables(self.max_pages * Z.CACHE_PAGE) if d.s.family == "llama" else None
@@ -143,7 +153,7 @@ class Session:
             self._att_ws = torch.empty(need, dtype=torch.uint8, device=d.dev)
 
         T = (rows + 1) // 2                        # rows of a half in the two-halves linears
-        few = d.mode == "int4" and rows <= Z.ROWS_MAX
+        few = rows <= self.few_rows
         B = {k: v[:2 * T] if v is not None else None for k, v in self._buf.items() if k not in ("emb", "pos")}
         pert = Z.pert_pair(0, 0, (0, 0), (0, 0), 0.0)
         d._cur = B
@@ -260,15 +270,17 @@ class Session:
 
 
 def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int = 1, max_rows: int = 2048,
-             n_pages: int | None = None) -> list:
+             n_pages: int | None = None, trained_weights: bool = False) -> list:
     """Continuations of the prompts (lists of token ids) by up to n_new tokens: the likeliest token each
     time, or with beams > 1 the likeliest of that many candidates followed at once (by their tokens' summed
-    log probabilities).  Ends a sequence at `eos`, which is not returned.  Returns lists of token ids."""
+    log probabilities).  Ends a sequence at `eos`, which is not returned.  max_rows, n_pages and trained_weights
+    are the Session's.  Returns lists of token ids."""
     if n_new < 1 or beams < 1 or not prompts:
         raise ValueError("expected prompts, n_new >= 1 and beams >= 1")
     n = len(prompts)
     longest = max(len(p) for p in prompts) + n_new
-    ses = Session(decoder, n * beams, longest, max_rows=max(max_rows, n * beams), n_pages=n_pages)
+    ses = Session(decoder, n * beams, longest, max_rows=max(max_rows, n * beams), n_pages=n_pages,
+                  trained_weights=trained_weights)
     first = [i * beams for i in range(n)]
     logits = ses.prefill(first, prompts)
     ses.check()

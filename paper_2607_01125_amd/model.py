@@ -662,7 +662,7 @@ class Decoder:
     # ---------------------------------------------------------------- answering
     def generate(self, prompts, n_new: int, **kw) -> list:
         """Continuations of the prompts (lists of token ids) by the model with C as it is now, over a paged
-        8-bit key/value cache: see generate.generate (eos, beams, max_rows, n_pages) and, for sequences
-        kept from call to call, generate.Session."""
+        8-bit key/value cache: see generate.generate (eos, beams, max_rows, n_pages, trained_weights) and, for
+        sequences kept from call to call, generate.Session."""
         from . import generate
         return generate.generate(self, prompts, n_new, **kw)
