@@ -239,7 +239,10 @@ __device__ float plain_sum(const RowsArgs& a, int64_t t, int64_t n, int gbeg, in
 // contiguous bytes), a stage ahead in registers (two stages ahead: the same times), and go through LDS to the
 // operands' order; read from memory in that order, where a quad touches four rows, 4096 x 28672 took 23 us at
 // one row and 27 at 13.  16-byte pieces are swapped by the row's number, so that neither side of LDS has bank
-// conflicts.  Scales come 32 groups at a time for the same reason.
+// conflicts (counted: none in the forms of 1, 13 and 48 rows).  x, whose quarter-waves read pieces four apart, is
+// swapped by the row's number less four: lanes 0-3 and 12-15 of a quarter are served with 4-11 of the next, and
+// without the four they meet on the same banks (20 and 28% of the cycles at 13 and 48 rows; 64 rows of 5120 x
+// 20480 41.9 us, now 39.9).  Scales come 32 groups at a time, so that they too are read in pieces of rows.
 // Wave w takes group w % WK of a stage and the tiles from w / WK on; the waves' sums meet in LDS in a
 // fixed order.  blockIdx.y: the part of the depth (partial sums go to part, rows_join_kernel adds them).
 // (Tried and left: one workgroup of 16 waves a compute unit with all of x in LDS and weights streamed
@@ -271,8 +274,9 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
   const __amdgpu_buffer_rsrc_t xrs =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(a.x), 0, a.rows * a.K * 2, 0x00020000);
   const uint16_t* const srow = a.sc + n0 * a.groups;
-  // pieces swapped within 16 (8) by the row's number
+  // pieces swapped within 16 (8)
   auto swap = [](int row, int piece) { return WK >= 4 ? piece ^ (row & 15) : piece ^ ((row >> 1) & 7); };
+  auto swap_x = [](int row, int piece) { return piece ^ ((row - 4) & 15); };
 
   uint4 wv[WL], xv[XL];
   uint16_t sv[SL];
@@ -356,7 +360,7 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
 #pragma unroll
     for (int j = 0; j < XL; ++j) {
       const int u = tid + j * TH, row = u / XP, piece = u % XP;
-      if ((XN % TH == 0 || u < XN) && row < a.rows) xb[row * XP + (piece ^ (row & 15))] = pair_order(xv[j]);
+      if ((XN % TH == 0 || u < XN) && row < a.rows) xb[row * XP + swap_x(row, piece)] = pair_order(xv[j]);
     }
     if (st + 1 < stages) load(st + 1);
     __syncthreads();
@@ -369,7 +373,7 @@ __global__ void __launch_bounds__(64 * NW) rows_kernel(RowsArgs a) {
       off[b] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        xf[b][j] = __builtin_bit_cast(bf16x8, xb[xrow * XP + ((wk * 16 + g * 4 + j) ^ (xrow & 15))]);
+        xf[b][j] = __builtin_bit_cast(bf16x8, xb[xrow * XP + swap_x(xrow, wk * 16 + g * 4 + j)]);
         off[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xf[b][j], minus24, off[b], 0, 0, 0);
       }
     }
