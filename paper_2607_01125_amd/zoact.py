@@ -678,13 +678,10 @@ class Cache:
                       _arg(self.v_scale, "v_scale", torch.float32, dev, (nl, npg, nh, 4)),
                       _arg(self.table, "table", i32, dev), _arg(self.len, "len", i32, dev, (ns,)),
                       _arg(self.refs, "refs", i32, dev, (npg,)), npg, nl, nh, hd, ns, mp)
-        object.__setattr__(self, "_kept", (self._places(), ctypes.byref(d)))
+        object.__setattr__(self, "_places", (d.k, d.v, d.k_scale, d.v_scale, d.table, d.len, d.refs))
+        object.__setattr__(self, "_kept", ctypes.byref(d))
         for name, value in (("index", dev), ("n_kv_heads", nh), ("head_dim", hd)):
             object.__setattr__(self, name, value)
-
-    def _places(self):
-        return (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
-                self.table.data_ptr(), self.len.data_ptr(), self.refs.data_ptr())
 
     def __reduce__(self):               # (a copy is checked anew)
         return Cache, (self.k, self.v, self.k_scale, self.v_scale, self.table, self.len, self.refs)
@@ -692,9 +689,10 @@ class Cache:
     @property
     def _ref(self):
         """The cache's descriptor, by reference."""
-        if self._kept[0] != self._places():
+        if self._places != (self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                            self.table.data_ptr(), self.len.data_ptr(), self.refs.data_ptr()):
             self.__post_init__()
-        return self._kept[1]
+        return self._kept
 
     @classmethod
     def alloc(cls, n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, n_slots: int, max_pages: int,
@@ -752,8 +750,12 @@ def _rope_args(rope, dev: int, hd: int):
     if rope is None:
         return None, None, 0
     c, s = rope
-    shape = (c.shape[0], hd // 2)
-    return _arg(c, "cos", torch.float32, dev, shape), _arg(s, "sin", torch.float32, dev, shape), shape[0]
+    shape, f32 = c.shape, torch.float32
+    if not (shape == s.shape and len(shape) == 2 and shape[1] == hd // 2 and c.dtype is f32 and s.dtype is f32
+            and c.get_device() == dev and s.get_device() == dev and c.is_contiguous() and s.is_contiguous()):
+        shape = (shape[0], hd // 2)
+        _arg(c, "cos", f32, dev, shape), _arg(s, "sin", f32, dev, shape)
+    return c.data_ptr(), s.data_ptr(), shape[0]
 
 
 def cache_workspace_bytes(cache: Cache) -> int:
