@@ -283,7 +283,7 @@ __device__ __forceinline__ Range split_range(const AttendArgs& a, const CacheEnt
 
 // Decoding: at most 16 columns, each wave its own pages.  Bound by the pages' bytes: one row behind 131071 tokens,
 // 8 key/value heads of 128 (268 MB), 51 us and 5 for the join, 5.3 TB/s; the same pages read in the same way
-// and nothing done with them, 45 us.  48 rows behind 70 to 8000 tokens (271 MB): 60 and 5.  Half of a wave's
+// and nothing done with them, 45 us.  48 rows behind 70 to 8000 tokens (271 MB): 60 and 5.  35 to 43% of a wave's
 // cycles wait for memory, a third issue vector instructions.  (Pages through LDS in whole rows' order: 67 us
 // where this order took 61.)
 template <typename T, int HD, int NT>
@@ -474,9 +474,11 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
 // neither side has bank conflicts), the next page's codes on their way meanwhile.  Two buffers and one barrier
 // a page, or one buffer and two where that lets a compute unit hold a third workgroup.
 // Bound by the vector units' share (16 scores a lane and page: scale, maximum, exponential, rounding), the LDS
-// reads and the products in turn: 333 rows of three sequences behind 500 to 1500, 40 heads of 128, 55 us, 366
-// TFLOP/s (with two buffers 63); 4 times 2048 rows, 32/8 heads, 212 us.  128 columns a workgroup, which halve the
-// LDS reads but take 248 registers, are no faster: 71 us and 213.
+// reads and the products in turn: 333 rows of three sequences behind 500 to 1500, 40 heads of 128, 56 us, 356
+// TFLOP/s (with two buffers 63; alone on the card 62, in fp32 82); 4 times 2048 rows, 32/8 heads, 210 us.  128
+// columns a workgroup, which halve the LDS reads but take 248 registers, are no faster: 71 us and 213.
+// One form and one number of splits serve a batch, by its longest entry's rows: a single token behind 131070 beside
+// a chunk of 512 rows walks its pages in one workgroup a head, 3.5 ms for the batch; apart they take 52 and 22 us.
 constexpr int chunk_buffers(int HD, int NT) { return HD == 128 && NT == 1 ? 1 : 2; }
 template <typename T, int HD, int NT>
 __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) attend_chunk_kernel(AttendArgs a) {

@@ -14,8 +14,8 @@ namespace {
 // page's block w.  The four lanes of a token take its 16-byte pieces in turn (a quad reads 64 contiguous
 // bytes), so the partner of a rotated value lies in the same lane, and the block's maximum is a reduction
 // over the wave.  V goes through LDS to its transposed place.  Bound by bytes, each read and written once: four
-// prompts of 2011 tokens, 40 heads of 128 (216 MB), 56 us, 3.9 TB/s; 32 single tokens, 8 heads, 8 us of launch
-// and trips to memory (batch, page number, rows).
+// prompts of 2011 tokens, 40 heads of 128 (216 MB), 62 us, 3.5 TB/s (on the same inputs again and again 49, in fp32
+// 74); 32 single tokens, 8 heads, 8 us of launch and trips to memory (batch, page number, rows).
 // Value i of a lane is dim ((i / V) * 4 + quarter) * V + i % V, V values a piece.
 template <typename T, int HD>
 struct Quarter {

@@ -526,6 +526,9 @@ hipError_t go(RowsArgs a, int splits, void* ws, hipStream_t s) {
 //   20480 x 5120  9.6: 1 part                  31.0 / 38.7;              33.4 / 38.7
 //                      4 parts                 16.7 / 21.1;              18.3 / 21.6
 //                      6 parts                 16.3 / 22.9;              16.6 / 18.3;  8 parts     18.4 / 19.7
+// The turn at 8192 columns lies where the sides meet for few rows; 4096 features, what is taken and the other side:
+// 8192 columns 9.0 / 11.9 (four parts 9.6 / 10.7), 10240 12.1 / 13.5 (one part of 16 weight rows 10.1 / 13.5),
+// 12288 11.7 / 12.9 (11.4 / 15.4).
 template <int XR>
 hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
   const bool swiglu = a.flags & ZOACT_EPI_SWIGLU;
@@ -540,10 +543,10 @@ hipError_t pick16(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStre
 }
 
 // 17 rows and more: 128 weight rows a workgroup, so that x, which every workgroup reads whole, is read
-// rarely; one workgroup a compute unit (4096 x 28672 at 64 rows 38 us, with 64 weight rows 55; 20480 x 5120
-// 38 us in 6 parts, 63 in 2).  Up to 32 rows layers of few tiles take 32, whose stages are shorter: 4096 x 4096
-// 10.4 us in two parts, with 128 in eight 12.1, 4096 x 6144 12.4 and 13.8 (but 4096 x 28672 44 and 24; at 48
-// rows 4096 x 4096 takes 14.1 either way, 4096 x 6144 16.5 and 16.1).
+// rarely; one workgroup a compute unit (4096 x 28672 at 64 rows 34 us, with 64 weight rows 48; 20480 x 5120
+// 33 us in 6 parts, 70 in 2).  Up to 32 rows layers of few tiles take 32, whose stages are shorter: 4096 x 4096
+// 9.8 us in two parts, with 128 in eight 11.9, 4096 x 6144 11.8 and 13.2, 8192 x 4096 14.0 and 14.4, 10240 x 4096
+// 16.3 and 15.3 (but 4096 x 28672 42 and 23; at 48 rows 4096 x 4096 12.9 and 13.9, 4096 x 6144 15.3 and 15.7).
 template <int NB>
 hipError_t pick_more(const RowsArgs& a, int cus, void* ws, size_t ws_bytes, hipStream_t s) {
   const int64_t t16 = a.N / 16;

@@ -28,10 +28,12 @@ from . import zoact as Z
 
 class Session:
     """Sequences in slots 0 .. max_seqs - 1 of up to max_tokens tokens each, over n_pages pages of 64 tokens
-    (default: enough for all at full length).  Decoders with heads of 32, 64 or 128 values.  max_rows: most new rows of one call; longer prompts are
-    taken in chunks.  trained_weights: INT4 weights as the training forward rounds them in calls of few rows
-    too (see above).  Calls on one Session, and on all Sessions of one decoder, whose workspaces they share,
-    follow each other on one stream of its device, the current one."""
+    (default: enough for all at full length).  Decoders with heads of 32, 64 or 128 values.  max_rows: most
+    new rows of one call; longer prompts are taken in chunks.  trained_weights: INT4 weights as the training
+    forward rounds them in calls of few rows too (see above).  Calls on one Session, and on all Sessions of one
+    decoder, whose workspaces they share, follow each other on one stream of its device, the current one.
+    Single tokens of long sequences are best decoded apart from prompts: see the attention's note on mixed
+    batches in zoact_cache.h."""
 
     def __init__(self, decoder, max_seqs: int, max_tokens: int, *, n_pages: int | None = None, max_rows: int = 2048,
                  trained_weights: bool = False):

@@ -729,8 +729,9 @@ class CacheBatch:
     def ref(self, dev: int):
         """The batch's descriptor, by reference, for a cache on device `dev`."""
         k, slots, begin, status = self.__dict__.get("_kept"), self.slots, self.row_begin, self.status
-        if (k is not None and k[0] == dev and k[1] == self.pos.data_ptr() and (slots is None or k[2] == slots.data_ptr())
-                and (begin is None or k[3] == begin.data_ptr()) and (status is None or k[4] == status.data_ptr())):
+        if (k is not None and k[0] == dev and k[1] == self.pos.data_ptr()
+                and (slots is None or k[2] == slots.data_ptr()) and (begin is None or k[3] == begin.data_ptr())
+                and (status is None or k[4] == status.data_ptr())):
             return k[5]
         n, i32 = self.pos.numel(), torch.int32
         d = CacheBatchDesc(n, self.max_new, self.rows, _arg(slots, "slots", i32, dev, (n,)),
