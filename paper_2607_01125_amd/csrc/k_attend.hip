@@ -30,8 +30,8 @@ struct AttendArgs {
   const float *ct, *st;
   int64_t n_pos;
   void* out;
-  float* part;                 // [n * max_new * H][S][HD], unnormalised
-  float2* ml;                  // [n * max_new * H][S] maximum (log2 domain) and sum
+  float* part;                 // [n * max_new * H][S][HD], each split's weighted mean of values
+  float2* ml;                  // [n * max_new * H][S] maximum (log2 domain) and sum of weights
 };
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -195,6 +195,10 @@ __device__ __forceinline__ void soft_page(float (&s)[4][4], float (&f)[4], int t
   }
   l += lsum;
 }
+
+// What a sum of weights is divided by, as a factor: 0 for the sum of nothing.  (A sum is no less than 2^(-1/16), the
+// weight of its own maximum.)
+__device__ __forceinline__ float inverse_sum(float l) { return l == 0.f ? 0.f : 1.f / l; }
 
 // q of one column as right operands: step s of a lane holds dims 64 (s / 2) + 16 g + 8 (s % 2) + 0..7 (HD 32:
 // 8 g + 0..7), rotated, times a power of two that brings the column's largest to [2^14, 2^15).
@@ -415,16 +419,17 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
       pg = next;
     }
   }
-  // the four waves' results (q and its maxima have been read by all)
+  // the four waves' results (q and its maxima have been read by all), means: sums of large values would overflow
   __syncthreads();
   constexpr int DV = HD / 16;
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  const float inverse = inverse_sum(l);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     floatx4 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i], vexp - kPExp);
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i] * inverse, vexp - kPExp);
     *reinterpret_cast<floatx4*>(&so[wave][lane & 15][d * 16 + 4 * g]) = r;
   }
   if (g == 0) {
@@ -438,26 +443,28 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : 2) attend_kernel(AttendArgs
 #pragma unroll
   for (int w = 0; w < 4; ++w) M = fmaxf(M, sm[w][oc]);
   const float base = M == -INFINITY ? 0.f : M;
-  float L = 0.f, r[DV];
+  float L = 0.f, r[DV], f[4];
 #pragma unroll
   for (int k = 0; k < DV; ++k) r[k] = 0.f;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const float f = __builtin_amdgcn_exp2f(sm[w][oc] - base);
-    L += f * sl[w][oc];
-#pragma unroll
-    for (int k = 0; k < DV; ++k) r[k] += f * so[w][oc][d0 + k];
+    f[w] = __builtin_amdgcn_exp2f(sm[w][oc] - base) * sl[w][oc];
+    L += f[w];
   }
+  const float share = inverse_sum(L);
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+#pragma unroll
+    for (int k = 0; k < DV; ++k) r[k] += f[w] * share * so[w][oc][d0 + k];
   const int oj = col / a.G, oh = hk * a.G + col % a.G;
   if (a.S == 1) {
-    const float div = L == 0.f ? 1.f : L;
     T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
 #pragma unroll
     for (int k = 0; k < DV; ++k) {
       if constexpr (sizeof(T) == 2)
-        op[k] = f2bf(r[k] / div);
+        op[k] = f2bf(r[k]);
       else
-        op[k] = r[k] / div;
+        op[k] = r[k];
     }
   } else {
     const int64_t R = (((int64_t)blockIdx.z * a.b.max_new + oj) * a.H + oh) * a.S + split;
@@ -596,35 +603,35 @@ __global__ void __launch_bounds__(256, chunk_buffers(HD, NT) == 1 ? 3 : 2) atten
   l += __shfl_xor(l, 32, 64);
   if (col >= ncol) return;
   const int oj = col / a.G, oh = hk * a.G + col % a.G;
-  const float div = l == 0.f ? 1.f : l;
+  const float inverse = inverse_sum(l);
   const int64_t R = (((int64_t)blockIdx.z * a.b.max_new + oj) * a.H + oh) * a.S + split;
   if (a.S > 1 && g == 0) a.ml[R] = make_float2(m, l);
 #pragma unroll
   for (int d = 0; d < DT; ++d) {
     float r[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i], vexp - kPExp);
+    for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_ldexpf(o[d][i] * inverse, vexp - kPExp);
     const int d0 = d * 16 + 4 * g;
     if (a.S > 1) {
       if (l != 0.f) *reinterpret_cast<float4*>(a.part + R * HD + d0) = make_float4(r[0], r[1], r[2], r[3]);
     } else {
       T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + oj) * a.H + oh) * HD + d0;
       if constexpr (sizeof(T) == 2) {
-        *reinterpret_cast<uint2*>(op) = make_uint2((uint32_t)f2bf(r[0] / div) | (uint32_t)f2bf(r[1] / div) << 16,
-                                                   (uint32_t)f2bf(r[2] / div) | (uint32_t)f2bf(r[3] / div) << 16);
+        *reinterpret_cast<uint2*>(op) = make_uint2((uint32_t)f2bf(r[0]) | (uint32_t)f2bf(r[1]) << 16,
+                                                   (uint32_t)f2bf(r[2]) | (uint32_t)f2bf(r[3]) << 16);
       } else {
-        *reinterpret_cast<float4*>(op) = make_float4(r[0] / div, r[1] / div, r[2] / div, r[3] / div);
+        *reinterpret_cast<float4*>(op) = make_float4(r[0], r[1], r[2], r[3]);
       }
     }
   }
 }
 
 constexpr int kMaxSplits = 128;
-// Weight of a split with sum l and maximum m in a row whose maximum is the base: below zero for an empty one, which
-// has written no sums.  Any other counts with its sums, even where the weight is 0, so that a NaN among its values
-// reaches the row as it does unsplit.
+// Weight of a split with sum l and maximum m in a row whose maximum is the base.  An empty one (l == 0) has written
+// no mean; any other counts with its mean, even where the weight is 0, so that a NaN among its values
+// reaches the row as it does unsplit: the joins mark the empty ones' shares by -1.
 __device__ __forceinline__ float split_weight(float m, float l, float base) {
-  return l == 0.f ? -1.f : __builtin_amdgcn_exp2f(m - base);
+  return l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - base) * l;
 }
 // Joins up to eight splits of a row and head in half a wave, HD / 32 columns a lane; sums and statistics (a lane
 // holds those of split lane % 8) are asked for at once.  Bound by the launch and one trip to memory: 48 rows of 32
@@ -650,25 +657,23 @@ __global__ void __launch_bounds__(256) attend_join_few_kernel(AttendArgs a) {
 #pragma unroll
   for (int k = 1; k < 8; k <<= 1) M = fmaxf(M, __shfl_xor(M, k, 64));
   const float base = M == -INFINITY ? 0.f : M;
-  const float f = split_weight(m, l, base);
-  float L = f * l;
+  float f = split_weight(m, l, base), L = f;
 #pragma unroll
   for (int k = 1; k < 8; k <<= 1) L += __shfl_xor(L, k, 64);
+  f = l == 0.f ? -1.f : f * inverse_sum(L);
   vec r = 0.f;
 #pragma unroll
   for (int k = 0; k < kFewSplits; ++k) {
     const float w = __shfl(f, (lane & ~7) | k, 64);
     if (!(w < 0.f)) r += w * v[k];      // (a NaN weight counts)
   }
-  const float div = L == 0.f ? 1.f : L;
   T* const op = static_cast<T*>(a.out) + ((int64_t)e.row0 * a.H + row) * HD + d0;
 #pragma unroll
   for (int d = 0; d < DV; ++d) {
-    const float y = L == 0.f ? 0.f : r[d] / div;
     if constexpr (sizeof(T) == 2)
-      op[d] = f2bf(y);
+      op[d] = f2bf(r[d]);
     else
-      op[d] = y;
+      op[d] = r[d];
   }
 }
 
@@ -703,20 +708,20 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   __syncthreads();
   if (wave < kMaxSplits / 64) {
     const float M = fmaxf(red[0], red[1]), base = M == -INFINITY ? 0.f : M;
-    const float f = split_weight(ml.x, ml.y, base);
-    wt[tid] = f;
-    float L = f * ml.y;
+    float L = split_weight(ml.x, ml.y, base);
+    wt[tid] = ml.y == 0.f ? -1.f : L;
 #pragma unroll
     for (int k = 1; k < 64; k <<= 1) L += __shfl_xor(L, k, 64);
     if (lane == 0) redl[wave] = L;
   }
   __syncthreads();
+  const float share = inverse_sum(redl[0] + redl[1]);
   vec r = 0.f;
 #pragma unroll
   for (int k = 0; k < NI; ++k)
     if (grp + k * NG < a.S) {
       const float w = wt[grp + k * NG];
-      if (!(w < 0.f)) r += w * v[k];    // (a NaN weight counts)
+      if (!(w < 0.f)) r += w * share * v[k];    // (a NaN weight counts)
     }
   sr[grp][tid & 31] = r;
   __syncthreads();
@@ -724,8 +729,6 @@ __global__ void __launch_bounds__(256) attend_join_kernel(AttendArgs a) {
   float y = 0.f;
 #pragma unroll
   for (int k = 0; k < NG; ++k) y += reinterpret_cast<const float*>(sr[k])[tid];
-  const float L = redl[0] + redl[1];
-  y = L == 0.f ? 0.f : y / L;
   T* const op = static_cast<T*>(a.out) + ((int64_t)(e.row0 + j) * a.H + h) * HD + tid;
   if constexpr (sizeof(T) == 2)
     *op = f2bf(y);

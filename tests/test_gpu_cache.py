@@ -828,3 +828,20 @@ def test_chunks_behind_long_prompts_in_splits(lens, counts, H, hkv, hd, dtype):
     Z.attention_cache(pr.c, 0, q, again, b, H, scale, n, rope=rp, ws=ws)
     r0, r1 = counts[0], counts[0] + counts[1]
     assert torch.equal(again[:r0], out[:r0]) and torch.equal(again[r1:], out[r1:]) and (again[r0:r1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lens,counts,H,hkv,hd", [([5, 300], [1, 1], 4, 2, 64), ([40, 200], [30, 9], 4, 2, 128),
+                                                  ([3000], [1], 2, 1, 32), ([5000], [2], 2, 1, 64), ([1500], [40], 2, 1, 32)])
+def test_values_near_the_top_of_the_range(lens, counts, H, hkv, hd, dtype):
+    """Values of about 2^126: their weighted sums pass fp32's range, their means do not (unsplit, in few and in many
+    splits, both tile forms)."""
+    pr, b, pos, q, rp = _filled(lens, counts, H, hkv, hd, dtype, False)
+    factor = 2.0 ** 126 / float(pr.c.v_scale[0, pr.c.table[0, 0].long(), 0, 0] * 127)
+    pr.c.v_scale.mul_(factor)
+    pr.m.vs *= np.float32(factor)
+    n = max(L + c for L, c in zip(lens, counts))
+    for split in (False, True):
+        out, ws = _check_attention(pr, b, pos, q, counts, H, dtype, rp, n, split=split, scale=0.01)
+    assert torch.isfinite(out.float()).all() and float(out.float().abs().max()) > 2.0 ** 115
+    assert ws is not None or n < 1000
