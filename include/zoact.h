@@ -306,8 +306,8 @@ size_t zoact_linear_workspace_bytes(void);
  * sum: unlike the products of two or more halves, q * s is not rounded to bf16 first (their
  * weight is up to 2^-9 away; outputs differ by 1.3e-3 of their norm, less than their own
  * rounding to bf16 takes).  An infinite x gives +-inf by the weight's sign and NaN where the
- * weight is 0; finite x overflow only where the result does (outputs that come out infinite or
- * NaN are formed a second time, about 0.1 ms a call).
+ * weight is 0; finite x overflow only where the result or its sum over a part of the depth does
+ * (outputs that come out infinite or NaN are formed a second time, about 0.1 ms a call).
  * 1 <= rows <= ZOACT_ROWS_MAX; d_in % 128 == 0, up to 2^23; d_out % 16 == 0 (32 with SWIGLU), below 2^29;
  * flags: ZOACT_EPI_SWIGLU or ZOACT_EPI_RELU; x, w, w_scales, p, y and residual 16-byte aligned.
  * L->ws (optional, as above) lets the depth of narrow layers be split over workgroups; the
