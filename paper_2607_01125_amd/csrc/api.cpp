@@ -6,7 +6,7 @@
 
 #include <string>
 
-#include "common.hpp"
+#include "packed.hpp"
 
 namespace {
 
@@ -319,8 +319,42 @@ zoact_status zoact_linear_xent_pair(const zoact_linear* L, const zoact_arena* A,
   const size_t need = zoact::linear_xent_ws_bytes(B * S, L->d_out);
   if (ws == nullptr || ws_bytes < need || !aligned16(ws))
     return fail(ZOACT_E_WORKSPACE, "linear_xent: workspace needs %zu bytes, 16-byte aligned", need);
-  return hip_status(zoact::launch_linear_xent(*L, A, x, B * S, p, *pp, tokens, S, loss_pm, ws, ws_bytes, st(stream)),
+  return hip_status(zoact::launch_linear_xent(*L, A, x, B * S, p, *pp, tokens, S, nullptr, loss_pm, ws, ws_bytes,
+                                              st(stream)),
                     "linear_xent");
+}
+
+zoact_status zoact_linear_xent_packed(const zoact_linear* L, const zoact_arena* A, const void* x, const zoact_packed* s,
+                                      const void* p, const zoact_pert_pair* pp, const int32_t* tokens, float* loss_pm,
+                                      void* ws, size_t ws_bytes, zoact_stream stream) {
+  zoact_status v = zoact::check_packed(s);
+  if (v != ZOACT_OK) return v;
+  CHECK(tokens != nullptr && loss_pm != nullptr, "linear_xent_packed: NULL tokens or loss");
+  CHECK(s->rows >= 1, "linear_xent_packed: no rows");
+  CHECK(L != nullptr && L->w_dtype == ZOACT_BF16, "linear_xent_packed: needs a BF16 layer");
+  v = validate_linear(L, A, x, ZOACT_BF16, s->rows, p, nullptr, 0, pp, x, ZOACT_F32);
+  if (v != ZOACT_OK) return v;
+  const size_t need = zoact::linear_xent_ws_bytes(s->rows, L->d_out);
+  if (ws == nullptr || ws_bytes < need || !aligned16(ws))
+    return fail(ZOACT_E_WORKSPACE, "linear_xent_packed: workspace needs %zu bytes, 16-byte aligned", need);
+  // (to the product all rows are one sequence: it keeps the next row's logit of each but the last)
+  return hip_status(zoact::launch_linear_xent(*L, A, x, s->rows, p, *pp, tokens, s->rows, s, loss_pm, ws, ws_bytes,
+                                              st(stream)),
+                    "linear_xent_packed");
+}
+
+zoact_status zoact_xent_packed(const float* logits, const int32_t* tokens, const zoact_packed* s, int64_t V,
+                               float* loss_pm, void* ws, size_t ws_bytes, zoact_stream stream) {
+  const zoact_status v = zoact::check_packed(s);
+  if (v != ZOACT_OK) return v;
+  CHECK(logits && tokens && loss_pm, "xent_packed: NULL pointer");
+  CHECK(s->rows >= 1 && V >= 1, "xent_packed: need rows >= 1 and V >= 1");
+  CHECK(zoact::aligned_to(logits, 4) && zoact::aligned_to(tokens, 4) && zoact::aligned_to(loss_pm, 4) &&
+            zoact::aligned_to(ws, 8),
+        "xent_packed: logits, tokens and loss must be 4-byte aligned, ws 8-byte");
+  if (ws == nullptr || ws_bytes < zoact_loss_workspace_bytes())
+    return fail(ZOACT_E_WORKSPACE, "xent_packed: workspace needs %zu bytes", zoact_loss_workspace_bytes());
+  return hip_status(zoact::launch_xent_rows(logits, tokens, *s, V, loss_pm, ws, st(stream)), "xent_packed");
 }
 
 size_t zoact_linear_mse_workspace_bytes(int64_t T, int64_t d_out) {

@@ -1,0 +1,412 @@
+// Selection of a beam search's candidates over beams and vocabulary (zoact_packed.h).
+//
+// Two launches: beam_rows reads the logits once, 4096 of a row a workgroup, and leaves of each such
+// part the maximum, the sum of exponentials relative to it and its `beams` largest logits in order
+// (within one beam the order of the values is that of the logits); beam_pick joins a prompt's sums
+// to log sums, ranks the parts' candidates by value and copies the kept candidates' histories.
+#include <math.h>
+
+#include "packed.hpp"
+
+namespace zoact {
+namespace {
+
+constexpr int PART = 4096;               // logits of a workgroup
+constexpr int NT = 256, PER = PART / NT;
+constexpr int KMAX = ZOACT_BEAMS_MAX;
+constexpr int WCAP = 512;                // candidates a wave gathers before it takes the slow way
+
+// Order of fp32 (fp64) values as that of unsigned numbers above 0.
+__device__ __forceinline__ uint32_t order32(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);          // (-0 counts as 0)
+  return (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ uint64_t order64(double x) {
+  if (x != x) return ~0ull;
+  const uint64_t b = (uint64_t)__double_as_longlong(x + 0.0);
+  return (b >> 63) ? ~b : b | (1ull << 63);
+}
+__device__ __forceinline__ float from_order32(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7FFFFFFFu : ~k);
+}
+
+struct Cand {
+  float x;
+  int32_t v;             // token, -1: none
+};
+
+// Workspace: [rows][splits] (maximum, sum), then [rows][splits][beams] candidates.
+struct Layout {
+  int64_t rows;
+  int splits;
+  size_t cand_at, bytes;
+};
+Layout layout_of(int32_t n, int32_t beams_in, int32_t beams, int64_t vocab) {
+  Layout l;
+  l.rows = (int64_t)n * beams_in;
+  l.splits = (int)((vocab + PART - 1) / PART);
+  const size_t parts = (size_t)l.rows * (size_t)l.splits;
+  l.cand_at = (parts * sizeof(float2) + 255) & ~(size_t)255;
+  l.bytes = l.cand_at + parts * (size_t)beams * sizeof(Cand);
+  return l;
+}
+
+__device__ __forceinline__ float ld1(const float* p) { return *p; }
+__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
+__device__ __forceinline__ void ld4(const float* p, float (&x)[4]) {
+  const float4 u = *reinterpret_cast<const float4*>(p);
+  x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+}
+__device__ __forceinline__ void ld4(const uint16_t* p, float (&x)[4]) {
+  const ushort4 u = *reinterpret_cast<const ushort4*>(p);
+  x[0] = bf2f(u.x), x[1] = bf2f(u.y), x[2] = bf2f(u.z), x[3] = bf2f(u.w);
+}
+
+// Key of a candidate within a row: larger values first, then lower tokens; 0: none.
+__device__ __forceinline__ uint64_t row_key(uint32_t ord, int v) { return ((uint64_t)ord << 32) | (0xFFFFFFFFu - (uint32_t)v); }
+
+// VEC: rows start on 16 bytes (fp32; 8 in bf16) and hold a multiple of four values.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, int64_t ldl, zoact_beams b, int splits,
+                                                float2* __restrict__ sums, Cand* __restrict__ cand) {
+  __shared__ uint64_t list[4][WCAP];
+  __shared__ uint64_t best[4][KMAX];
+  __shared__ float2 wsum[4];
+  const int row = blockIdx.y, part = blockIdx.x, K = b.beams;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (b.eos >= 0 && b.length > 0 && b.hist[(int64_t)row * b.ld_hist + b.length - 1] == b.eos) return;   // it has ended
+  const T* lr = logits + (int64_t)row * ldl;
+  const int V = (int)b.vocab, v0 = part * PART + threadIdx.x * 4;      // this thread: v0 + 1024 j + e
+  float x[PER];
+  uint32_t key[PER];                     // 0: behind the row, or NaN (the row's sum tells of it)
+  float mx = -INFINITY;
+  uint32_t kmax = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    const int64_t v = (int64_t)v0 + j * (NT * 4);
+    if (VEC) {
+      if (v < V) ld4(lr + v, t);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v + e < V) t[e] = ld1(lr + v + e);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      x[j * 4 + e] = t[e];
+      mx = fmaxf(mx, t[e]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int64_t v = (int64_t)v0 + (i >> 2) * (NT * 4) + (i & 3);
+    key[i] = v < V && x[i] == x[i] ? order32(x[i]) : 0;
+    kmax = key[i] > kmax ? key[i] : kmax;
+  }
+  // maximum and sum of the wave's 1024
+  float wm = mx;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor(wm, o, 64));
+  const float base = wm == -INFINITY ? 0.f : wm;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) sum += expf(x[i] - base);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) wsum[wave] = make_float2(wm, sum);
+
+  // the K-th largest of the lanes' maxima: at least K of the wave's values reach it
+  uint32_t thr = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t t = thr | (1u << bit);
+    if (__popcll(__ballot(kmax >= t)) >= K) thr = t;
+  }
+  thr = thr ? thr : 1;
+  // gather what lies above it, and of what equals it the K lowest tokens
+  int cnt = 0, eq = 0;
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t km = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) km = key[j * 4 + e] > km ? key[j * 4 + e] : km;
+    if (__ballot(km >= thr) == 0) continue;
+    uint64_t at[4];
+    int lower = 0, all = 0;               // equal ones of lower lanes, of all lanes
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      at[e] = __ballot(key[j * 4 + e] == thr);
+      lower += __popcll(at[e] & below);
+      all += __popcll(at[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t k = key[j * 4 + e];
+      const bool take = k > thr || (k == thr && eq + lower < K);
+      if (k == thr) ++lower;
+      const uint64_t m = __ballot(take);
+      const int p = cnt + __popcll(m & below);
+      if (take && p < WCAP) list[wave][p] = row_key(k, v0 + j * (NT * 4) + e);
+      cnt += __popcll(m);
+    }
+    eq += all;
+  }
+  // the wave's K largest, in order (best[][i] = 0: fewer)
+  if (lane < K) best[wave][lane] = 0;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (cnt <= WCAP) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (every lane's entries)
+    for (int i = lane; i < cnt; i += 64) {
+      const uint64_t mine = list[wave][i];
+      int rank = 0;
+      for (int t = 0; t < cnt; ++t) rank += list[wave][t] > mine;
+      if (rank < K) best[wave][rank] = mine;
+    }
+  } else {
+    uint64_t last = ~0ull;
+    for (int r = 0; r < K; ++r) {
+      uint64_t mine = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const uint64_t c = key[i] ? row_key(key[i], v0 + (i >> 2) * (NT * 4) + (i & 3)) : 0;
+        if (c < last && c > mine) mine = c;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t c = __shfl_xor((unsigned long long)mine, o, 64);
+        mine = c > mine ? c : mine;
+      }
+      if (lane == 0) best[wave][r] = mine;
+      last = mine;
+      if (mine == 0) break;
+    }
+  }
+  __syncthreads();
+  // the part's: each wave's list is in order
+  const int64_t at = (int64_t)row * splits + part;
+  Cand* const out = cand + at * K;
+  for (int i = threadIdx.x; i < 4 * K; i += NT) {
+    const int w = i / K;
+    const uint64_t mine = best[w][i - w * K];
+    int rank = 0, any = 0;
+    for (int u = 0; u < 4; ++u)
+      for (int t = 0; t < K; ++t) {
+        const uint64_t c = best[u][t];
+        rank += c > mine;
+        any += c != 0;
+      }
+    if (mine && rank < K) out[rank] = Cand{from_order32((uint32_t)(mine >> 32)), (int)(0xFFFFFFFFu - (uint32_t)mine)};
+    if (i < K && i >= any) out[i] = Cand{0.f, -1};
+  }
+  if (threadIdx.x == 0) {
+    float M = wsum[0].x;
+    for (int u = 1; u < 4; ++u) M = fmaxf(M, wsum[u].x);
+    const float mb = M == -INFINITY ? 0.f : M;
+    float S = 0.f;
+    for (int u = 0; u < 4; ++u) S += wsum[u].y * (wsum[u].x == -INFINITY ? 1.f : expf(wsum[u].x - mb));
+    sums[at] = make_float2(M, S);        // (a NaN among the values is in S)
+  }
+}
+
+enum { BEAM_PLAIN, BEAM_ENDED, BEAM_NAN, BEAM_LOST };   // LOST: every value is -inf
+
+__global__ void __launch_bounds__(NT) beam_pick(zoact_beams b, int splits, const float2* __restrict__ sums,
+                                                const Cand* __restrict__ cand) {
+  constexpr int CAP = 1024;
+  __shared__ double lse[KMAX], sc[KMAX];
+  __shared__ int kind[KMAX];
+  __shared__ uint64_t key[CAP];
+  __shared__ int64_t flat[CAP];
+  __shared__ uint64_t tmax[NT], thr;
+  __shared__ int n_got;
+  __shared__ uint64_t wkey[4];
+  __shared__ int64_t wflat[4];
+  __shared__ int parent[KMAX];
+  const int i0 = blockIdx.x, BI = b.beams_in, K = b.beams, V = (int)b.vocab;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  if (threadIdx.x == 0) n_got = 0, thr = 0;
+  for (int j = wave; j < BI; j += 4) {
+    const int64_t row = (int64_t)i0 * BI + j;
+    const double s = (double)b.score[row];
+    int kd = BEAM_PLAIN;
+    double l = 0.0;
+    if (s != s || s == INFINITY) kd = BEAM_NAN;
+    else if (b.eos >= 0 && b.length > 0 && b.hist[row * b.ld_hist + b.length - 1] == b.eos)
+      kd = s == -INFINITY ? BEAM_LOST : BEAM_ENDED;
+    else {
+      float M = -INFINITY;
+      for (int t = lane; t < splits; t += 64) M = fmaxf(M, sums[row * splits + t].x);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+      double S = 0.0;
+      for (int t = lane; t < splits; t += 64) {
+        const float2 p = sums[row * splits + t];
+        // (a part of nothing but -inf has the sum 0, or NaN)
+        S += p.x == -INFINITY ? (double)p.y : (double)p.y * exp((double)p.x - (double)M);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) S += __shfl_xor(S, o, 64);
+      l = (double)M + log(S);
+      if (!(l - l == 0.0)) kd = BEAM_NAN;
+      else if (s == -INFINITY) kd = BEAM_LOST;
+    }
+    if (lane == 0) lse[j] = l, sc[j] = s, kind[j] = kd;
+  }
+  __syncthreads();
+  // Candidate c of the prompt: beam j's part and place, or for beams whose values do not follow the
+  // logits the lowest tokens (an ended one's eos first).
+  const int per = splits * K;
+  const int64_t total = (int64_t)BI * per;
+  auto read = [&](int64_t c, uint64_t& k, int64_t& f) {
+    const int j = (int)(c / per), t = (int)(c - (int64_t)j * per);
+    k = 0;
+    f = 0;
+    if (kind[j] == BEAM_PLAIN) {
+      const Cand d = cand[((int64_t)i0 * BI + j) * per + t];
+      if (d.v < 0) return;
+      k = order64(sc[j] + ((double)d.x - lse[j]));
+      f = (int64_t)j * V + d.v;
+    } else if (t < K) {
+      int v = t;
+      double val = kind[j] == BEAM_NAN ? (double)NAN : -INFINITY;
+      if (kind[j] == BEAM_ENDED && b.eos < V) {
+        if (t == 0) v = b.eos, val = sc[j];
+        else v = t - 1 < b.eos ? t - 1 : t;
+      }
+      k = order64(val);
+      f = (int64_t)j * V + v;
+    }
+  };
+  auto better = [](uint64_t k, int64_t f, uint64_t k2, int64_t f2) { return k > k2 || (k == k2 && f < f2); };
+  auto value = [](uint64_t k) -> float {
+    if (k == ~0ull) return NAN;
+    return (float)__longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
+  };
+  auto emit = [&](int m, uint64_t k, int64_t f) {
+    const int j = (int)(f / V), v = (int)(f - (int64_t)j * V);
+    const int64_t o = (int64_t)i0 * K + m;
+    b.score_out[o] = value(k);
+    if (b.token) b.token[o] = v;
+    if (b.src) b.src[o] = i0 * K + j;
+    b.hist_out[o * b.ld_hist_out + b.length] = v;
+    parent[m] = j;
+  };
+  uint64_t mine = 0;
+  for (int64_t c = threadIdx.x; c < total; c += NT) {
+    uint64_t k;
+    int64_t f;
+    read(c, k, f);
+    mine = k > mine ? k : mine;
+  }
+  tmax[threadIdx.x] = mine;
+  __syncthreads();
+  {
+    int rank = 0;
+    for (int t = 0; t < NT; ++t) rank += tmax[t] > mine || (tmax[t] == mine && t < (int)threadIdx.x);
+    if (rank == K - 1) thr = mine ? mine : 1;
+  }
+  __syncthreads();
+  for (int64_t c = threadIdx.x; c < total; c += NT) {
+    uint64_t k;
+    int64_t f;
+    read(c, k, f);
+    if (k >= thr) {
+      const int p = atomicAdd(&n_got, 1);      // (the order of arrival changes nothing: ranks decide)
+      if (p < CAP) key[p] = k, flat[p] = f;
+    }
+  }
+  __syncthreads();
+  const int got = n_got;
+  if (got <= CAP) {
+    for (int c = threadIdx.x; c < got; c += NT) {
+      int rank = 0;
+      for (int t = 0; t < got; ++t) rank += better(key[t], flat[t], key[c], flat[c]);
+      if (rank < K) emit(rank, key[c], flat[c]);
+    }
+  } else {
+    // very many equal ones: one at a time
+    uint64_t lk = ~0ull;
+    int64_t lf = -1;
+    for (int m = 0; m < K; ++m) {
+      uint64_t bk = 0;
+      int64_t bf = 0;
+      for (int64_t c = threadIdx.x; c < total; c += NT) {
+        uint64_t k;
+        int64_t f;
+        read(c, k, f);
+        if (k && better(lk, lf, k, f) && better(k, f, bk, bf)) bk = k, bf = f;
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t k = __shfl_xor((unsigned long long)bk, o, 64);
+        const int64_t f = __shfl_xor((long long)bf, o, 64);
+        if (better(k, f, bk, bf)) bk = k, bf = f;
+      }
+      if (lane == 0) wkey[wave] = bk, wflat[wave] = bf;
+      __syncthreads();
+      for (int u = 0; u < 4; ++u)
+        if (better(wkey[u], wflat[u], bk, bf)) bk = wkey[u], bf = wflat[u];
+      if (threadIdx.x == 0) emit(m, bk, bf);
+      lk = bk;
+      lf = bf;
+      __syncthreads();
+    }
+  }
+  __syncthreads();
+  for (int64_t c = threadIdx.x; c < K * b.length; c += NT) {
+    const int m = (int)(c / b.length);
+    const int64_t t = c - m * b.length;
+    b.hist_out[((int64_t)i0 * K + m) * b.ld_hist_out + t] = b.hist[((int64_t)i0 * BI + parent[m]) * b.ld_hist + t];
+  }
+}
+
+}  // namespace
+}  // namespace zoact
+
+using namespace zoact;
+
+extern "C" size_t zoact_beam_workspace_bytes(int32_t n, int32_t beams_in, int32_t beams, int64_t vocab) {
+  if (n < 1 || beams_in < 1 || beams_in > ZOACT_BEAMS_MAX || beams < 1 || beams > ZOACT_BEAMS_MAX || vocab < 1 ||
+      vocab > (int64_t(1) << 30) || (int64_t)n * beams_in > 65535)
+    return 0;
+  return layout_of(n, beams_in, beams, vocab).bytes;
+}
+
+extern "C" zoact_status zoact_beam_select(const zoact_beams* b, const void* logits, int64_t ldl, int32_t dtype, void* ws,
+                                          size_t ws_bytes, zoact_stream stream) {
+  ZP_CHECK(b && logits && b->score && b->score_out && b->hist_out, "beam_select: NULL pointer");
+  ZP_CHECK(dtype == ZOACT_F32 || dtype == ZOACT_BF16, "beam_select: dtype must be F32 or BF16");
+  ZP_CHECK(b->n >= 1 && b->beams_in >= 1 && b->beams_in <= ZOACT_BEAMS_MAX && b->beams >= 1 &&
+               b->beams <= ZOACT_BEAMS_MAX && (int64_t)b->n * b->beams_in <= 65535,
+           "beam_select: n, beams_in or beams out of range");
+  ZP_CHECK((int64_t)b->n * b->beams < (int64_t(1) << 31), "beam_select: n * beams past 32 bits");
+  ZP_CHECK(b->vocab >= b->beams && b->vocab <= (int64_t(1) << 30), "beam_select: vocab outside [beams, 2^30]");
+  ZP_CHECK(ldl >= b->vocab, "beam_select: rows of logits overlap");
+  ZP_CHECK(b->eos >= -1 && b->eos < b->vocab, "beam_select: eos outside [-1, vocab)");
+  ZP_CHECK(b->length >= 0 && (b->length == 0 || (b->hist && b->length <= b->ld_hist)) && b->length < b->ld_hist_out,
+           "beam_select: histories do not hold the tokens");
+  ZP_CHECK(aligned_to(logits, dtype == ZOACT_F32 ? 4 : 2) && aligned_to(b->score, 4) && aligned_to(b->score_out, 4) &&
+               aligned_to(b->hist, 4) && aligned_to(b->hist_out, 4) && aligned_to(b->token, 4) && aligned_to(b->src, 4),
+           "beam_select: pointers must be aligned to their types");
+  const Layout l = layout_of(b->n, b->beams_in, b->beams, b->vocab);
+  if (ws == nullptr || ws_bytes < l.bytes) return set_error(ZOACT_E_WORKSPACE, "beam_select: workspace too small");
+  ZP_CHECK(aligned_to(ws, 16), "beam_select: ws must be 16-byte aligned");
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  float2* const sums = static_cast<float2*>(ws);
+  Cand* const cand = reinterpret_cast<Cand*>(static_cast<char*>(ws) + l.cand_at);
+  const dim3 grid((unsigned)l.splits, (unsigned)l.rows);
+  const bool vec = b->vocab % 4 == 0 && ldl % 4 == 0 && aligned_to(logits, dtype == ZOACT_F32 ? 16 : 8);
+#define ZO_ROWS(T, VEC) beam_rows<T, VEC><<<grid, NT, 0, s>>>((const T*)logits, ldl, *b, l.splits, sums, cand)
+  if (dtype == ZOACT_F32) {
+    if (vec) ZO_ROWS(float, true);
+    else ZO_ROWS(float, false);
+  } else {
+    if (vec) ZO_ROWS(uint16_t, true);
+    else ZO_ROWS(uint16_t, false);
+  }
+#undef ZO_ROWS
+  beam_pick<<<(unsigned)b->n, NT, 0, s>>>(*b, l.splits, sums, cand);
+  return launched_or("beam_select");
+}

@@ -1080,8 +1080,8 @@ size_t linear_xent_ws_bytes(int64_t T, int64_t d_out) {
 }
 
 hipError_t launch_linear_xent(const zoact_linear& L, const zoact_arena* A, const void* x, int64_t T, const void* p,
-                              const zoact_pert_pair& pert, const int32_t* tokens, int64_t S, float* loss_pm, void* ws,
-                              size_t ws_bytes, hipStream_t s) {
+                              const zoact_pert_pair& pert, const int32_t* tokens, int64_t S, const zoact_packed* seqs,
+                              float* loss_pm, void* ws, size_t ws_bytes, hipStream_t s) {
   GemmArgs a = bf16_args(L, A, x, T, p, nullptr, pert, nullptr);
   const int64_t nblk = (L.d_out + 127) / 128;
   char* w = static_cast<char*>(ws);
@@ -1099,7 +1099,7 @@ hipError_t launch_linear_xent(const zoact_linear& L, const zoact_arena* A, const
   a.tail_ws_bytes = ws_bytes > own ? (int64_t)(ws_bytes - own) : 0;
   const hipError_t e = launch_linear_pm_4w64(a, L.w_dtype, EPI_XENT, false, false, s);
   if (e != hipSuccess) return e;
-  return launch_xent_combine(a.xpart, a.xtgt, T, S, (int)nblk, T / S, part, loss_pm, s);
+  return launch_xent_combine(a.xpart, a.xtgt, T, S, (int)nblk, T / S, part, seqs, loss_pm, s);
 }
 
 hipError_t launch_dequant_int4(const void* w, const void* scales, int64_t d_out, int64_t d_in, void* out,

@@ -8,7 +8,7 @@
 //    row computes log-sum-exp over the vocabulary with an online max / sum of
 //    exponentials (wave64 shuffles, then the block), minus the target logit.
 // Both are HBM-bound single passes over y or the logits.
-#include "common.hpp"
+#include "packed.hpp"
 
 namespace zoact {
 
@@ -95,15 +95,18 @@ __global__ void __launch_bounds__(256) sum_mean(const double* __restrict__ part,
 // Cross entropy from the fused LM-head epilogue's per-block (max, sum of exp): one wave per
 // row merges its nblk blocks (lanes strided, then a butterfly, in the online-softmax rule of
 // xent_partial), and lane 0 adds max + log(sum) - next-token logit; kLossBlocks fixed
-// partial sums per half as in xent_partial.
+// partial sums per half as in xent_partial.  PACKED: rows count that have a next one in their
+// sequence of `seqs`.
+template <bool PACKED>
 __global__ void __launch_bounds__(256) xent_combine(const float2* __restrict__ xpart, const float* __restrict__ xtgt,
-                                                    int64_t T, int64_t S, int nblk, double* __restrict__ part) {
+                                                    int64_t T, int64_t S, int nblk, double* __restrict__ part,
+                                                    zoact_packed seqs) {
   __shared__ double sh[4];
   const int h = blockIdx.y;
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
   double acc = 0.0;
   for (int64_t m = (int64_t)blockIdx.x * 4 + w; m < T; m += (int64_t)gridDim.x * 4) {
-    if (m % S == S - 1) continue;              // the last position has no next token
+    if (PACKED ? !packed_has_next(seqs.begin, seqs.n, T, (int)m) : m % S == S - 1) continue;   // no next token
     const float2* pr = xpart + ((int64_t)h * T + m) * nblk;
     float mm = -INFINITY, se = 0.f;
     for (int i = l; i < nblk; i += 64) {
@@ -133,6 +136,74 @@ __global__ void __launch_bounds__(256) finish_mean(const double* __restrict__ pa
   for (int i = threadIdx.x; i < kLossBlocks; i += blockDim.x) v += part[h * kLossBlocks + i];
   const double s = block_sum_d(v, sh);
   if (threadIdx.x == 0) loss_pm[h] = (float)(s / count);
+}
+
+// The same over packed sequences: as many rows count as have a next one.
+__global__ void __launch_bounds__(256) finish_mean_packed(const double* __restrict__ part, zoact_packed seqs,
+                                                          float* loss_pm) {
+  __shared__ double sh[4];
+  const int h = blockIdx.x;
+  double v = 0.0;
+  for (int i = threadIdx.x; i < kLossBlocks; i += blockDim.x) v += part[h * kLossBlocks + i];
+  int64_t c = 0;
+  for (int i = threadIdx.x; i < seqs.n; i += blockDim.x) {
+    const int64_t end = seqs.begin[i + 1], len = (end < seqs.rows ? end : seqs.rows) - seqs.begin[i];
+    c += len > 1 ? len - 1 : 0;
+  }
+  const double s = block_sum_d(v, sh), count = block_sum_d((double)c, sh);
+  if (threadIdx.x == 0) loss_pm[h] = (float)(s / count);
+}
+
+// Cross entropy of packed rows from their logits: one block per row that has a next one in its
+// sequence; its threads' values are independent loads, the maximum and the sum of exponentials
+// joined as in xent_partial.
+__global__ void __launch_bounds__(256) xent_rows(const float* __restrict__ logits, const int32_t* __restrict__ tokens,
+                                                 zoact_packed seqs, int64_t V, double* __restrict__ part) {
+  __shared__ float smax[4], ssum[4];
+  const int h = blockIdx.y;
+  const int64_t T = seqs.rows;
+  double acc = 0.0;
+  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
+    if (!packed_has_next(seqs.begin, seqs.n, T, (int)row)) continue;   // (the same for all threads)
+    const float* lg = logits + ((int64_t)h * T + row) * V;
+    float m = -INFINITY, se = 0.f;
+    for (int64_t v0 = threadIdx.x; v0 < V; v0 += 8 * 256) {
+      float x[8], mx = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int64_t v = v0 + u * 256;
+        x[u] = v < V ? lg[v] : -INFINITY;
+        mx = fmaxf(mx, x[u]);
+      }
+      const float base = mx == -INFINITY ? 0.f : mx;      // (so that nothing but -inf so far adds 0)
+      se *= __expf(m - base);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) se += __expf(x[u] - base);
+      m = mx;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float m2 = __shfl_xor(m, o, 64), s2 = __shfl_xor(se, o, 64);
+      const float mm = fmaxf(m, m2), base = mm == -INFINITY ? 0.f : mm;
+      se = se * __expf(m - base) + s2 * __expf(m2 - base);
+      m = mm;
+    }
+    if ((threadIdx.x & 63) == 0) {
+      smax[threadIdx.x >> 6] = m;
+      ssum[threadIdx.x >> 6] = se;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const float mm = fmaxf(fmaxf(smax[0], smax[1]), fmaxf(smax[2], smax[3])), base = mm == -INFINITY ? 0.f : mm;
+      float ss = 0.f;
+      for (int i = 0; i < 4; ++i) ss += ssum[i] * __expf(smax[i] - base);
+      int64_t tok = tokens[row + 1];
+      tok = tok < 0 ? 0 : (tok >= V ? V - 1 : tok);
+      acc += (double)mm + log((double)ss) - (double)lg[tok];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) part[h * kLossBlocks + blockIdx.x] = acc;
 }
 
 __global__ void __launch_bounds__(256) xent_partial(const float* __restrict__ logits, const int32_t* __restrict__ tokens,
@@ -189,8 +260,13 @@ __global__ void __launch_bounds__(256) xent_partial(const float* __restrict__ lo
 }  // namespace
 
 hipError_t launch_xent_combine(const float2* xpart, const float* xtgt, int64_t T, int64_t S, int nblk, int64_t B,
-                               double* part, float* loss_pm, hipStream_t s) {
-  xent_combine<<<dim3(kLossBlocks, 2), dim3(256), 0, s>>>(xpart, xtgt, T, S, nblk, part);
+                               double* part, const zoact_packed* seqs, float* loss_pm, hipStream_t s) {
+  if (seqs) {
+    xent_combine<true><<<dim3(kLossBlocks, 2), dim3(256), 0, s>>>(xpart, xtgt, T, S, nblk, part, *seqs);
+    finish_mean_packed<<<2, 256, 0, s>>>(part, *seqs, loss_pm);
+    return hipGetLastError();
+  }
+  xent_combine<false><<<dim3(kLossBlocks, 2), dim3(256), 0, s>>>(xpart, xtgt, T, S, nblk, part, zoact_packed{});
   finish_mean<<<dim3(2), dim3(256), 0, s>>>(part, (double)(B * (S - 1)), loss_pm);
   return hipGetLastError();
 }
@@ -209,6 +285,14 @@ hipError_t launch_mse_pm(const void* y, int32_t dtype, const void* target, int64
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   finish_mean<<<2, 256, 0, s>>>(part, (double)n, loss_pm);
+  return hipGetLastError();
+}
+
+hipError_t launch_xent_rows(const float* logits, const int32_t* tokens, const zoact_packed& seqs, int64_t V,
+                            float* loss_pm, void* ws, hipStream_t s) {
+  double* part = static_cast<double*>(ws);
+  xent_rows<<<dim3(kLossBlocks, 2), dim3(256), 0, s>>>(logits, tokens, seqs, V, part);
+  finish_mean_packed<<<2, 256, 0, s>>>(part, seqs, loss_pm);
   return hipGetLastError();
 }
 

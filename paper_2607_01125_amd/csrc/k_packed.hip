@@ -1,0 +1,177 @@
+// Rotary positions and causal attention over packed sequences (zoact_packed.h).
+#include <math.h>
+
+#include "packed.hpp"
+
+namespace zoact {
+namespace {
+
+__device__ __forceinline__ float ld1(const float* p) { return *p; }
+__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
+__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f2bf(v); }
+
+// ---------------------------------------------------------------- rotary positions
+// One thread a pair or a copied value: any head_dim, rot_dim, stride and alignment.
+template <typename T>
+__global__ void __launch_bounds__(256) rope_at_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
+                                                      int heads, int hd, int rot, int layout,
+                                                      const int32_t* __restrict__ pos, const float* __restrict__ cos_t,
+                                                      const float* __restrict__ sin_t, int64_t n_pos) {
+  const int half = rot / 2, per = half + (hd - rot);        // units of a head: pairs, then single values
+  const int64_t total = rows * heads * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / ((int64_t)heads * per);
+    const int u = (int)(i - row * heads * per), h = u / per, j = u - h * per;
+    const T* xr = x + row * ldx + (int64_t)h * hd;
+    T* yr = out + row * ldo + (int64_t)h * hd;
+    if (j >= half) {
+      if (out != x) yr[rot + j - half] = xr[rot + j - half];
+      continue;
+    }
+    int64_t p = pos ? pos[row] : row;
+    p = p < 0 ? 0 : (p >= n_pos ? n_pos - 1 : p);
+    const float c = cos_t[p * half + j], s = sin_t[p * half + j];
+    const int ja = layout == ZOACT_ROPE_HALF ? j : 2 * j, jb = layout == ZOACT_ROPE_HALF ? j + half : 2 * j + 1;
+    const float a = ld1(xr + ja), b = ld1(xr + jb);
+    st1(yr + ja, a * c - b * s);
+    st1(yr + jb, b * c + a * s);
+  }
+}
+
+// ---------------------------------------------------------------- attention, any shape
+// One wave a (row, head): 64 keys at a time, a key a lane for the scores and a column a lane for
+// the sums, with the running maximum m and sum l of the softmax.
+template <typename T>
+__global__ void __launch_bounds__(256) attention_packed_any(zoact_packed s, const T* __restrict__ q, int64_t ldq,
+                                                            const T* __restrict__ k, int64_t ldk,
+                                                            const T* __restrict__ v, int64_t ldv, int heads,
+                                                            int kv_heads, int hd, float scale, T* __restrict__ out) {
+  __shared__ float qs[4][256];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t total = s.rows * heads;
+  for (int64_t w0 = (int64_t)blockIdx.x * 4; w0 < total; w0 += (int64_t)gridDim.x * 4) {
+    const int64_t w = w0 + wave;
+    bool live = w < total;
+    const int row = live ? (int)(w / heads) : 0, h = live ? (int)(w - (int64_t)row * heads) : 0;
+    int b0 = 0;
+    if (live) {
+      const int i = packed_find(s.begin, s.n, row);
+      live = i >= 0 && i < s.n && row < s.begin[i + 1];
+      if (live) b0 = s.begin[i];
+      live = live && b0 >= 0;
+    }
+    __syncthreads();
+    if (live)
+      for (int d = lane; d < hd; d += 64) qs[wave][d] = ld1(q + (int64_t)row * ldq + (int64_t)h * hd + d);
+    __syncthreads();
+    if (!live) continue;
+    const int g = h / (heads / kv_heads);
+    const T* kp = k + (int64_t)g * hd;
+    const T* vp = v + (int64_t)g * hd;
+    // (-inf scores, which a formula's softmax gives weight 0, stay below every m)
+    float m = -3.4028235e38f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int key0 = b0; key0 <= row; key0 += 64) {
+      const int key = key0 + lane;
+      float sc = -INFINITY;
+      if (key <= row) {
+        const T* kr = kp + (int64_t)key * ldk;
+        float t = 0.f;
+        for (int d = 0; d < hd; ++d) t = fmaf(qs[wave][d], ld1(kr + d), t);
+        sc = t * scale;
+      }
+      float mx = sc == sc ? sc : -INFINITY;
+#pragma unroll
+      for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+      const float mn = fmaxf(m, mx);
+      const float p = key <= row ? expf(sc - mn) : 0.f, a = expf(m - mn);
+      m = mn;
+      l = l * a + p;
+      const int cnt = row - key0 + 1 < 64 ? row - key0 + 1 : 64;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= a;
+      for (int t = 0; t < cnt; ++t) {
+        const float pt = __shfl(p, t, 64);
+        const T* vr = vp + (int64_t)(key0 + t) * ldv;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (e * 64 + lane < hd) o[e] = fmaf(pt, ld1(vr + e * 64 + lane), o[e]);
+      }
+    }
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
+    T* op = out + (int64_t)row * heads * hd + (int64_t)h * hd;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e * 64 + lane < hd) st1(op + e * 64 + lane, o[e] / l);
+  }
+}
+
+}  // namespace
+}  // namespace zoact
+
+using namespace zoact;
+
+extern "C" zoact_status zoact_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, int32_t dtype, int64_t rows,
+                                      int32_t n_heads, int32_t head_dim, int32_t rot_dim, int32_t layout,
+                                      const int32_t* pos, const float* cos_t, const float* sin_t, int64_t n_pos,
+                                      zoact_stream stream) {
+  ZP_CHECK(dtype == ZOACT_F32 || dtype == ZOACT_BF16, "rope_at: dtype must be F32 or BF16");
+  ZP_CHECK(rows >= 0 && rows < (int64_t(1) << 31), "rope_at: rows outside [0, 2^31)");
+  ZP_CHECK(n_heads >= 1 && n_heads <= 65535 && head_dim >= 1 && head_dim <= 65535, "rope_at: bad heads");
+  ZP_CHECK(rot_dim >= 2 && rot_dim % 2 == 0 && rot_dim <= head_dim, "rope_at: rot_dim must be even, 2 .. head_dim");
+  ZP_CHECK(layout == ZOACT_ROPE_HALF || layout == ZOACT_ROPE_INTERLEAVED, "rope_at: unknown layout");
+  ZP_CHECK((x && out) || rows == 0, "rope_at: NULL pointer");
+  ZP_CHECK(cos_t && sin_t, "rope_at: NULL rotary table");
+  ZP_CHECK(n_pos >= 1, "rope_at: empty rotary table");
+  const int64_t width = (int64_t)n_heads * head_dim;
+  ZP_CHECK(ldx >= width && ldo >= width, "rope_at: heads exceed the row");
+  ZP_CHECK(out != x || ldo == ldx, "rope_at: in place with another row stride");
+  const size_t esize = dtype == ZOACT_F32 ? 4 : 2;
+  ZP_CHECK(aligned_to(x, esize) && aligned_to(out, esize), "rope_at: x and out must be aligned to their type");
+  ZP_CHECK(aligned_to(cos_t, 4) && aligned_to(sin_t, 4) && aligned_to(pos, 4),
+           "rope_at: tables and pos must be 4-byte aligned");
+  if (rows == 0) return ZOACT_OK;
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const int64_t units = rows * n_heads * (head_dim - rot_dim / 2), g = (units + 255) / 256;
+  const unsigned grid = (unsigned)(g < 65536 ? g : 65536);
+  if (dtype == ZOACT_BF16)
+    rope_at_kernel<uint16_t><<<grid, 256, 0, s>>>((const uint16_t*)x, ldx, (uint16_t*)out, ldo, rows, n_heads, head_dim,
+                                                  rot_dim, layout, pos, cos_t, sin_t, n_pos);
+  else
+    rope_at_kernel<float><<<grid, 256, 0, s>>>((const float*)x, ldx, (float*)out, ldo, rows, n_heads, head_dim, rot_dim,
+                                               layout, pos, cos_t, sin_t, n_pos);
+  return launched_or("rope_at");
+}
+
+extern "C" zoact_status zoact_attention_packed(const zoact_packed* s, const void* q, int64_t ldq, const void* k,
+                                               int64_t ldk, const void* v, int64_t ldv, int32_t n_heads,
+                                               int32_t n_kv_heads, int32_t head_dim, float scale, int32_t dtype,
+                                               void* out, zoact_stream stream) {
+  const zoact_status st = check_packed(s);
+  if (st != ZOACT_OK) return st;
+  ZP_CHECK(dtype == ZOACT_F32 || dtype == ZOACT_BF16, "attention_packed: dtype must be F32 or BF16");
+  ZP_CHECK(n_heads >= 1 && n_heads <= 65535 && n_kv_heads >= 1 && n_heads % n_kv_heads == 0,
+           "attention_packed: bad head grouping");
+  ZP_CHECK(head_dim >= 1 && head_dim <= 256, "attention_packed: head_dim outside [1, 256]");
+  ZP_CHECK(scale - scale == 0.f, "attention_packed: scale must be finite");
+  ZP_CHECK((q && k && v && out) || s->rows == 0, "attention_packed: NULL pointer");
+  const int64_t kvw = (int64_t)n_kv_heads * head_dim;
+  ZP_CHECK(ldq >= (int64_t)n_heads * head_dim && ldk >= kvw && ldv >= kvw,
+           "attention_packed: row strides smaller than the heads");
+  const size_t esize = dtype == ZOACT_F32 ? 4 : 2;
+  ZP_CHECK(aligned_to(q, esize) && aligned_to(k, esize) && aligned_to(v, esize) && aligned_to(out, esize),
+           "attention_packed: tensors must be aligned to their type");
+  if (s->rows == 0) return ZOACT_OK;
+  hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const int64_t waves = s->rows * n_heads, g = (waves + 3) / 4;
+  const unsigned grid = (unsigned)(g < (1 << 20) ? g : (1 << 20));
+  if (dtype == ZOACT_BF16)
+    attention_packed_any<uint16_t><<<grid, 256, 0, hs>>>(*s, (const uint16_t*)q, ldq, (const uint16_t*)k, ldk,
+                                                         (const uint16_t*)v, ldv, n_heads, n_kv_heads, head_dim, scale,
+                                                         (uint16_t*)out);
+  else
+    attention_packed_any<float><<<grid, 256, 0, hs>>>(*s, (const float*)q, ldq, (const float*)k, ldk, (const float*)v,
+                                                      ldv, n_heads, n_kv_heads, head_dim, scale, (float*)out);
+  return launched_or("attention_packed");
+}

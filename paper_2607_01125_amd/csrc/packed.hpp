@@ -1,0 +1,53 @@
+// What the kernels of packed sequences and of the beam search share (zoact_packed.h).
+#pragma once
+#include <string>
+
+#include "common.hpp"
+#include "zoact_packed.h"
+
+#define ZP_CHECK(cond, msg)                                 \
+  do {                                                      \
+    if (!(cond)) return zoact::set_error(ZOACT_E_INVALID, msg); \
+  } while (0)
+
+namespace zoact {
+
+inline bool aligned_to(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+inline zoact_status launched_or(const char* who) {
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return ZOACT_OK;
+  const std::string m = std::string(who) + ": " + hipGetErrorString(e);
+  return set_error(ZOACT_E_HIP, m.c_str());
+}
+
+inline zoact_status check_packed(const zoact_packed* s) {
+  ZP_CHECK(s && s->begin, "packed: NULL pointer");
+  ZP_CHECK(aligned_to(s->begin, 4), "packed: begin must be 4-byte aligned");
+  ZP_CHECK(s->n >= 1 && s->n <= (1 << 24), "packed: n outside [1, 2^24]");
+  // (a tile that begins in the last row still numbers its keys in 32 bits)
+  ZP_CHECK(s->rows >= 0 && s->rows <= (int64_t(1) << 31) - 1024, "packed: rows outside [0, 2^31 - 1024]");
+  ZP_CHECK(s->max_len >= 1, "packed: max_len must be at least 1");
+  return ZOACT_OK;
+}
+
+// The last i with begin[i] <= row, or -1: row's sequence if row < begin[i + 1].
+__device__ __forceinline__ int packed_find(const int32_t* __restrict__ begin, int n, int row) {
+  int lo = -1, hi = n;                  // begin[lo] <= row < begin[hi + 1], as far as they exist
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (begin[mid] <= row) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Whether row has a next row in its own sequence.
+__device__ __forceinline__ bool packed_has_next(const int32_t* __restrict__ begin, int n, int64_t rows, int row) {
+  const int i = packed_find(begin, n, row);
+  if (i < 0 || i >= n) return false;
+  const int64_t end = begin[i + 1];
+  return row + 1 < (end < rows ? end : rows);
+}
+
+}  // namespace zoact

@@ -2,8 +2,8 @@
 
 A Session holds the cache of a Decoder's layers and runs the unperturbed model (C as trained, no halves)
 over new tokens of any of its sequences: prompts in chunks, single tokens, or both in one call.  As in the
-decoder module, every operation of the forward is a libzoact call; this module lays out buffers and picks
-tokens from the logits.
+decoder module, every operation of the forward is a libzoact call, and so is a beam search's selection; this
+module lays out buffers and picks single candidates' tokens from the logits.
 
 Layers with INT4 weights run on zoact_linear_rows up to ROWS_MAX rows; larger chunks, and bf16 and fp32
 models, run the two-halves linears of the training forward with sign 0, the rows shared out over the
@@ -77,6 +77,11 @@ class Session:
         new = [self.lens[s] for s in src]
         for t, n in zip(dst, new):
             self.lens[t] = n
+
+    def _fork_beams(self, src: torch.Tensor, dst: torch.Tensor):
+        """fork of beams by device lists whose sources and destinations are of one length (the host's need no
+        change, and does not wait)."""
+        Z.cache_fork(self.cache, src, dst, self.cache_ws, self.status)
 
     def free(self, slots):
         """Empty the slots; pages that nobody else holds are free again."""
@@ -314,27 +319,37 @@ def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int
         raise ValueError("more beams than tokens")
     slots = list(range(n * beams))
     ses.fork([f for f in first for _ in range(beams)], slots)
-    score, tok = torch.log_softmax(logits, dim=1).topk(beams, dim=1)            # [n][beams]
-    done = tok == eos if eos is not None else torch.zeros_like(tok, dtype=torch.bool)
-    hist = tok[:, :, None]
-    for step in range(1, n_new):
-        if bool(done.all()):
+    ids = ses._slots(slots)
+    tok, src = torch.empty_like(ids), torch.empty_like(ids)
+    eos = eos if eos is not None and 0 <= eos < V else None
+    ws = torch.empty(Z.beam_workspace_bytes(n, beams, beams, V), dtype=torch.uint8, device=dev)
+    select = Z.beam_select if beams <= Z.BEAMS_MAX else _select_many
+    now, then = Z.Beams.alloc(n, 1, n_new, dev), Z.Beams.alloc(n, beams, n_new, dev)
+    for step in range(n_new):
+        select(logits, now, step, eos, then, tok, src, ws)
+        now, then = then, now if step else Z.Beams.alloc(n, beams, n_new, dev)
+        if step == n_new - 1 or (eos is not None and bool((tok == eos).all())):
             break
-        logits = ses.decode(slots, tok.reshape(-1).to(torch.int32).contiguous())
+        if step:
+            ses._fork_beams(src, ids)
+        logits = ses.decode(slots, tok)
         ses.check()
-        lp = torch.log_softmax(logits, dim=1).view(n, beams, V)
-        if eos is not None:       # an ended candidate goes on as it is
-            stay = torch.full((V,), -math.inf, device=dev)
-            stay[eos] = 0.0
-            lp = torch.where(done[:, :, None], stay, lp)
-        score, best = (score[:, :, None] + lp).view(n, -1).topk(beams, dim=1)
-        parent, tok = best // V, best % V
-        hist = torch.cat([hist.gather(1, parent[:, :, None].expand(-1, -1, hist.shape[2])), tok[:, :, None]], dim=2)
-        done = done.gather(1, parent)
-        if eos is not None:
-            done = done | (tok == eos)
-        src = (parent + torch.arange(n, device=dev)[:, None] * beams).reshape(-1).tolist()
-        if src != slots and step < n_new - 1:
-            ses.fork(src, slots)
-    best = hist[:, 0].tolist()
+    best = now.hist[:, 0, :step + 1].tolist()
     return [row[:row.index(eos)] if eos is not None and eos in row else row for row in best]
+
+
+def _select_many(logits, now: Z.Beams, length: int, eos: int | None, to: Z.Beams, tok, src, ws):
+    """beam_select for more candidates than it keeps."""
+    (n, _), b, V = now.score.shape, to.score.shape[1], logits.shape[1]
+    lp = torch.log_softmax(logits, dim=1).view(n, -1, V)
+    if eos is not None and length:            # an ended candidate goes on as it is
+        stay = torch.full((V,), -math.inf, device=logits.device)
+        stay[eos] = 0.0
+        lp = torch.where((now.hist[:, :, length - 1] == eos)[:, :, None], stay, lp)
+    score, best = (now.score[:, :, None] + lp).view(n, -1).topk(b, dim=1)
+    parent = best // V
+    to.score.copy_(score)
+    to.hist[:, :, :length] = now.hist[:, :, :length].gather(1, parent[:, :, None].expand(-1, -1, length))
+    to.hist[:, :, length] = best % V
+    tok.copy_((best % V).view(-1))
+    src.copy_((parent + torch.arange(n, device=best.device)[:, None] * b).view(-1))

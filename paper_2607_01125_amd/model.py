@@ -65,6 +65,28 @@ class Block:
     site: str
 
 
+@dataclass(frozen=True)
+class PackedBatch:
+    """Sequences of different lengths for Decoder.forward, losses, step, step_q and basis_init, packed one
+    behind the other: tokens int32 [T]; `seqs` their rows, `both` those of the two halves [2][T]; `pos` int32
+    [2 T], each row's token index."""
+    tokens: torch.Tensor
+    seqs: Z.Packed
+    both: Z.Packed
+    pos: torch.Tensor
+
+    @classmethod
+    def of(cls, sequences, device="cuda"):
+        """From sequences of token ids (lists or tensors, none empty)."""
+        ts = [torch.as_tensor(t, dtype=torch.int32, device="cpu").reshape(-1) for t in sequences]
+        if not ts or any(t.numel() < 1 for t in ts):
+            raise ValueError("expected sequences of at least one token")
+        lens = [t.numel() for t in ts]
+        pos = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens])
+        return cls(torch.cat(ts).to(device), Z.Packed.of(lens, device), Z.Packed.of(lens + lens, device),
+                   torch.cat([pos, pos]).to(device))
+
+
 def arena_layout(shape) -> list:
     d, dkv, ff, r = shape.d_model, shape.n_kv_heads * shape.head_dim, shape.d_ff, shape.rank
     ad = set(shape.adapted)
@@ -190,6 +212,7 @@ class Decoder:
         self.loss_ws = torch.empty(Z.loss_workspace_bytes(), dtype=torch.uint8, device=self.dev)
         self._proj_ws = None     # the depth-split projection's partial sums (grown on demand)
         self._bufs = {}
+        self._packed_T = 0       # rows a half that the buffers of packed batches hold
         self._rope = {}
         self._ch = self._ch_all = None   # per-step C +/- eps Z of the whole arena (bf16 modes)
         # the perturbation the last update pass wrote into _ch_all for the next step:
@@ -326,14 +349,21 @@ class Decoder:
         self._bufs[key] = B
         return B
 
+    def _packed_buffers(self, T: int):
+        """The same for two halves of T packed rows: the beginning of one set, kept for the most rows so far
+        (batches of packed sequences are hardly ever of one size)."""
+        if self._packed_T < T:
+            self._bufs.pop((1, self._packed_T), None)
+            self._packed_T = -(-T // 256) * 256
+        B = self._buffers(1, self._packed_T)
+        return {k: None if v is None else v[:2 * T] for k, v in B.items()}
+
     def _rope_tables(self, seq: int):
+        """Tables of the positions below seq; shape.extra["rope"] (a dict) holds rope_tables' arguments of a model
+        with scaled positions."""
         if seq not in self._rope:
-            half = self.hd // 2
-            j = torch.arange(half, dtype=torch.float64)
-            inv = self.s.rope_theta ** (-2.0 * j / self.hd)
-            ang = torch.arange(seq, dtype=torch.float64)[:, None] * inv[None, :]
-            self._rope[seq] = (torch.cos(ang).float().to(self.dev).contiguous(),
-                               torch.sin(ang).float().to(self.dev).contiguous())
+            self._rope[seq] = Z.rope_tables(seq, self.hd, self.s.rope_theta, self.dev,
+                                            **getattr(self.s, "extra", {}).get("rope", {}))
         return self._rope[seq]
 
     # ---------------------------------------------------------------- forward of both halves
@@ -403,20 +433,28 @@ class Decoder:
                 and 8 <= self.r <= 32 and self.r % 8 == 0 and lin.d_in % 64 == 0 and lin.d_in >= 128
                 and lin.plain[0] == lin.plain[1])
 
-    def forward(self, tokens: torch.Tensor, pert: Z.Pert | Z.PertPair, *, calibrate=None, distinct_halves=False,
-                head: bool = True):
+    def forward(self, tokens: torch.Tensor | PackedBatch, pert: Z.Pert | Z.PertPair, *, calibrate=None,
+                distinct_halves=False, head: bool = True):
         """Both halves of the forward; logits fp32 [2][n_seq][seq][V] in the buffer set.
 
-        tokens int32 [n_seq][seq] (or [2][n_seq][seq] with distinct_halves).  With a Pert,
+        tokens int32 [n_seq][seq] (or [2][n_seq][seq] with distinct_halves), or a PackedBatch of T rows
+        (logits [2][T][V]).  With a Pert,
         half 0 uses C + eps Z and half 1 C - eps Z; with a PertPair, half h uses
         C + sign[h] eps Z(query[h]).  With `calibrate` (a callable taking (layer, site, x))
         the linears are not adapted and each site's input [2 T][d_in] is handed over
         before it is consumed (Algorithm 1's calibration forward).
         """
         s = self.s
-        n_seq, seq = tokens.shape[-2], tokens.shape[-1]
-        T = n_seq * seq
-        B = self._cur = self._buffers(n_seq, seq)
+        packed = tokens if isinstance(tokens, PackedBatch) else None
+        if packed is not None:
+            if distinct_halves:
+                raise ValueError("a packed batch has the same tokens in both halves")
+            T = packed.seqs.rows
+            B = self._cur = self._packed_buffers(T)
+        else:
+            n_seq, seq = tokens.shape[-2], tokens.shape[-1]
+            T = n_seq * seq
+            B = self._cur = self._buffers(n_seq, seq)
         adapt = calibrate is None
         # C +/- eps Z for the whole arena in one streaming pass; every adapted GEMM reads its
         # slice instead of regenerating Z per workgroup
@@ -429,9 +467,14 @@ class Decoder:
                 Z.perturb_coeffs(self.arena, 0, self.k, pert, self._ch_all)
             self._ch = self._ch_all
         self._ch_next = None
-        Z.embed(tokens, self.emb, B["h0"], seq, self.pos, pos_offset=2, distinct_halves=distinct_halves)
+        if packed is None:
+            Z.embed(tokens, self.emb, B["h0"], seq, self.pos, pos_offset=2, distinct_halves=distinct_halves)
+            positions = seq
+        else:
+            self._embed_packed(packed, B)
+            positions = -(-packed.seqs.max_len // 256) * 256      # (few tables for batches of many lengths)
         h, h_alt = B["h0"], B["h1"]
-        cos_sin = self._rope_tables(seq) if s.family == "llama" else None
+        cos_sin = self._rope_tables(positions) if s.family == "llama" else None
         d, dkv, H, Hkv, hd = self.d, self.dkv, self.H, self.Hkv, self.hd
         scale = float(np.float32(1.0 / math.sqrt(hd)))
         for l, P in enumerate(self.layers):
@@ -457,7 +500,11 @@ class Decoder:
                 self._apply(P["qv"], B["a"], T, qkv, pert, ut, adapt=adapt)
                 self._apply(P["k"], B["a"], T, B["k"], pert, None, adapt=False)
                 q, k, v = qkv[:, :d], B["k"], qkv[:, d:]
-            if cos_sin is not None:
+            if packed is not None:
+                if cos_sin is not None:
+                    self._rope_packed(qkv, None if "qkv" in P else k, packed.pos, cos_sin)
+                Z.attention_packed(packed.both, q, k, v, B["att"], H, Hkv, hd, scale)
+            elif cos_sin is not None:
                 # rotary on q and k, inside the attention where it holds the sequence in LDS
                 Z.attention_rope(q, k, v, B["att"], 2 * n_seq, seq, H, Hkv, hd, scale, *cos_sin)
             else:
@@ -478,7 +525,26 @@ class Decoder:
         if B["logits"] is None:
             B["logits"] = torch.empty(2 * T, s.vocab, dtype=torch.float32, device=self.dev)
         Z.linear_fwd_pm(self.head, None, B["a"], T, None, B["logits"], pert)
-        return B["logits"].view(2, n_seq, seq, s.vocab)
+        return B["logits"].view(2, T, s.vocab) if packed is not None else B["logits"].view(2, n_seq, seq, s.vocab)
+
+    def _embed_packed(self, batch: PackedBatch, B: dict):
+        """Token (and learned position) embeddings of a packed batch into both halves of B["h0"]."""
+        T = batch.seqs.rows
+        if self.pos is None:
+            Z.embed(batch.tokens, self.emb, B["h0"], T)
+            return
+        # the rows' positions, looked up first (learned positions start at row 2 of their table), stand in
+        # for a position table of T rows
+        Z.embed(batch.pos[:T] + 2, self.pos, B["h1"], T)
+        Z.embed(batch.tokens, self.emb, B["h0"], T, B["h1"][:T], pos_offset=0)
+
+    def _rope_packed(self, qkv, k, pos, cos_sin):
+        """Rotary in place on a packed batch's queries and keys, which lie side by side unless k is apart."""
+        width = self.d if k is not None else self.d + self.dkv
+        x = qkv[:, :width]
+        Z.rope_at(x, x, width // self.hd, self.hd, pos, *cos_sin)
+        if k is not None:
+            Z.rope_at(k, k, self.Hkv, self.hd, pos, *cos_sin)
 
     def _site(self, l, site, x, adapt, calibrate, rows=None):
         """U^T of an adapted site after projecting its input into P (None if not adapted), in the
@@ -508,7 +574,7 @@ class Decoder:
                    report=False, concurrency: int = 4):
         """Unperturbed calibration forward, then the top-r basis of each adapted site's inputs.
 
-        calib_tokens int32 [n_seq][seq] with n_seq even: the two halves of the stacked
+        calib_tokens: a PackedBatch, or int32 [n_seq][seq] with n_seq even: the two halves of the stacked
         forward carry the first and second n_seq/2 sequences, so every site sees all
         n_seq * seq calibration tokens once.  With `report` each site's convergence report
         (residual, gap theta_r / theta_{r+1}, iterations, converged) lands in
@@ -521,8 +587,8 @@ class Decoder:
         checks wait on the host, so one site leaves most of the GPU idle).  Every site's
         result is the same as when solved alone.  1 solves each site inside the forward.
         """
-        n_seq, seq = calib_tokens.shape
-        if n_seq % 2:
+        packed = isinstance(calib_tokens, PackedBatch)
+        if not packed and calib_tokens.shape[0] % 2:
             raise ValueError("the calibration batch needs an even number of sequences")
         dims = self.site_dims()
         nws = max(Z.basis_init_workspace_bytes(dd, self.r, opts) for dd in set(dims.values()))
@@ -542,14 +608,16 @@ class Decoder:
                 reps[key] = rep
             return ut, ev, rep
 
-        tok = calib_tokens.reshape(2, n_seq // 2, seq).contiguous()
+        # (both halves of a packed batch are its tokens: the first half's rows are the calibration's)
+        rows = slice(0, calib_tokens.seqs.rows if packed else None)
+        tok = calib_tokens if packed else calib_tokens.reshape(2, calib_tokens.shape[0] // 2, -1).contiguous()
         if k == 1:
             def hook(l, site, x):
                 if (l, site) in dims:
                     ut, ev, rep = outputs((l, site))
-                    Z.basis_init(x, self.r, ut, wss[0], opts, eigvals=ev, report=rep)
+                    Z.basis_init(x[rows], self.r, ut, wss[0], opts, eigvals=ev, report=rep)
 
-            self.forward(tok, Z.Pert(0, 0, 0, 0.0), calibrate=hook, distinct_halves=True)
+            self.forward(tok, Z.Pert(0, 0, 0, 0.0), calibrate=hook, distinct_halves=not packed)
         else:
             streams = [torch.cuda.Stream(device=self.dev) for _ in range(k)]
             idle = queue.SimpleQueue()
@@ -574,13 +642,13 @@ class Decoder:
                 def hook(l, site, x):
                     if (l, site) not in dims:
                         return
-                    xc = x.clone()
+                    xc = x[rows].clone()
                     out = outputs((l, site))
                     ready = torch.cuda.Event()
                     ready.record()
                     futures.append(pool.submit(work, xc, out, ready))
 
-                self.forward(tok, Z.Pert(0, 0, 0, 0.0), calibrate=hook, distinct_halves=True)
+                self.forward(tok, Z.Pert(0, 0, 0, 0.0), calibrate=hook, distinct_halves=not packed)
                 for f in futures:
                     f.result()
             for st in streams:
@@ -599,13 +667,19 @@ class Decoder:
     def _loss_pair(self, tokens: torch.Tensor, pert, out: torch.Tensor):
         """Forward both halves and write their next-token cross entropies into out[0:2]; in
         bf16 modes the LM head and the loss run fused (logits not stored)."""
+        packed = isinstance(tokens, PackedBatch)
         if self.act == torch.bfloat16:
             a = self.forward(tokens, pert, head=False)
-            T = tokens.numel()
+            T = tokens.seqs.rows if packed else tokens.numel()
             need = Z.linear_xent_workspace_bytes(T, self.s.vocab)
             if getattr(self, "_xent_ws", None) is None or self._xent_ws.numel() < need:
                 self._xent_ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
-            Z.linear_xent(self.head, None, a, tokens, None, pert, out, self._xent_ws)
+            if packed:
+                Z.linear_xent_packed(self.head, None, a, tokens.tokens, tokens.seqs, None, pert, out, self._xent_ws)
+            else:
+                Z.linear_xent(self.head, None, a, tokens, None, pert, out, self._xent_ws)
+        elif packed:
+            Z.xent_packed(self.forward(tokens, pert), tokens.tokens, tokens.seqs, out, self.loss_ws)
         else:
             self.forward(tokens, pert)
             Z.xent_pm(self._cur["logits"], tokens, out, self.loss_ws)

@@ -45,6 +45,19 @@ def pert_pair(seed: int, step: int, queries, signs, eps: float) -> PertPair:
     return PertPair(seed, step, (ctypes.c_uint32 * 2)(*queries), (ctypes.c_int32 * 2)(*signs), eps)
 
 
+class PackedDesc(ctypes.Structure):
+    _fields_ = [("begin", ctypes.c_void_p), ("n", ctypes.c_int32), ("rows", ctypes.c_int64),
+                ("max_len", ctypes.c_int64)]
+
+
+class BeamsDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32), ("beams_in", ctypes.c_int32), ("beams", ctypes.c_int32), ("eos", ctypes.c_int32),
+                ("vocab", ctypes.c_int64), ("length", ctypes.c_int64), ("score", ctypes.c_void_p),
+                ("hist", ctypes.c_void_p), ("ld_hist", ctypes.c_int64), ("score_out", ctypes.c_void_p),
+                ("hist_out", ctypes.c_void_p), ("ld_hist_out", ctypes.c_int64), ("token", ctypes.c_void_p),
+                ("src", ctypes.c_void_p)]
+
+
 class LinearDesc(ctypes.Structure):
     _fields_ = [("w_dtype", ctypes.c_int32), ("w", ctypes.c_void_p), ("w_scales", ctypes.c_void_p),
                 ("bias", ctypes.c_void_p), ("ut", ctypes.c_void_p), ("d_in", ctypes.c_int64),
@@ -162,6 +175,14 @@ SIGNATURES = {
     "zoact_attention_rope_in_place": ([_I64, _I64, _I32, _I32, _I32, _I32], _I32),
     "zoact_attention_rope": ([_P, _I64, _P, _I64, _P, _I64, _I64, _I64, _I32, _I32, _I32, _F, _I32, _P, _P, _P, _P],
                              _I32),
+    "zoact_attention_packed": ([ctypes.POINTER(PackedDesc), _P, _I64, _P, _I64, _P, _I64, _I32, _I32, _I32, _F, _I32,
+                                _P, _P], _I32),
+    "zoact_rope_at": ([_P, _I64, _P, _I64, _I32, _I64, _I32, _I32, _I32, _I32, _P, _P, _P, _I64, _P], _I32),
+    "zoact_xent_packed": ([_P, _P, ctypes.POINTER(PackedDesc), _I64, _P, _P, _SZ, _P], _I32),
+    "zoact_linear_xent_packed": ([ctypes.POINTER(LinearDesc), ctypes.POINTER(ArenaDesc), _P, ctypes.POINTER(PackedDesc),
+                                  _P, ctypes.POINTER(PertPair), _P, _P, _P, _SZ, _P], _I32),
+    "zoact_beam_workspace_bytes": ([_I32, _I32, _I32, _I64], _SZ),
+    "zoact_beam_select": ([ctypes.POINTER(BeamsDesc), _P, _I64, _I32, _P, _SZ, _P], _I32),
 }
 
 _lib = None
@@ -817,3 +838,160 @@ def attention_cache(cache: Cache, layer: int, q: torch.Tensor, out: torch.Tensor
     op = _arg(out, "out", out.dtype, dev, (batch.rows, n_heads * hd))
     _on_device(lib().zoact_attention_cache, dev, stream, ref, layer, qp, ldq, dtype_code(out), n_heads,
                batch.ref(dev), scale, max_len, *_rope_args(rope, dev, hd), op, *_ws(ws, dev))
+
+
+# ---------------------------------------------------------------- packed sequences (zoact_packed.h)
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+BEAMS_MAX = 64
+
+
+@dataclass(frozen=True)
+class Packed:
+    """Sequences packed one behind the other: sequence i is rows begin[i] .. begin[i + 1] - 1 of tensors of
+    `rows` rows (begin int32 [n + 1], ascending, on the device); max_len: a length that none is expected to
+    pass.  Checked here, and again where `begin` has other memory."""
+    begin: torch.Tensor
+    rows: int
+    max_len: int
+
+    def __post_init__(self):
+        b = self.begin
+        if b.dim() != 1 or b.numel() < 2:
+            raise ValueError("packed: begin must be a list of n + 1 rows, n >= 1")
+        dev = _device(b)
+        d = PackedDesc(_arg(b, "begin", torch.int32, dev), b.numel() - 1, self.rows, max(int(self.max_len), 1))
+        object.__setattr__(self, "index", dev)
+        object.__setattr__(self, "_place", d.begin)
+        object.__setattr__(self, "_kept", ctypes.byref(d))
+
+    def __reduce__(self):               # (a copy is checked anew)
+        return Packed, (self.begin, self.rows, self.max_len)
+
+    @property
+    def _ref(self):
+        if self._place != self.begin.data_ptr():
+            self.__post_init__()
+        return self._kept
+
+    @classmethod
+    def of(cls, lengths, device="cuda"):
+        """The sequences of these lengths, one behind the other from row 0 on."""
+        lengths = [int(x) for x in lengths]
+        if not lengths or min(lengths) < 0:
+            raise ValueError("packed: expected lengths of 0 or more")
+        begin = [0]
+        for x in lengths:
+            begin.append(begin[-1] + x)
+        return cls(torch.tensor(begin, dtype=torch.int32, device=device), begin[-1], max(lengths))
+
+
+def attention_packed(seqs: Packed, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, n_heads: int,
+                     n_kv_heads: int, head_dim: int, scale: float, stream=None):
+    """Causal attention within each sequence; q, k, v may be column slices of wider row-major buffers."""
+    dev, dt, rows = seqs.index, out.dtype, seqs.rows
+    qp, ldq = _heads_arg(q, "q", dt, dev, rows, n_heads * head_dim)
+    kp, ldk = _heads_arg(k, "k", dt, dev, rows, n_kv_heads * head_dim)
+    vp, ldv = _heads_arg(v, "v", dt, dev, rows, n_kv_heads * head_dim)
+    op = _arg(out, "out", dt, dev, (rows, n_heads * head_dim))
+    _on_device(lib().zoact_attention_packed, dev, stream, seqs._ref, qp, ldq, kp, ldk, vp, ldv, n_heads, n_kv_heads,
+               head_dim, scale, dtype_code(out), op)
+
+
+def rope_at(x: torch.Tensor, out: torch.Tensor, n_heads: int, head_dim: int, pos: torch.Tensor | None,
+            cos_t: torch.Tensor, sin_t: torch.Tensor, layout: int = ROPE_HALF, stream=None):
+    """out = x with the first 2 * cos_t.shape[1] values of each head turned to the rows' positions pos (None:
+    their indexes); x and out [rows][n_heads * head_dim] may be column slices, and the same one."""
+    dev, dt, f32 = _device(x), x.dtype, torch.float32
+    rows = x.shape[0] if x.dim() == 2 else -1
+    xp, ldx = _heads_arg(x, "x", dt, dev, rows, n_heads * head_dim)
+    op, ldo = _heads_arg(out, "out", dt, dev, rows, n_heads * head_dim)
+    if cos_t.dim() != 2:
+        raise ValueError("rope_at: tables must be [n_pos][rot_dim / 2]")
+    cp, sp = _arg(cos_t, "cos", f32, dev), _arg(sin_t, "sin", f32, dev, cos_t.shape)
+    _on_device(lib().zoact_rope_at, dev, stream, xp, ldx, op, ldo, dtype_code(x), rows, n_heads, head_dim,
+               2 * cos_t.shape[1], layout, _arg(pos, "pos", torch.int32, dev, (rows,)), cp, sp, cos_t.shape[0])
+
+
+def rope_tables(n_pos: int, rot_dim: int, theta: float, device="cuda", *, factor: float = 1.0, original: int = 0,
+                low: float = 1.0, high: float = 1.0, magnitude: float = 1.0):
+    """Rotary tables (cos, sin), fp32 [n_pos][rot_dim / 2], of positions 0 .. n_pos - 1, in fp64 and rounded once.
+
+    Pair j turns by f_j = theta^(-2 j / rot_dim) a position.  For contexts longer than a model was trained on:
+    with `factor` > 1 all pairs turn `factor` times slower, except, with the trained length `original`, those
+    that turn often within it: with n_j = original f_j / 2 pi turns, pairs of n_j <= low are slowed, of
+    n_j >= high left as they are, and between the two g_j = (n_j - low) / (high - low) joins them,
+    f_j ((1 - g_j) / factor + g_j).  `magnitude` multiplies both tables."""
+    if n_pos < 1 or rot_dim < 2 or rot_dim % 2 or factor <= 0 or original < 0 or not low <= high:
+        raise ValueError("rope_tables: expected n_pos >= 1, rot_dim even, factor > 0 and low <= high")
+    f = theta ** (-2.0 * torch.arange(rot_dim // 2, dtype=torch.float64) / rot_dim)
+    if factor != 1.0:
+        g = torch.zeros_like(f)
+        if original:
+            turns = original * f / (2.0 * math.pi)
+            g = ((turns - low) / (high - low)).clamp(0.0, 1.0) if high > low else (turns >= high).double()
+        f = f * ((1.0 - g) / factor + g)
+    ang = torch.arange(n_pos, dtype=torch.float64)[:, None] * f[None, :]
+    table = lambda t: (t * magnitude).float().to(device).contiguous()
+    return table(torch.cos(ang)), table(torch.sin(ang))
+
+
+def linear_xent_packed(layer: Linear, arena: Arena | None, x: torch.Tensor, tokens: torch.Tensor, seqs: Packed,
+                       p: torch.Tensor | None, pert: Pert | PertPair, loss_pm: torch.Tensor, ws: torch.Tensor,
+                       stream=None):
+    """LM head of both halves (x [2][rows][d_in]) with the next-token cross entropy of packed rows in its
+    epilogue; tokens int32 [rows]; ws of linear_xent_workspace_bytes(rows, vocab)."""
+    dev, rows = seqs.index, seqs.rows
+    d = layer.desc()
+    a = arena.desc() if arena is not None else None
+    xp = _arg(x.reshape(-1, layer.d_in) if x.is_contiguous() else x, "x", torch.bfloat16, dev, (2 * rows, layer.d_in))
+    pp = _arg(p.reshape(-1, layer.r) if p.is_contiguous() else p, "p", torch.bfloat16, dev,
+              (2 * rows, layer.r)) if layer.r else None
+    _on_device(lib().zoact_linear_xent_packed, dev, stream, ctypes.byref(d), ctypes.byref(a) if a is not None else None,
+               xp, seqs._ref, pp, ctypes.byref(as_pair(pert)), _arg(tokens, "tokens", torch.int32, dev, (rows,)),
+               _arg(loss_pm, "loss_pm", torch.float32, dev, (2,)), *_ws(ws, dev))
+
+
+def xent_packed(logits: torch.Tensor, tokens: torch.Tensor, seqs: Packed, loss_pm: torch.Tensor, ws: torch.Tensor,
+                stream=None):
+    """Next-token cross entropy of both halves over packed rows, from logits fp32 [2][rows][vocab]."""
+    dev, rows, f32 = seqs.index, seqs.rows, torch.float32
+    if logits.dim() != 3:
+        raise ValueError("xent_packed: logits must be [2][rows][vocab]")
+    lp = _arg(logits, "logits", f32, dev, (2, rows, logits.shape[2]))
+    _on_device(lib().zoact_xent_packed, dev, stream, lp, _arg(tokens, "tokens", torch.int32, dev, (rows,)), seqs._ref,
+               logits.shape[2], _arg(loss_pm, "loss_pm", f32, dev, (2,)), *_ws(ws, dev))
+
+
+@dataclass(frozen=True)
+class Beams:
+    """Candidates of a beam search: summed log probabilities fp32 [n][beams] and tokens int32
+    [n][beams][room]."""
+    score: torch.Tensor
+    hist: torch.Tensor
+
+    @classmethod
+    def alloc(cls, n: int, beams: int, room: int, device="cuda"):
+        return cls(torch.zeros(n, beams, dtype=torch.float32, device=device),
+                   torch.zeros(n, beams, room, dtype=torch.int32, device=device))
+
+
+def beam_workspace_bytes(n: int, beams_in: int, beams: int, vocab: int) -> int:
+    return int(lib().zoact_beam_workspace_bytes(n, beams_in, beams, vocab))
+
+
+def beam_select(logits: torch.Tensor, now: Beams, length: int, eos: int | None, to: Beams, token: torch.Tensor | None,
+                src: torch.Tensor | None, ws: torch.Tensor, stream=None):
+    """Keep the likeliest candidates of each prompt in `to`, of those in `now` (with `length` tokens each) continued
+    by every token; logits [n * beams][vocab] (rows may be apart).  token, src int32 [n * beams of `to`]: the
+    kept tokens, and the slots prompt * beams + beam that they continue."""
+    dev, i32 = _device(logits), torch.int32
+    if now.score.dim() != 2 or to.score.dim() != 2 or now.hist.dim() != 3 or to.hist.dim() != 3 or logits.dim() != 2:
+        raise ValueError("beam_select: expected scores [n][beams], hist [n][beams][room] and logits [rows][vocab]")
+    (n, bi), b, V = now.score.shape, to.score.shape[1], logits.shape[1]
+    lp, ldl = _heads_arg(logits, "logits", logits.dtype, dev, n * bi, V)
+    d = BeamsDesc(n, bi, b, -1 if eos is None else eos, V, length, _arg(now.score, "score", torch.float32, dev),
+                  _arg(now.hist, "hist", i32, dev, (n, bi, now.hist.shape[2])), now.hist.shape[2],
+                  _arg(to.score, "to.score", torch.float32, dev, (n, b)),
+                  _arg(to.hist, "to.hist", i32, dev, (n, b, to.hist.shape[2])), to.hist.shape[2],
+                  _arg(token, "token", i32, dev, (n * b,)), _arg(src, "src", i32, dev, (n * b,)))
+    _on_device(lib().zoact_beam_select, dev, stream, ctypes.byref(d), lp, ldl, dtype_code(logits), *_ws(ws, dev))
