@@ -164,6 +164,10 @@ extern "C" zoact_status zoact_attention_packed(const zoact_packed* s, const void
            "attention_packed: tensors must be aligned to their type");
   if (s->rows == 0) return ZOACT_OK;
   hipStream_t hs = reinterpret_cast<hipStream_t>(stream);
+  const hipError_t e = launch_attention_packed(*s, q, ldq, k, ldk, v, ldv, n_heads, n_kv_heads, head_dim, scale, dtype,
+                                               out, hs);
+  if (e == hipSuccess) return ZOACT_OK;
+  if (e != hipErrorNotSupported) return set_error(ZOACT_E_HIP, hipGetErrorString(e));
   const int64_t waves = s->rows * n_heads, g = (waves + 3) / 4;
   const unsigned grid = (unsigned)(g < (1 << 20) ? g : (1 << 20));
   if (dtype == ZOACT_BF16)

@@ -31,6 +31,11 @@ inline zoact_status check_packed(const zoact_packed* s) {
   return ZOACT_OK;
 }
 
+// Matrix-core form of zoact_attention_packed; hipErrorNotSupported outside its shapes.
+hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                                   const void* v, int64_t ldv, int32_t heads, int32_t kv_heads, int32_t hd, float scale,
+                                   int32_t dtype, void* out, hipStream_t hs);
+
 // The last i with begin[i] <= row, or -1: row's sequence if row < begin[i + 1].
 __device__ __forceinline__ int packed_find(const int32_t* __restrict__ begin, int n, int row) {
   int lo = -1, hi = n;                  // begin[lo] <= row < begin[hi + 1], as far as they exist
