@@ -80,8 +80,10 @@ struct Tile {
   static constexpr int BYTES = KT * ROW;
   static constexpr int PER = KT * CH / 256;                  // 16-byte chunks a thread of K, and of V
   static constexpr int NB = HD / 32;                         // 32-column blocks of O
-  __device__ static int kswz(int row) { return CH >= 8 ? row & (CH - 1) : (row >> 1) & 3; }
-  __device__ static int vswz(int row) { return !BF ? 0 : CH >= 8 ? (row & 3) << 1 : ((row >> 1) & 1) << 1; }
+  // Chunk c of a row lies at c ^ swz(row): the 16 lanes of a read of K's chunk (rows in turn), and the
+  // lanes of a transposed read of V (4 rows of 64 bytes), then cover all banks (256 bytes) once.
+  __device__ static int kswz(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
+  __device__ static int vswz(int row) { return !BF ? 0 : CH == 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
 };
 
 template <typename T, int HD, int QB>
@@ -93,8 +95,9 @@ __global__ void __launch_bounds__(256, QB == 1 ? 2 : 1)
   constexpr bool BF = C::BF;
   constexpr int KT = C::KT, SUBS = C::SUBS, ROW = C::ROW, CH = C::CH, PER = C::PER, NB = C::NB;
   constexpr int QF = BF ? HD / 16 : HD / 8;                  // 16-byte pieces of a lane's query
-  __shared__ __align__(16) char tile[2][2][C::BYTES];        // [buffer][K, V]
-  __shared__ T pw[4][32][34];                                // a wave's probabilities for the vector product
+  // (arrays of their own, so that a read of one does not wait for the loads into another)
+  __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
+  __shared__ T pw[4][32][32];                                // a wave's probabilities for the vector product
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
             lh = lane >> 5;
   const int hgs = heads / gh, R = (4 / gh) * 32 * QB;
@@ -122,36 +125,34 @@ __global__ void __launch_bounds__(256, QB == 1 ? 2 : 1)
   }
   const float c2 = fabsf(scale) * 1.4426950408889634f;
 
-  // tiles: global -> registers while the one before is multiplied -> LDS
-  u32x4 kr[PER], vr[PER];
+  // Tiles go from global memory straight to LDS, a wave's 64 chunks side by side; the swizzle is in the
+  // choice of each lane's chunk.  Rows past the sequence read as its last.
   const int row_t = threadIdx.x / CH, ch_t = threadIdx.x % CH;
-  const int64_t kstep = ldk * (int64_t)sizeof(T), vstep = ldv * (int64_t)sizeof(T);
+  const int kstep = (int)(ldk * (int64_t)sizeof(T)), vstep = (int)(ldv * (int64_t)sizeof(T));
   const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
   const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
-  auto rows_of = [&](const char* p, int64_t step, int t) {   // descriptor of a tile's rows: what is past the
-    const int left = len - t * KT;                           // sequence reads as zeros
-    const uint64_t a = reinterpret_cast<uint64_t>(p + (int64_t)t * KT * step);
+  auto load = [&](const char* from, int step, int (*swz)(int), char* to, int t) {
+    typedef __attribute__((address_space(3))) void lds_t;
+    const int left = len - t * KT < KT ? len - t * KT : KT;
+    const uint64_t a = reinterpret_cast<uint64_t>(from + (int64_t)t * KT * step);
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0,
-                                             ((left < KT ? left : KT) - 1) * (int)step + ROW, 0x00020000);
-  };
-  const int ko = row_t * (int)kstep + ch_t * 16, vo = row_t * (int)vstep + ch_t * 16;
-  auto fetch = [&](int t) {
-    const __amdgpu_buffer_rsrc_t ks = rows_of(kb, kstep, t), vs = rows_of(vb, vstep, t);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + ROW, 0x00020000);
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      kr[u] = __builtin_amdgcn_raw_buffer_load_b128(ks, ko + u * (256 / CH) * (int)kstep, 0, 0);
-      vr[u] = __builtin_amdgcn_raw_buffer_load_b128(vs, vo + u * (256 / CH) * (int)vstep, 0, 0);
+      int row = row_t + u * (256 / CH);
+      const int chunk = ch_t ^ swz(row);
+      row = row < left ? row : left - 1;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, row * step + chunk * 16, 0,
+                                               0, 0);
     }
   };
-  auto stage = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int row = row_t + u * (256 / CH);
-      *reinterpret_cast<u32x4*>(tile[buf][0] + row * ROW + (ch_t ^ C::kswz(row)) * 16) = kr[u];
-      *reinterpret_cast<u32x4*>(tile[buf][1] + row * ROW + (ch_t ^ C::vswz(row)) * 16) = vr[u];
-    }
+  auto load_k = [&](char* to, int t) { load(kb, kstep, C::kswz, to, t); };
+  auto load_v = [&](char* to, int t) { load(vb, vstep, C::vswz, to, t); };
+  auto arrived = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's part; then everybody's
+    __syncthreads();
   };
 
   floatx16 o[QB][NB];
@@ -191,9 +192,14 @@ __global__ void __launch_bounds__(256, QB == 1 ? 2 : 1)
       }
     }
   };
-  // the maximum of a block's rows over both halves moves m where it has to
+  // a row's maximum over both halves of the wave
+  auto both = [&](float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  };
+  // moves m where the maximum mx of the coming scores has passed it
   auto follow = [&](int b, float mx) {
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+    mx *= c2;
     if (__ballot(mx > m[b] + 8.f)) {
       const float mn = fmaxf(m[b], mx), a = __builtin_amdgcn_exp2f(m[b] - mn);
       m[b] = mn;
@@ -277,16 +283,16 @@ __global__ void __launch_bounds__(256, QB == 1 ? 2 : 1)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int key = 8 * (i / 4) + 4 * lh + i % 4;
-      if constexpr (BF) pw[wave][lq][key] = f2bf(st[i]);
-      else pw[wave][lq][key] = st[i];
+      if constexpr (BF) pw[wave][lq][key ^ lq] = f2bf(st[i]);
+      else pw[wave][lq][key ^ lq] = st[i];
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
     for (int t = 0; t < 32; ++t) {
       const int row = sub * 32 + t;
       float p;
-      if constexpr (BF) p = bf2f(pw[wave][lq][t]);
-      else p = pw[wave][lq][t];
+      if constexpr (BF) p = bf2f(pw[wave][lq][t ^ lq]);
+      else p = pw[wave][lq][t ^ lq];
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -301,61 +307,99 @@ __global__ void __launch_bounds__(256, QB == 1 ? 2 : 1)
     }
   };
 
-  fetch(0);
-  stage(0);
-  __syncthreads();
-  for (int t = 0; t < n_tiles; ++t) {
-    if (t + 1 < n_tiles) fetch(t + 1);
-    const char* const kt = tile[t & 1][0];
-    const char* const vt = tile[t & 1][1];
-    const int s0 = t * SUBS, d0 = w0 / 32;                   // sub-tiles d0 + b are the blocks' diagonals
-    if (s0 + SUBS <= d0) {
-      floatx16 st[SUBS][QB];
+  const int d0 = w0 / 32;                                    // sub-tiles d0 + b are the blocks' diagonals
+  const int n_full = pl.q0 / KT;                             // tiles that every row of the workgroup sees
+  floatx16 st[SUBS][QB];
+  float mx[QB];
+  auto maxima = [&] {
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) scores(kt, u, st[u]);
+    for (int b = 0; b < QB; ++b) {
+      mx[b] = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx[b] = fmaxf(mx[b], st[u][b][i]);
+      mx[b] = both(mx[b]);
+    }
+  };
+  // One tile t: its scores are in st; the next one's are formed while these become probabilities, then
+  // the product with V, the next maxima under it.  K of t + 2 and V of t + 1 are on their way meanwhile.
+  auto full = [&](char* kt, char* kn, char* vt, char* vn, int t) {
+    if (t + 2 < n_tiles) load_k(kt, t + 2);
+    load_v(vn, t + 1);
+#pragma unroll
+    for (int b = 0; b < QB; ++b) follow(b, mx[b]);
+    floatx16 nx[SUBS][QB];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) scores(kn, u, nx[u]);
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+      for (int b = 0; b < QB; ++b) weigh(b, st[u][b], false);
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) add(vt, u, st[u], 0);
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+      for (int b = 0; b < QB; ++b) st[u][b] = nx[u][b];
+    maxima();
+    arrived();
+  };
+  load_k(k0, 0);
+  load_v(v0, 0);
+  if (n_tiles > 1) load_k(k1, 1);
+  arrived();
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u) scores(k0, u, st[u]);
+  if (n_full > 0) maxima();
+  __syncthreads();                                           // (K of tile 0 is overwritten next)
+#pragma unroll 1
+  for (int t = 0; t < n_full; t += 2) {
+    full(k0, k1, v0, v1, t);
+    if (t + 1 == n_full) break;
+    full(k1, k0, v1, v0, t + 1);
+  }
+  // tiles that some rows of the workgroup do not see, or not whole
+#pragma unroll 1
+  for (int t = n_full; t < n_tiles; ++t) {
+    char* const vt = t & 1 ? v1 : v0;
+    if (t + 1 < n_tiles) load_v(t & 1 ? v0 : v1, t + 1);
+    if (t + 2 < n_tiles) load_k(t & 1 ? k1 : k0, t + 2);
+#pragma unroll 1
+    for (int u = 0; u < SUBS; ++u) {
+      const int over = t * SUBS + u - d0;                    // block `over` is on the diagonal, those before are past it
+      if (over >= QB || w0 + over * 32 >= len) break;
+      floatx16 x[QB];
 #pragma unroll
       for (int b = 0; b < QB; ++b) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[u][b][i]);
-        follow(b, mx);
-#pragma unroll
-        for (int u = 0; u < SUBS; ++u) weigh(b, st[u][b], false);
+        x[b] = st[0][b];
+        if (SUBS > 1 && u > 0) x[b] = st[SUBS - 1][b];
       }
+      const bool broken = over >= 0 && v_broken(vt, u);
 #pragma unroll
-      for (int u = 0; u < SUBS; ++u) add(vt, u, st[u], 0);
-    } else {
-#pragma unroll 1
-      for (int u = 0; u < SUBS; ++u) {
-        const int over = s0 + u - d0;                        // block `over` is on the diagonal, those before are past it
-        if (over >= QB || w0 + over * 32 >= len) break;
-        floatx16 st[QB];
-        scores(kt, u, st);
-        const bool broken = over >= 0 && v_broken(vt, u);
+      for (int b = 0; b < QB; ++b) {
+        if (b < over) continue;
+        float mb = -INFINITY;
 #pragma unroll
-        for (int b = 0; b < QB; ++b) {
-          if (b < over) continue;
-          float mx = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const bool seen = b > over || 8 * (i / 4) + 4 * lh + i % 4 <= lq;
-            mx = fmaxf(mx, seen ? st[b][i] : -INFINITY);
-          }
-          follow(b, mx);
-          weigh(b, st[b], b == over);
+        for (int i = 0; i < 16; ++i) {
+          const bool seen = b > over || 8 * (i / 4) + 4 * lh + i % 4 <= lq;
+          mb = fmaxf(mb, seen ? x[b][i] : -INFINITY);
         }
-        add(vt, u, st, over + (broken ? 1 : 0));
-        if (broken) {
+        follow(b, both(mb));
+        weigh(b, x[b], b == over);
+      }
+      add(vt, u, x, over + (broken ? 1 : 0));
+      if (broken) {
 #pragma unroll
-          for (int b = 0; b < QB; ++b)
-            if (b == over) add_by_rows(vt, u, b, st[b]);
-        }
+        for (int b = 0; b < QB; ++b)
+          if (b == over) add_by_rows(vt, u, b, x[b]);
       }
     }
-    if (t + 1 < n_tiles) stage((t + 1) & 1);
-    __syncthreads();
+    if (t + 1 == n_tiles) break;
+    const char* const kn = t & 1 ? k0 : k1;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) scores(kn, u, st[u]);
+    arrived();
   }
 
 #pragma unroll
