@@ -124,9 +124,17 @@ __global__ void __launch_bounds__(256, OCC)
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
         reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + ROW, 0x00020000);
+    constexpr int NEXT = 256 / CH;                           // rows between a thread's chunks
+    if (NEXT % 16 == 0 && left == KT) {                      // (the swizzles are the same there: one offset for all)
+      const int off = row_t * step + (ch_t ^ swz(row_t)) * 16;
+#pragma unroll
+      for (int u = 0; u < PER; ++u)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, off, u * NEXT * step, 0, 0);
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      int row = row_t + u * (256 / CH);
+      int row = row_t + u * NEXT;
       const int chunk = ch_t ^ swz(row);
       row = row < left ? row : left - 1;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, row * step + chunk * 16, 0,
