@@ -30,8 +30,6 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ float ld1(const float* p) { return *p; }
-__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   typedef float f32x2 __attribute__((ext_vector_type(2)));
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -71,61 +69,25 @@ __device__ __forceinline__ Place place_of(const zoact_packed& s, int64_t slot, i
   return p;
 }
 
-template <typename T, int HD, int KT_>
-struct Tile {
-  static constexpr bool BF = std::is_same<T, uint16_t>::value;
-  static constexpr int KT = KT_;                             // keys of a staged tile
-  static constexpr int SUBS = KT / 32;
-  static constexpr int ROW = HD * (int)sizeof(T), CH = ROW / 16;
-  static constexpr int BYTES = KT * ROW;
-  static constexpr int PER = KT * CH / 256;                  // 16-byte chunks a thread of K, and of V
-  static constexpr int NB = HD / 32;                         // 32-column blocks of O
-  // Chunk c of a row lies at c ^ swz(row): the 16 lanes of a read of K's chunk (rows in turn), and the
-  // lanes of a transposed read of V (4 rows of 64 bytes), then cover all banks (256 bytes) once.
-  __device__ static int kswz(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
-  __device__ static int vswz(int row) { return !BF ? 0 : CH == 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
-};
+__device__ __forceinline__ int no_swizzle(int) { return 0; }
 
-template <typename T, int HD, int KT_, int OCC>
-__global__ void __launch_bounds__(256, OCC)
-    attention_packed_kernel(zoact_packed s, const T* __restrict__ q, int64_t ldq, const T* __restrict__ k, int64_t ldk,
-                            const T* __restrict__ v, int64_t ldv, int heads, int kv_heads, int gh, float scale,
-                            T* __restrict__ out) {
-  using C = Tile<T, HD, KT_>;
-  constexpr bool BF = C::BF;
-  constexpr int KT = C::KT, SUBS = C::SUBS, ROW = C::ROW, CH = C::CH, PER = C::PER, NB = C::NB;
-  constexpr int QF = BF ? HD / 16 : HD / 8;                  // 16-byte pieces of a lane's query
-  // (arrays of their own, so that a read of one does not wait for the loads into another)
-  __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
-  __shared__ T pw[4][32][32];                                // a wave's probabilities for the vector product
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
-            lh = lane >> 5;
-  const int hgs = heads / gh, R = (4 / gh) * 32;
-  const int64_t slot = blockIdx.x / hgs;
-  const int hg = blockIdx.x - (int)slot * hgs;
-  const Place pl = place_of(s, slot, R);
-  if (pl.len == 0) return;
-  const int h = hg * gh + wave % gh, g = hg * gh / (heads / kv_heads);
-  const int len = pl.len, w0 = pl.q0 + wave / gh * 32;       // the wave's first row
-  const int last = pl.q0 + R < len ? pl.q0 + R : len;        // keys the workgroup needs
-  const int n_tiles = (last + KT - 1) / KT;
-
-  // Tiles go from global memory straight to LDS, a wave's 64 chunks side by side; the swizzle is in the
-  // choice of each lane's chunk.  Rows past the sequence read as its last.
-  const int row_t = threadIdx.x / CH, ch_t = threadIdx.x % CH;
-  const int kstep = (int)(ldk * (int64_t)sizeof(T)), vstep = (int)(ldv * (int64_t)sizeof(T));
-  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
-  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
-  auto load = [&](const char* from, int step, int (*swz)(int), char* to, int t) {
+// Rows of a K or V tile from global memory straight to LDS, 256 threads with PER chunks of 16 bytes each, a
+// wave's 64 side by side; the swizzle is in the choice of each lane's chunk.  Rows past the sequence read as its
+// last.
+template <int CH, int PER>
+struct TileLoad {
+  int wave, len;
+  __device__ __forceinline__ void run(const char* from, int step, int (*swz)(int), char* to, int first, int rows) const {
     typedef __attribute__((address_space(3))) void lds_t;
-    const int left = len - t * KT < KT ? len - t * KT : KT;
-    const uint64_t a = reinterpret_cast<uint64_t>(from + (int64_t)t * KT * step);
+    const int row_t = threadIdx.x / CH, ch_t = threadIdx.x % CH;
+    const int left = len - first < rows ? len - first : rows;
+    const uint64_t a = reinterpret_cast<uint64_t>(from + (int64_t)first * step);
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + ROW, 0x00020000);
+        reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + CH * 16, 0x00020000);
     constexpr int NEXT = 256 / CH;                           // rows between a thread's chunks
-    if (NEXT % 16 == 0 && left == KT) {                      // (the swizzles are the same there: one offset for all)
+    if (NEXT % 16 == 0 && left == rows) {                    // (the swizzles are the same there: one offset for all)
       const int off = row_t * step + (ch_t ^ swz(row_t)) * 16;
 #pragma unroll
       for (int u = 0; u < PER; ++u)
@@ -140,16 +102,59 @@ __global__ void __launch_bounds__(256, OCC)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, row * step + chunk * 16, 0,
                                                0, 0);
     }
-  };
-  auto load_k = [&](char* to, int t) { load(kb, kstep, C::kswz, to, t); };
-  auto load_v = [&](char* to, int t) { load(vb, vstep, C::vswz, to, t); };
+  }
+};
+
+template <int HD>
+struct Tile {
+  static constexpr int KT = 64;                              // keys of a staged tile
+  static constexpr int SUBS = KT / 32;
+  static constexpr int ROW = HD * 2, CH = ROW / 16;
+  static constexpr int BYTES = KT * ROW;
+  static constexpr int PER = KT * CH / 256;                  // 16-byte chunks a thread of K, and of V
+  static constexpr int NB = HD / 32;                         // 32-column blocks of O
+  // Chunk c of a row lies at c ^ swz(row): the 16 lanes of a read of K's chunk (rows in turn), and the
+  // lanes of a transposed read of V (4 rows of 64 bytes), then cover all banks (256 bytes) once.
+  __device__ static int kswz(int row) { return CH >= 16 ? row & 15 : CH == 8 ? (row >> 1) & 7 : (row >> 2) & 3; }
+  __device__ static int vswz(int row) { return CH == 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(256, 2)
+    attention_packed_bf16_kernel(zoact_packed s, const uint16_t* __restrict__ q, int64_t ldq,
+                                 const uint16_t* __restrict__ k, int64_t ldk, const uint16_t* __restrict__ v, int64_t ldv,
+                                 int heads, int kv_heads, int gh, float scale, uint16_t* __restrict__ out) {
+  using C = Tile<HD>;
+  constexpr int KT = C::KT, SUBS = C::SUBS, ROW = C::ROW, CH = C::CH, PER = C::PER, NB = C::NB;
+  constexpr int QF = HD / 16;                                // 16-byte pieces of a lane's query
+  // (arrays of their own, so that a read of one does not wait for the loads into another)
+  __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
+  __shared__ uint16_t pw[4][32][32];                                // a wave's probabilities for the vector product
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
+            lh = lane >> 5;
+  const int hgs = heads / gh, R = (4 / gh) * 32;
+  const int64_t slot = blockIdx.x / hgs;
+  const int hg = blockIdx.x - (int)slot * hgs;
+  const Place pl = place_of(s, slot, R);
+  if (pl.len == 0) return;
+  const int h = hg * gh + wave % gh, g = hg * gh / (heads / kv_heads);
+  const int len = pl.len, w0 = pl.q0 + wave / gh * 32;       // the wave's first row
+  const int last = pl.q0 + R < len ? pl.q0 + R : len;        // keys the workgroup needs
+  const int n_tiles = (last + KT - 1) / KT;
+
+  const int kstep = (int)(ldk * 2), vstep = (int)(ldv * 2);
+  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
+  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
+  const TileLoad<CH, PER> tl{wave, len};
+  auto load_k = [&](char* to, int t) { tl.run(kb, kstep, C::kswz, to, t * KT, KT); };
+  auto load_v = [&](char* to, int t) { tl.run(vb, vstep, C::vswz, to, t * KT, KT); };
   auto arrived = [&] {
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's part; then everybody's
     __syncthreads();
   };
   load_k(k0, 0);
 
-  // queries: lane's own row, pieces of 8 (4) values by halves
+  // queries: lane's own row, pieces of 8 values by halves
   u32x4 qf[QF];
   {
     const int r = w0 + lq < len ? w0 + lq : len - 1;
@@ -161,7 +166,7 @@ __global__ void __launch_bounds__(256, OCC)
   if (n_tiles > 1) load_k(k1, 1);
   if (scale < 0.f) {
 #pragma unroll
-    for (int c = 0; c < QF; ++c) qf[c] ^= BF ? 0x80008000u : 0x80000000u;
+    for (int c = 0; c < QF; ++c) qf[c] ^= 0x80008000u;
   }
   const float c2 = fabsf(scale) * 1.4426950408889634f;
 
@@ -182,14 +187,8 @@ __global__ void __launch_bounds__(256, OCC)
 #pragma unroll
     for (int c = 0; c < QF; ++c) {
       const u32x4 kf = *reinterpret_cast<const u32x4*>(kp + ((2 * c + lh) ^ C::kswz(key)) * 16);
-      if constexpr (BF) {
-        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), st,
-                                                     0, 0, 0);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          st = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]), st, 0, 0, 0);
-      }
+      st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[c]), st, 0,
+                                                   0, 0);
     }
     return st;
   };
@@ -221,7 +220,7 @@ __global__ void __launch_bounds__(256, OCC)
     }
     l += t0 + t1;
   };
-  // V^T of block n, keys 16 c .. + 15 of sub (BF16): the order of the packed probabilities
+  // V^T of block n, keys 16 c .. + 15 of sub: the order of the packed probabilities
   const int gl = lane & 15, g1 = (lane >> 4) & 1, vrow = gl >> 2;
   auto v_frag = [&](const char* vt, int sub, int c, int n) {
     typedef __attribute__((address_space(3))) bf16x4* lp;
@@ -233,23 +232,14 @@ __global__ void __launch_bounds__(256, OCC)
     return u32x4{a.x, a.y, z.x, z.y};
   };
   auto add = [&](const char* vt, int sub, const floatx16& st) {
-    if constexpr (BF) {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const u32x4 pb = u32x4{pack2(st[8 * c], st[8 * c + 1]), pack2(st[8 * c + 2], st[8 * c + 3]),
-                               pack2(st[8 * c + 4], st[8 * c + 5]), pack2(st[8 * c + 6], st[8 * c + 7])};
+    for (int c = 0; c < 2; ++c) {
+      const u32x4 pb = u32x4{pack2(st[8 * c], st[8 * c + 1]), pack2(st[8 * c + 2], st[8 * c + 3]),
+                             pack2(st[8 * c + 4], st[8 * c + 5]), pack2(st[8 * c + 6], st[8 * c + 7])};
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
-          o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_frag(vt, sub, c, n)),
-                                                         __builtin_bit_cast(bf16x8, pb), o[n], 0, 0, 0);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float* vp = reinterpret_cast<const float*>(vt + (sub * 32 + 8 * (i / 4) + 4 * lh + i % 4) * ROW) + lq;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) o[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(vp[n * 32], st[i], o[n], 0, 0, 0);
-      }
+      for (int n = 0; n < NB; ++n)
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v_frag(vt, sub, c, n)),
+                                                       __builtin_bit_cast(bf16x8, pb), o[n], 0, 0, 0);
     }
   };
   // whether a sub-tile of V holds something that is not finite (its rows spread over the wave)
@@ -261,30 +251,29 @@ __global__ void __launch_bounds__(256, OCC)
       const u32x4 x = *reinterpret_cast<const u32x4*>(vt + sub * 32 * ROW + (c * 64 + lane) * 16);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[e] & (BF ? 0x7FFF7FFFu : 0x7FFF0000u)));
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
     }
     return __ballot(most.x >= 0x7F80 || most.y >= 0x7F80) != 0;
   };
   // the diagonal sub-tile key by key, for the rows from each on
   auto add_by_rows = [&](const char* vt, int sub, const floatx16& st) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int key = 8 * (i / 4) + 4 * lh + i % 4;
-      if constexpr (BF) pw[wave][lq][key ^ lq] = f2bf(st[i]);
-      else pw[wave][lq][key ^ lq] = st[i];
-    }
+    for (int i = 0; i < 16; ++i) pw[wave][lq][(8 * (i / 4) + 4 * lh + i % 4) ^ lq] = f2bf(st[i]);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
     for (int t = 0; t < 32; ++t) {
       const int row = sub * 32 + t;
-      const float p = ld1(&pw[wave][lq][t ^ lq]);
+      const float p = bf2f(pw[wave][lq][t ^ lq]);
+      const bool seen = t <= lq;
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int at = (32 * n + 8 * (i / 4) + 4 * lh + i % 4) * (int)sizeof(T);
-          const float x = ld1(reinterpret_cast<const T*>(vt + row * ROW + ((at / 16) ^ C::vswz(row)) * 16 + at % 16));
-          o[n][i] = t <= lq ? fmaf(p, x, o[n][i]) : o[n][i];
+        for (int i = 0; i < 4; ++i) {
+          const uint2 x = *reinterpret_cast<const uint2*>(vt + row * ROW + ((4 * n + i) ^ C::vswz(row)) * 16 + lh * 8);
+          o[n][4 * i] = seen ? fmaf(p, __uint_as_float(x.x << 16), o[n][4 * i]) : o[n][4 * i];
+          o[n][4 * i + 1] = seen ? fmaf(p, __uint_as_float(x.x & 0xFFFF0000u), o[n][4 * i + 1]) : o[n][4 * i + 1];
+          o[n][4 * i + 2] = seen ? fmaf(p, __uint_as_float(x.y << 16), o[n][4 * i + 2]) : o[n][4 * i + 2];
+          o[n][4 * i + 3] = seen ? fmaf(p, __uint_as_float(x.y & 0xFFFF0000u), o[n][4 * i + 3]) : o[n][4 * i + 3];
         }
     }
   };
@@ -364,20 +353,15 @@ __global__ void __launch_bounds__(256, OCC)
   // lines are written
   const float inv = 1.f / (l + __shfl_xor(l, 32, 64));
   __syncthreads();
-  const int at = wave / SUBS;
-  char* const mine = (at == 0 ? k0 : at == 1 ? k1 : at == 2 ? v0 : v1) + wave % SUBS * 32 * ROW;
+  char* const mine = (wave < 2 ? k0 : k1) + wave % 2 * 32 * ROW;
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float a0 = o[n][4 * i] * inv, a1 = o[n][4 * i + 1] * inv, a2 = o[n][4 * i + 2] * inv,
                   a3 = o[n][4 * i + 3] * inv;
-      if constexpr (BF)
-        *reinterpret_cast<uint2*>(mine + lq * ROW + ((4 * n + i) ^ C::kswz(lq)) * 16 + lh * 8) =
-            make_uint2(pack2(a0, a1), pack2(a2, a3));
-      else
-        *reinterpret_cast<float4*>(mine + lq * ROW + ((8 * n + 2 * i + lh) ^ C::kswz(lq)) * 16) =
-            make_float4(a0, a1, a2, a3);
+      *reinterpret_cast<uint2*>(mine + lq * ROW + ((4 * n + i) ^ C::kswz(lq)) * 16 + lh * 8) =
+          make_uint2(pack2(a0, a1), pack2(a2, a3));
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   char* const op = reinterpret_cast<char*>(out + ((pl.row0 + w0) * heads + h) * HD);
@@ -387,6 +371,239 @@ __global__ void __launch_bounds__(256, OCC)
     const u32x4 x = *reinterpret_cast<const u32x4*>(mine + row * ROW + (c ^ C::kswz(row)) * 16);
     if (w0 + row < len) *reinterpret_cast<u32x4*>(op + (int64_t)row * heads * ROW + c * 16) = x;
   }
+}
+
+
+// ---------------------------------------------------------------- fp32
+// The same on v_mfma_f32_16x16x4_f32 with 16 rows a wave: the products, 64 flops a cycle and SIMD, take
+// nearly all of the time, so that short workgroups matter more than what LDS gives.
+template <int HD>
+struct TileF {
+  static constexpr int KT = 32, ROW = HD * 4, CH = HD / 4, BYTES = KT * ROW;
+  static constexpr int QF = HD / 16;                         // 16-byte pieces of a lane's query
+  static constexpr int W = HD >= 64 ? 4 : 2, NV = HD / (16 * W); // columns of V a lane reads at once, and how often
+  __device__ static int kswz(int row) { return CH >= 16 ? row & 15 : (row >> 1) & 7; }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
+    attention_packed_f32_kernel(zoact_packed s, const float* __restrict__ q, int64_t ldq, const float* __restrict__ k,
+                                int64_t ldk, const float* __restrict__ v, int64_t ldv, int heads, int kv_heads, int gh,
+                                float scale, float* __restrict__ out) {
+  using C = TileF<HD>;
+  constexpr int KT = C::KT, ROW = C::ROW, CH = C::CH, QF = C::QF, W = C::W, NV = C::NV;
+  typedef float floatw __attribute__((ext_vector_type(W)));
+  __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
+  __shared__ float pw[4][16][32];                            // a wave's probabilities for the vector product
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15,
+            lg = lane >> 4;
+  const int hgs = heads / gh, R = 4 / gh * 16;
+  const int64_t slot = blockIdx.x / hgs;
+  const int hg = blockIdx.x - (int)slot * hgs;
+  const Place pl = place_of(s, slot, R);
+  if (pl.len == 0) return;
+  const int h = hg * gh + wave % gh, g = hg * gh / (heads / kv_heads);
+  const int len = pl.len, w0 = pl.q0 + wave / gh * 16;       // the wave's first row
+  const int last = pl.q0 + R < len ? pl.q0 + R : len;        // keys the workgroup needs
+  const int n_tiles = (last + KT - 1) / KT;
+
+  const int kstep = (int)(ldk * 4), vstep = (int)(ldv * 4);
+  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
+  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
+  const TileLoad<CH, KT * CH / 256> tl{wave, len};
+  auto load_k = [&](char* to, int t) { tl.run(kb, kstep, C::kswz, to, t * KT, KT); };
+  auto load_v = [&](char* to, int t) { tl.run(vb, vstep, no_swizzle, to, t * KT, KT); };
+  auto arrived = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's part; then everybody's
+    __syncthreads();
+  };
+  load_k(k0, 0);
+  // queries: lane's own row, chunks 4 c + lg
+  u32x4 qf[QF];
+  {
+    const int r = w0 + lq < len ? w0 + lq : len - 1;
+    const char* qp = reinterpret_cast<const char*>(q + (pl.row0 + r) * ldq + (int64_t)h * HD);
+#pragma unroll
+    for (int c = 0; c < QF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(qp + (4 * c + lg) * 16);
+  }
+  load_v(v0, 0);
+  if (n_tiles > 1) load_k(k1, 1);
+  if (scale < 0.f) {
+#pragma unroll
+    for (int c = 0; c < QF; ++c) qf[c] ^= 0x80000000u;
+  }
+  const float c2 = fabsf(scale) * 1.4426950408889634f;
+
+  floatx4 o[NV][W];                                          // o[n][e][i]: column 16 W n + W (4 lg + i) + e
+  float l = 0.f, m = -1.0e38f;           // (finite: a score of -inf has weight 0 also where nothing else came before)
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+#pragma unroll
+    for (int e = 0; e < W; ++e) o[n][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  // scores of a block of 16 keys; register i: key 4 lg + i.  One product takes a value of each of four chunks.
+  auto scores = [&](const char* kt, int blk) {
+    floatx4 st = {0.f, 0.f, 0.f, 0.f};
+    const int key = blk * 16 + lq;
+#pragma unroll
+    for (int c = 0; c < QF; ++c) {
+      const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + key * ROW + ((4 * c + lg) ^ C::kswz(key)) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        st = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[e]), __uint_as_float(qf[c][e]), st, 0, 0, 0);
+    }
+    return st;
+  };
+  // a row's maximum over the four parts of the wave
+  auto all = [&](float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    const auto z = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+  };
+  auto follow = [&](float mx) {
+    mx *= c2;
+    if (__ballot(mx > m + 8.f)) {
+      const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= a;
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int e = 0; e < W; ++e) o[n][e] *= a;
+    }
+  };
+  auto weigh = [&](floatx4& st, auto cut, int lim) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      st[i] = __builtin_amdgcn_exp2f(fmaf(st[i], c2, -m));
+      if (decltype(cut)::value && i > lim) st[i] = 0.f;
+    }
+    l += (st[0] + st[1]) + (st[2] + st[3]);
+  };
+  auto add = [&](const char* vt, int blk, const floatx4& st) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const char* vp = vt + (blk * 16 + 4 * lg + i) * ROW + lq * W * 4;
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const floatw x = *reinterpret_cast<const floatw*>(vp + n * 16 * W * 4);
+#pragma unroll
+        for (int e = 0; e < W; ++e) o[n][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], st[i], o[n][e], 0, 0, 0);
+      }
+    }
+  };
+  // whether a tile of V holds something that is not finite
+  auto v_broken = [&](const char* vt) {
+    uint32_t most = 0;
+#pragma unroll 4
+    for (int c = 0; c < KT * CH / 64; ++c) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(vt + (c * 64 + lane) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) most = max(most, x[e] & 0x7FFFFFFFu);
+    }
+    return __ballot(most >= 0x7F800000u) != 0;
+  };
+  // a tile key by key, for the rows from each on (lim: the lane's row in the tile)
+  auto add_by_rows = [&](const char* vt, const floatx4 (&st)[2], int lim) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      pw[wave][lq][(4 * lg + i) ^ lq] = st[0][i];
+      pw[wave][lq][(16 + 4 * lg + i) ^ lq] = st[1][i];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+    for (int t = 0; t < KT; ++t) {
+      const float p = pw[wave][lq][t ^ lq];
+      const bool seen = t <= lim;
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const floatw x = *reinterpret_cast<const floatw*>(vt + t * ROW + (16 * W * n + W * (4 * lg + i)) * 4);
+#pragma unroll
+          for (int e = 0; e < W; ++e) o[n][e][i] = seen ? fmaf(p, x[e], o[n][e][i]) : o[n][e][i];
+        }
+    }
+  };
+
+  const int n_full = pl.q0 / KT;                             // tiles that every row of the workgroup sees
+  floatx4 st[2];
+  float mx;
+  auto maximum = [&] {
+    mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(st[0][i], st[1][i]));
+    mx = all(mx);
+  };
+  auto full = [&](char* kt, char* kn, char* vt, char* vn, int t) {
+    if (t + 2 < n_tiles) load_k(kt, t + 2);
+    load_v(vn, t + 1);
+    follow(mx);
+    const floatx4 n0 = scores(kn, 0), n1 = scores(kn, 1);
+    weigh(st[0], std::false_type{}, 0);
+    weigh(st[1], std::false_type{}, 0);
+    add(vt, 0, st[0]);
+    add(vt, 1, st[1]);
+    st[0] = n0;
+    st[1] = n1;
+    maximum();
+    arrived();
+  };
+  arrived();
+  st[0] = scores(k0, 0);
+  st[1] = scores(k0, 1);
+  maximum();
+  __syncthreads();                                           // (K of tile 0 is overwritten next)
+#pragma unroll 1
+  for (int t = 0; t < n_full; t += 2) {
+    full(k0, k1, v0, v1, t);
+    if (t + 1 == n_full) break;
+    full(k1, k0, v1, v0, t + 1);
+  }
+#pragma unroll 1
+  for (int t = n_full; t < n_tiles; ++t) {
+    char* const vt = t & 1 ? v1 : v0;
+    if (t + 1 < n_tiles) load_v(t & 1 ? v0 : v1, t + 1);
+    if (t + 2 < n_tiles) load_k(t & 1 ? k1 : k0, t + 2);
+    if (t * KT <= w0 && w0 < len) {
+      const int lim = w0 + lq - t * KT;
+      float mb = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mb = fmaxf(mb, 16 * u + i <= lim - 4 * lg ? st[u][i] : -INFINITY);
+      follow(all(mb));
+      weigh(st[0], std::true_type{}, lim - 4 * lg);
+      weigh(st[1], std::true_type{}, lim - 4 * lg - 16);
+      if (w0 - t * KT < KT && v_broken(vt)) {
+        add_by_rows(vt, st, lim);
+      } else {
+        add(vt, 0, st[0]);
+        if (w0 - t * KT >= 16) add(vt, 1, st[1]);
+      }
+    }
+    if (t + 1 == n_tiles) break;
+    const char* const kn = t & 1 ? k0 : k1;
+    st[0] = scores(kn, 0);
+    st[1] = scores(kn, 1);
+    arrived();
+  }
+
+  l += __shfl_xor(l, 32, 64);
+  l += __shfl_xor(l, 16, 64);
+  const float inv = 1.f / l;
+  if (w0 + lq >= len) return;
+  float* const op = out + ((pl.row0 + w0 + lq) * heads + h) * HD;
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      floatw x;
+#pragma unroll
+      for (int e = 0; e < W; ++e) x[e] = o[n][e][i] * inv;
+      *reinterpret_cast<floatw*>(op + 16 * W * n + W * (4 * lg + i)) = x;
+    }
 }
 
 }  // namespace
@@ -401,21 +618,20 @@ hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t
   // (a tile's rows are addressed with 32 bits)
   if (ldk >= (int64_t(1) << 22) || ldv >= (int64_t(1) << 22)) return hipErrorNotSupported;
   const int G = heads / kv_heads, gh = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
-  const int R = (4 / gh) * 32;
-  const int64_t slots = s.rows / R + s.n, grid = slots * (heads / gh);
+  const int R = 4 / gh * (dtype == ZOACT_BF16 ? 32 : 16);
+  const int64_t grid = (s.rows / R + s.n) * (heads / gh);
   if (grid >= (int64_t(1) << 31)) return hipErrorNotSupported;
-#define ZO_ATT(T, HD, KT, OCC)                                                                                          \
-  attention_packed_kernel<T, HD, KT, OCC><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk,        \
-                                                                          (const T*)v, ldv, heads, kv_heads, gh, scale, \
-                                                                          (T*)out)
+#define ZO_ATT(T, KERNEL, HD)                                                                                     \
+  KERNEL<HD><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk, (const T*)v, ldv, heads, kv_heads, \
+                                             gh, scale, (T*)out)
   if (dtype == ZOACT_BF16) {
-    if (hd == 128) ZO_ATT(uint16_t, 128, 64, 2);
-    else if (hd == 64) ZO_ATT(uint16_t, 64, 64, 2);
-    else ZO_ATT(uint16_t, 32, 64, 2);
+    if (hd == 128) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 128);
+    else if (hd == 64) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 64);
+    else ZO_ATT(uint16_t, attention_packed_bf16_kernel, 32);
   } else {
-    if (hd == 128) ZO_ATT(float, 128, 32, 2);
-    else if (hd == 64) ZO_ATT(float, 64, 32, 2);
-    else ZO_ATT(float, 32, 32, 2);
+    if (hd == 128) ZO_ATT(float, attention_packed_f32_kernel, 128);
+    else if (hd == 64) ZO_ATT(float, attention_packed_f32_kernel, 64);
+    else ZO_ATT(float, attention_packed_f32_kernel, 32);
   }
 #undef ZO_ATT
   return hipGetLastError();
