@@ -61,12 +61,77 @@ __device__ __forceinline__ Place place_of(const zoact_packed& s, int64_t slot, i
   Place p{0, 0, 0};
   if (b < 0 || e <= b || e > s.rows) return p;
   const int64_t k = slot - ((int64_t)(b / R) + lo);
-  const int tiles = (e - b + R - 1) / R;
+  const int tiles = (int)(((int64_t)e - b + R - 1) / R);
   if (k < 0 || k >= tiles) return p;
   p.row0 = b;
   p.len = e - b;
   p.q0 = (tiles - 1 - (int)k) * R;
   return p;
+}
+
+// Sum over the wave, in every lane.
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The same with the tiles of 64 sequences at a time (a lane each) in the order of the keys before them, most
+// first, whichever sequence they are of: the last to start are then short.  Sequences 64 g on have the slots
+// from begin[64 g] / R + 64 g on.  For fp32, which the products bind (8 sequences of 700 tokens 105 -> 85 us);
+// in bf16 what tiles of one sequence find in the cache weighs more (OPT's heads 190 -> 200 us).
+__device__ __forceinline__ Place longest_first(const zoact_packed& s, int64_t slot, int R) {
+  const int lane = threadIdx.x & 63, sh = 31 - __builtin_clz(R);       // (R is a power of two)
+  int lo = 0, hi = (s.n + 63) >> 6;                // the last group in [lo, hi) whose slots begin at or before slot
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) >> 6, i = lo + lane * step;
+    bool at = false;
+    if (i < hi) {
+      const int x = s.begin[i << 6];
+      at = (int64_t)((x > 0 ? x : 0) >> sh) + (i << 6) <= slot;
+    }
+    const int c = __popcll(__ballot(at));
+    lo += (c > 0 ? c - 1 : 0) * step;
+    hi = lo + step < hi ? lo + step : hi;
+  }
+  const int i = (lo << 6) + lane;
+  const int b = s.begin[i < s.n ? i : s.n], e = s.begin[i < s.n ? i + 1 : s.n];
+  const int tiles = b >= 0 && e > b && e <= s.rows ? (int)(((int64_t)e - b + R - 1) >> sh) : 0;
+  const int b0 = __builtin_amdgcn_readfirstlane(b);
+  const int64_t k64 = slot - ((int64_t)((b0 > 0 ? b0 : 0) >> sh) + (lo << 6));
+  Place p{0, 0, 0};
+  if (k64 < 0 || k64 >= wave_sum(tiles)) return p;
+  // the highest tile number t of which, and of higher ones, there are more than k
+  const int k = (int)k64;
+  int t = 0, top = 1;
+  while (__ballot(tiles > top)) top <<= 1;         // (all tile numbers are below top)
+  while (top - t > 1) {
+    const int mid = (t + top) >> 1;
+    if (wave_sum(tiles > mid ? tiles - mid : 0) > k) t = mid;
+    else top = mid;
+  }
+  const int above = wave_sum(tiles > t + 1 ? tiles - t - 1 : 0);
+  const int rank = __popcll(__ballot(tiles > t) & ((1ull << lane) - 1));
+  const int who = __ffsll((unsigned long long)__ballot(tiles > t && rank == k - above)) - 1;
+  const int row0 = __builtin_amdgcn_readlane(b, who);
+  p.row0 = row0;
+  p.len = __builtin_amdgcn_readlane(e, who) - row0;
+  p.q0 = t << sh;
+  return p;
+}
+
+// A workgroup's number in the order of its work.  Where all workgroups of a launch find room at once, those that
+// share a compute unit are 256 apart: every second 256 are taken backwards (by eights, each of which goes to its own
+// XCD), so that long ones share with short ones (2 sequences of 1000 tokens 35.7 -> 29.7 us, one of 4000 in fp32
+// 349 -> 314).
+__device__ __forceinline__ unsigned turn_about() {
+  const unsigned turn = blockIdx.x >> 8;
+  return (turn & 1) && (turn + 1) << 8 <= gridDim.x
+             ? (turn << 8) + ((31 - ((blockIdx.x & 255) >> 3)) << 3) + (blockIdx.x & 7) : blockIdx.x;
 }
 
 __device__ __forceinline__ int no_swizzle(int) { return 0; }
@@ -133,8 +198,8 @@ __global__ void __launch_bounds__(256, 2)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
             lh = lane >> 5;
   const int hgs = heads / gh, R = (4 / gh) * 32;
-  const int64_t slot = blockIdx.x / hgs;
-  const int hg = blockIdx.x - (int)slot * hgs;
+  const unsigned id = turn_about(), slot = id / hgs;
+  const int hg = (int)(id - slot * hgs);
   const Place pl = place_of(s, slot, R);
   if (pl.len == 0) return;
   const int h = hg * gh + wave % gh, g = hg * gh / (heads / kv_heads);
@@ -398,10 +463,13 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15,
             lg = lane >> 4;
   const int hgs = heads / gh, R = 4 / gh * 16;
-  const int64_t slot = blockIdx.x / hgs;
-  const int hg = blockIdx.x - (int)slot * hgs;
-  const Place pl = place_of(s, slot, R);
-  if (pl.len == 0) return;
+  const unsigned id = turn_about(), slot = id / hgs;
+  const int hg = (int)(id - slot * hgs);
+  Place pl = longest_first(s, slot, R);
+  if (__builtin_amdgcn_readfirstlane(pl.len) == 0) return;
+  // (the same in all lanes, which the compiler does not see through the search)
+  pl = Place{__builtin_amdgcn_readfirstlane((int)pl.row0), __builtin_amdgcn_readfirstlane(pl.len),
+             __builtin_amdgcn_readfirstlane(pl.q0)};
   const int h = hg * gh + wave % gh, g = hg * gh / (heads / kv_heads);
   const int len = pl.len, w0 = pl.q0 + wave / gh * 16;       // the wave's first row
   const int last = pl.q0 + R < len ? pl.q0 + R : len;        // keys the workgroup needs
