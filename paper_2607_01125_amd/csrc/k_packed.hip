@@ -39,6 +39,86 @@ __global__ void __launch_bounds__(256) rope_at_kernel(const T* x, int64_t ldx, T
   }
 }
 
+// Pieces of 16 bytes: a thread takes one place of a row -- a pair of pieces half the turned part apart (HALF), a
+// piece of whole pairs (INTERLEAVED), or a piece to copy -- in RT rows, all of whose loads are on their way before
+// the first is used.  Bound by memory: 16411 rows of 40 heads of 128 bf16 values, 64 of them turned in pairs, a copy
+// of the same bytes ... us.
+template <typename T, bool HALF, int RT>
+__global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
+                                                           int heads, int hd, int rot, const int32_t* __restrict__ pos,
+                                                           const float* __restrict__ cos_t,
+                                                           const float* __restrict__ sin_t, int64_t n_pos) {
+  constexpr int V = 16 / sizeof(T), NT = HALF ? V : V / 2;   // values of a piece, angles of it
+  typedef T piece __attribute__((ext_vector_type(V)));
+  typedef float angles __attribute__((ext_vector_type(NT)));
+  const int turned = HALF ? rot / (2 * V) : rot / V, per = turned + (out == x ? 0 : (hd - rot) / V);
+  const int units = heads * per, half = rot / 2;
+  const int64_t row0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * RT;
+  for (int u = threadIdx.x; u < units; u += blockDim.x) {
+    const int h = u / per, j = u - h * per;
+    const int64_t col = (int64_t)h * hd + (j < turned ? j * V : rot + (j - turned) * V);
+    piece a[RT], b[RT];
+    angles c[RT], s[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
+      a[r] = *reinterpret_cast<const piece*>(x + row * ldx + col);
+      if (j < turned) {
+        int64_t p = pos ? pos[row] : row;
+        p = p < 0 ? 0 : (p >= n_pos ? n_pos - 1 : p);
+        if (HALF) b[r] = *reinterpret_cast<const piece*>(x + row * ldx + col + half);
+        c[r] = *reinterpret_cast<const angles*>(cos_t + p * half + j * NT);
+        s[r] = *reinterpret_cast<const angles*>(sin_t + p * half + j * NT);
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+      if (row0 + r >= rows) break;
+      T* const y = out + (row0 + r) * ldo + col;
+      if (j < turned) {
+        piece m, n;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+          T ea = a[r][HALF ? i : 2 * i], eb = HALF ? b[r][i] : a[r][2 * i + 1];
+          const float fa = ld1(&ea), fb = ld1(&eb);
+          T ma, mb;
+          st1(&ma, fa * c[r][i] - fb * s[r][i]);
+          st1(&mb, fb * c[r][i] + fa * s[r][i]);
+          if (HALF) m[i] = ma, n[i] = mb;
+          else m[2 * i] = ma, m[2 * i + 1] = mb;
+        }
+        *reinterpret_cast<piece*>(y) = m;
+        if (HALF) *reinterpret_cast<piece*>(y + half) = n;
+      } else {
+        *reinterpret_cast<piece*>(y) = a[r];
+      }
+    }
+  }
+}
+
+template <typename T>
+bool rope_at_vec(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows, int heads, int hd, int rot, int layout,
+                 const int32_t* pos, const float* cos_t, const float* sin_t, int64_t n_pos, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  const bool halves = layout == ZOACT_ROPE_HALF;
+  if (hd % V || rot % (halves ? 2 * V : V) || ldx % V || ldo % V || !aligned_to(x, 16) || !aligned_to(out, 16) ||
+      !aligned_to(cos_t, 16) || !aligned_to(sin_t, 16))
+    return false;
+  const int64_t units = (int64_t)heads * (rot / (halves ? 2 * V : V) + (out == x ? 0 : (hd - rot) / V));
+  const int bx = (int)(units < 512 ? units : 512), by = bx < 256 ? 256 / bx : 1;
+  // (one row a thread until there are workgroups enough for every compute unit several times)
+  const bool many = rows * units >= (int64_t)512 * 1024 * 4;
+  const int64_t step = (int64_t)by * (many ? 4 : 1), grid = (rows + step - 1) / step;
+  if (grid >= (int64_t(1) << 31)) return false;
+#define ZO_ROPE(HALF, RT)                                                                                             \
+  rope_at_vec_kernel<T, HALF, RT><<<(unsigned)grid, dim3(bx, by), 0, s>>>(x, ldx, out, ldo, rows, heads, hd, rot, pos, \
+                                                                          cos_t, sin_t, n_pos)
+  if (halves) many ? ZO_ROPE(true, 4) : ZO_ROPE(true, 1);
+  else many ? ZO_ROPE(false, 4) : ZO_ROPE(false, 1);
+#undef ZO_ROPE
+  return true;
+}
+
 // ---------------------------------------------------------------- attention, any shape
 // One wave a (row, head): 64 keys at a time, a key a lane for the scores and a column a lane for
 // the sums, with the running maximum m and sum l of the softmax.
@@ -133,6 +213,11 @@ extern "C" zoact_status zoact_rope_at(const void* x, int64_t ldx, void* out, int
            "rope_at: tables and pos must be 4-byte aligned");
   if (rows == 0) return ZOACT_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  if (dtype == ZOACT_BF16 ? rope_at_vec((const uint16_t*)x, ldx, (uint16_t*)out, ldo, rows, n_heads, head_dim, rot_dim,
+                                        layout, pos, cos_t, sin_t, n_pos, s)
+                          : rope_at_vec((const float*)x, ldx, (float*)out, ldo, rows, n_heads, head_dim, rot_dim, layout,
+                                        pos, cos_t, sin_t, n_pos, s))
+    return launched_or("rope_at");
   const int64_t units = rows * n_heads * (head_dim - rot_dim / 2), g = (units + 255) / 256;
   const unsigned grid = (unsigned)(g < 65536 ? g : 65536);
   if (dtype == ZOACT_BF16)
