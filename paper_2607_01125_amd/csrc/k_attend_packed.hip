@@ -69,17 +69,6 @@ __device__ __forceinline__ Place place_of(const zoact_packed& s, int64_t slot, i
   return p;
 }
 
-// Sum over the wave, in every lane.
-__device__ __forceinline__ int wave_sum(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31
-  return __builtin_amdgcn_readlane(x, 63);
-}
-
 // The same with the tiles of 64 sequences at a time (a lane each) in the order of the keys before them, most
 // first, whichever sequence they are of: the last to start are then short.  Sequences 64 g on have the slots
 // from begin[64 g] / R + 64 g on.  For fp32, which the products bind (8 sequences of 700 tokens 105 -> 85 us);

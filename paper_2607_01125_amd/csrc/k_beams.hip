@@ -13,6 +13,7 @@ namespace {
 
 constexpr int PART = 4096;               // logits of a workgroup
 constexpr int NT = 256, PER = PART / NT;
+constexpr int NP = 1024;                 // threads of a prompt's workgroup
 constexpr int KMAX = ZOACT_BEAMS_MAX;
 constexpr int WCAP = 512;                // candidates a wave gathers before it takes the slow way
 
@@ -77,10 +78,8 @@ __global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, in
   if (b.eos >= 0 && b.length > 0 && b.hist[(int64_t)row * b.ld_hist + b.length - 1] == b.eos) return;   // it has ended
   const T* lr = logits + (int64_t)row * ldl;
   const int V = (int)b.vocab, v0 = part * PART + threadIdx.x * 4;      // this thread: v0 + 1024 j + e
-  float x[PER];
-  uint32_t key[PER];                     // 0: behind the row, or NaN (the row's sum tells of it)
-  float mx = -INFINITY;
-  uint32_t kmax = 0;
+  const bool whole = (part + 1) * (int64_t)PART <= V;
+  float x[PER], mx = -INFINITY;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -98,57 +97,53 @@ __global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, in
       mx = fmaxf(mx, t[e]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int64_t v = (int64_t)v0 + (i >> 2) * (NT * 4) + (i & 3);
-    key[i] = v < V && x[i] == x[i] ? order32(x[i]) : 0;
-    kmax = key[i] > kmax ? key[i] : kmax;
-  }
-  // maximum and sum of the wave's 1024
-  float wm = mx;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) wm = fmaxf(wm, __shfl_xor(wm, o, 64));
+  // maximum and sum of the wave's 1024 (a NaN stays out of the maximum and goes into the sum)
+  const float wm = wave_max(mx);
   const float base = wm == -INFINITY ? 0.f : wm;
   float sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) sum += expf(x[i] - base);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  for (int i = 0; i < PER; ++i) sum += __expf(x[i] - base);
+  sum = wave_sum(sum);
   if (lane == 0) wsum[wave] = make_float2(wm, sum);
-
-  // the K-th largest of the lanes' maxima: at least K of the wave's values reach it
-  uint32_t thr = 0;
+  if (!whole) {                          // what is behind the row is no candidate: NaN is above no threshold
 #pragma unroll
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t t = thr | (1u << bit);
-    if (__popcll(__ballot(kmax >= t)) >= K) thr = t;
+    for (int i = 0; i < PER; ++i)
+      if ((int64_t)v0 + (i >> 2) * (NT * 4) + (i & 3) >= V) x[i] = NAN;
   }
-  thr = thr ? thr : 1;
-  // gather what lies above it, and of what equals it the K lowest tokens
+
+  // The K-th largest of the lanes' maxima, or a little less (its upper 20 bits): at least K of the wave's
+  // values reach it, and few others.
+  uint32_t to = 0;
+  const uint32_t ord = order32(mx);
+#pragma unroll
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t t = to | (1u << bit);
+    if (__popcll(__ballot(ord >= t)) >= K) to = t;
+  }
+  const float thr = from_order32(to > order32(-INFINITY) ? to : order32(-INFINITY));
+  // gather what lies above it, and of what equals it (-inf in a masked vocabulary) the K lowest tokens
   int cnt = 0, eq = 0;
   const uint64_t below = (1ull << lane) - 1;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    uint32_t km = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) km = key[j * 4 + e] > km ? key[j * 4 + e] : km;
-    if (__ballot(km >= thr) == 0) continue;
+    const float m4 = fmaxf(fmaxf(x[j * 4], x[j * 4 + 1]), fmaxf(x[j * 4 + 2], x[j * 4 + 3]));
+    if (__ballot(m4 >= thr) == 0) continue;
     uint64_t at[4];
     int lower = 0, all = 0;               // equal ones of lower lanes, of all lanes
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      at[e] = __ballot(key[j * 4 + e] == thr);
+      at[e] = __ballot(x[j * 4 + e] == thr);
       lower += __popcll(at[e] & below);
       all += __popcll(at[e]);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const uint32_t k = key[j * 4 + e];
-      const bool take = k > thr || (k == thr && eq + lower < K);
-      if (k == thr) ++lower;
+      const float y = x[j * 4 + e];
+      const bool take = y > thr || (y == thr && eq + lower < K);
+      if (y == thr) ++lower;
       const uint64_t m = __ballot(take);
       const int p = cnt + __popcll(m & below);
-      if (take && p < WCAP) list[wave][p] = row_key(k, v0 + j * (NT * 4) + e);
+      if (take && p < WCAP) list[wave][p] = row_key(order32(y), v0 + j * (NT * 4) + e);
       cnt += __popcll(m);
     }
     eq += all;
@@ -170,7 +165,7 @@ __global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, in
       uint64_t mine = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const uint64_t c = key[i] ? row_key(key[i], v0 + (i >> 2) * (NT * 4) + (i & 3)) : 0;
+        const uint64_t c = x[i] == x[i] ? row_key(order32(x[i]), v0 + (i >> 2) * (NT * 4) + (i & 3)) : 0;
         if (c < last && c > mine) mine = c;
       }
 #pragma unroll
@@ -212,142 +207,172 @@ __global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, in
 
 enum { BEAM_PLAIN, BEAM_ENDED, BEAM_NAN, BEAM_LOST };   // LOST: every value is -inf
 
-__global__ void __launch_bounds__(NT) beam_pick(zoact_beams b, int splits, const float2* __restrict__ sums,
+// One workgroup a prompt.  Candidates are compared as (key, place): the value's order, then minus beam and token, so
+// that the larger one comes first.
+__global__ void __launch_bounds__(NP) beam_pick(zoact_beams b, int splits, const float2* __restrict__ sums,
                                                 const Cand* __restrict__ cand) {
-  constexpr int CAP = 1024;
+  constexpr int CAP = 1024, WAVES = NP / 64;
   __shared__ double lse[KMAX], sc[KMAX];
+  __shared__ float top[KMAX];
   __shared__ int kind[KMAX];
-  __shared__ uint64_t key[CAP];
-  __shared__ int64_t flat[CAP];
-  __shared__ uint64_t tmax[NT], thr;
+  __shared__ uint64_t key[CAP], place[CAP];
+  __shared__ uint64_t wkey[WAVES], wplace[WAVES];
+  __shared__ uint32_t wthr[WAVES];
   __shared__ int n_got;
-  __shared__ uint64_t wkey[4];
-  __shared__ int64_t wflat[4];
   __shared__ int parent[KMAX];
-  const int i0 = blockIdx.x, BI = b.beams_in, K = b.beams, V = (int)b.vocab;
+  const int i0 = blockIdx.x, BI = b.beams_in, K = b.beams;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  if (threadIdx.x == 0) n_got = 0, thr = 0;
-  for (int j = wave; j < BI; j += 4) {
-    const int64_t row = (int64_t)i0 * BI + j;
-    const double s = (double)b.score[row];
+  if (threadIdx.x == 0) n_got = 0;
+  // (asked for before the sums are joined)
+  const bool mine_j = (int)threadIdx.x < BI;
+  const int64_t row_j = (int64_t)i0 * BI + (mine_j ? threadIdx.x : 0);
+  const float score_j = b.score[row_j];
+  const bool ended_j = b.eos >= 0 && b.length > 0 && b.hist[row_j * b.ld_hist + b.length - 1] == b.eos;
+  const uint32_t per = (uint32_t)splits * (uint32_t)K, total = (uint32_t)BI * per;      // (at most 2^30)
+  constexpr int KEEP = 4;                // candidates that a thread keeps from the first look to the second
+  Cand raw[KEEP];
+#pragma unroll
+  for (int q = 0; q < KEEP; ++q) {
+    const uint32_t c = threadIdx.x + q * NP;
+    raw[q] = c < total ? cand[(int64_t)i0 * total + c] : Cand{0.f, -1};
+  }
+  for (int j = wave; j < BI; j += WAVES) {
+    const float2* const p = sums + ((int64_t)i0 * BI + j) * splits;
+    const float2 first = lane < splits ? p[lane] : make_float2(-INFINITY, 0.f);
+    float M = first.x;
+    for (int t = lane + 64; t < splits; t += 64) M = fmaxf(M, p[t].x);
+    M = wave_max(M);
+    // (a part of nothing but -inf has the sum 0, or NaN)
+    auto part = [&](float2 y) { return y.x == -INFINITY ? y.y : y.y * expf(y.x - M); };
+    float S = part(first);
+    for (int t = lane + 64; t < splits; t += 64) S += part(p[t]);
+    S = wave_sum(S);
+    if (lane == 0) lse[j] = (double)S, top[j] = M;
+  }
+  __syncthreads();
+  if (mine_j) {
+    const int j = threadIdx.x;
+    const double s = (double)score_j, l = (double)top[j] + log(lse[j]);
     int kd = BEAM_PLAIN;
-    double l = 0.0;
     if (s != s || s == INFINITY) kd = BEAM_NAN;
-    else if (b.eos >= 0 && b.length > 0 && b.hist[row * b.ld_hist + b.length - 1] == b.eos)
-      kd = s == -INFINITY ? BEAM_LOST : BEAM_ENDED;
-    else {
-      float M = -INFINITY;
-      for (int t = lane; t < splits; t += 64) M = fmaxf(M, sums[row * splits + t].x);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-      double S = 0.0;
-      for (int t = lane; t < splits; t += 64) {
-        const float2 p = sums[row * splits + t];
-        // (a part of nothing but -inf has the sum 0, or NaN)
-        S += p.x == -INFINITY ? (double)p.y : (double)p.y * exp((double)p.x - (double)M);
-      }
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) S += __shfl_xor(S, o, 64);
-      l = (double)M + log(S);
-      if (!(l - l == 0.0)) kd = BEAM_NAN;
-      else if (s == -INFINITY) kd = BEAM_LOST;
-    }
-    if (lane == 0) lse[j] = l, sc[j] = s, kind[j] = kd;
+    else if (ended_j) kd = s == -INFINITY ? BEAM_LOST : BEAM_ENDED;      // (nothing was left of its row)
+    else if (!(l - l == 0.0)) kd = BEAM_NAN;
+    else if (s == -INFINITY) kd = BEAM_LOST;
+    lse[j] = l, sc[j] = s, kind[j] = kd;
   }
   __syncthreads();
   // Candidate c of the prompt: beam j's part and place, or for beams whose values do not follow the
   // logits the lowest tokens (an ended one's eos first).
-  const int per = splits * K;
-  const int64_t total = (int64_t)BI * per;
-  auto read = [&](int64_t c, uint64_t& k, int64_t& f) {
-    const int j = (int)(c / per), t = (int)(c - (int64_t)j * per);
-    k = 0;
-    f = 0;
+  auto place_at = [](uint32_t j, int v) { return ~(((uint64_t)j << 32) | (uint32_t)v); };
+  auto rate = [&](uint32_t c, Cand d, uint64_t& k, uint64_t& f) {
+    const uint32_t j = c / per, t = c - j * per;
+    k = f = 0;
     if (kind[j] == BEAM_PLAIN) {
-      const Cand d = cand[((int64_t)i0 * BI + j) * per + t];
       if (d.v < 0) return;
       k = order64(sc[j] + ((double)d.x - lse[j]));
-      f = (int64_t)j * V + d.v;
-    } else if (t < K) {
-      int v = t;
+      f = place_at(j, d.v);
+    } else if (t < (uint32_t)K) {
+      int v = (int)t;
       double val = kind[j] == BEAM_NAN ? (double)NAN : -INFINITY;
-      if (kind[j] == BEAM_ENDED && b.eos < V) {
+      if (kind[j] == BEAM_ENDED) {
         if (t == 0) v = b.eos, val = sc[j];
-        else v = t - 1 < b.eos ? t - 1 : t;
+        else v = (int)t - 1 < b.eos ? (int)t - 1 : (int)t;
       }
       k = order64(val);
-      f = (int64_t)j * V + v;
+      f = place_at(j, v);
     }
   };
-  auto better = [](uint64_t k, int64_t f, uint64_t k2, int64_t f2) { return k > k2 || (k == k2 && f < f2); };
-  auto value = [](uint64_t k) -> float {
-    if (k == ~0ull) return NAN;
-    return (float)__longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
-  };
-  auto emit = [&](int m, uint64_t k, int64_t f) {
-    const int j = (int)(f / V), v = (int)(f - (int64_t)j * V);
+  auto read = [&](uint32_t c, uint64_t& k, uint64_t& f) { rate(c, cand[(int64_t)i0 * total + c], k, f); };
+  auto better = [](uint64_t k, uint64_t f, uint64_t k2, uint64_t f2) { return k > k2 || (k == k2 && f > f2); };
+  auto emit = [&](int m, uint64_t k, uint64_t f) {
+    const int j = (int)(~f >> 32), v = (int)(uint32_t)~f;
     const int64_t o = (int64_t)i0 * K + m;
-    b.score_out[o] = value(k);
+    b.score_out[o] = k == ~0ull ? NAN : (float)__longlong_as_double((long long)((k >> 63) ? k & ~(1ull << 63) : ~k));
     if (b.token) b.token[o] = v;
     if (b.src) b.src[o] = i0 * K + j;
     b.hist_out[o * b.ld_hist_out + b.length] = v;
     parent[m] = j;
   };
-  uint64_t mine = 0;
-  for (int64_t c = threadIdx.x; c < total; c += NT) {
-    uint64_t k;
-    int64_t f;
+  const bool few = total <= 128;         // all of them are ranked then
+  uint64_t kk[KEEP], kf[KEEP], mine = 0;
+#pragma unroll
+  for (int q = 0; q < KEEP; ++q) {
+    kk[q] = kf[q] = 0;
+    const uint32_t c = threadIdx.x + q * NP;
+    if (c < total) rate(c, raw[q], kk[q], kf[q]);
+    mine = kk[q] > mine ? kk[q] : mine;
+  }
+#pragma unroll 8
+  for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
+    uint64_t k, f;
     read(c, k, f);
     mine = k > mine ? k : mine;
   }
-  tmax[threadIdx.x] = mine;
-  __syncthreads();
-  {
-    int rank = 0;
-    for (int t = 0; t < NT; ++t) rank += tmax[t] > mine || (tmax[t] == mine && t < (int)threadIdx.x);
-    if (rank == K - 1) thr = mine ? mine : 1;
-  }
-  __syncthreads();
-  for (int64_t c = threadIdx.x; c < total; c += NT) {
-    uint64_t k;
-    int64_t f;
-    read(c, k, f);
-    if (k >= thr) {
-      const int p = atomicAdd(&n_got, 1);      // (the order of arrival changes nothing: ranks decide)
-      if (p < CAP) key[p] = k, flat[p] = f;
+  // In each wave the K-th largest of the lanes' maxima, or a little less (20 bits of it), is reached by K
+  // candidates at least: the largest of the waves' is the threshold.
+  uint64_t thr = 1;
+  if (!few) {
+    uint32_t to = 0;
+    const uint32_t upper = (uint32_t)(mine >> 32);
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) {
+      const uint32_t x = to | (1u << bit);
+      if (__popcll(__ballot(upper >= x)) >= K) to = x;
     }
+    if (lane == 0) wthr[wave] = to;
+    __syncthreads();
+    uint32_t most = 0;
+#pragma unroll
+    for (int u = 0; u < WAVES; ++u) most = wthr[u] > most ? wthr[u] : most;
+    thr = most ? (uint64_t)most << 32 : 1;
+  }
+  auto gather = [&](uint64_t k, uint64_t f) {
+    if (k < thr) return;
+    const int p = atomicAdd(&n_got, 1);  // (the order of arrival changes nothing: ranks decide)
+    if (p < CAP) key[p] = k, place[p] = f;
+  };
+#pragma unroll
+  for (int q = 0; q < KEEP; ++q) gather(kk[q], kf[q]);
+#pragma unroll 8
+  for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
+    uint64_t k, f;
+    read(c, k, f);
+    gather(k, f);
   }
   __syncthreads();
   const int got = n_got;
   if (got <= CAP) {
-    for (int c = threadIdx.x; c < got; c += NT) {
-      int rank = 0;
-      for (int t = 0; t < got; ++t) rank += better(key[t], flat[t], key[c], flat[c]);
-      if (rank < K) emit(rank, key[c], flat[c]);
+    // (a candidate's rank is counted by as many neighbouring threads as there are for each, up to 16)
+    int each = 16;
+    while (each * got > NP) each >>= 1;
+    const int c = threadIdx.x / each;
+    int rank = 0;
+    uint64_t k = 0, f = 0;
+    if (c < got) {
+      k = key[c], f = place[c];
+      for (int t = threadIdx.x & (each - 1); t < got; t += each) rank += better(key[t], place[t], k, f);
     }
+    for (int o = each >> 1; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
+    if (c < got && rank < K && (threadIdx.x & (each - 1)) == 0) emit(rank, k, f);
   } else {
     // very many equal ones: one at a time
-    uint64_t lk = ~0ull;
-    int64_t lf = -1;
+    uint64_t lk = ~0ull, lf = ~0ull;
     for (int m = 0; m < K; ++m) {
-      uint64_t bk = 0;
-      int64_t bf = 0;
-      for (int64_t c = threadIdx.x; c < total; c += NT) {
-        uint64_t k;
-        int64_t f;
+      uint64_t bk = 0, bf = 0;
+      for (uint32_t c = threadIdx.x; c < total; c += NP) {
+        uint64_t k, f;
         read(c, k, f);
         if (k && better(lk, lf, k, f) && better(k, f, bk, bf)) bk = k, bf = f;
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
-        const uint64_t k = __shfl_xor((unsigned long long)bk, o, 64);
-        const int64_t f = __shfl_xor((long long)bf, o, 64);
+        const uint64_t k = __shfl_xor((unsigned long long)bk, o, 64), f = __shfl_xor((unsigned long long)bf, o, 64);
         if (better(k, f, bk, bf)) bk = k, bf = f;
       }
-      if (lane == 0) wkey[wave] = bk, wflat[wave] = bf;
+      if (lane == 0) wkey[wave] = bk, wplace[wave] = bf;
       __syncthreads();
-      for (int u = 0; u < 4; ++u)
-        if (better(wkey[u], wflat[u], bk, bf)) bk = wkey[u], bf = wflat[u];
+      for (int u = 0; u < WAVES; ++u)
+        if (better(wkey[u], wplace[u], bk, bf)) bk = wkey[u], bf = wplace[u];
       if (threadIdx.x == 0) emit(m, bk, bf);
       lk = bk;
       lf = bf;
@@ -355,9 +380,9 @@ __global__ void __launch_bounds__(NT) beam_pick(zoact_beams b, int splits, const
     }
   }
   __syncthreads();
-  for (int64_t c = threadIdx.x; c < K * b.length; c += NT) {
-    const int m = (int)(c / b.length);
-    const int64_t t = c - m * b.length;
+  const uint32_t len = (uint32_t)b.length;
+  for (uint64_t c = threadIdx.x; c < (uint64_t)K * len; c += NP) {
+    const uint32_t m = (uint64_t)K * len >> 32 ? (uint32_t)(c / len) : (uint32_t)c / len, t = (uint32_t)(c - (uint64_t)m * len);
     b.hist_out[((int64_t)i0 * K + m) * b.ld_hist_out + t] = b.hist[((int64_t)i0 * BI + parent[m]) * b.ld_hist + t];
   }
 }
@@ -385,7 +410,8 @@ extern "C" zoact_status zoact_beam_select(const zoact_beams* b, const void* logi
   ZP_CHECK(b->vocab >= b->beams && b->vocab <= (int64_t(1) << 30), "beam_select: vocab outside [beams, 2^30]");
   ZP_CHECK(ldl >= b->vocab, "beam_select: rows of logits overlap");
   ZP_CHECK(b->eos >= -1 && b->eos < b->vocab, "beam_select: eos outside [-1, vocab)");
-  ZP_CHECK(b->length >= 0 && (b->length == 0 || (b->hist && b->length <= b->ld_hist)) && b->length < b->ld_hist_out,
+  ZP_CHECK(b->length >= 0 && (b->length == 0 || (b->hist && b->length <= b->ld_hist)) && b->length < b->ld_hist_out &&
+               b->length < (int64_t(1) << 31),
            "beam_select: histories do not hold the tokens");
   ZP_CHECK(aligned_to(logits, dtype == ZOACT_F32 ? 4 : 2) && aligned_to(b->score, 4) && aligned_to(b->score_out, 4) &&
                aligned_to(b->hist, 4) && aligned_to(b->hist_out, 4) && aligned_to(b->token, 4) && aligned_to(b->src, 4),
@@ -407,6 +433,6 @@ extern "C" zoact_status zoact_beam_select(const zoact_beams* b, const void* logi
     else ZO_ROWS(uint16_t, false);
   }
 #undef ZO_ROWS
-  beam_pick<<<(unsigned)b->n, NT, 0, s>>>(*b, l.splits, sums, cand);
+  beam_pick<<<(unsigned)b->n, NP, 0, s>>>(*b, l.splits, sums, cand);
   return launched_or("beam_select");
 }

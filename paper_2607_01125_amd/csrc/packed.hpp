@@ -36,6 +36,32 @@ hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t
                                    const void* v, int64_t ldv, int32_t heads, int32_t kv_heads, int32_t hd, float scale,
                                    int32_t dtype, void* out, hipStream_t hs);
 
+// Lane 63 of the wave gets op over all lanes (`none` where a lane has no partner), every lane the result.
+template <typename Op>
+__device__ __forceinline__ int wave_reduce(int x, int none, Op op) {
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x111, 0xf, 0xf, false));   // row_shr:1
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x112, 0xf, 0xf, false));   // row_shr:2
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x114, 0xf, 0xf, false));   // row_shr:4
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x118, 0xf, 0xf, false));   // row_shr:8
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x142, 0xa, 0xf, false));   // row_bcast:15
+  x = op(x, __builtin_amdgcn_update_dpp(none, x, 0x143, 0xc, 0xf, false));   // row_bcast:31
+  return __builtin_amdgcn_readlane(x, 63);
+}
+__device__ __forceinline__ int wave_sum(int x) {
+  return wave_reduce(x, 0, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  return __int_as_float(wave_reduce(__float_as_int(x), 0, [](int a, int b) {
+    return __float_as_int(__int_as_float(a) + __int_as_float(b));
+  }));
+}
+// (NaN stays out)
+__device__ __forceinline__ float wave_max(float x) {
+  return __int_as_float(wave_reduce(__float_as_int(x), (int)0xFF800000u, [](int a, int b) {
+    return __float_as_int(fmaxf(__int_as_float(a), __int_as_float(b)));
+  }));
+}
+
 // The last i with begin[i] <= row, or -1: row's sequence if row < begin[i + 1].
 __device__ __forceinline__ int packed_find(const int32_t* __restrict__ begin, int n, int row) {
   int lo = -1, hi = n;                  // begin[lo] <= row < begin[hi + 1], as far as they exist
