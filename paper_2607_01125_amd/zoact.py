@@ -885,31 +885,51 @@ class Packed:
         return cls(torch.tensor(begin, dtype=torch.int32, device=device), begin[-1], max(lengths))
 
 
+def _plain(t: torch.Tensor, dtype, dev: int, shape) -> bool:
+    """Whether an argument is a contiguous tensor of this type, device and shape (what _arg checks, at once)."""
+    return t.dtype is dtype and t.get_device() == dev and t.shape == shape and t.is_contiguous()
+
+
+def _rows_of(t: torch.Tensor, name: str, dtype, dev: int, shape):
+    """What _heads_arg gives, for rows that are apart in the usual way with less work."""
+    if t.dtype is dtype and t.get_device() == dev and t.shape == shape:
+        ld, unit = t.stride()
+        if unit == 1 and ld >= shape[1]:
+            return t.data_ptr(), ld
+    return _heads_arg(t, name, dtype, dev, *shape)
+
+
 def attention_packed(seqs: Packed, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, n_heads: int,
                      n_kv_heads: int, head_dim: int, scale: float, stream=None):
     """Causal attention within each sequence; q, k, v may be column slices of wider row-major buffers."""
-    dev, dt, rows = seqs.index, out.dtype, seqs.rows
-    qp, ldq = _heads_arg(q, "q", dt, dev, rows, n_heads * head_dim)
-    kp, ldk = _heads_arg(k, "k", dt, dev, rows, n_kv_heads * head_dim)
-    vp, ldv = _heads_arg(v, "v", dt, dev, rows, n_kv_heads * head_dim)
-    op = _arg(out, "out", dt, dev, (rows, n_heads * head_dim))
-    _on_device(lib().zoact_attention_packed, dev, stream, seqs._ref, qp, ldq, kp, ldk, vp, ldv, n_heads, n_kv_heads,
-               head_dim, scale, dtype_code(out), op)
+    ref, dev, dt, rows = seqs._ref, seqs.index, out.dtype, seqs.rows
+    wq, wk = n_heads * head_dim, n_kv_heads * head_dim
+    qp, ldq = _rows_of(q, "q", dt, dev, (rows, wq))
+    kp, ldk = _rows_of(k, "k", dt, dev, (rows, wk))
+    vp, ldv = _rows_of(v, "v", dt, dev, (rows, wk))
+    if not _plain(out, dt, dev, (rows, wq)):
+        _arg(out, "out", dt, dev, (rows, wq))
+    _on_device(lib().zoact_attention_packed, dev, stream, ref, qp, ldq, kp, ldk, vp, ldv, n_heads, n_kv_heads, head_dim,
+               scale, dtype_code(out), out.data_ptr())
 
 
 def rope_at(x: torch.Tensor, out: torch.Tensor, n_heads: int, head_dim: int, pos: torch.Tensor | None,
             cos_t: torch.Tensor, sin_t: torch.Tensor, layout: int = ROPE_HALF, stream=None):
     """out = x with the first 2 * cos_t.shape[1] values of each head turned to the rows' positions pos (None:
     their indexes); x and out [rows][n_heads * head_dim] may be column slices, and the same one."""
-    dev, dt, f32 = _device(x), x.dtype, torch.float32
-    rows = x.shape[0] if x.dim() == 2 else -1
-    xp, ldx = _heads_arg(x, "x", dt, dev, rows, n_heads * head_dim)
-    op, ldo = _heads_arg(out, "out", dt, dev, rows, n_heads * head_dim)
-    if cos_t.dim() != 2:
-        raise ValueError("rope_at: tables must be [n_pos][rot_dim / 2]")
-    cp, sp = _arg(cos_t, "cos", f32, dev), _arg(sin_t, "sin", f32, dev, cos_t.shape)
-    _on_device(lib().zoact_rope_at, dev, stream, xp, ldx, op, ldo, dtype_code(x), rows, n_heads, head_dim,
-               2 * cos_t.shape[1], layout, _arg(pos, "pos", torch.int32, dev, (rows,)), cp, sp, cos_t.shape[0])
+    dev, dt, f32, shape, tab = x.get_device(), x.dtype, torch.float32, x.shape, cos_t.shape
+    if dev < 0 or len(shape) != 2 or len(tab) != 2:
+        raise ValueError("rope_at: expected x [rows][heads * head_dim] on a device, tables [n_pos][rot_dim / 2]")
+    rows, shape = shape[0], (shape[0], n_heads * head_dim)
+    xp, ldx = _rows_of(x, "x", dt, dev, shape)
+    op, ldo = (xp, ldx) if out is x else _rows_of(out, "out", dt, dev, shape)
+    for t, name in ((cos_t, "cos"), (sin_t, "sin")):
+        if not _plain(t, f32, dev, tab):
+            _arg(t, name, f32, dev, tab)
+    if pos is not None and not _plain(pos, torch.int32, dev, (rows,)):
+        _arg(pos, "pos", torch.int32, dev, (rows,))
+    _on_device(lib().zoact_rope_at, dev, stream, xp, ldx, op, ldo, dtype_code(x), rows, n_heads, head_dim, 2 * tab[1],
+               layout, None if pos is None else pos.data_ptr(), cos_t.data_ptr(), sin_t.data_ptr(), tab[0])
 
 
 def rope_tables(n_pos: int, rot_dim: int, theta: float, device="cuda", *, factor: float = 1.0, original: int = 0,
@@ -954,20 +974,42 @@ def linear_xent_packed(layer: Linear, arena: Arena | None, x: torch.Tensor, toke
 def xent_packed(logits: torch.Tensor, tokens: torch.Tensor, seqs: Packed, loss_pm: torch.Tensor, ws: torch.Tensor,
                 stream=None):
     """Next-token cross entropy of both halves over packed rows, from logits fp32 [2][rows][vocab]."""
-    dev, rows, f32 = seqs.index, seqs.rows, torch.float32
-    if logits.dim() != 3:
+    ref, dev, rows, f32, shape = seqs._ref, seqs.index, seqs.rows, torch.float32, logits.shape
+    if len(shape) != 3:
         raise ValueError("xent_packed: logits must be [2][rows][vocab]")
-    lp = _arg(logits, "logits", f32, dev, (2, rows, logits.shape[2]))
-    _on_device(lib().zoact_xent_packed, dev, stream, lp, _arg(tokens, "tokens", torch.int32, dev, (rows,)), seqs._ref,
-               logits.shape[2], _arg(loss_pm, "loss_pm", f32, dev, (2,)), *_ws(ws, dev))
+    if not _plain(logits, f32, dev, (2, rows, shape[2])):
+        _arg(logits, "logits", f32, dev, (2, rows, shape[2]))
+    if not _plain(tokens, torch.int32, dev, (rows,)):
+        _arg(tokens, "tokens", torch.int32, dev, (rows,))
+    _on_device(lib().zoact_xent_packed, dev, stream, logits.data_ptr(), tokens.data_ptr(), ref, shape[2],
+               _arg(loss_pm, "loss_pm", f32, dev, (2,)), *_ws(ws, dev))
 
 
 @dataclass(frozen=True)
 class Beams:
     """Candidates of a beam search: summed log probabilities fp32 [n][beams] and tokens int32
-    [n][beams][room]."""
+    [n][beams][room].  Checked here, and again where a tensor has other memory."""
     score: torch.Tensor
     hist: torch.Tensor
+
+    def __post_init__(self):
+        if self.score.dim() != 2 or self.hist.dim() != 3:
+            raise ValueError("beams: expected score [n][beams] and hist [n][beams][room]")
+        (n, b), room, dev = self.score.shape, self.hist.shape[2], _device(self.score)
+        object.__setattr__(self, "_kept", (_arg(self.score, "score", torch.float32, dev),
+                                           _arg(self.hist, "hist", torch.int32, dev, (n, b, room)), dev, n, b, room))
+
+    def __reduce__(self):               # (a copy is checked anew)
+        return Beams, (self.score, self.hist)
+
+    @property
+    def _at(self):
+        """(address of score, of hist, device, n, beams, room)"""
+        k = self._kept
+        if k[0] != self.score.data_ptr() or k[1] != self.hist.data_ptr():
+            self.__post_init__()
+            k = self._kept
+        return k
 
     @classmethod
     def alloc(cls, n: int, beams: int, room: int, device="cuda"):
@@ -984,14 +1026,16 @@ def beam_select(logits: torch.Tensor, now: Beams, length: int, eos: int | None, 
     """Keep the likeliest candidates of each prompt in `to`, of those in `now` (with `length` tokens each) continued
     by every token; logits [n * beams][vocab] (rows may be apart).  token, src int32 [n * beams of `to`]: the
     kept tokens, and the slots prompt * beams + beam that they continue."""
-    dev, i32 = _device(logits), torch.int32
-    if now.score.dim() != 2 or to.score.dim() != 2 or now.hist.dim() != 3 or to.hist.dim() != 3 or logits.dim() != 2:
-        raise ValueError("beam_select: expected scores [n][beams], hist [n][beams][room] and logits [rows][vocab]")
-    (n, bi), b, V = now.score.shape, to.score.shape[1], logits.shape[1]
-    lp, ldl = _heads_arg(logits, "logits", logits.dtype, dev, n * bi, V)
-    d = BeamsDesc(n, bi, b, -1 if eos is None else eos, V, length, _arg(now.score, "score", torch.float32, dev),
-                  _arg(now.hist, "hist", i32, dev, (n, bi, now.hist.shape[2])), now.hist.shape[2],
-                  _arg(to.score, "to.score", torch.float32, dev, (n, b)),
-                  _arg(to.hist, "to.hist", i32, dev, (n, b, to.hist.shape[2])), to.hist.shape[2],
-                  _arg(token, "token", i32, dev, (n * b,)), _arg(src, "src", i32, dev, (n * b,)))
+    (sp, hp, dev, n, bi, room), (sop, hop, dev_to, n_to, b, room_to) = now._at, to._at
+    if dev != dev_to or n != n_to:
+        raise ValueError("beam_select: candidates of other prompts, or on another device")
+    shape, dt, i32 = logits.shape, logits.dtype, torch.int32
+    if len(shape) != 2:
+        raise ValueError("beam_select: logits must be [n * beams][vocab]")
+    lp, ldl = _rows_of(logits, "logits", dt, dev, (n * bi, shape[1]))
+    for t, name in ((token, "token"), (src, "src")):
+        if t is not None and not _plain(t, i32, dev, (n * b,)):
+            _arg(t, name, i32, dev, (n * b,))
+    d = BeamsDesc(n, bi, b, -1 if eos is None else eos, shape[1], length, sp, hp, room, sop, hop, room_to,
+                  None if token is None else token.data_ptr(), None if src is None else src.data_ptr())
     _on_device(lib().zoact_beam_select, dev, stream, ctypes.byref(d), lp, ldl, dtype_code(logits), *_ws(ws, dev))
