@@ -32,8 +32,6 @@ typedef struct {
   const int32_t* begin; /* [n + 1]                                                     */
   int32_t n;            /* sequences, 1 .. 2^24                                        */
   int64_t rows;         /* rows of the tensors, 0 .. 2^31 - 1024                       */
-  int64_t max_len;      /* host: a length that no sequence is expected to pass; shapes
-                           the split of the work only, longer ones are served too      */
 } zoact_packed;
 
 /* Causal attention within each sequence: for rows t of sequence i and heads h,
@@ -58,8 +56,8 @@ zoact_status zoact_attention_packed(const zoact_packed* s, const void* q, int64_
  * (x[2 j], x[2 j + 1]) with ZOACT_ROPE_INTERLEAVED.  x and out [rows][ldo] in dtype, out
  * may be x itself (ldo == ldx) and must not overlap it otherwise; tables fp32
  * [n_pos][rot_dim / 2].  fp32 arithmetic, one rounding of out.  1 <= rot_dim / 2,
- * rot_dim even and at most head_dim; tables and pos 4-byte aligned, x and out to their
- * type. */
+ * rot_dim even and at most head_dim, n_heads * head_dim < 2^31; tables and pos 4-byte
+ * aligned, x and out to their type. */
 enum { ZOACT_ROPE_HALF = 0, ZOACT_ROPE_INTERLEAVED = 1 };
 zoact_status zoact_rope_at(const void* x, int64_t ldx, void* out, int64_t ldo, int32_t dtype, int64_t rows,
                            int32_t n_heads, int32_t head_dim, int32_t rot_dim, int32_t layout, const int32_t* pos,
@@ -90,13 +88,13 @@ zoact_status zoact_linear_xent_packed(const zoact_linear* L, const zoact_arena* 
  * is not finite (a NaN or +inf among its logits, or nothing but -inf) gives NaN, and so
  * does a score of NaN or +inf.  Kept candidate m of prompt i:
  *   score_out[i][m] its value, token[i][m] = v, src[i][m] = i * beams + b (where beam b's
- *   sequence lives, for zoact_cache_fork), hist_out[i][m] = hist[i][b], then v.
+ *   sequence lives, for zoact_cache_fork, if beams_in <= beams), hist_out[i][m] = hist[i][b], then v.
  * Values are compared in fp64 from fp32 sums and rounded once.  logits [n * beams_in][ldl]
  * in dtype (F32 or BF16, aligned to its type), score, score_out fp32, hist
  * [n][beams_in][ld_hist], hist_out [n][beams][ld_hist_out], token, src int32 [n * beams]
  * (token and src may be NULL); 0 <= length <= ld_hist, length < ld_hist_out.  Outputs must
  * not overlap inputs.  1 <= beams_in, beams <= ZOACT_BEAMS_MAX, beams <= vocab <= 2^30,
- * n * beams_in <= 65535.  ws: zoact_beam_workspace_bytes() bytes, 16-byte aligned. */
+ * n * beams_in <= 65535, length < 2^31.  ws: zoact_beam_workspace_bytes() bytes, 16-byte aligned. */
 enum { ZOACT_BEAMS_MAX = 64 };
 typedef struct {
   int32_t n;

@@ -14,6 +14,9 @@
 // head a wave; K and V tiles go through LDS for all four, chunks of 16 bytes swizzled so that
 // neither the K rows nor the V columns (read transposed by ds_read_tr16) meet in a bank.
 //
+// Where a maximum passes 2^27 the fused S^T c - m is off by the rounding of the product that became m, which 2^x no
+// longer bears: such a wave takes its rows one by one in the end.
+//
 // Keys that some of a wave's rows may not see are in its last tiles only, from its first row's tile
 // of 32 on; there the scores are masked, and where a masked V is not finite (0 * inf is NaN) the
 // product runs on the vector unit, for the rows that see each key.
@@ -106,9 +109,11 @@ __device__ __forceinline__ Place longest_first(const zoact_packed& s, int64_t sl
   const int above = wave_sum(tiles > t + 1 ? tiles - t - 1 : 0);
   const int rank = __popcll(__ballot(tiles > t) & ((1ull << lane) - 1));
   const int who = __ffsll((unsigned long long)__ballot(tiles > t && rank == k - above)) - 1;
-  const int row0 = __builtin_amdgcn_readlane(b, who);
+  const int row0 = __builtin_amdgcn_readlane(b, who), end = __builtin_amdgcn_readlane(e, who);
+  // (nobody where bounds that do not ascend count more tiles than 32 bits hold)
+  if (row0 < 0 || end <= row0 || end > s.rows || ((int64_t)t << sh) >= end - row0) return p;
   p.row0 = row0;
-  p.len = __builtin_amdgcn_readlane(e, who) - row0;
+  p.len = end - row0;
   p.q0 = t << sh;
   return p;
 }
@@ -174,7 +179,7 @@ struct Tile {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(256, 2)
+__global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
     attention_packed_bf16_kernel(zoact_packed s, const uint16_t* __restrict__ q, int64_t ldq,
                                  const uint16_t* __restrict__ k, int64_t ldk, const uint16_t* __restrict__ v, int64_t ldv,
                                  int heads, int kv_heads, int gh, float scale, uint16_t* __restrict__ out) {
@@ -224,8 +229,9 @@ __global__ void __launch_bounds__(256, 2)
   }
   const float c2 = fabsf(scale) * 1.4426950408889634f;
 
+  bool far = false;                      // the wave's scores are too large for all this
   floatx16 o[NB];
-  float l = 0.f, m = -1.0e38f;           // (finite: a score of -inf has weight 0 also where nothing else came before)
+  float l = 0.f, m = -3.4028235e38f;     // (finite: a score of -inf has weight 0 also where nothing else came before)
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -257,6 +263,7 @@ __global__ void __launch_bounds__(256, 2)
     if (__ballot(mx > m + 8.f)) {
       const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
+      if (__ballot(fabsf(m) > 0x1p27f)) far = true;
       l *= a;
 #pragma unroll
       for (int n = 0; n < NB; ++n) o[n] *= a;
@@ -408,6 +415,13 @@ __global__ void __launch_bounds__(256, 2)
   const float inv = 1.f / (l + __shfl_xor(l, 32, 64));
   __syncthreads();
   char* const mine = (wave < 2 ? k0 : k1) + wave % 2 * 32 * ROW;
+  if (far) {
+    for (int r = w0; r < w0 + 32 && r < len; ++r)
+      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
+                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, reinterpret_cast<float*>(mine),
+                 out + ((pl.row0 + r) * heads + h) * HD);
+    return;
+  }
 #pragma unroll
   for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -491,8 +505,9 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
   }
   const float c2 = fabsf(scale) * 1.4426950408889634f;
 
+  bool far = false;                                          // the wave's scores are too large for all this
   floatx4 o[NV][W];                                          // o[n][e][i]: column 16 W n + W (4 lg + i) + e
-  float l = 0.f, m = -1.0e38f;           // (finite: a score of -inf has weight 0 also where nothing else came before)
+  float l = 0.f, m = -3.4028235e38f;     // (finite: a score of -inf has weight 0 also where nothing else came before)
 #pragma unroll
   for (int n = 0; n < NV; ++n)
 #pragma unroll
@@ -523,6 +538,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     if (__ballot(mx > m + 8.f)) {
       const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
+      if (__ballot(fabsf(m) > 0x1p27f)) far = true;
       l *= a;
 #pragma unroll
       for (int n = 0; n < NV; ++n)
@@ -647,6 +663,13 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     arrived();
   }
 
+  if (far) {
+    for (int r = w0; r < w0 + 16 && r < len; ++r)
+      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
+                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, &pw[wave][0][0],
+                 out + ((pl.row0 + r) * heads + h) * HD);
+    return;
+  }
   l += __shfl_xor(l, 32, 64);
   l += __shfl_xor(l, 16, 64);
   const float inv = 1.f / l;
@@ -672,12 +695,13 @@ hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t
   if ((hd != 32 && hd != 64 && hd != 128) || ldq % vec || ldk % vec || ldv % vec || !aligned_to(q, 16) ||
       !aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(out, 16))
     return hipErrorNotSupported;
+  if (!isfinite(fabsf(scale) * 1.4426950408889634f)) return hipErrorNotSupported;
   // (a tile's rows are addressed with 32 bits)
   if (ldk >= (int64_t(1) << 22) || ldv >= (int64_t(1) << 22)) return hipErrorNotSupported;
   const int G = heads / kv_heads, gh = G % 4 == 0 ? 4 : G % 2 == 0 ? 2 : 1;
   const int R = 4 / gh * (dtype == ZOACT_BF16 ? 32 : 16);
   const int64_t grid = (s.rows / R + s.n) * (heads / gh);
-  if (grid >= (int64_t(1) << 31)) return hipErrorNotSupported;
+  if (grid >= (int64_t(1) << 24)) return hipErrorNotSupported;    // (a launch has less than 2^32 threads)
 #define ZO_ATT(T, KERNEL, HD)                                                                                     \
   KERNEL<HD><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk, (const T*)v, ldv, heads, kv_heads, \
                                              gh, scale, (T*)out)

@@ -52,8 +52,6 @@ Layout layout_of(int32_t n, int32_t beams_in, int32_t beams, int64_t vocab) {
   return l;
 }
 
-__device__ __forceinline__ float ld1(const float* p) { return *p; }
-__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
 __device__ __forceinline__ void ld4(const float* p, float (&x)[4]) {
   const float4 u = *reinterpret_cast<const float4*>(p);
   x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;

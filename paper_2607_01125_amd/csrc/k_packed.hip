@@ -6,11 +6,6 @@
 namespace zoact {
 namespace {
 
-__device__ __forceinline__ float ld1(const float* p) { return *p; }
-__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
-__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f2bf(v); }
-
 // ---------------------------------------------------------------- rotary positions
 // One thread a pair or a copied value: any head_dim, rot_dim, stride and alignment.
 template <typename T>
@@ -41,8 +36,8 @@ __global__ void __launch_bounds__(256) rope_at_kernel(const T* x, int64_t ldx, T
 
 // Pieces of 16 bytes: a thread takes one place of a row -- a pair of pieces half the turned part apart (HALF), a
 // piece of whole pairs (INTERLEAVED), or a piece to copy -- in RT rows, all of whose loads are on their way before
-// the first is used.  Bound by memory: 16411 rows of 40 heads of 128 bf16 values, 64 of them turned in pairs, a copy
-// of the same bytes ... us.
+// the first is used.  Bound by memory: 16411 rows of 40 heads of 128 bf16 values, 64 of them turned in pairs, 78 us where a
+// copy of the same 337 MB takes 71.
 template <typename T, bool HALF, int RT>
 __global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
                                                            int heads, int hd, int rot, const int32_t* __restrict__ pos,
@@ -120,8 +115,7 @@ bool rope_at_vec(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows, int
 }
 
 // ---------------------------------------------------------------- attention, any shape
-// One wave a (row, head): 64 keys at a time, a key a lane for the scores and a column a lane for
-// the sums, with the running maximum m and sum l of the softmax.
+// One wave a (row, head).
 template <typename T>
 __global__ void __launch_bounds__(256) attention_packed_any(zoact_packed s, const T* __restrict__ q, int64_t ldq,
                                                             const T* __restrict__ k, int64_t ldk,
@@ -134,56 +128,18 @@ __global__ void __launch_bounds__(256) attention_packed_any(zoact_packed s, cons
     const int64_t w = w0 + wave;
     bool live = w < total;
     const int row = live ? (int)(w / heads) : 0, h = live ? (int)(w - (int64_t)row * heads) : 0;
-    int b0 = 0;
+    int64_t b0 = 0;
     if (live) {
       const int i = packed_find(s.begin, s.n, row);
       live = i >= 0 && i < s.n && row < s.begin[i + 1];
       if (live) b0 = s.begin[i];
       live = live && b0 >= 0;
     }
-    __syncthreads();
-    if (live)
-      for (int d = lane; d < hd; d += 64) qs[wave][d] = ld1(q + (int64_t)row * ldq + (int64_t)h * hd + d);
-    __syncthreads();
     if (!live) continue;
     const int g = h / (heads / kv_heads);
-    const T* kp = k + (int64_t)g * hd;
-    const T* vp = v + (int64_t)g * hd;
-    // (-inf scores, which a formula's softmax gives weight 0, stay below every m)
-    float m = -3.4028235e38f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int key0 = b0; key0 <= row; key0 += 64) {
-      const int key = key0 + lane;
-      float sc = -INFINITY;
-      if (key <= row) {
-        const T* kr = kp + (int64_t)key * ldk;
-        float t = 0.f;
-        for (int d = 0; d < hd; ++d) t = fmaf(qs[wave][d], ld1(kr + d), t);
-        sc = t * scale;
-      }
-      float mx = sc == sc ? sc : -INFINITY;
-#pragma unroll
-      for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-      const float mn = fmaxf(m, mx);
-      const float p = key <= row ? expf(sc - mn) : 0.f, a = expf(m - mn);
-      m = mn;
-      l = l * a + p;
-      const int cnt = row - key0 + 1 < 64 ? row - key0 + 1 : 64;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] *= a;
-      for (int t = 0; t < cnt; ++t) {
-        const float pt = __shfl(p, t, 64);
-        const T* vr = vp + (int64_t)(key0 + t) * ldv;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e * 64 + lane < hd) o[e] = fmaf(pt, ld1(vr + e * 64 + lane), o[e]);
-      }
-    }
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-    T* op = out + (int64_t)row * heads * hd + (int64_t)h * hd;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e * 64 + lane < hd) st1(op + e * 64 + lane, o[e] / l);
+    attend_row(q + (int64_t)row * ldq + (int64_t)h * hd, k + b0 * ldk + (int64_t)g * hd, ldk,
+               v + b0 * ldv + (int64_t)g * hd, ldv, row - b0, hd, scale, qs[wave],
+               out + (int64_t)row * heads * hd + (int64_t)h * hd);
   }
 }
 
@@ -205,6 +161,7 @@ extern "C" zoact_status zoact_rope_at(const void* x, int64_t ldx, void* out, int
   ZP_CHECK(cos_t && sin_t, "rope_at: NULL rotary table");
   ZP_CHECK(n_pos >= 1, "rope_at: empty rotary table");
   const int64_t width = (int64_t)n_heads * head_dim;
+  ZP_CHECK(width < (int64_t(1) << 31), "rope_at: n_heads * head_dim past 32 bits");
   ZP_CHECK(ldx >= width && ldo >= width, "rope_at: heads exceed the row");
   ZP_CHECK(out != x || ldo == ldx, "rope_at: in place with another row stride");
   const size_t esize = dtype == ZOACT_F32 ? 4 : 2;

@@ -27,7 +27,6 @@ inline zoact_status check_packed(const zoact_packed* s) {
   ZP_CHECK(s->n >= 1 && s->n <= (1 << 24), "packed: n outside [1, 2^24]");
   // (a tile that begins in the last row still numbers its keys in 32 bits)
   ZP_CHECK(s->rows >= 0 && s->rows <= (int64_t(1) << 31) - 1024, "packed: rows outside [0, 2^31 - 1024]");
-  ZP_CHECK(s->max_len >= 1, "packed: max_len must be at least 1");
   return ZOACT_OK;
 }
 
@@ -71,6 +70,57 @@ __device__ __forceinline__ int packed_find(const int32_t* __restrict__ begin, in
     else hi = mid - 1;
   }
   return lo;
+}
+
+__device__ __forceinline__ float ld1(const float* p) { return *p; }
+__device__ __forceinline__ float ld1(const uint16_t* p) { return bf2f(*p); }
+__device__ __forceinline__ void st1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f2bf(v); }
+
+// Attention of one row and head by one wave: q over the keys 0 .. row, 64 at a time, a key a lane for the scores and
+// a column a lane for the sums, with the running maximum m and sum l of the softmax; head_dim at most 256, which qs
+// (in LDS, the wave's own) holds in fp32.
+template <typename T>
+__device__ __forceinline__ void attend_row(const T* q, const T* k, int64_t ldk, const T* v, int64_t ldv, int row, int hd,
+                                           float scale, float* qs, T* out) {
+  const int lane = threadIdx.x & 63;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // (qs was read for another row)
+  for (int d = lane; d < hd; d += 64) qs[d] = ld1(q + d);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  // (-inf scores, which a formula's softmax gives weight 0, stay below every m)
+  float m = -3.4028235e38f, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int key0 = 0; key0 <= row; key0 += 64) {
+    const int key = key0 + lane;
+    float sc = -INFINITY;
+    if (key <= row) {
+      const T* kr = k + key * ldk;
+      float t = 0.f;
+      for (int d = 0; d < hd; ++d) t = fmaf(qs[d], ld1(kr + d), t);
+      sc = t * scale;
+    }
+    float mx = sc == sc ? sc : -INFINITY;
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+    const float mn = fmaxf(m, mx);
+    const float p = key <= row ? expf(sc - mn) : 0.f, a = expf(m - mn);
+    m = mn;
+    l = l * a + p;
+    const int cnt = row - key0 + 1 < 64 ? row - key0 + 1 : 64;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= a;
+    for (int t = 0; t < cnt; ++t) {
+      const float pt = __shfl(p, t, 64);
+      const T* vr = v + (key0 + t) * ldv;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (e * 64 + lane < hd) o[e] = fmaf(pt, ld1(vr + e * 64 + lane), o[e]);
+    }
+  }
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (e * 64 + lane < hd) st1(out + e * 64 + lane, o[e] / l);
 }
 
 // Whether row has a next row in its own sequence.

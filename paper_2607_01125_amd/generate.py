@@ -323,7 +323,7 @@ def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int
     tok, src = torch.empty_like(ids), torch.empty_like(ids)
     eos = eos if eos is not None and 0 <= eos < V else None
     ws = torch.empty(Z.beam_workspace_bytes(n, beams, beams, V), dtype=torch.uint8, device=dev)
-    select = Z.beam_select if beams <= Z.BEAMS_MAX else _select_many
+    select = Z.beam_select if ws.numel() else _select_many
     now, then = Z.Beams.alloc(n, 1, n_new, dev), Z.Beams.alloc(n, beams, n_new, dev)
     for step in range(n_new):
         select(logits, now, step, eos, then, tok, src, ws)
@@ -339,7 +339,7 @@ def generate(decoder, prompts, n_new: int, *, eos: int | None = None, beams: int
 
 
 def _select_many(logits, now: Z.Beams, length: int, eos: int | None, to: Z.Beams, tok, src, ws):
-    """beam_select for more candidates than it keeps."""
+    """beam_select for more candidates than it takes."""
     (n, _), b, V = now.score.shape, to.score.shape[1], logits.shape[1]
     lp = torch.log_softmax(logits, dim=1).view(n, -1, V)
     if eos is not None and length:            # an ended candidate goes on as it is

@@ -75,6 +75,13 @@ class PackedBatch:
     both: Z.Packed
     pos: torch.Tensor
 
+    def __post_init__(self):
+        T, dev = self.seqs.rows, self.seqs.index
+        Z._arg(self.tokens, "tokens", torch.int32, dev, (T,))
+        Z._arg(self.pos, "pos", torch.int32, dev, (2 * T,))
+        if self.both.rows != 2 * T or self.both.index != dev:
+            raise ValueError("a packed batch needs both halves' rows, on one device")
+
     @classmethod
     def of(cls, sequences, device="cuda"):
         """From sequences of token ids (lists or tensors, none empty)."""
@@ -213,6 +220,7 @@ class Decoder:
         self._proj_ws = None     # the depth-split projection's partial sums (grown on demand)
         self._bufs = {}
         self._packed_T = 0       # rows a half that the buffers of packed batches hold
+        self._held = []          # buffers that grow with the batch and that a graph may replay on
         self._rope = {}
         self._ch = self._ch_all = None   # per-step C +/- eps Z of the whole arena (bf16 modes)
         # the perturbation the last update pass wrote into _ch_all for the next step:
@@ -330,9 +338,9 @@ class Decoder:
         return Z.Linear(w, d_in, d_out, r=0, coef_offset=b.offset if b else 0, bias=bias, w_scales=scales), b
 
     # ---------------------------------------------------------------- buffers
-    def _buffers(self, n_seq: int, seq: int):
-        """Activation buffers for 2 halves of n_seq sequences of length seq (cached per shape)."""
-        key = (n_seq, seq)
+    def _buffers(self, n_seq: int, seq: int, key=None):
+        """Activation buffers for 2 halves of n_seq sequences of length seq (cached per shape, or by `key`)."""
+        key = key or (n_seq, seq)
         if key in self._bufs:
             return self._bufs[key]
         s, T = self.s, n_seq * seq
@@ -351,12 +359,18 @@ class Decoder:
 
     def _packed_buffers(self, T: int):
         """The same for two halves of T packed rows: the beginning of one set, kept for the most rows so far
-        (batches of packed sequences are hardly ever of one size)."""
+        (batches of packed sequences are hardly ever of one size; what a graph was captured on stays)."""
         if self._packed_T < T:
-            self._bufs.pop((1, self._packed_T), None)
+            self._bufs.pop("packed", None)
             self._packed_T = -(-T // 256) * 256
-        B = self._buffers(1, self._packed_T)
+        B = self._buffers(1, self._packed_T, "packed")
+        self._hold(B)
         return {k: None if v is None else v[:2 * T] for k, v in B.items()}
+
+    def _hold(self, x):
+        """Keep a buffer that a later batch may replace, if a graph is being captured that uses it."""
+        if torch.cuda.is_current_stream_capturing() and not any(x is h for h in self._held):
+            self._held.append(x)
 
     def _rope_tables(self, seq: int):
         """Tables of the positions below seq; shape.extra["rope"] (a dict) holds rope_tables' arguments of a model
@@ -449,6 +463,8 @@ class Decoder:
         if packed is not None:
             if distinct_halves:
                 raise ValueError("a packed batch has the same tokens in both halves")
+            if packed.tokens.device != self.emb.device:
+                raise ValueError(f"the batch is on {packed.tokens.device}, the model on {self.emb.device}")
             T = packed.seqs.rows
             B = self._cur = self._packed_buffers(T)
         else:
@@ -674,6 +690,7 @@ class Decoder:
             need = Z.linear_xent_workspace_bytes(T, self.s.vocab)
             if getattr(self, "_xent_ws", None) is None or self._xent_ws.numel() < need:
                 self._xent_ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+            self._hold(self._xent_ws)
             if packed:
                 Z.linear_xent_packed(self.head, None, a, tokens.tokens, tokens.seqs, None, pert, out, self._xent_ws)
             else:

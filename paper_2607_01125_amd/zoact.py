@@ -46,8 +46,7 @@ def pert_pair(seed: int, step: int, queries, signs, eps: float) -> PertPair:
 
 
 class PackedDesc(ctypes.Structure):
-    _fields_ = [("begin", ctypes.c_void_p), ("n", ctypes.c_int32), ("rows", ctypes.c_int64),
-                ("max_len", ctypes.c_int64)]
+    _fields_ = [("begin", ctypes.c_void_p), ("n", ctypes.c_int32), ("rows", ctypes.c_int64)]
 
 
 class BeamsDesc(ctypes.Structure):
@@ -848,8 +847,8 @@ BEAMS_MAX = 64
 @dataclass(frozen=True)
 class Packed:
     """Sequences packed one behind the other: sequence i is rows begin[i] .. begin[i + 1] - 1 of tensors of
-    `rows` rows (begin int32 [n + 1], ascending, on the device); max_len: a length that none is expected to
-    pass.  Checked here, and again where `begin` has other memory."""
+    `rows` rows (begin int32 [n + 1], ascending, on the device); max_len: the longest one's length, or more
+    (what tables of positions have to hold).  Checked here, and again where `begin` has other memory."""
     begin: torch.Tensor
     rows: int
     max_len: int
@@ -859,7 +858,7 @@ class Packed:
         if b.dim() != 1 or b.numel() < 2:
             raise ValueError("packed: begin must be a list of n + 1 rows, n >= 1")
         dev = _device(b)
-        d = PackedDesc(_arg(b, "begin", torch.int32, dev), b.numel() - 1, self.rows, max(int(self.max_len), 1))
+        d = PackedDesc(_arg(b, "begin", torch.int32, dev), b.numel() - 1, self.rows)
         object.__setattr__(self, "index", dev)
         object.__setattr__(self, "_place", d.begin)
         object.__setattr__(self, "_kept", ctypes.byref(d))

@@ -47,12 +47,12 @@ def _split(x, H, Hkv, hd):
     return x[:, :a], x[:, a:b], x[:, b:]
 
 
-def _attend(x, begin, H, Hkv, hd, dt, scale, out=None, max_len=None):
+def _attend(x, begin, H, Hkv, hd, dt, scale, out=None):
     t = _act(x, dt)
     rows = len(x)
     if out is None:
         out = torch.full((rows, H * hd), -7.0, dtype=t.dtype, device=dev())
-    seqs = Z.Packed(t_i32(begin), rows, max_len or int(np.diff(begin).max()))
+    seqs = Z.Packed(t_i32(begin), rows, int(np.diff(begin).max()))
     Z.attention_packed(seqs, *_split(t, H, Hkv, hd), out, H, Hkv, hd, scale)
     return out
 
@@ -190,20 +190,63 @@ def test_scores_of_minus_infinity_have_no_weight(dt):
     assert np.all(np.abs(got[kept] - want) <= tol)
 
 
-def test_lengths_past_max_len_and_bounds_that_do_not_ascend():
-    """max_len only shapes the work; bounds outside the rows, or that descend, touch nothing else."""
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_bounds_that_do_not_ascend(dt):
+    """Bounds outside the rows, or that descend, touch nothing else."""
     H, Hkv, hd = 4, 2, 64
-    x, begin = _qkv([300, 20], H, Hkv, hd, "bf16")
-    for m in (1, 64, 5000):
-        announce("attention_packed max_len", m)
-        _check(_attend(x, begin, H, Hkv, hd, "bf16", 0.125, max_len=m), x, begin, H, Hkv, hd, "bf16", 0.125)
-    for wrong in ([0, 300, 400], [-5, 300, 320], [200, 100, 320], [400, 500, 600], [0, 320, 0]):
-        announce("attention_packed bad bounds", wrong)
-        guard = torch.full((3 * 320, H * hd), -7.0, dtype=torch.bfloat16, device=dev())
+    x, _ = _qkv([300, 20], H, Hkv, hd, dt)
+    for wrong in ([0, 300, 400], [-5, 300, 320], [200, 100, 320], [400, 500, 600], [0, 320, 0],
+                  [0, 320] * 100):
+        announce("attention_packed bad bounds", dt, wrong[:4])
+        guard = torch.full((3 * 320, H * hd), -7.0, dtype=_act(x[:1], dt).dtype, device=dev())
         out = guard[320:640]
-        _attend(x, np.array(wrong, np.int32), H, Hkv, hd, "bf16", 0.125, out=out, max_len=320)
+        _attend(x, np.array(wrong, np.int32), H, Hkv, hd, dt, 0.125, out=out)
         g = host(guard)
         assert np.all(g[:320] == -7.0) and np.all(g[640:] == -7.0)
+
+
+@pytest.mark.parametrize("Hkv", [1, 4])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("n", [62, 63, 64, 65, 129, 4097])
+def test_many_sequences(n, dt, Hkv):
+    """Numbers of sequences around those that one read of the bounds covers, most of them a few rows or none."""
+    H, hd = 4, 32
+    lens = [(i * 7919) % 6 for i in range(n)]
+    lens[n // 2], lens[n - 1] = 70, 41
+    x, begin = _qkv(lens, H, Hkv, hd, dt, seed=n, first=3, behind=2)
+    announce("attention_packed many", n, dt, Hkv)
+    _check(_attend(x, begin, H, Hkv, hd, dt, 0.2), x, begin, H, Hkv, hd, dt, 0.2)
+
+
+def test_as_many_sequences_as_are_allowed():
+    """2^24 sequences of one row (more workgroups than one launch has in the tiles' kernel): each row is its V."""
+    n, hd = 1 << 24, 32
+    v = torch.randint(-100, 100, (n, hd), device=dev(), dtype=torch.int8).to(torch.bfloat16)
+    out = torch.zeros_like(v)
+    announce("attention_packed 2^24 sequences")
+    seqs = Z.Packed(torch.arange(n + 1, device=dev(), dtype=torch.int32), n, 1)
+    Z.attention_packed(seqs, v, v, v, out, 1, 1, hd, 0.01)
+    assert torch.equal(out, v)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_scores_near_the_ends_of_the_range(dt):
+    """Scores between -1e38 and -2.2e38, far apart: the largest key's V and nothing else; and a scale whose product
+    with log2(e) is not finite, with scores of 0: the mean."""
+    L, hd = 150, 64
+    x = np.zeros((L, 3 * hd), np.float32)
+    x[:, 0] = 2.0 ** 63
+    x[:, hd] = -2.0 ** 63 * (1.25 + (np.arange(L) * 37 % 64) / 64.0)           # (exact in bf16; each score at most twice)
+    x[:, 2 * hd:] = (np.arange(L * hd).reshape(L, hd) * 7919 % 128)
+    begin = np.array([0, 64, L], np.int32)
+    announce("attention_packed ends of the range", dt)
+    got = host(_attend(x, begin, 1, 1, hd, dt, 1.0))
+    for b, e in zip(begin[:-1], begin[1:]):
+        for t in range(b, e):
+            s = x[b:t + 1, hd]
+            assert np.array_equal(got[t], x[b:t + 1, 2 * hd:][s == s.max()].mean(axis=0)), t
+    x[:, 0] = 0.0
+    _check(_attend(x, begin, 1, 1, hd, dt, 3.0e38), x, begin, 1, 1, hd, dt, 3.0e38)
 
 
 # ------------------------------------------------------------------ rotary positions
@@ -337,6 +380,49 @@ def test_a_packed_step_against_the_oracle(shape, mode):
     toks = synth.uniform_tokens(4, 12, shape.vocab, 6, 1)
     rect = host(g.losses(t_i32(toks), 3, 2, eps)).copy()
     assert_rel_close(host(g.losses(gm.PackedBatch.of(list(toks), dev()), 3, 2, eps)), rect, bar, "packed and rectangular")
+
+
+def test_packed_batches_that_do_not_fit():
+    b = gm.PackedBatch.of([[1, 2, 3], [4]], dev())
+    _, g = _models(synth.TINY, "fp32", 4)
+    for bad in (dict(tokens=b.tokens[:3]), dict(pos=b.pos[:4]), dict(both=b.seqs), dict(tokens=b.tokens.long()),
+                dict(tokens=b.tokens.cpu())):
+        f = dict(tokens=b.tokens, seqs=b.seqs, both=b.both, pos=b.pos)
+        f.update(bad)
+        with pytest.raises(ValueError):
+            gm.PackedBatch(**f)
+    with pytest.raises(ValueError):
+        g.forward(b, Z.Pert(0, 0, 0, 0.0), distinct_halves=True)
+
+
+@pytest.mark.parametrize("mode", ["fp32", "bf16"])
+def test_a_packed_forward_in_a_graph_outlives_larger_batches(mode):
+    """Losses captured over a packed batch, replayed after larger packed and other batches have come: the eager
+    values."""
+    _, g = _models(LLAMA_S if mode == "bf16" else synth.TINY, mode, 4)
+    shape, pert = g.s, Z.Pert(0, 0, 0, 0.0)
+    batch = gm.PackedBatch.of(_texts(shape, [17, 40, 3]), dev())
+    out = torch.zeros(2, device=dev())
+    announce("packed graph", mode)
+    g._loss_pair(batch, pert, out)
+    want = out.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        g._loss_pair(batch, pert, out)
+    for lens in ([300, 200], [700, 1, 90]):
+        larger = gm.PackedBatch.of(_texts(shape, lens), dev())
+        other = torch.zeros(2, device=dev())
+        g._loss_pair(larger, pert, other)
+        kept = other.clone()
+        fresh = [torch.full((1 << 16,), 7.0, device=dev()) for _ in range(64)]   # (what was freed is used again)
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+        g._loss_pair(larger, pert, other)
+        assert torch.equal(other, kept) and all(bool((f == 7.0).all()) for f in fresh)
 
 
 def test_packed_query_steps_and_calibration():

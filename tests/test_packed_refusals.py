@@ -14,7 +14,7 @@ P, ODD = ctypes.c_void_p(256), ctypes.c_void_p(257)
 
 
 def _seqs(**kw):
-    f = dict(begin=256, n=3, rows=20, max_len=9)
+    f = dict(begin=256, n=3, rows=20)
     f.update(kw)
     return Z.PackedDesc(**f)
 
@@ -49,7 +49,7 @@ def _beams(logits=P, ldl=100, dt=Z.F32, ws=P, nb=1 << 40, **kw):
 
 
 @pytest.mark.parametrize("s", [dict(begin=None), dict(begin=258), dict(n=0), dict(n=(1 << 24) + 1), dict(rows=-1),
-                               dict(rows=2 ** 31 - 1023), dict(max_len=0)])
+                               dict(rows=2 ** 31 - 1023)])
 def test_sequences_that_are_none(s):
     for f in (_attend, _xent, _head):
         assert f(_seqs(**s)) == Z.E_INVALID
@@ -64,7 +64,7 @@ def test_sequences_that_are_none(s):
     lambda: _attend(v=ctypes.c_void_p(258), dt=Z.F32),
     lambda: _rope(x=None), lambda: _rope(out=None), lambda: _rope(x=ODD), lambda: _rope(ldx=255), lambda: _rope(ldo=255),
     lambda: _rope(ldo=264), lambda: _rope(dt=2), lambda: _rope(rows=-1), lambda: _rope(rows=1 << 31), lambda: _rope(heads=0),
-    lambda: _rope(hd=0), lambda: _rope(rot=0), lambda: _rope(rot=63), lambda: _rope(rot=66), lambda: _rope(layout=2),
+    lambda: _rope(heads=65535, hd=32769, ldx=1 << 32, ldo=1 << 32), lambda: _rope(hd=0), lambda: _rope(rot=0), lambda: _rope(rot=63), lambda: _rope(rot=66), lambda: _rope(layout=2),
     lambda: _rope(pos=ODD), lambda: _rope(cos=None), lambda: _rope(sin=ctypes.c_void_p(258)), lambda: _rope(n_pos=0),
     lambda: _rope(x=ctypes.c_void_p(258), dt=Z.F32),
     lambda: _xent(logits=None), lambda: _xent(tokens=None), lambda: _xent(loss=None), lambda: _xent(V=0),
