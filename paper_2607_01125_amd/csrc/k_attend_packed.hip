@@ -14,12 +14,10 @@
 // head a wave; K and V tiles go through LDS for all four, chunks of 16 bytes swizzled so that
 // neither the K rows nor the V columns (read transposed by ds_read_tr16) meet in a bank.
 //
-// Where a maximum passes 2^27 the fused S^T c - m is off by the rounding of the product that became m, which 2^x no
-// longer bears: such a wave takes its rows one by one in the end.
-//
-// Keys that some of a wave's rows may not see are in its last tiles only, from its first row's tile
-// of 32 on; there the scores are masked, and where a masked V is not finite (0 * inf is NaN) the
-// product runs on the vector unit, for the rows that see each key.
+// Keys that some of a wave's rows may not see are in its last tiles only, from its first row's tile of 32 on; there
+// the scores are masked.  Two things make a wave take its rows one by one in the end: a masked V that is not finite
+// (0 * inf is NaN), looked for where an output is not; and a maximum past 2^27, where S^T c - m, fused, is off by the
+// rounding of the product that became m, which 2^x no longer bears.
 #include <math.h>
 
 #include <type_traits>
@@ -130,6 +128,17 @@ __device__ __forceinline__ unsigned turn_about() {
 
 __device__ __forceinline__ int no_swizzle(int) { return 0; }
 
+// Whether rows first .. last of a head's V hold something that is not finite.
+template <typename T>
+__device__ __forceinline__ bool not_finite(const T* v, int64_t ldv, int first, int last, int hd) {
+  bool bad = false;
+  for (int i = threadIdx.x & 63; i < (last - first + 1) * hd; i += 64) {
+    const float x = ld1(v + (first + i / hd) * ldv + i % hd);
+    bad |= !(x - x == 0.f);
+  }
+  return __ballot(bad) != 0;
+}
+
 // Rows of a K or V tile from global memory straight to LDS, 256 threads with PER chunks of 16 bytes each, a
 // wave's 64 side by side; the swizzle is in the choice of each lane's chunk.  Rows past the sequence read as its
 // last.
@@ -188,7 +197,6 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
   constexpr int QF = HD / 16;                                // 16-byte pieces of a lane's query
   // (arrays of their own, so that a read of one does not wait for the loads into another)
   __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
-  __shared__ uint16_t pw[4][32][32];                                // a wave's probabilities for the vector product
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
             lh = lane >> 5;
   const int hgs = heads / gh, R = (4 / gh) * 32;
@@ -263,7 +271,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
     if (__ballot(mx > m + 8.f)) {
       const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
-      if (__ballot(fabsf(m) > 0x1p27f)) far = true;
+      if (__ballot(fabsf(m) > 0x1p27f && m < INFINITY)) far = true;
       l *= a;
 #pragma unroll
       for (int n = 0; n < NB; ++n) o[n] *= a;
@@ -303,42 +311,6 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
                                                        __builtin_bit_cast(bf16x8, pb), o[n], 0, 0, 0);
     }
   };
-  // whether a sub-tile of V holds something that is not finite (its rows spread over the wave)
-  auto v_broken = [&](const char* vt, int sub) {
-    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-    u16x2 most = {0, 0};
-#pragma unroll
-    for (int c = 0; c < 32 * CH / 64; ++c) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(vt + sub * 32 * ROW + (c * 64 + lane) * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, x[e] & 0x7FFF7FFFu));
-    }
-    return __ballot(most.x >= 0x7F80 || most.y >= 0x7F80) != 0;
-  };
-  // the diagonal sub-tile key by key, for the rows from each on
-  auto add_by_rows = [&](const char* vt, int sub, const floatx16& st) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) pw[wave][lq][(8 * (i / 4) + 4 * lh + i % 4) ^ lq] = f2bf(st[i]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
-    for (int t = 0; t < 32; ++t) {
-      const int row = sub * 32 + t;
-      const float p = bf2f(pw[wave][lq][t ^ lq]);
-      const bool seen = t <= lq;
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint2 x = *reinterpret_cast<const uint2*>(vt + row * ROW + ((4 * n + i) ^ C::vswz(row)) * 16 + lh * 8);
-          o[n][4 * i] = seen ? fmaf(p, __uint_as_float(x.x << 16), o[n][4 * i]) : o[n][4 * i];
-          o[n][4 * i + 1] = seen ? fmaf(p, __uint_as_float(x.x & 0xFFFF0000u), o[n][4 * i + 1]) : o[n][4 * i + 1];
-          o[n][4 * i + 2] = seen ? fmaf(p, __uint_as_float(x.y << 16), o[n][4 * i + 2]) : o[n][4 * i + 2];
-          o[n][4 * i + 3] = seen ? fmaf(p, __uint_as_float(x.y & 0xFFFF0000u), o[n][4 * i + 3]) : o[n][4 * i + 3];
-        }
-    }
-  };
-
   const int n_full = pl.q0 / KT;                             // tiles that every row of the workgroup sees
   floatx16 st[SUBS];
   float mx;
@@ -358,21 +330,24 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
     follow(mx);
     floatx16 nx[SUBS];
 #pragma unroll
-    for (int u = 0; u < SUBS; ++u) nx[u] = scores(kn, u);
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u) weigh(st[u], std::false_type{}, 0);
-#pragma unroll
-    for (int u = 0; u < SUBS; ++u) add(vt, u, st[u]);
+    for (int u = 0; u < SUBS; ++u) {
+      weigh(st[u], std::false_type{}, 0);
+      nx[u] = scores(kn, u);
+      add(vt, u, st[u]);
+    }
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) st[u] = nx[u];
     maximum();
     arrived();
   };
-  arrived();
+  // (V of tile 0 and K of tile 1 may still be on their way)
+  if (n_tiles > 1) __builtin_amdgcn_s_waitcnt(0x0F70 | 2 * PER);
+  else __builtin_amdgcn_s_waitcnt(0x0F70 | PER);
+  __syncthreads();
 #pragma unroll
   for (int u = 0; u < SUBS; ++u) st[u] = scores(k0, u);
   maximum();
-  __syncthreads();                                           // (K of tile 0 is overwritten next)
+  arrived();                                                 // (K of tile 0 is overwritten next)
 #pragma unroll 1
   for (int t = 0; t < n_full; t += 2) {
     full(k0, k1, v0, v1, t);
@@ -394,13 +369,11 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
 #pragma unroll
         for (int i = 0; i < 16; ++i) mb = fmaxf(mb, u * 32 + 8 * (i / 4) + i % 4 <= lim ? st[u][i] : -INFINITY);
       follow(both(mb));
-      const bool broken = ahead < SUBS && v_broken(vt, ahead);
 #pragma unroll
       for (int u = 0; u < SUBS; ++u) {
         if (u > ahead) break;
         weigh(st[u], std::true_type{}, lim - u * 32);
-        if (u == ahead && broken) add_by_rows(vt, u, st[u]);
-        else add(vt, u, st[u]);
+        add(vt, u, st[u]);
       }
     }
     if (t + 1 == n_tiles) break;
@@ -412,9 +385,18 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
 
   // O^T has four columns of a row in a lane: rows are put together in the tiles' LDS, so that whole
   // lines are written
-  const float inv = 1.f / (l + __shfl_xor(l, 32, 64));
+  l += __shfl_xor(l, 32, 64);
+  const float inv = 1.f / l;
+  float any = 0.f;
+#pragma unroll
+  for (int n = 0; n < NB; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) any += o[n][i] *= inv;
   __syncthreads();
   char* const mine = (wave < 2 ? k0 : k1) + wave % 2 * 32 * ROW;
+  // (of a row whose l is not finite nothing is, whatever V holds)
+  if (!far && __ballot(any - any != 0.f && l - l == 0.f))
+    far = not_finite(v + pl.row0 * ldv + (int64_t)g * HD, ldv, w0, w0 + 31 < len ? w0 + 31 : len - 1, HD);
   if (far) {
     for (int r = w0; r < w0 + 32 && r < len; ++r)
       attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
@@ -426,10 +408,8 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
   for (int n = 0; n < NB; ++n)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a0 = o[n][4 * i] * inv, a1 = o[n][4 * i + 1] * inv, a2 = o[n][4 * i + 2] * inv,
-                  a3 = o[n][4 * i + 3] * inv;
       *reinterpret_cast<uint2*>(mine + lq * ROW + ((4 * n + i) ^ C::kswz(lq)) * 16 + lh * 8) =
-          make_uint2(pack2(a0, a1), pack2(a2, a3));
+          make_uint2(pack2(o[n][4 * i], o[n][4 * i + 1]), pack2(o[n][4 * i + 2], o[n][4 * i + 3]));
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   char* const op = reinterpret_cast<char*>(out + ((pl.row0 + w0) * heads + h) * HD);
@@ -462,7 +442,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
   constexpr int KT = C::KT, ROW = C::ROW, CH = C::CH, QF = C::QF, W = C::W, NV = C::NV;
   typedef float floatw __attribute__((ext_vector_type(W)));
   __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
-  __shared__ float pw[4][16][32];                            // a wave's probabilities for the vector product
+  __shared__ float qs[4][HD];                                // a row's query, where rows are taken one by one
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 15,
             lg = lane >> 4;
   const int hgs = heads / gh, R = 4 / gh * 16;
@@ -538,7 +518,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     if (__ballot(mx > m + 8.f)) {
       const float mn = fmaxf(m, mx), a = __builtin_amdgcn_exp2f(m - mn);
       m = mn;
-      if (__ballot(fabsf(m) > 0x1p27f)) far = true;
+      if (__ballot(fabsf(m) > 0x1p27f && m < INFINITY)) far = true;
       l *= a;
 #pragma unroll
       for (int n = 0; n < NV; ++n)
@@ -566,40 +546,6 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
       }
     }
   };
-  // whether a tile of V holds something that is not finite
-  auto v_broken = [&](const char* vt) {
-    uint32_t most = 0;
-#pragma unroll 4
-    for (int c = 0; c < KT * CH / 64; ++c) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(vt + (c * 64 + lane) * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) most = max(most, x[e] & 0x7FFFFFFFu);
-    }
-    return __ballot(most >= 0x7F800000u) != 0;
-  };
-  // a tile key by key, for the rows from each on (lim: the lane's row in the tile)
-  auto add_by_rows = [&](const char* vt, const floatx4 (&st)[2], int lim) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      pw[wave][lq][(4 * lg + i) ^ lq] = st[0][i];
-      pw[wave][lq][(16 + 4 * lg + i) ^ lq] = st[1][i];
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 1
-    for (int t = 0; t < KT; ++t) {
-      const float p = pw[wave][lq][t ^ lq];
-      const bool seen = t <= lim;
-#pragma unroll
-      for (int n = 0; n < NV; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const floatw x = *reinterpret_cast<const floatw*>(vt + t * ROW + (16 * W * n + W * (4 * lg + i)) * 4);
-#pragma unroll
-          for (int e = 0; e < W; ++e) o[n][e][i] = seen ? fmaf(p, x[e], o[n][e][i]) : o[n][e][i];
-        }
-    }
-  };
-
   const int n_full = pl.q0 / KT;                             // tiles that every row of the workgroup sees
   floatx4 st[2];
   float mx;
@@ -649,12 +595,8 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
       follow(all(mb));
       weigh(st[0], std::true_type{}, lim - 4 * lg);
       weigh(st[1], std::true_type{}, lim - 4 * lg - 16);
-      if (w0 - t * KT < KT && v_broken(vt)) {
-        add_by_rows(vt, st, lim);
-      } else {
-        add(vt, 0, st[0]);
-        if (w0 - t * KT >= 16) add(vt, 1, st[1]);
-      }
+      add(vt, 0, st[0]);
+      if (w0 - t * KT >= 16) add(vt, 1, st[1]);
     }
     if (t + 1 == n_tiles) break;
     const char* const kn = t & 1 ? k0 : k1;
@@ -663,16 +605,26 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     arrived();
   }
 
-  if (far) {
-    for (int r = w0; r < w0 + 16 && r < len; ++r)
-      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
-                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, &pw[wave][0][0],
-                 out + ((pl.row0 + r) * heads + h) * HD);
-    return;
-  }
   l += __shfl_xor(l, 32, 64);
   l += __shfl_xor(l, 16, 64);
   const float inv = 1.f / l;
+  float any = 0.f;
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) any += o[n][e][i] *= inv;
+  // (of a row whose l is not finite nothing is, whatever V holds)
+  if (!far && __ballot(any - any != 0.f && l - l == 0.f))
+    far = not_finite(v + pl.row0 * ldv + (int64_t)g * HD, ldv, w0, w0 + 15 < len ? w0 + 15 : len - 1, HD);
+  if (far) {
+    for (int r = w0; r < w0 + 16 && r < len; ++r)
+      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
+                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, qs[wave],
+                 out + ((pl.row0 + r) * heads + h) * HD);
+    return;
+  }
   if (w0 + lq >= len) return;
   float* const op = out + ((pl.row0 + w0 + lq) * heads + h) * HD;
 #pragma unroll
@@ -681,7 +633,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     for (int i = 0; i < 4; ++i) {
       floatw x;
 #pragma unroll
-      for (int e = 0; e < W; ++e) x[e] = o[n][e][i] * inv;
+      for (int e = 0; e < W; ++e) x[e] = o[n][e][i];
       *reinterpret_cast<floatw*>(op + 16 * W * n + W * (4 * lg + i)) = x;
     }
 }
