@@ -154,24 +154,32 @@ __global__ void __launch_bounds__(256) finish_mean_packed(const double* __restri
   if (threadIdx.x == 0) loss_pm[h] = (float)(s / count);
 }
 
-// Cross entropy of packed rows from their logits: one block per row that has a next one in its
-// sequence; its threads' values are independent loads, the maximum and the sum of exponentials
-// joined as in xent_partial.
-__global__ void __launch_bounds__(256) xent_rows(const float* __restrict__ logits, const int32_t* __restrict__ tokens,
-                                                 zoact_packed seqs, int64_t V, double* __restrict__ part) {
-  __shared__ float smax[4], ssum[4];
-  const int h = blockIdx.y;
+// Cross entropy of packed rows from their logits: PER threads take a row that has a next one in its
+// sequence; their values are independent loads, the maximum and the sum of exponentials joined as in
+// xent_partial.  Bound by memory: 2000 rows of 50272 logits in 143 us, 5.6 TB/s.  A wave a row where rows
+// are short (16000 of 1000: 59 us with 256 threads each, 31 so; 100 of 5000: 8.6 against 9.5), 1024
+// threads where long rows are few (100 of 50272: 22 against 15; 300: 25 against 29).
+template <int PER>
+__global__ void __launch_bounds__(PER < 256 ? 256 : PER)
+    xent_rows(const float* __restrict__ logits, const int32_t* __restrict__ tokens, zoact_packed seqs, int64_t V,
+              double* __restrict__ part) {
+  constexpr int ROWS = PER < 256 ? 256 / PER : 1, WAVES = PER / 64;
+  __shared__ float smax[ROWS * WAVES], ssum[ROWS * WAVES];
+  __shared__ double sacc[ROWS];
+  const int h = blockIdx.y, mine = threadIdx.x / PER, at = threadIdx.x % PER;
   const int64_t T = seqs.rows;
   double acc = 0.0;
-  for (int64_t row = blockIdx.x; row < T; row += gridDim.x) {
-    if (!packed_has_next(seqs.begin, seqs.n, T, (int)row)) continue;   // (the same for all threads)
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < T; row0 += (int64_t)gridDim.x * ROWS) {
+    const int64_t row = row0 + mine;
+    // (the same for all of a row's threads: with one row a block for all)
+    if (row >= T || !packed_has_next(seqs.begin, seqs.n, T, (int)row)) continue;
     const float* lg = logits + ((int64_t)h * T + row) * V;
     float m = -INFINITY, se = 0.f;
-    for (int64_t v0 = threadIdx.x; v0 < V; v0 += 8 * 256) {
+    for (int64_t v0 = at; v0 < V; v0 += 8 * PER) {
       float x[8], mx = m;
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        const int64_t v = v0 + u * 256;
+        const int64_t v = v0 + u * PER;
         x[u] = v < V ? lg[v] : -INFINITY;
         mx = fmaxf(mx, x[u]);
       }
@@ -188,22 +196,35 @@ __global__ void __launch_bounds__(256) xent_rows(const float* __restrict__ logit
       se = se * __expf(m - base) + s2 * __expf(m2 - base);
       m = mm;
     }
-    if ((threadIdx.x & 63) == 0) {
-      smax[threadIdx.x >> 6] = m;
-      ssum[threadIdx.x >> 6] = se;
+    if (WAVES > 1) {
+      if ((at & 63) == 0) {
+        smax[at >> 6] = m;
+        ssum[at >> 6] = se;
+      }
+      __syncthreads();
+      float mm = smax[0];
+#pragma unroll
+      for (int i = 1; i < WAVES; ++i) mm = fmaxf(mm, smax[i]);
+      const float base = mm == -INFINITY ? 0.f : mm;
+      m = mm;
+      se = 0.f;
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) se += ssum[i] * __expf(smax[i] - base);
+      __syncthreads();
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const float mm = fmaxf(fmaxf(smax[0], smax[1]), fmaxf(smax[2], smax[3])), base = mm == -INFINITY ? 0.f : mm;
-      float ss = 0.f;
-      for (int i = 0; i < 4; ++i) ss += ssum[i] * __expf(smax[i] - base);
+    if (at == 0) {
       int64_t tok = tokens[row + 1];
       tok = tok < 0 ? 0 : (tok >= V ? V - 1 : tok);
-      acc += (double)mm + log((double)ss) - (double)lg[tok];
+      acc += (double)m + log((double)se) - (double)lg[tok];
     }
-    __syncthreads();
   }
-  if (threadIdx.x == 0) part[h * kLossBlocks + blockIdx.x] = acc;
+  if (at == 0) sacc[mine] = acc;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double s = 0.0;
+    for (int i = 0; i < ROWS; ++i) s += sacc[i];
+    part[h * kLossBlocks + blockIdx.x] = s;
+  }
 }
 
 __global__ void __launch_bounds__(256) xent_partial(const float* __restrict__ logits, const int32_t* __restrict__ tokens,
@@ -291,7 +312,10 @@ hipError_t launch_mse_pm(const void* y, int32_t dtype, const void* target, int64
 hipError_t launch_xent_rows(const float* logits, const int32_t* tokens, const zoact_packed& seqs, int64_t V,
                             float* loss_pm, void* ws, hipStream_t s) {
   double* part = static_cast<double*>(ws);
-  xent_rows<<<dim3(kLossBlocks, 2), dim3(256), 0, s>>>(logits, tokens, seqs, V, part);
+  const dim3 grid(kLossBlocks, 2);
+  if (V <= 2048) xent_rows<64><<<grid, 256, 0, s>>>(logits, tokens, seqs, V, part);
+  else if (seqs.rows > 128 || V < 16384) xent_rows<256><<<grid, 256, 0, s>>>(logits, tokens, seqs, V, part);
+  else xent_rows<1024><<<grid, 1024, 0, s>>>(logits, tokens, seqs, V, part);
   finish_mean_packed<<<2, 256, 0, s>>>(part, seqs, loss_pm);
   return hipGetLastError();
 }

@@ -290,11 +290,11 @@ def test_rope_at_gives_what_rope_gives():
 
 
 # ------------------------------------------------------------------ losses
-@pytest.mark.parametrize("V", [1, 5, 512, 2051])
-def test_xent_from_logits(V):
-    """fp32 sums of exponentials: each of at most V roundings by 2^-24 and its exponential within 2^-20 (__expf of
-    arguments down to -30); the logits are at most 20: below 1e-5 in all."""
-    lens = [1, 0, 5, 2, 64, 1]
+@pytest.mark.parametrize("lens,V", [([1, 0, 5, 2, 64, 1], V) for V in (1, 5, 512, 2048, 2051, 16391)]
+                         + [([3000, 1, 2200], 40), ([1100, 900], 2050)])
+def test_xent_from_logits(lens, V):
+    """fp32 sums of exponentials: a thread's chain and the joins are below 60 roundings by 2^-24, an exponential is
+    within 2^-20 (__expf of arguments down to -30); the logits are at most 20: below 1e-5 in all."""
     begin = ref.begins(lens, 2)
     rows = int(begin[-1]) + 3
     lg = synth.normal((2, rows, V), 3.0, 9, V)
@@ -302,7 +302,7 @@ def test_xent_from_logits(V):
     tok = synth.gen(2, V).integers(-1, V + 1, rows).astype(np.int32)       # ids outside are clamped
     loss = torch.empty(2, device=dev())
     ws = torch.empty(Z.loss_workspace_bytes(), dtype=torch.uint8, device=dev())
-    announce("xent_packed", V)
+    announce("xent_packed", lens, V)
     Z.xent_packed(t_f32(lg), t_i32(tok), Z.Packed(t_i32(begin), rows, 64), loss, ws)
     want = [ref.loss(lg[h].astype(np.float64), tok, begin) for h in range(2)]
     assert np.all(np.abs(host(loss) - want) <= 1e-5 * (1 + np.abs(want))), (host(loss), want)
