@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
   __shared__ int kind[KMAX];
   __shared__ uint64_t key[CAP], place[CAP];
   __shared__ uint64_t wkey[WAVES], wplace[WAVES];
-  __shared__ uint32_t wthr[WAVES];
+  __shared__ uint32_t tops[WAVES][64];
   __shared__ int n_got;
   __shared__ int parent[KMAX];
   const int i0 = blockIdx.x, BI = b.beams_in, K = b.beams;
@@ -361,23 +361,21 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
     read(c, k, f);
     mine = k > mine ? k : mine;
   }
-  // In each wave the K-th largest of the lanes' maxima, or a little less (20 bits of it), is reached by K
-  // candidates at least: the largest of the waves' is the threshold.
+  // Of the maxima of 64 groups of candidates (a lane's in all waves) the K-th largest, or a little less (20 bits of
+  // it), is reached by K candidates at least, and few others: the threshold.
   uint64_t thr = 1;
   if (!few) {
-    uint32_t to = 0;
-    const uint32_t upper = (uint32_t)(mine >> 32);
+    tops[wave][lane] = (uint32_t)(mine >> 32);
+    __syncthreads();
+    uint32_t upper = 0, to = 0;
+#pragma unroll
+    for (int u = 0; u < WAVES; ++u) upper = tops[u][lane] > upper ? tops[u][lane] : upper;
 #pragma unroll
     for (int bit = 31; bit >= 12; --bit) {
       const uint32_t x = to | (1u << bit);
       if (__popcll(__ballot(upper >= x)) >= K) to = x;
     }
-    if (lane == 0) wthr[wave] = to;
-    __syncthreads();
-    uint32_t most = 0;
-#pragma unroll
-    for (int u = 0; u < WAVES; ++u) most = wthr[u] > most ? wthr[u] : most;
-    thr = most ? (uint64_t)most << 32 : 1;
+    thr = to ? (uint64_t)to << 32 : 1;
   }
   auto gather = [&](uint64_t k, uint64_t f) {
     if (k < thr) return;
