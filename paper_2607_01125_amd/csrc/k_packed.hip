@@ -36,8 +36,8 @@ __global__ void __launch_bounds__(256) rope_at_kernel(const T* x, int64_t ldx, T
 
 // Pieces of 16 bytes: a thread takes one place of a row -- a pair of pieces half the turned part apart (HALF), a
 // piece of whole pairs (INTERLEAVED), or a piece to copy -- in RT rows, all of whose loads are on their way before
-// the first is used.  Bound by memory: 16411 rows of 40 heads of 128 bf16 values, 64 of them turned in pairs, 78 us where a
-// copy of the same 337 MB takes 71.
+// the first is used.  Bound by memory: 16411 rows of 40 heads of 128 bf16 values, 64 of them turned in pairs, 65 us,
+// 5.2 TB/s; torch's copy of the same 337 MB takes 66.
 template <typename T, bool HALF, int RT>
 __global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
                                                            int heads, int hd, int rot, const int32_t* __restrict__ pos,
@@ -46,19 +46,21 @@ __global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t l
   constexpr int V = 16 / sizeof(T), NT = HALF ? V : V / 2;   // values of a piece, angles of it
   typedef T piece __attribute__((ext_vector_type(V)));
   typedef float angles __attribute__((ext_vector_type(NT)));
-  const int turned = HALF ? rot / (2 * V) : rot / V, per = turned + (out == x ? 0 : (hd - rot) / V);
-  const int units = heads * per, half = rot / 2;
+  const int turned = HALF ? rot / (2 * V) : rot / V, copied = out == x ? 0 : (hd - rot) / V, n_turned = heads * turned;
+  const int units = n_turned + heads * copied, half = rot / 2;
   const int64_t row0 = ((int64_t)blockIdx.x * blockDim.y + threadIdx.y) * RT;
   for (int u = threadIdx.x; u < units; u += blockDim.x) {
-    const int h = u / per, j = u - h * per;
-    const int64_t col = (int64_t)h * hd + (j < turned ? j * V : rot + (j - turned) * V);
+    // (all heads' turned pieces first, so that lanes do the same)
+    const bool turn = u < n_turned;
+    const int w = turn ? u : u - n_turned, per = turn ? turned : copied, h = w / per, j = w - h * per;
+    const int64_t col = (int64_t)h * hd + (turn ? j * V : rot + j * V);
     piece a[RT], b[RT];
     angles c[RT], s[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       const int64_t row = row0 + r < rows ? row0 + r : rows - 1;
       a[r] = *reinterpret_cast<const piece*>(x + row * ldx + col);
-      if (j < turned) {
+      if (turn) {
         int64_t p = pos ? pos[row] : row;
         p = p < 0 ? 0 : (p >= n_pos ? n_pos - 1 : p);
         if (HALF) b[r] = *reinterpret_cast<const piece*>(x + row * ldx + col + half);
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t l
     for (int r = 0; r < RT; ++r) {
       if (row0 + r >= rows) break;
       T* const y = out + (row0 + r) * ldo + col;
-      if (j < turned) {
+      if (turn) {
         piece m, n;
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -91,25 +93,85 @@ __global__ void __launch_bounds__(1024) rope_at_vec_kernel(const T* x, int64_t l
   }
 }
 
+// Where less than half a head is turned, and not in whole pieces: a thread forms a piece of out, value by value where
+// it is turned, so that rows are still written in whole lines; in place, where a pair belongs to one thread, it turns a
+// head's pairs (16411 rows of 40 heads of 128, 10 of them turned: 128 us, 250 value by
+// value throughout).
+template <typename T>
+__global__ void __launch_bounds__(512) rope_at_part_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
+                                                           int heads, int hd, int rot, int layout,
+                                                           const int32_t* __restrict__ pos,
+                                                           const float* __restrict__ cos_t,
+                                                           const float* __restrict__ sin_t, int64_t n_pos) {
+  constexpr int V = 16 / sizeof(T);
+  typedef T piece __attribute__((ext_vector_type(V)));
+  const int half = rot / 2, sa = layout == ZOACT_ROPE_HALF ? 1 : 2, sb = layout == ZOACT_ROPE_HALF ? half : 1;
+  const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (row >= rows) return;
+  int64_t p = pos ? pos[row] : row;
+  p = p < 0 ? 0 : (p >= n_pos ? n_pos - 1 : p);
+  if (out == x) {
+    for (int h = threadIdx.x; h < heads; h += blockDim.x) {
+      T* const y = out + row * ldo + (int64_t)h * hd;
+#pragma unroll 4
+      for (int i = 0; i < half; ++i) {
+        const float c = cos_t[p * half + i], s = sin_t[p * half + i];
+        const float a = ld1(y + i * sa), b = ld1(y + i * sa + sb);
+        st1(y + i * sa, a * c - b * s);
+        st1(y + i * sa + sb, b * c + a * s);
+      }
+    }
+    return;
+  }
+  const int per = hd / V;
+  for (int u = threadIdx.x; u < heads * per; u += blockDim.x) {
+    const int h = u / per, first = (u - h * per) * V;
+    const T* const xr = x + row * ldx + (int64_t)h * hd;
+    piece y = *reinterpret_cast<const piece*>(xr + first);
+    if (first < rot) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const int at = first + e;
+        if (at >= rot) break;
+        const int i = layout == ZOACT_ROPE_HALF ? (at < half ? at : at - half) : at >> 1;
+        const float c = cos_t[p * half + i], s = sin_t[p * half + i];
+        const float a = ld1(xr + i * sa), b = ld1(xr + i * sa + sb);
+        T r;
+        st1(&r, at == i * sa ? a * c - b * s : b * c + a * s);
+        y[e] = r;
+      }
+    }
+    *reinterpret_cast<piece*>(out + row * ldo + (int64_t)h * hd + first) = y;
+  }
+}
+
 template <typename T>
 bool rope_at_vec(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows, int heads, int hd, int rot, int layout,
                  const int32_t* pos, const float* cos_t, const float* sin_t, int64_t n_pos, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
   const bool halves = layout == ZOACT_ROPE_HALF;
-  if (hd % V || rot % (halves ? 2 * V : V) || ldx % V || ldo % V || !aligned_to(x, 16) || !aligned_to(out, 16) ||
-      !aligned_to(cos_t, 16) || !aligned_to(sin_t, 16))
-    return false;
-  const int64_t units = (int64_t)heads * (rot / (halves ? 2 * V : V) + (out == x ? 0 : (hd - rot) / V));
+  if (hd % V || ldx % V || ldo % V || !aligned_to(x, 16) || !aligned_to(out, 16)) return false;
+  const bool whole = rot % (halves ? 2 * V : V) == 0 && aligned_to(cos_t, 16) && aligned_to(sin_t, 16);
+  if (!whole && rot > hd / 2) return false;
+  const int64_t units = whole ? (int64_t)heads * (rot / (halves ? 2 * V : V) + (out == x ? 0 : (hd - rot) / V))
+                              : (int64_t)heads * (out == x ? 1 : hd / V);
   const int bx = (int)(units < 512 ? units : 512), by = bx < 256 ? 256 / bx : 1;
-  // (one row a thread until there are workgroups enough for every compute unit several times)
-  const bool many = rows * units >= (int64_t)512 * 1024 * 4;
-  const int64_t step = (int64_t)by * (many ? 4 : 1), grid = (rows + step - 1) / step;
+  // (two rows a thread in pairs once there are workgroups enough: 65 us at the size above, 69 with one, 80 with four;
+  // halves keep twice the loads on their way with one: 62 us where all 128 values are turned, 71 with two)
+  const bool many = !halves && whole && rows * units >= (int64_t)512 * 1024 * 4;
+  const int64_t step = (int64_t)by * (many ? 2 : 1), grid = (rows + step - 1) / step;
   if (grid >= (int64_t(1) << 31)) return false;
+  if (!whole) {
+    rope_at_part_kernel<T><<<(unsigned)grid, dim3(bx, by), 0, s>>>(x, ldx, out, ldo, rows, heads, hd, rot, layout, pos,
+                                                                   cos_t, sin_t, n_pos);
+    return true;
+  }
 #define ZO_ROPE(HALF, RT)                                                                                             \
   rope_at_vec_kernel<T, HALF, RT><<<(unsigned)grid, dim3(bx, by), 0, s>>>(x, ldx, out, ldo, rows, heads, hd, rot, pos, \
                                                                           cos_t, sin_t, n_pos)
-  if (halves) many ? ZO_ROPE(true, 4) : ZO_ROPE(true, 1);
-  else many ? ZO_ROPE(false, 4) : ZO_ROPE(false, 1);
+  if (halves) ZO_ROPE(true, 1);
+  else if (many) ZO_ROPE(false, 2);
+  else ZO_ROPE(false, 1);
 #undef ZO_ROPE
   return true;
 }
