@@ -7,7 +7,8 @@ namespace zoact {
 namespace {
 
 // ---------------------------------------------------------------- rotary positions
-// One thread a pair or a copied value: any head_dim, rot_dim, stride and alignment.
+// One thread a pair or a copied value: any head_dim, rot_dim, stride and alignment (16411 rows of 40 heads of 128 bf16
+// values, 64 of them turned: 215 us where pieces of 16 bytes take 61 to 65).
 template <typename T>
 __global__ void __launch_bounds__(256) rope_at_kernel(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows,
                                                       int heads, int hd, int rot, int layout,
@@ -160,7 +161,7 @@ bool rope_at_vec(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows, int
   // halves keep twice the loads on their way with one: 62 us where all 128 values are turned, 71 with two)
   const bool many = !halves && whole && rows * units >= (int64_t)512 * 1024 * 4;
   const int64_t step = (int64_t)by * (many ? 2 : 1), grid = (rows + step - 1) / step;
-  if (grid >= (int64_t(1) << 31)) return false;
+  if (grid * bx * by >= (int64_t(1) << 32)) return false;    // (more threads than a launch has)
   if (!whole) {
     rope_at_part_kernel<T><<<(unsigned)grid, dim3(bx, by), 0, s>>>(x, ldx, out, ldo, rows, heads, hd, rot, layout, pos,
                                                                    cos_t, sin_t, n_pos);
@@ -177,7 +178,8 @@ bool rope_at_vec(const T* x, int64_t ldx, T* out, int64_t ldo, int64_t rows, int
 }
 
 // ---------------------------------------------------------------- attention, any shape
-// One wave a (row, head).
+// One wave a (row, head): what the tiles' kernels do not take.  Bound by latency and by K and V read again for every
+// row: 2018 tokens in 8 sequences, 8 heads of 80, 986 us.
 template <typename T>
 __global__ void __launch_bounds__(256) attention_packed_any(zoact_packed s, const T* __restrict__ q, int64_t ldq,
                                                             const T* __restrict__ k, int64_t ldk,
