@@ -185,3 +185,17 @@ def test_the_selection_and_the_torch_way_choose_alike():
     G._select_many(t_f32(lg), Z.Beams(t_f32(score), t_i32(hist)), 4, 7, other, t2, s2, None)
     assert torch.equal(tok, t2) and torch.equal(src, s2) and torch.equal(to.hist[:, :, :5], other.hist[:, :, :5])
     assert float((to.score - other.score).abs().max()) < 1e-4
+
+
+def test_rows_of_logits_further_apart_than_32_bits():
+    far = 2 ** 31 + 64
+    buf = torch.zeros(far + 4096, device=dev())
+    lg, score, hist = _case(2, 1, 600, 3, 17)
+    wide = buf.as_strided((2, 600), (far, 1))
+    wide.copy_(t_f32(lg))
+    announce("beam_select rows far apart")
+    want, tok, src = _select(lg, score, hist, 3, None, 5)
+    to, t2, s2 = Z.Beams.alloc(2, 5, want.hist.shape[2], dev()), torch.empty_like(tok), torch.empty_like(src)
+    ws = torch.empty(Z.beam_workspace_bytes(2, 1, 5, 600), dtype=torch.uint8, device=dev())
+    Z.beam_select(wide, Z.Beams(t_f32(score), t_i32(hist)), 3, None, to, t2, s2, ws)
+    assert torch.equal(t2, tok) and torch.equal(s2, src) and torch.equal(to.score, want.score)

@@ -249,6 +249,43 @@ def test_scores_near_the_ends_of_the_range(dt):
     _check(_attend(x, begin, 1, 1, hd, dt, 3.0e38), x, begin, 1, 1, hd, dt, 3.0e38)
 
 
+# ------------------------------------------------------------------ offsets past 32 bits
+@pytest.mark.parametrize("dt,hd", [("bf16", 64), ("fp32", 64), ("bf16", 24)])
+def test_attention_and_rotary_past_two_to_the_31_values(dt, hd):
+    """A sequence at the end of tensors of more than 2^31 values, and rows turned there: as at the beginning."""
+    H, Hkv, n = 8, 1, 150
+    width = (H + 2 * Hkv) * hd
+    rows = -(-(2 ** 31 + 2 ** 20) // width) + n
+    small, _ = _qkv([n], H, Hkv, hd, dt, seed=31)
+    few = _act(small, dt)
+    x = torch.zeros(rows, width, dtype=few.dtype, device=dev())
+    x[rows - n:] = few
+    announce("attention_packed past 2^31", dt, hd)
+    out = torch.empty(rows, H * hd, dtype=few.dtype, device=dev())
+    near = torch.empty(n, H * hd, dtype=few.dtype, device=dev())
+    Z.attention_packed(Z.Packed(t_i32([rows - n, rows]), rows, n), *_split(x, H, Hkv, hd), out, H, Hkv, hd, 0.2)
+    Z.attention_packed(Z.Packed.of([n], dev()), *_split(few, H, Hkv, hd), near, H, Hkv, hd, 0.2)
+    # (the same rows of a sequence in a workgroup, whose order of work alone differs)
+    assert torch.equal(out[rows - n:], near)
+    cos, sin = Z.rope_tables(64, hd, 1.0e4, dev())
+    pos = torch.full((rows,), 3, dtype=torch.int32, device=dev())
+    Z.rope_at(x, x, H + 2 * Hkv, hd, pos, cos, sin)
+    Z.rope_at(few, few, H + 2 * Hkv, hd, pos[:n], cos, sin)
+    assert torch.equal(x[rows - n:], few)
+
+
+def test_losses_past_two_to_the_31_logits():
+    V = 2 ** 29 + 4
+    lg = torch.zeros(2, 3, V, device=dev())
+    lg[1, 1, V - 1] = 7.0
+    loss, ws = torch.empty(2, device=dev()), torch.empty(Z.loss_workspace_bytes(), dtype=torch.uint8, device=dev())
+    announce("xent_packed past 2^31")
+    Z.xent_packed(lg, t_i32([0, 1, V - 1]), Z.Packed.of([3], dev()), loss, ws)
+    # two rows each of log V; one logit of 7 takes 3.5 of the mean (and adds 1100 to a sum of 5e8: 2e-6)
+    want = np.log(float(V)) - np.array([0.0, 3.5])
+    assert np.abs(host(loss) - want).max() < 1e-4
+
+
 # ------------------------------------------------------------------ rotary positions
 @pytest.mark.parametrize("layout", [Z.ROPE_HALF, Z.ROPE_INTERLEAVED])
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
