@@ -42,8 +42,9 @@ typedef struct {
  * Scores, softmax and sums fp32; with BF16 a probability, relative to the largest so far
  * of its row or to one within a factor 2^8 of it, is rounded to bf16 as it enters the
  * product with v (the normaliser sums it unrounded); one rounding of out.  What a row may
- * not attend to does not reach it, whatever it holds.  head_dim 32, 64 or 128 with
- * 16-byte aligned rows runs on the matrix cores; others run one wave a row and head. */
+ * not attend to does not reach it, whatever it holds.  A head_dim up to 128 of whole
+ * 16-byte pieces runs on the matrix cores if rows are 16-byte aligned (as the next of 32,
+ * 64 and 128); others run one wave a row and head. */
 zoact_status zoact_attention_packed(const zoact_packed* s, const void* q, int64_t ldq, const void* k, int64_t ldk,
                                     const void* v, int64_t ldv, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                     float scale, int32_t dtype, void* out, zoact_stream stream);

@@ -1,5 +1,5 @@
-// Causal attention over packed sequences on the matrix cores (zoact_packed.h): head_dim 32, 64 or
-// 128, rows of 16-byte aligned heads.
+// Causal attention over packed sequences on the matrix cores (zoact_packed.h): rows of 16-byte
+// aligned heads of 32, 64 or 128 values, or fewer with zeros in place of the rest.
 //
 // One pass over the keys with the running maximum m and sum l of each row's softmax:
 //   S^T = K Q^T (32 keys x 32 queries an MFMA),  P^T = 2^(S^T c - m),  O^T += V^T P^T,
@@ -148,10 +148,10 @@ __device__ __forceinline__ bool not_finite(const T* v, int64_t ldv, int first, i
 
 // Rows of a K or V tile from global memory straight to LDS, 256 threads with PER chunks of 16 bytes each, a
 // wave's 64 side by side; the swizzle is in the choice of each lane's chunk.  Rows past the sequence read as its
-// last.
-template <int CH, int PER>
+// last.  With PAD rows hold `chunks` chunks only, and the lanes of others load nothing.
+template <int CH, int PER, bool PAD>
 struct TileLoad {
-  int wave, len;
+  int wave, len, chunks;
   __device__ __forceinline__ void run(const char* from, int step, int (*swz)(int), char* to, int first, int rows) const {
     typedef __attribute__((address_space(3))) void lds_t;
     const int row_t = threadIdx.x / CH, ch_t = threadIdx.x % CH;
@@ -160,10 +160,11 @@ struct TileLoad {
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a);
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32));
     const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-        reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + CH * 16, 0x00020000);
+        reinterpret_cast<void*>(((uint64_t)hi << 32) | lo), (short)0, (left - 1) * step + (PAD ? chunks : CH) * 16, 0x00020000);
     constexpr int NEXT = 256 / CH;                           // rows between a thread's chunks
     if (NEXT % 16 == 0 && left == rows) {                    // (the swizzles are the same there: one offset for all)
       const int off = row_t * step + (ch_t ^ swz(row_t)) * 16;
+      if (PAD && (ch_t ^ swz(row_t)) >= chunks) return;
 #pragma unroll
       for (int u = 0; u < PER; ++u)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, off, u * NEXT * step, 0, 0);
@@ -173,12 +174,22 @@ struct TileLoad {
     for (int u = 0; u < PER; ++u) {
       int row = row_t + u * NEXT;
       const int chunk = ch_t ^ swz(row);
+      if (PAD && chunk >= chunks) continue;
       row = row < left ? row : left - 1;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_t*)(to + wave * 1024 + u * 4096), 16, row * step + chunk * 16, 0,
                                                0, 0);
     }
   }
 };
+
+// The chunks of a tile that PAD loads leave out, as zeros.
+template <int CH, int ROWS>
+__device__ __forceinline__ void clear_rest(char* tile, int (*swz)(int), int chunks) {
+  for (int i = threadIdx.x; i < ROWS * CH; i += 256) {
+    const int row = i / CH, c = i % CH;
+    if (c >= chunks) *reinterpret_cast<u32x4*>(tile + (row * CH + (c ^ swz(row))) * 16) = u32x4{0, 0, 0, 0};
+  }
+}
 
 template <int HD>
 struct Tile {
@@ -194,14 +205,17 @@ struct Tile {
   __device__ static int vswz(int row) { return CH == 16 ? (row & 3) << 2 : CH == 8 ? ((row >> 1) & 1) << 2 : 0; }
 };
 
-template <int HD>
+// PAD: heads are hd < HD values wide, a multiple of 8; the rest of HD is zero in q, K and V.
+template <int HD, bool PAD>
 __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
     attention_packed_bf16_kernel(zoact_packed s, const uint16_t* __restrict__ q, int64_t ldq,
                                  const uint16_t* __restrict__ k, int64_t ldk, const uint16_t* __restrict__ v, int64_t ldv,
-                                 int heads, int kv_heads, int gh, float scale, uint16_t* __restrict__ out) {
+                                 int heads, int kv_heads, int hd, int gh, float scale,
+                                 uint16_t* __restrict__ out) {
   using C = Tile<HD>;
   constexpr int KT = C::KT, SUBS = C::SUBS, ROW = C::ROW, CH = C::CH, PER = C::PER, NB = C::NB;
   constexpr int QF = HD / 16;                                // 16-byte pieces of a lane's query
+  const int WD = PAD ? hd : HD, chunks = WD / 8;
   // (arrays of their own, so that a read of one does not wait for the loads into another)
   __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, lq = lane & 31,
@@ -217,24 +231,31 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
   const int n_tiles = (last + KT - 1) / KT;
 
   const int kstep = (int)(ldk * 2), vstep = (int)(ldv * 2);
-  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
-  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
-  const TileLoad<CH, PER> tl{wave, len};
+  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * WD);
+  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * WD);
+  const TileLoad<CH, PER, PAD> tl{wave, len, chunks};
   auto load_k = [&](char* to, int t) { tl.run(kb, kstep, C::kswz, to, t * KT, KT); };
   auto load_v = [&](char* to, int t) { tl.run(vb, vstep, C::vswz, to, t * KT, KT); };
   auto arrived = [&] {
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's part; then everybody's
     __syncthreads();
   };
+  if (PAD) {
+    clear_rest<CH, KT>(k0, C::kswz, chunks);
+    clear_rest<CH, KT>(k1, C::kswz, chunks);
+    clear_rest<CH, KT>(v0, C::vswz, chunks);
+    clear_rest<CH, KT>(v1, C::vswz, chunks);
+  }
   load_k(k0, 0);
 
   // queries: lane's own row, pieces of 8 values by halves
   u32x4 qf[QF];
   {
     const int r = w0 + lq < len ? w0 + lq : len - 1;
-    const char* qp = reinterpret_cast<const char*>(q + (pl.row0 + r) * ldq + (int64_t)h * HD);
+    const char* qp = reinterpret_cast<const char*>(q + (pl.row0 + r) * ldq + (int64_t)h * WD);
 #pragma unroll
-    for (int c = 0; c < QF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(qp + (2 * c + lh) * 16);
+    for (int c = 0; c < QF; ++c)
+      qf[c] = !PAD || 2 * c + lh < chunks ? *reinterpret_cast<const u32x4*>(qp + (2 * c + lh) * 16) : u32x4{0, 0, 0, 0};
   }
   load_v(v0, 0);
   if (n_tiles > 1) load_k(k1, 1);
@@ -403,12 +424,12 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
   char* const mine = (wave < 2 ? k0 : k1) + wave % 2 * 32 * ROW;
   // (of a row whose l is not finite nothing is, whatever V holds)
   if (!far && __ballot(any - any != 0.f && l - l == 0.f))
-    far = not_finite(v + pl.row0 * ldv + (int64_t)g * HD, ldv, w0, w0 + 31 < len ? w0 + 31 : len - 1, HD);
+    far = not_finite(v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, w0 + 31 < len ? w0 + 31 : len - 1, WD);
   if (far) {
     for (int r = w0; r < w0 + 32 && r < len; ++r)
-      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
-                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, reinterpret_cast<float*>(mine),
-                 out + ((pl.row0 + r) * heads + h) * HD);
+      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * WD, k + pl.row0 * ldk + (int64_t)g * WD, ldk,
+                 v + pl.row0 * ldv + (int64_t)g * WD, ldv, r, WD, scale, reinterpret_cast<float*>(mine),
+                 out + ((pl.row0 + r) * heads + h) * WD);
     return;
   }
 #pragma unroll
@@ -419,12 +440,13 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
           make_uint2(pack2(o[n][4 * i], o[n][4 * i + 1]), pack2(o[n][4 * i + 2], o[n][4 * i + 3]));
     }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  char* const op = reinterpret_cast<char*>(out + ((pl.row0 + w0) * heads + h) * HD);
+  char* const op = reinterpret_cast<char*>(out + ((pl.row0 + w0) * heads + h) * WD);
 #pragma unroll
   for (int u = 0; u < 32 * CH / 64; ++u) {
     const int row = (u * 64 + lane) / CH, c = lane % CH;
     const u32x4 x = *reinterpret_cast<const u32x4*>(mine + row * ROW + (c ^ C::kswz(row)) * 16);
-    if (w0 + row < len) *reinterpret_cast<u32x4*>(op + (int64_t)row * heads * ROW + c * 16) = x;
+    if (w0 + row < len && (!PAD || c < chunks))
+      *reinterpret_cast<u32x4*>(op + (int64_t)row * heads * WD * 2 + c * 16) = x;
   }
 }
 
@@ -441,13 +463,15 @@ struct TileF {
   __device__ static int kswz(int row) { return CH >= 16 ? row & 15 : (row >> 1) & 7; }
 };
 
-template <int HD>
+// (PAD: a multiple of 4)
+template <int HD, bool PAD>
 __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
     attention_packed_f32_kernel(zoact_packed s, const float* __restrict__ q, int64_t ldq, const float* __restrict__ k,
-                                int64_t ldk, const float* __restrict__ v, int64_t ldv, int heads, int kv_heads, int gh,
-                                float scale, float* __restrict__ out) {
+                                int64_t ldk, const float* __restrict__ v, int64_t ldv, int heads, int kv_heads, int hd,
+                                int gh, float scale, float* __restrict__ out) {
   using C = TileF<HD>;
   constexpr int KT = C::KT, ROW = C::ROW, CH = C::CH, QF = C::QF, W = C::W, NV = C::NV;
+  const int WD = PAD ? hd : HD, chunks = WD / 4;
   typedef float floatw __attribute__((ext_vector_type(W)));
   __shared__ __align__(16) char k0[C::BYTES], k1[C::BYTES], v0[C::BYTES], v1[C::BYTES];
   __shared__ float qs[4][HD];                                // a row's query, where rows are taken one by one
@@ -467,23 +491,30 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
   const int n_tiles = (last + KT - 1) / KT;
 
   const int kstep = (int)(ldk * 4), vstep = (int)(ldv * 4);
-  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * HD);
-  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * HD);
-  const TileLoad<CH, KT * CH / 256> tl{wave, len};
+  const char* const kb = reinterpret_cast<const char*>(k + pl.row0 * ldk + (int64_t)g * WD);
+  const char* const vb = reinterpret_cast<const char*>(v + pl.row0 * ldv + (int64_t)g * WD);
+  const TileLoad<CH, KT * CH / 256, PAD> tl{wave, len, chunks};
   auto load_k = [&](char* to, int t) { tl.run(kb, kstep, C::kswz, to, t * KT, KT); };
   auto load_v = [&](char* to, int t) { tl.run(vb, vstep, no_swizzle, to, t * KT, KT); };
   auto arrived = [&] {
     __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's part; then everybody's
     __syncthreads();
   };
+  if (PAD) {
+    clear_rest<CH, KT>(k0, C::kswz, chunks);
+    clear_rest<CH, KT>(k1, C::kswz, chunks);
+    clear_rest<CH, KT>(v0, no_swizzle, chunks);
+    clear_rest<CH, KT>(v1, no_swizzle, chunks);
+  }
   load_k(k0, 0);
   // queries: lane's own row, chunks 4 c + lg
   u32x4 qf[QF];
   {
     const int r = w0 + lq < len ? w0 + lq : len - 1;
-    const char* qp = reinterpret_cast<const char*>(q + (pl.row0 + r) * ldq + (int64_t)h * HD);
+    const char* qp = reinterpret_cast<const char*>(q + (pl.row0 + r) * ldq + (int64_t)h * WD);
 #pragma unroll
-    for (int c = 0; c < QF; ++c) qf[c] = *reinterpret_cast<const u32x4*>(qp + (4 * c + lg) * 16);
+    for (int c = 0; c < QF; ++c)
+      qf[c] = !PAD || 4 * c + lg < chunks ? *reinterpret_cast<const u32x4*>(qp + (4 * c + lg) * 16) : u32x4{0, 0, 0, 0};
   }
   load_v(v0, 0);
   if (n_tiles > 1) load_k(k1, 1);
@@ -625,16 +656,16 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
       for (int i = 0; i < 4; ++i) any += o[n][e][i] *= inv;
   // (of a row whose l is not finite nothing is, whatever V holds)
   if (!far && __ballot(any - any != 0.f && l - l == 0.f))
-    far = not_finite(v + pl.row0 * ldv + (int64_t)g * HD, ldv, w0, w0 + 15 < len ? w0 + 15 : len - 1, HD);
+    far = not_finite(v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, w0 + 15 < len ? w0 + 15 : len - 1, WD);
   if (far) {
     for (int r = w0; r < w0 + 16 && r < len; ++r)
-      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * HD, k + pl.row0 * ldk + (int64_t)g * HD, ldk,
-                 v + pl.row0 * ldv + (int64_t)g * HD, ldv, r, HD, scale, qs[wave],
-                 out + ((pl.row0 + r) * heads + h) * HD);
+      attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * WD, k + pl.row0 * ldk + (int64_t)g * WD, ldk,
+                 v + pl.row0 * ldv + (int64_t)g * WD, ldv, r, WD, scale, qs[wave],
+                 out + ((pl.row0 + r) * heads + h) * WD);
     return;
   }
   if (w0 + lq >= len) return;
-  float* const op = out + ((pl.row0 + w0 + lq) * heads + h) * HD;
+  float* const op = out + ((pl.row0 + w0 + lq) * heads + h) * WD;
 #pragma unroll
   for (int n = 0; n < NV; ++n)
 #pragma unroll
@@ -642,7 +673,8 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
       floatw x;
 #pragma unroll
       for (int e = 0; e < W; ++e) x[e] = o[n][e][i];
-      *reinterpret_cast<floatw*>(op + 16 * W * n + W * (4 * lg + i)) = x;
+      const int col = 16 * W * n + W * (4 * lg + i);
+      if (!PAD || col < hd) *reinterpret_cast<floatw*>(op + col) = x;
     }
 }
 
@@ -652,7 +684,7 @@ hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t
                                    const void* v, int64_t ldv, int32_t heads, int32_t kv_heads, int32_t hd, float scale,
                                    int32_t dtype, void* out, hipStream_t hs) {
   const int64_t vec = dtype == ZOACT_BF16 ? 8 : 4;
-  if ((hd != 32 && hd != 64 && hd != 128) || ldq % vec || ldk % vec || ldv % vec || !aligned_to(q, 16) ||
+  if (hd > 128 || hd % vec || ldq % vec || ldk % vec || ldv % vec || !aligned_to(q, 16) ||
       !aligned_to(k, 16) || !aligned_to(v, 16) || !aligned_to(out, 16))
     return hipErrorNotSupported;
   if (!isfinite(fabsf(scale) * 1.4426950408889634f)) return hipErrorNotSupported;
@@ -662,16 +694,22 @@ hipError_t launch_attention_packed(const zoact_packed& s, const void* q, int64_t
   const int R = 4 / gh * (dtype == ZOACT_BF16 ? 32 : 16);
   const int64_t grid = (s.rows / R + s.n) * (heads / gh);
   if (grid >= (int64_t(1) << 24)) return hipErrorNotSupported;    // (a launch has less than 2^32 threads)
-#define ZO_ATT(T, KERNEL, HD)                                                                                     \
-  KERNEL<HD><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk, (const T*)v, ldv, heads, kv_heads, \
-                                             gh, scale, (T*)out)
+#define ZO_ATT(T, KERNEL, HD)                                                                                       \
+  do {                                                                                                              \
+    if (hd == HD)                                                                                                   \
+      KERNEL<HD, false><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk, (const T*)v, ldv, heads, \
+                                                        kv_heads, hd, gh, scale, (T*)out);                          \
+    else                                                                                                            \
+      KERNEL<HD, true><<<(unsigned)grid, 256, 0, hs>>>(s, (const T*)q, ldq, (const T*)k, ldk, (const T*)v, ldv, heads, \
+                                                       kv_heads, hd, gh, scale, (T*)out);                           \
+  } while (0)
   if (dtype == ZOACT_BF16) {
-    if (hd == 128) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 128);
-    else if (hd == 64) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 64);
+    if (hd > 64) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 128);
+    else if (hd > 32) ZO_ATT(uint16_t, attention_packed_bf16_kernel, 64);
     else ZO_ATT(uint16_t, attention_packed_bf16_kernel, 32);
   } else {
-    if (hd == 128) ZO_ATT(float, attention_packed_f32_kernel, 128);
-    else if (hd == 64) ZO_ATT(float, attention_packed_f32_kernel, 64);
+    if (hd > 64) ZO_ATT(float, attention_packed_f32_kernel, 128);
+    else if (hd > 32) ZO_ATT(float, attention_packed_f32_kernel, 64);
     else ZO_ATT(float, attention_packed_f32_kernel, 32);
   }
 #undef ZO_ATT

@@ -87,7 +87,7 @@ def test_attention(batch, dt, hd):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
-@pytest.mark.parametrize("hd", [1, 24, 40, 96, 200, 256])
+@pytest.mark.parametrize("hd", [1, 4, 8, 20, 24, 40, 80, 96, 120, 200, 256])
 def test_attention_of_other_heads(hd, dt):
     announce("attention_packed any", hd, dt)
     x, begin = _qkv([1, 70, 0, 33], 4, 2, hd, dt, first=1, behind=1)
@@ -139,7 +139,7 @@ def _round(a, dt):
     return synth.bf16_round(a) if dt == "bf16" else a
 
 
-@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("hd", [24, 32, 64, 80, 128])
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 def test_what_a_row_may_not_attend_to_does_not_reach_it(bad, dt, hd):
@@ -250,7 +250,7 @@ def test_scores_near_the_ends_of_the_range(dt):
 
 
 # ------------------------------------------------------------------ offsets past 32 bits
-@pytest.mark.parametrize("dt,hd", [("bf16", 64), ("fp32", 64), ("bf16", 24)])
+@pytest.mark.parametrize("dt,hd", [("bf16", 64), ("fp32", 64), ("bf16", 24), ("bf16", 20)])
 def test_attention_and_rotary_past_two_to_the_31_values(dt, hd):
     """A sequence at the end of tensors of more than 2^31 values, and rows turned there: as at the beginning."""
     H, Hkv, n = 8, 1, 150
