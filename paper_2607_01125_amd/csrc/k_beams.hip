@@ -471,6 +471,7 @@ extern "C" zoact_status zoact_beam_select(const zoact_beams* b, const void* logi
   ZP_CHECK(aligned_to(logits, dtype == ZOACT_F32 ? 4 : 2) && aligned_to(b->score, 4) && aligned_to(b->score_out, 4) &&
                aligned_to(b->hist, 4) && aligned_to(b->hist_out, 4) && aligned_to(b->token, 4) && aligned_to(b->src, 4),
            "beam_select: pointers must be aligned to their types");
+  ZP_CHECK(b->score_out != b->score && b->hist_out != b->hist, "beam_select: candidates selected into themselves");
   const Layout l = layout_of(b->n, b->beams_in, b->beams, b->vocab);
   if (ws == nullptr || ws_bytes < l.bytes) return set_error(ZOACT_E_WORKSPACE, "beam_select: workspace too small");
   ZP_CHECK(aligned_to(ws, 16), "beam_select: ws must be 16-byte aligned");

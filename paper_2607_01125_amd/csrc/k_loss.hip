@@ -4,7 +4,7 @@
 // one block adds them in a fixed tree order.  No atomics.
 //
 //  * MSE (single-layer workload): mean over T*N of (y[h] - target)^2.
-//  * Next-token cross entropy (decoder models): one block per (half, position)
+//  * Next-token cross entropy (decoder models; packed rows in xent_rows): one block per (half, position)
 //    row computes log-sum-exp over the vocabulary with an online max / sum of
 //    exponentials (wave64 shuffles, then the block), minus the target logit.
 // Both are HBM-bound single passes over y or the logits.

@@ -42,8 +42,8 @@ def _head(s=None, x=P, tokens=P, loss=P, ws=P, nb=1 << 40, **kw):
 
 
 def _beams(logits=P, ldl=100, dt=Z.F32, ws=P, nb=1 << 40, **kw):
-    f = dict(n=2, beams_in=3, beams=3, eos=2, vocab=100, length=4, score=256, hist=256, ld_hist=8, score_out=256,
-             hist_out=256, ld_hist_out=8, token=256, src=256)
+    f = dict(n=2, beams_in=3, beams=3, eos=2, vocab=100, length=4, score=256, hist=256, ld_hist=8, score_out=512,
+             hist_out=512, ld_hist_out=8, token=256, src=256)
     f.update(kw)
     return Z.lib().zoact_beam_select(ctypes.byref(Z.BeamsDesc(**f)), logits, ldl, dt, ws, nb, None)
 
@@ -77,7 +77,7 @@ def test_sequences_that_are_none(s):
     lambda: _beams(n=21846), lambda: _beams(vocab=2, ldl=2, eos=1), lambda: _beams(ldl=99), lambda: _beams(eos=100),
     lambda: _beams(eos=-2), lambda: _beams(length=-1), lambda: _beams(length=9, ld_hist_out=20),
     lambda: _beams(length=8), lambda: _beams(vocab=(1 << 30) + 1, ldl=1 << 31), lambda: _beams(token=258),
-    lambda: _beams(src=257), lambda: _beams(ws=ctypes.c_void_p(264)), lambda: _beams(logits=ctypes.c_void_p(258)),
+    lambda: _beams(score_out=256), lambda: _beams(hist_out=256), lambda: _beams(src=257), lambda: _beams(ws=ctypes.c_void_p(264)), lambda: _beams(logits=ctypes.c_void_p(258)),
 ])
 def test_bad_arguments(call):
     assert call() == Z.E_INVALID
