@@ -577,6 +577,8 @@ class Decoder:
         need = Z.project_workspace_bytes(n_tok, x.shape[1], self.r) if self.act == torch.bfloat16 else 0
         if need and (self._proj_ws is None or self._proj_ws.numel() < need):
             self._proj_ws = torch.empty(need, dtype=torch.uint8, device=self.dev)
+        if need:
+            self._hold(self._proj_ws)
         Z.project(x, ut, self._cur["p"][:n_tok], self._proj_ws if need else None, n_all=rows)
         return ut
 
