@@ -410,14 +410,15 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
     for (int o = each >> 1; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
     if (c < got && rank < K && (threadIdx.x & (each - 1)) == 0) emit(rank, k, f);
   } else {
-    // very many equal ones: one at a time
-    uint64_t lk = ~0ull, lf = ~0ull;
+    // very many equal ones: one at a time, each behind the one before (a NaN of the first beam and token has the
+    // highest key and place that there are: nothing is behind what the first would start from)
+    uint64_t lk = 0, lf = 0;
     for (int m = 0; m < K; ++m) {
       uint64_t bk = 0, bf = 0;
       for (uint32_t c = threadIdx.x; c < total; c += NP) {
         uint64_t k, f;
         read(c, k, f);
-        if (k && better(lk, lf, k, f) && better(k, f, bk, bf)) bk = k, bf = f;
+        if (k && (m == 0 || better(lk, lf, k, f)) && better(k, f, bk, bf)) bk = k, bf = f;
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
