@@ -15,9 +15,10 @@
 // neither the K rows nor the V columns (read transposed by ds_read_tr16) meet in a bank.
 //
 // Keys that some of a wave's rows may not see are in its last tiles only, from its first row's tile of 32 on; there
-// the scores are masked.  Two things make a wave take its rows one by one in the end: a masked V that is not finite
-// (0 * inf is NaN), looked for where an output is not; and a maximum past 2^27, where S^T c - m, fused, is off by the
-// rounding of the product that became m, which 2^x no longer bears.
+// the scores are masked.  Three things make a wave take its rows one by one in the end: a masked V that is not finite
+// (0 * inf is NaN) and values whose weighted sum passes the range though their mean does not, both looked for where an
+// output is not finite; and a maximum past 2^27, where S^T c - m, fused, is off by the rounding of the product that
+// became m, which 2^x no longer bears.
 //
 // Long sequences are bound by the matrix cores (60% busy at 1.7 GHz) and as many cycles of exponentials, sums and
 // conversions beside them: 12001 tokens and 30 short sequences, 32/8 heads of 128, in 1.09 ms, 1080 TFLOP/s.  Short
@@ -135,15 +136,26 @@ __device__ __forceinline__ unsigned turn_about() {
 
 __device__ __forceinline__ int no_swizzle(int) { return 0; }
 
-// Whether rows first .. last of a head's V hold something that is not finite.
-template <typename T>
-__device__ __forceinline__ bool not_finite(const T* v, int64_t ldv, int first, int last, int hd) {
-  bool bad = false;
-  for (int i = threadIdx.x & 63; i < (last - first + 1) * hd; i += 64) {
-    const float x = ld1(v + (first + i / hd) * ldv + i % hd);
-    bad |= !(x - x == 0.f);
+// Bits of what a value is that is not finite.
+enum { IS_NAN = 1, IS_POS = 2, IS_NEG = 4 };
+__device__ __forceinline__ int kind_of(float x) { return x - x == 0.f ? 0 : x != x ? IS_NAN : x > 0.f ? IS_POS : IS_NEG; }
+
+// Whether the formula may have others in place of a wave's outputs that are not finite (outs(c): what those of column
+// c are): not where V holds their cause in a row that all of the wave's rows see, 0 .. seen.  It may where that cause
+// is in a row that some do not see (0 * inf is NaN), or where the weighted sum passed the range and the mean does not.
+template <typename T, typename Outs>
+__device__ __forceinline__ bool in_doubt(Outs outs, const T* v, int64_t ldv, int seen, int hd) {
+  bool doubt = false;
+  for (int c = threadIdx.x & 63; c < hd; c += 64) {
+    const int got = outs(c);
+    if (got == 0) continue;
+    int have = 0;
+    for (int r = 0; r <= seen && !(have & IS_NAN); r += 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) have |= kind_of(ld1(v + (r + u < seen ? r + u : seen) * ldv + c));
+    doubt |= !(have & IS_NAN) && have != (IS_POS | IS_NEG) && have != got;
   }
-  return __ballot(bad) != 0;
+  return __ballot(doubt) != 0;
 }
 
 // Rows of a K or V tile from global memory straight to LDS, 256 threads with PER chunks of 16 bytes each, a
@@ -422,9 +434,29 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
     for (int i = 0; i < 16; ++i) any += o[n][i] *= inv;
   __syncthreads();
   char* const mine = (wave < 2 ? k0 : k1) + wave % 2 * 32 * ROW;
+  auto put_rows = [&] {
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        *reinterpret_cast<uint2*>(mine + lq * ROW + ((4 * n + i) ^ C::kswz(lq)) * 16 + lh * 8) =
+            make_uint2(pack2(o[n][4 * i], o[n][4 * i + 1]), pack2(o[n][4 * i + 2], o[n][4 * i + 3]));
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  };
   // (of a row whose l is not finite nothing is, whatever V holds)
-  if (!far && __ballot(any - any != 0.f && l - l == 0.f))
-    far = not_finite(v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, w0 + 31 < len ? w0 + 31 : len - 1, WD);
+  if (!far && w0 < len && __ballot(any - any != 0.f && l - l == 0.f)) {
+    put_rows();
+    const uint32_t sums = (uint32_t)__ballot(l - l == 0.f);
+    far = in_doubt([&](int c) {
+      int got = 0;
+      for (int r = 0; r < 32; ++r) {
+        const char* const at = mine + r * ROW + ((c >> 3) ^ C::kswz(r)) * 16 + (c & 7) * 2;
+        got |= sums >> r & 1 ? kind_of(bf2f(*reinterpret_cast<const uint16_t*>(at))) : 0;
+      }
+      return got;
+    }, v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, WD);
+  }
   if (far) {
     for (int r = w0; r < w0 + 32 && r < len; ++r)
       attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * WD, k + pl.row0 * ldk + (int64_t)g * WD, ldk,
@@ -432,14 +464,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
                  out + ((pl.row0 + r) * heads + h) * WD);
     return;
   }
-#pragma unroll
-  for (int n = 0; n < NB; ++n)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      *reinterpret_cast<uint2*>(mine + lq * ROW + ((4 * n + i) ^ C::kswz(lq)) * 16 + lh * 8) =
-          make_uint2(pack2(o[n][4 * i], o[n][4 * i + 1]), pack2(o[n][4 * i + 2], o[n][4 * i + 3]));
-    }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  put_rows();
   char* const op = reinterpret_cast<char*>(out + ((pl.row0 + w0) * heads + h) * WD);
 #pragma unroll
   for (int u = 0; u < 32 * CH / 64; ++u) {
@@ -655,8 +680,22 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 4)
 #pragma unroll
       for (int i = 0; i < 4; ++i) any += o[n][e][i] *= inv;
   // (of a row whose l is not finite nothing is, whatever V holds)
-  if (!far && __ballot(any - any != 0.f && l - l == 0.f))
-    far = not_finite(v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, w0 + 15 < len ? w0 + 15 : len - 1, WD);
+  if (!far && w0 < len && __ballot(any - any != 0.f && l - l == 0.f)) {
+    int* const cols = reinterpret_cast<int*>(qs[wave]);
+    for (int c = lane; c < HD; c += 64) cols[c] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (l - l == 0.f) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (const int x = kind_of(o[n][e][i])) atomicOr(cols + 16 * W * n + W * (4 * lg + i) + e, x);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    far = in_doubt([&](int c) { return cols[c]; }, v + pl.row0 * ldv + (int64_t)g * WD, ldv, w0, WD);
+  }
   if (far) {
     for (int r = w0; r < w0 + 16 && r < len; ++r)
       attend_row(q + (pl.row0 + r) * ldq + (int64_t)h * WD, k + pl.row0 * ldk + (int64_t)g * WD, ldk,

@@ -78,8 +78,9 @@ __device__ __forceinline__ void st1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st1(uint16_t* p, float v) { *p = f2bf(v); }
 
 // Attention of one row and head by one wave: q over the keys 0 .. row, 64 at a time, a key a lane for the scores and
-// a column a lane for the sums, with the running maximum m and sum l of the softmax; head_dim at most 256, which qs
-// (in LDS, the wave's own) holds in fp32.
+// a column a lane for the means, with the running maximum m and sum l of the softmax; head_dim at most 256, which qs
+// (in LDS, the wave's own) holds in fp32.  What is carried is the mean of the values so far, not their weighted sum,
+// which large values would take past the range.
 template <typename T>
 __device__ __forceinline__ void attend_row(const T* q, const T* k, int64_t ldk, const T* v, int64_t ldv, int row, int hd,
                                            float scale, float* qs, T* out) {
@@ -98,29 +99,25 @@ __device__ __forceinline__ void attend_row(const T* q, const T* k, int64_t ldk, 
       for (int d = 0; d < hd; ++d) t = fmaf(qs[d], ld1(kr + d), t);
       sc = t * scale;
     }
-    float mx = sc == sc ? sc : -INFINITY;
-#pragma unroll
-    for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-    const float mn = fmaxf(m, mx);
-    const float p = key <= row ? expf(sc - mn) : 0.f, a = expf(m - mn);
+    const float mn = fmaxf(m, wave_max(sc));
+    const float p = key <= row ? expf(sc - mn) : 0.f, was = l * expf(m - mn);
     m = mn;
-    l = l * a + p;
+    l = was + wave_sum(p);
+    const float unit = l != 0.f ? 1.f / l : 0.f, share = was * unit, w = p * unit;
     const int cnt = row - key0 + 1 < 64 ? row - key0 + 1 : 64;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] *= a;
+    for (int e = 0; e < 4; ++e) o[e] *= share;
     for (int t = 0; t < cnt; ++t) {
-      const float pt = __shfl(p, t, 64);
+      const float wt = __shfl(w, t, 64);
       const T* vr = v + (key0 + t) * ldv;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (e * 64 + lane < hd) o[e] = fmaf(pt, ld1(vr + e * 64 + lane), o[e]);
+        if (e * 64 + lane < hd) o[e] = fmaf(wt, ld1(vr + e * 64 + lane), o[e]);
     }
   }
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) l += __shfl_xor(l, x, 64);
-#pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (e * 64 + lane < hd) st1(out + e * 64 + lane, o[e] / l);
+    if (e * 64 + lane < hd) st1(out + e * 64 + lane, l != 0.f ? o[e] : NAN);
 }
 
 // Whether row has a next row in its own sequence.

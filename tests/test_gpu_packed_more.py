@@ -1,4 +1,5 @@
 """Packed sequences on the GPU where buffers, sizes and values are at their ends.  Tolerances as in test_gpu_packed."""
+import numpy as np
 import pytest
 import torch
 
@@ -6,9 +7,9 @@ import synth
 from paper_2607_01125_amd import model as gm
 from paper_2607_01125_amd import zoact as Z
 
-from gpu_helpers import announce, dev
+from gpu_helpers import announce, dev, host
 from test_gpu_model import LLAMA_S, _models
-from test_gpu_packed import _texts
+from test_gpu_packed import _attend, _check, _qkv, _split, _texts
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +45,46 @@ def test_a_graph_of_deep_projections_outlives_larger_batches():
             assert torch.equal(out, want)
         assert all(bool((f == 7).all()) for f in fresh)
     assert any(h.data_ptr() == at for h in g._held if isinstance(h, torch.Tensor))
+
+
+@pytest.mark.parametrize("hd", [20, 24, 32, 64, 80, 128, 200])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_values_near_the_top_of_the_range(dt, hd):
+    """Values of about 2^126, of one sign or of both: their weighted sums pass fp32's range, their means do not."""
+    H, Hkv = 4, 2
+    x, begin = _qkv([1, 150, 0, 333, 33], H, Hkv, hd, dt, seed=41, first=1, behind=2)
+    v = _split(x, H, Hkv, hd)[2]
+    v *= np.float32(2.0 ** 124)                # (exact in either type; below 2^127)
+    assert np.nanmax(np.abs(v)) < 2.0 ** 127.5
+    announce("attention_packed large values", dt, hd)
+    for sign in (False, True):
+        if sign:
+            v[:] = np.abs(v)
+        out = _attend(x, begin, H, Hkv, hd, dt, 0.1)
+        _check(out, x, begin, H, Hkv, hd, dt, 0.1)
+    assert np.nanmax(host(out)) > 2.0 ** 120
+
+
+@pytest.mark.parametrize("hd", [32, 64, 80, 128])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_infinities_beside_large_values_and_masked_ones(dt, hd):
+    """An infinity that rows see, beside values whose weighted sum passes the range on the other side, or beside a NaN
+    that only later rows see: the formula's infinity; finite columns stay finite."""
+    H, Hkv, L = 4, 2, 140
+    x, begin = _qkv([L], H, Hkv, hd, dt, seed=42)
+    v = _split(x, H, Hkv, hd)[2]
+    v[:] = 1.0
+    v[:, 0] = -2.0 ** 126
+    v[10, 0] = np.inf
+    v[10, 1], v[50, 1], v[60, 1] = np.inf, np.nan, -np.inf
+    v[70, 2] = -np.inf
+    v[:, 3] = 2.0 ** 127
+    announce("attention_packed infinities beside large values", dt, hd)
+    got = host(_attend(x, begin, H, Hkv, hd, dt, 0.02)).reshape(L, H, hd)[:, :H // Hkv]
+    # means of equal values: a rounding of each weight and one of the mean in bf16; L + 64 of 2^-24 in fp32
+    half = 2.0 ** -8 if dt == "bf16" else 2.0 ** -17
+    assert np.all(np.abs(got[:10, :, 0] + 2.0 ** 126) <= half * 2.0 ** 127) and np.all(got[10:, :, 0] == np.inf)
+    assert np.all(np.isfinite(got[:10, :, 1])) and np.all(got[10:50, :, 1] == np.inf) and np.isnan(got[50:, :, 1]).all()
+    assert np.all(np.abs(got[:70, :, 2] - 1.0) <= 2 * half) and np.all(got[70:, :, 2] == -np.inf)
+    assert np.all(np.abs(got[:, :, 3] - 2.0 ** 127) <= half * 2.0 ** 128)
+    assert np.all(np.abs(got[:, :, 4:] - 1.0) <= 2 * half)
