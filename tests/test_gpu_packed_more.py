@@ -88,3 +88,26 @@ def test_infinities_beside_large_values_and_masked_ones(dt, hd):
     assert np.all(np.abs(got[:70, :, 2] - 1.0) <= 2 * half) and np.all(got[70:, :, 2] == -np.inf)
     assert np.all(np.abs(got[:, :, 3] - 2.0 ** 127) <= half * 2.0 ** 128)
     assert np.all(np.abs(got[:, :, 4:] - 1.0) <= 2 * half)
+
+
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("hd", [24, 32, 64, 128])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+def test_scores_whose_exponents_pass_the_range(dt, hd, sign):
+    """Scores between 2^127 (1.5 and 1.98) of either sign, which log2(e) takes past fp32's range: the largest key's V
+    and nothing else, or the mean of equal ones."""
+    L = 150
+    x = np.zeros((L, 3 * hd), np.float32)
+    x[:, 0] = 2.0 ** 64
+    x[:, hd] = sign * 2.0 ** 63 * (1.5 + (np.arange(L) * 37 % 32) / 66.0).astype(np.float32)
+    x[:, hd] = synth.bf16_round(x[:, hd])
+    x[:, 2 * hd:] = (np.arange(L * hd).reshape(L, hd) * 7919 % 128)
+    begin = np.array([0, 64, L], np.int32)
+    announce("attention_packed exponents past the range", dt, hd, sign)
+    got = host(_attend(x, begin, 1, 1, hd, dt, 1.0))
+    for b, e in zip(begin[:-1], begin[1:]):
+        for t in range(b, e):
+            s = x[b:t + 1, hd]
+            want = x[b:t + 1, 2 * hd:][s == s.max()].astype(np.float64).mean(axis=0)
+            # (values below 128: a rounding of the mean, and in fp32 some of the weights and sums)
+            assert np.all(np.abs(got[t] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -16), t
