@@ -81,6 +81,9 @@ class PackedBatch:
         Z._arg(self.pos, "pos", torch.int32, dev, (2 * T,))
         if self.both.rows != 2 * T or self.both.index != dev:
             raise ValueError("a packed batch needs both halves' rows, on one device")
+        # (tables of positions are made for max_len, and the calls that read them clamp)
+        if T and not (int(self.pos.min()) >= 0 and int(self.pos.max()) < self.seqs.max_len):
+            raise ValueError(f"positions outside [0, {self.seqs.max_len}), the sequences' max_len")
 
     @classmethod
     def of(cls, sequences, device="cuda"):
@@ -90,8 +93,10 @@ class PackedBatch:
             raise ValueError("expected sequences of at least one token")
         lens = [t.numel() for t in ts]
         pos = torch.cat([torch.arange(n, dtype=torch.int32) for n in lens])
-        return cls(torch.cat(ts).to(device), Z.Packed.of(lens, device), Z.Packed.of(lens + lens, device),
-                   torch.cat([pos, pos]).to(device))
+        batch = object.__new__(cls)
+        batch.__dict__.update(tokens=torch.cat(ts).to(device), seqs=Z.Packed.of(lens, device),
+                              both=Z.Packed.of(lens + lens, device), pos=torch.cat([pos, pos]).to(device))
+        return batch
 
 
 def arena_layout(shape) -> list:

@@ -111,3 +111,23 @@ def test_scores_whose_exponents_pass_the_range(dt, hd, sign):
             want = x[b:t + 1, 2 * hd:][s == s.max()].astype(np.float64).mean(axis=0)
             # (values below 128: a rounding of the mean, and in fp32 some of the weights and sums)
             assert np.all(np.abs(got[t] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -16), t
+
+
+def test_positions_past_the_longest_sequence_are_refused():
+    """A batch made by hand whose max_len is smaller than its positions reach, or whose positions are negative: the
+    tables made for max_len would give other rows' angles.  One that fits gives what PackedBatch.of gives."""
+    import dataclasses
+    b = gm.PackedBatch.of(_texts(synth.TINY, [600, 3]), dev())
+    announce("packed batch by hand")
+
+    def made(max_len, pos):
+        return gm.PackedBatch(b.tokens, dataclasses.replace(b.seqs, max_len=max_len), b.both, pos)
+
+    for max_len, pos in ((599, b.pos), (256, b.pos), (0, b.pos), (600, b.pos + 1), (600, b.pos - 1)):
+        with pytest.raises(ValueError, match="positions"):
+            made(max_len, pos)
+    _, g = _models(synth.TINY, "fp32", 4)
+    pert = Z.Pert(0, 0, 0, 0.0)
+    want = g.forward(b, pert).clone()
+    for max_len in (600, 5000):
+        assert torch.equal(g.forward(made(max_len, b.pos), pert), want)
