@@ -227,6 +227,7 @@ class Decoder:
         self._packed_T = 0       # rows a half that the buffers of packed batches hold
         self._held = []          # buffers that grow with the batch and that a graph may replay on
         self._rope = {}
+        self._packed_rope = None
         self._ch = self._ch_all = None   # per-step C +/- eps Z of the whole arena (bf16 modes)
         # the perturbation the last update pass wrote into _ch_all for the next step:
         # (pair key, arena.c._version after the pass); any torch-side write to C bumps the
@@ -377,13 +378,23 @@ class Decoder:
         if torch.cuda.is_current_stream_capturing() and not any(x is h for h in self._held):
             self._held.append(x)
 
+    def _packed_rope_tables(self, max_len: int):
+        """Tables of packed batches, whose lengths are hardly ever the same: one pair, for the next power of two of the
+        longest sequence so far (each holds the shorter ones' rows; one that a graph was captured on stays)."""
+        if self._packed_rope is None or self._packed_rope[0].shape[0] < max_len:
+            self._packed_rope = self._make_rope_tables(max(256, 1 << (max_len - 1).bit_length()))
+        self._hold(self._packed_rope)
+        return self._packed_rope
+
     def _rope_tables(self, seq: int):
         """Tables of the positions below seq; shape.extra["rope"] (a dict) holds rope_tables' arguments of a model
         with scaled positions."""
         if seq not in self._rope:
-            self._rope[seq] = Z.rope_tables(seq, self.hd, self.s.rope_theta, self.dev,
-                                            **getattr(self.s, "extra", {}).get("rope", {}))
+            self._rope[seq] = self._make_rope_tables(seq)
         return self._rope[seq]
+
+    def _make_rope_tables(self, seq: int):
+        return Z.rope_tables(seq, self.hd, self.s.rope_theta, self.dev, **getattr(self.s, "extra", {}).get("rope", {}))
 
     # ---------------------------------------------------------------- forward of both halves
     def _norm_site(self, l, site, x, w, b, y, adapt, calibrate, rows):
@@ -490,12 +501,12 @@ class Decoder:
         self._ch_next = None
         if packed is None:
             Z.embed(tokens, self.emb, B["h0"], seq, self.pos, pos_offset=2, distinct_halves=distinct_halves)
-            positions = seq
         else:
             self._embed_packed(packed, B)
-            positions = -(-packed.seqs.max_len // 256) * 256      # (few tables for batches of many lengths)
         h, h_alt = B["h0"], B["h1"]
-        cos_sin = self._rope_tables(positions) if s.family == "llama" else None
+        cos_sin = None
+        if s.family == "llama":
+            cos_sin = self._rope_tables(seq) if packed is None else self._packed_rope_tables(packed.seqs.max_len)
         d, dkv, H, Hkv, hd = self.d, self.dkv, self.H, self.Hkv, self.hd
         scale = float(np.float32(1.0 / math.sqrt(hd)))
         for l, P in enumerate(self.layers):
