@@ -7,9 +7,10 @@ import synth
 from paper_2607_01125_amd import model as gm
 from paper_2607_01125_amd import zoact as Z
 
-from gpu_helpers import announce, dev, host
+import packed_ref as ref
+from gpu_helpers import announce, dev, host, t_f32, t_i32
 from test_gpu_model import LLAMA_S, _models
-from test_gpu_packed import _attend, _check, _qkv, _split, _texts
+from test_gpu_packed import _act, _attend, _check, _draw, _qkv, _split, _texts
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +132,37 @@ def test_positions_past_the_longest_sequence_are_refused():
     want = g.forward(b, pert).clone()
     for max_len in (600, 5000):
         assert torch.equal(g.forward(made(max_len, b.pos), pert), want)
+
+
+@pytest.mark.parametrize("dt,hd,H,Hkv", [("bf16", 128, 4, 1), ("bf16", 64, 2, 2), ("bf16", 32, 4, 2), ("bf16", 80, 2, 1),
+                                         ("fp32", 64, 2, 1), ("fp32", 128, 2, 2)])
+def test_attention_of_thousands_of_tokens(dt, hd, H, Hkv):
+    """A long sequence among short ones: whole tiles in their steady order, maxima that are followed late."""
+    x, begin = _qkv([40, 3001, 7, 129], H, Hkv, hd, dt, seed=43, first=2, behind=3)
+    announce("attention_packed long", dt, hd, H, Hkv)
+    scale = float(np.float32(1 / np.sqrt(hd)))
+    _check(_attend(x, begin, H, Hkv, hd, dt, scale), x, begin, H, Hkv, hd, dt, scale)
+
+
+@pytest.mark.parametrize("heads,hd,rot", [(40, 128, 64), (40, 128, 128)])
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows", [16411, 16412])
+def test_rope_at_of_many_rows_in_pairs(rows, dt, heads, hd, rot):
+    """So many rows that a thread takes two of them, an odd number among them; nothing behind the last is written."""
+    n_pos = 300
+    few = _draw((64, heads * hd), 1.0, 44, hd, rot, dt=dt)
+    x = torch.empty(rows + 2, heads * hd, dtype=_act(few[:1], dt).dtype, device=dev())
+    x[:rows] = _act(few, dt).repeat(rows // 64 + 1, 1)[:rows]
+    x[rows:] = 9.0
+    pos = synth.gen(44, rows).integers(-2, n_pos + 2, rows).astype(np.int32)
+    cos, sin = (t.cpu().numpy() for t in Z.rope_tables(n_pos, rot, 1.0e4, "cpu"))
+    out = torch.full_like(x, -7.0)
+    announce("rope_at many rows", rows, dt, heads, hd, rot)
+    for a, b in ((x, out), (x, x)):
+        Z.rope_at(a[:rows], b[:rows], heads, hd, t_i32(pos), t_f32(cos), t_f32(sin), Z.ROPE_INTERLEAVED)
+    assert torch.equal(out[:rows], x[:rows]) and bool((out[rows:] == -7.0).all()) and bool((x[rows:] == 9.0).all())
+    half = 2.0 ** -8 if dt == "bf16" else 2.0 ** -24
+    at = np.r_[0:5, 8000:8064, rows - 5:rows]
+    want, bound = ref.turn(few[at % 64].astype(np.float64), heads, hd, rot, Z.ROPE_INTERLEAVED,
+                           np.clip(pos[at], 0, n_pos - 1), cos, sin)
+    assert np.all(np.abs(host(out[torch.from_numpy(at).to(dev())]) - want) <= half * np.abs(want) + bound)
