@@ -85,7 +85,8 @@ zoact_status zoact_linear_xent_packed(const zoact_linear* L, const zoact_arena* 
  *   score[i][b] + logits[b][v] - log sum_u exp(logits[b][u])
  * or, where b has ended (eos >= 0, length > 0 and its last token is eos), score[i][b] for
  * v = eos and -inf for every other v.  The `beams` largest of a prompt's are kept, largest
- * first, of equal ones the lowest (b, v) first; NaN counts as largest.  A row whose log sum
+ * first, of equal ones the lowest (b, v) first; NaN counts as largest.  Finite values of one
+ * beam are in the order of their logits, also where fp64 does not resolve it.  A row whose log sum
  * is not finite (a NaN or +inf among its logits, or nothing but -inf) gives NaN, and so
  * does a score of NaN or +inf.  Kept candidate m of prompt i:
  *   score_out[i][m] its value, token[i][m] = v, src[i][m] = i * beams + b (where beam b's

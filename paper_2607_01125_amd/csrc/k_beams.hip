@@ -255,8 +255,9 @@ __global__ void __launch_bounds__(NT) beam_rows(const T* __restrict__ logits, in
 
 enum { BEAM_PLAIN, BEAM_ENDED, BEAM_NAN, BEAM_LOST };   // LOST: every value is -inf
 
-// One workgroup a prompt.  Candidates are compared as (key, place): the value's order, then minus beam and token, so
-// that the larger one comes first.  OWN: the prompt's part, its only one, is not there yet.
+// One workgroup a prompt.  Candidates are compared as (key, place, logit): the value's order, then the lower beam, then
+// the larger logit (which 64 bits may not resolve beside the log sum: the parts' lists are in its order), then the lower
+// token.  OWN: the prompt's part, its only one, is not there yet.
 template <typename T, bool VEC, bool OWN>
 __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, int64_t ldl, zoact_beams b, int splits,
                                                 float2* sums, Cand* cand) {
@@ -265,7 +266,9 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
   __shared__ float top[KMAX];
   __shared__ int kind[KMAX];
   __shared__ uint64_t key[CAP], place[CAP];
+  __shared__ uint32_t logit[CAP];
   __shared__ uint64_t wkey[WAVES], wplace[WAVES];
+  __shared__ uint32_t wlogit[WAVES];
   __shared__ uint32_t tops[WAVES][64];
   __shared__ int n_got;
   __shared__ int parent[KMAX];
@@ -321,11 +324,12 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
   // Candidate c of the prompt: beam j's part and place, or for beams whose values do not follow the
   // logits the lowest tokens (an ended one's eos first).
   auto place_at = [](uint32_t j, int v) { return ~(((uint64_t)j << 32) | (uint32_t)v); };
-  auto rate = [&](uint32_t c, Cand d, uint64_t& k, uint64_t& f) {
+  auto rate = [&](uint32_t c, Cand d, uint64_t& k, uint64_t& f, uint32_t& x) {
     const uint32_t j = c / per, t = c - j * per;
-    k = f = 0;
+    k = f = x = 0;
     if (kind[j] == BEAM_PLAIN) {
       if (d.v < 0) return;
+      x = order32(d.x);
       k = order64(sc[j] + ((double)d.x - lse[j]));
       f = place_at(j, d.v);
     } else if (t < (uint32_t)K) {
@@ -339,8 +343,14 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
       f = place_at(j, v);
     }
   };
-  auto read = [&](uint32_t c, uint64_t& k, uint64_t& f) { rate(c, cand[(int64_t)i0 * total + c], k, f); };
-  auto better = [](uint64_t k, uint64_t f, uint64_t k2, uint64_t f2) { return k > k2 || (k == k2 && f > f2); };
+  auto read = [&](uint32_t c, uint64_t& k, uint64_t& f, uint32_t& x) { rate(c, cand[(int64_t)i0 * total + c], k, f, x); };
+  // (of equal keys)
+  auto before = [](uint64_t f, uint32_t x, uint64_t f2, uint32_t x2) {
+    return f >> 32 == f2 >> 32 && x != x2 ? x > x2 : f > f2;
+  };
+  auto better = [&](uint64_t k, uint64_t f, uint32_t x, uint64_t k2, uint64_t f2, uint32_t x2) {
+    return k > k2 || (k == k2 && before(f, x, f2, x2));
+  };
   auto emit = [&](int m, uint64_t k, uint64_t f) {
     const int j = (int)(~f >> 32), v = (int)(uint32_t)~f;
     const int64_t o = (int64_t)i0 * K + m;
@@ -352,17 +362,19 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
   };
   const bool few = total <= 128;         // all of them are ranked then
   uint64_t kk[KEEP], kf[KEEP], mine = 0;
+  uint32_t kx[KEEP];
 #pragma unroll
   for (int q = 0; q < KEEP; ++q) {
-    kk[q] = kf[q] = 0;
+    kk[q] = kf[q] = kx[q] = 0;
     const uint32_t c = threadIdx.x + q * NP;
-    if (c < total) rate(c, raw[q], kk[q], kf[q]);
+    if (c < total) rate(c, raw[q], kk[q], kf[q], kx[q]);
     mine = kk[q] > mine ? kk[q] : mine;
   }
 #pragma unroll 8
   for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
     uint64_t k, f;
-    read(c, k, f);
+    uint32_t x;
+    read(c, k, f, x);
     mine = k > mine ? k : mine;
   }
   // Of the maxima of 64 groups of candidates (a lane's in all waves) the K-th largest, or a little less (20 bits of
@@ -381,18 +393,19 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
     }
     thr = to ? (uint64_t)to << 32 : 1;
   }
-  auto gather = [&](uint64_t k, uint64_t f) {
+  auto gather = [&](uint64_t k, uint64_t f, uint32_t x) {
     if (k < thr) return;
     const int p = atomicAdd(&n_got, 1);  // (the order of arrival changes nothing: ranks decide)
-    if (p < CAP) key[p] = k, place[p] = f;
+    if (p < CAP) key[p] = k, place[p] = f, logit[p] = x;
   };
 #pragma unroll
-  for (int q = 0; q < KEEP; ++q) gather(kk[q], kf[q]);
+  for (int q = 0; q < KEEP; ++q) gather(kk[q], kf[q], kx[q]);
 #pragma unroll 8
   for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
     uint64_t k, f;
-    read(c, k, f);
-    gather(k, f);
+    uint32_t x;
+    read(c, k, f, x);
+    gather(k, f, x);
   }
   __syncthreads();
   const int got = n_got;
@@ -405,7 +418,11 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
     uint64_t k = 0, f = 0;
     if (c < got) {
       k = key[c], f = place[c];
-      for (int t = threadIdx.x & (each - 1); t < got; t += each) rank += better(key[t], place[t], k, f);
+      for (int t = threadIdx.x & (each - 1); t < got; t += each) {
+        const uint64_t other = key[t];
+        rank += other > k;
+        if (other == k && t != c) rank += before(place[t], logit[t], f, logit[c]);
+      }
     }
     for (int o = each >> 1; o > 0; o >>= 1) rank += __shfl_xor(rank, o, 64);
     if (c < got && rank < K && (threadIdx.x & (each - 1)) == 0) emit(rank, k, f);
@@ -413,25 +430,28 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
     // very many equal ones: one at a time, each behind the one before (a NaN of the first beam and token has the
     // highest key and place that there are: nothing is behind what the first would start from)
     uint64_t lk = 0, lf = 0;
+    uint32_t lx = 0;
     for (int m = 0; m < K; ++m) {
       uint64_t bk = 0, bf = 0;
+      uint32_t bx = 0;
       for (uint32_t c = threadIdx.x; c < total; c += NP) {
         uint64_t k, f;
-        read(c, k, f);
-        if (k && (m == 0 || better(lk, lf, k, f)) && better(k, f, bk, bf)) bk = k, bf = f;
+        uint32_t x;
+        read(c, k, f, x);
+        if (k && (m == 0 || better(lk, lf, lx, k, f, x)) && better(k, f, x, bk, bf, bx)) bk = k, bf = f, bx = x;
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
         const uint64_t k = __shfl_xor((unsigned long long)bk, o, 64), f = __shfl_xor((unsigned long long)bf, o, 64);
-        if (better(k, f, bk, bf)) bk = k, bf = f;
+        const uint32_t x = __shfl_xor(bx, o, 64);
+        if (better(k, f, x, bk, bf, bx)) bk = k, bf = f, bx = x;
       }
-      if (lane == 0) wkey[wave] = bk, wplace[wave] = bf;
+      if (lane == 0) wkey[wave] = bk, wplace[wave] = bf, wlogit[wave] = bx;
       __syncthreads();
       for (int u = 0; u < WAVES; ++u)
-        if (better(wkey[u], wplace[u], bk, bf)) bk = wkey[u], bf = wplace[u];
+        if (better(wkey[u], wplace[u], wlogit[u], bk, bf, bx)) bk = wkey[u], bf = wplace[u], bx = wlogit[u];
       if (threadIdx.x == 0) emit(m, bk, bf);
-      lk = bk;
-      lf = bf;
+      lk = bk, lf = bf, lx = bx;
       __syncthreads();
     }
   }

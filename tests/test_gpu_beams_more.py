@@ -6,7 +6,7 @@ import pytest
 import synth
 
 from gpu_helpers import announce
-from test_gpu_beams import _case, _check
+from test_gpu_beams import _case, _check, _select
 
 pytestmark = pytest.mark.gpu
 
@@ -51,3 +51,22 @@ def test_rows_of_more_parts_than_a_wave_has_lanes(n, bi, kept, V, bf16):
     _check(lg, score, hist, 2, None, kept, bf16=bf16)
     lg[:, synth.gen(23, 1).permutation(V)[: V - V // 7]] = -np.inf
     _check(lg, score, hist, 2, None, kept, bf16=bf16, pad=3)
+
+
+@pytest.mark.parametrize("bi,V,kept", [(2, 300, 9), (2, 6000, 9), (2, 6000, 1), (1, 300, 4), (64, 300, 64)])
+def test_logits_closer_than_their_values_resolve(bi, V, kept):
+    """Logits of 1e-20 and their like beside a log sum of some units: equal values in 64 bits.  Within a beam the larger
+    logit comes first, then the lower token; between beams the larger value, then the lower beam."""
+    lg = np.full((bi, V), -5.0, np.float32)
+    rng = synth.gen(24, V, bi)
+    at = np.r_[V - 7, rng.permutation(V - 7)[:39]]          # (the same of every beam, so that the log sums are equal)
+    lg[:, at] = np.float32(1.0e-20) * rng.integers(-3, 4, (bi, 40)).astype(np.float32)
+    lg[0, V - 7] = np.float32(9.0e-20)
+    score, hist = np.zeros((1, bi), np.float32), np.zeros((1, bi, 3), np.int32)
+    x = lg.astype(np.float64)
+    lse = x.max(axis=1) + np.log(np.exp(x - x.max(axis=1)[:, None]).sum(axis=1))
+    assert np.unique((x - lse[:, None])[x > -1.0]).size == 1
+    order = sorted((-(x[j, v] - lse[j]), j, -x[j, v], v) for j in range(bi) for v in range(V))[:kept]
+    announce("beam_select unresolved logits", bi, V, kept)
+    to, tok, src = _select(lg, score, hist, 1, None, kept)
+    assert src.tolist() == [o[1] for o in order] and tok.tolist() == [o[3] for o in order]
