@@ -16,9 +16,9 @@
 //
 // Keys that some of a wave's rows may not see are in its last tiles only, from its first row's tile of 32 on; there
 // the scores are masked.  Three things make a wave take its rows one by one in the end: a masked V that is not finite
-// (0 * inf is NaN) and values whose weighted sum passes the range though their mean does not, both looked for where an
-// output is not finite; and a maximum past 2^27, where S^T c - m, fused, is off by the rounding of the product that
-// became m, which 2^x no longer bears.
+// (0 * inf is NaN) and values whose weighted sum, or scores whose product with c, passes the range though their mean, or
+// score, does not, both looked for where an output is not finite; and a maximum past 2^27, where S^T c - m, fused, is off
+// by the rounding of the product that became m, which 2^x no longer bears.
 //
 // Long sequences are bound by the matrix cores (60% busy at 1.7 GHz) and as many cycles of exponentials, sums and
 // conversions beside them: 12001 tokens and 30 short sequences, 32/8 heads of 128, in 1.09 ms, 1080 TFLOP/s.  Short
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(256, HD == 128 ? 2 : 3)
 // ---------------------------------------------------------------- fp32
 // The same on v_mfma_f32_16x16x4_f32 with 16 rows a wave: the products, 64 flops a cycle and SIMD, take
 // nearly all of the time, so that short workgroups matter more than what LDS gives (16 rows instead of 32: 131 ->
-// 109 us).  6 sequences up to 1501 tokens, 16 heads of 64, in 87 us; one of 4000 in 315, 102 TFLOP/s.
+// 109 us).  6 sequences up to 1501 tokens, 16 heads of 64, in 87 us; one of 4000 in 285, 115 TFLOP/s.
 template <int HD>
 struct TileF {
   static constexpr int KT = 32, ROW = HD * 4, CH = HD / 4, BYTES = KT * ROW;
