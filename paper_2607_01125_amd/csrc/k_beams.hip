@@ -9,7 +9,7 @@
 //
 // Bound by the logits' bytes for many rows (128 of 128256: 19 us of beam_rows, 3.5 TB/s, loads 12 of them, then a wave's
 // threshold by ballots and its short list), by chains of trips to memory and LDS for few (48 rows of 50272, 16 kept:
-// 9 + 9).
+// 9 + 7).
 #include <math.h>
 
 #include "packed.hpp"
@@ -22,6 +22,7 @@ constexpr int NT = 256, PER = PART / NT;
 constexpr int NP = 1024;                 // threads of a prompt's workgroup
 constexpr int KMAX = ZOACT_BEAMS_MAX;
 constexpr int WCAP = 512;                // candidates a wave gathers before it takes the slow way
+constexpr int FEW_GROUPS = 48;           // beams of which 64 groups' maxima give a threshold
 
 // Order of fp32 (fp64) values as that of unsigned numbers above 0.
 __device__ __forceinline__ uint32_t order32(float x) {
@@ -290,10 +291,14 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
   const bool ended_j = has_ended(b, row_j);
   const uint32_t per = (uint32_t)splits * (uint32_t)K, total = (uint32_t)BI * per;      // (at most 2^30)
   constexpr int KEEP = 4;                // candidates that a thread keeps from the first look to the second
+  // A thread's q-th candidate: each time 7 further round, so that a thread meets all ranks of the parts' lists (1031 is
+  // prime), not the first of each list or the last.
+  auto nth = [](int q) { return (uint32_t)q * NP + ((threadIdx.x + 7 * q) & (NP - 1)); };
+  const int rounds = (int)((total + NP - 1) / NP);
   Cand raw[KEEP];
 #pragma unroll
   for (int q = 0; q < KEEP; ++q) {
-    const uint32_t c = threadIdx.x + q * NP;
+    const uint32_t c = nth(q);
     raw[q] = c < total ? cand[(int64_t)i0 * total + c] : Cand{0.f, -1};
   }
   for (int j = wave; j < BI; j += WAVES) {
@@ -366,30 +371,48 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
 #pragma unroll
   for (int q = 0; q < KEEP; ++q) {
     kk[q] = kf[q] = kx[q] = 0;
-    const uint32_t c = threadIdx.x + q * NP;
+    const uint32_t c = nth(q);
     if (c < total) rate(c, raw[q], kk[q], kf[q], kx[q]);
     mine = kk[q] > mine ? kk[q] : mine;
   }
 #pragma unroll 8
-  for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
-    uint64_t k, f;
+  for (int q = KEEP; q < rounds; ++q) {
+    const uint32_t c = nth(q);
+    uint64_t k = 0, f;
     uint32_t x;
-    read(c, k, f, x);
+    if (c < total) read(c, k, f, x);
     mine = k > mine ? k : mine;
   }
-  // Of the maxima of 64 groups of candidates (a lane's in all waves) the K-th largest, or a little less (20 bits of
-  // it), is reached by K candidates at least, and few others: the threshold.
+  // The threshold is reached by K candidates at least, and few others: of the maxima of 64 groups (a lane's in all
+  // waves) the K-th largest (24 bits of it: scores of -1500 still differ by a quarter), or with many beams of those of
+  // all threads, since K of 64 groups are nearly all then and more than CAP candidates, where there are as many, may
+  // reach the least of them.  (32 of 32 x 16000 logits: groups 18 to 20 us, threads 25 to 27; 48 of 48 x 128256: 112,
+  // 120; 64 of 64 x 16000: 54 to 99, 48; 64 of 64 x 128256: 227 to 4485, 225.)
   uint64_t thr = 1;
   if (!few) {
     tops[wave][lane] = (uint32_t)(mine >> 32);
     __syncthreads();
-    uint32_t upper = 0, to = 0;
+    uint32_t to = 0, part[WAVES];
 #pragma unroll
-    for (int u = 0; u < WAVES; ++u) upper = tops[u][lane] > upper ? tops[u][lane] : upper;
+    for (int u = 0; u < WAVES; ++u) part[u] = tops[u][lane];
+    if (K <= FEW_GROUPS || total <= CAP) {
+      uint32_t upper = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 12; --bit) {
-      const uint32_t x = to | (1u << bit);
-      if (__popcll(__ballot(upper >= x)) >= K) to = x;
+      for (int u = 0; u < WAVES; ++u) upper = part[u] > upper ? part[u] : upper;
+#pragma unroll
+      for (int bit = 31; bit >= 8; --bit) {
+        const uint32_t x = to | (1u << bit);
+        if (__popcll(__ballot(upper >= x)) >= K) to = x;
+      }
+    } else {
+#pragma unroll 1
+      for (uint32_t bit = 1u << 31; bit; bit >>= 1) {
+        int reach = 0;
+#pragma unroll
+        for (int u = 0; u < WAVES; ++u) reach += __popcll(__ballot(part[u] >= (to | bit)));
+        if (reach >= K) to |= bit;
+        if (reach == K) break;
+      }
     }
     thr = to ? (uint64_t)to << 32 : 1;
   }
@@ -401,10 +424,11 @@ __global__ void __launch_bounds__(NP) beam_pick(const T* __restrict__ logits, in
 #pragma unroll
   for (int q = 0; q < KEEP; ++q) gather(kk[q], kf[q], kx[q]);
 #pragma unroll 8
-  for (uint32_t c = threadIdx.x + KEEP * NP; c < total; c += NP) {
-    uint64_t k, f;
-    uint32_t x;
-    read(c, k, f, x);
+  for (int q = KEEP; q < rounds; ++q) {
+    const uint32_t c = nth(q);
+    uint64_t k = 0, f = 0;
+    uint32_t x = 0;
+    if (c < total) read(c, k, f, x);
     gather(k, f, x);
   }
   __syncthreads();

@@ -70,3 +70,13 @@ def test_logits_closer_than_their_values_resolve(bi, V, kept):
     announce("beam_select unresolved logits", bi, V, kept)
     to, tok, src = _select(lg, score, hist, 1, None, kept)
     assert src.tolist() == [o[1] for o in order] and tok.tolist() == [o[3] for o in order]
+
+
+@pytest.mark.parametrize("bi,kept,V", [(16, 16, 50272), (33, 33, 9000), (48, 48, 9000), (49, 49, 9000), (64, 64, 20000)])
+def test_long_histories_whose_scores_are_near_one_another(bi, kept, V):
+    """Scores of about -1500 within a few of each other, which differ in the lower bits of their order only."""
+    lg, score, hist = _case(2, bi, V, 5, 25)
+    score[0] = -1500.0 - 2.0 * synth.gen(25, 3).random(bi).astype(np.float32)
+    score[1] = -90.0 - 40.0 * synth.gen(25, 4).random(bi).astype(np.float32)
+    announce("beam_select long histories", bi, kept, V)
+    _check(lg, score, hist, 5, 2, kept)
